@@ -278,6 +278,63 @@ ss_status ss_commit_gather(ss_ctx* ctx, ss_tensor K_loc, ss_tensor V_loc, int32_
                            ss_tensor K_dst, ss_tensor V_dst, int32_t cap, const int32_t* dst_off,
                            void* stream);
 
+/* ---- 8-bit KV cache -----------------------------------------------------------------------
+ * (The paper keeps its history in the model's type; an 8-bit history halves the bytes of every
+ * round.)  A row - one token of one kv-head, d values - is held as d codes in e4m3 and one byte
+ * e + 127: e is the smallest integer with max|x| <= 448 * 2^e over the row's finite values, at
+ * least -32 and at most 80, a value is code * 2^e, and its code is x * 2^-e rounded to e4m3
+ * (nearest even; infinities and what exceeds 448 * 2^80 saturate, NaN stays NaN).  So a value is
+ * off by at most 2^-4 of itself or 2^-10 * 2^e, whichever is more, and a row read back and written
+ * again keeps its values.
+ *
+ * ss_cache8 describes a cache.  Paged (page_table not NULL): K, V are pools [n_pages, H_kv,
+ * page_size, d] of codes, K_scale, V_scale [n_pages, H_kv, page_size] of bytes (stride_b = page
+ * stride), page_table (device int32 [B, pages_per_req]) lists a request's pages, which hold
+ * page_size * pages_per_req tokens.  Dense (page_table NULL): [B, H_kv, page_size, d], n_pages =
+ * requests in the buffer (>= the call's B), pages_per_req ignored.  Strides are in bytes; for the
+ * codes d is contiguous and base and strides are multiples of 16; the scales' strides and base are
+ * free.  Table entries of pages that a call does not touch may hold anything. */
+typedef struct {
+  ss_tensor K, V;               /* codes, device                                             */
+  ss_tensor K_scale, V_scale;   /* one byte per row, device                                  */
+  int32_t n_pages, page_size, pages_per_req;
+  const int32_t* page_table;    /* device [B, pages_per_req], or NULL                        */
+} ss_cache8;
+
+/* Rows join the cache (ss_commit_gather's counterpart): for each request b and k < row_cnt[b], row
+ * row_idx[b][k] of K, V [B, H_kv, T, d] (bf16) becomes token dst_off[b] + k.  row_idx (device int32
+ * [B, T]) NULL = rows in order, row_cnt (device [B]) NULL = all T, dst_off (device [B]) NULL = 0.
+ * Nothing else of the cache is written.  The tokens of one call must be distinct slots (no page in
+ * two requests' tables where both write).  A count outside [0, T] is clamped, a row outside [0, T)
+ * skipped (SS_DEV_BAD_ACCEPT); a token outside the request's room (SS_DEV_DST_OVERFLOW) or in a page
+ * id outside [0, n_pages) (SS_DEV_BAD_PAGE) is skipped.  Independent of the round state.
+ * B * T * H_kv * 2 < 2^31 (SS_ERR_SHAPE); T is not bound by max_Tloc. */
+ss_status ss_kv8_write(ss_ctx* ctx, const ss_cache8* cache, ss_tensor K, ss_tensor V, int32_t B, int32_t T,
+                       const int32_t* row_idx, const int32_t* row_cnt, const int32_t* dst_off, void* stream);
+
+/* Rows back to bf16: token src_off[b] + k of request b becomes row k of K, V [B, H_kv, T, d] for
+ * k < row_cnt[b]; rows from row_cnt[b] on are left as they are.  src_off NULL = 0, row_cnt NULL = T.
+ * Exact: every value of the cache is a bf16 value.  A count outside [0, T] is clamped and a token
+ * outside the request's room skipped (SS_DEV_BAD_VALID_LEN); tokens of a page id outside the pool
+ * read as zeros (SS_DEV_BAD_PAGE).  Independent of the round state. */
+ss_status ss_kv8_read(ss_ctx* ctx, const ss_cache8* cache, ss_tensor K, ss_tensor V, int32_t B, int32_t T,
+                      const int32_t* src_off, const int32_t* row_cnt, void* stream);
+
+/* A history chunk that is held in 8 bits: like ss_verify_chunk_paged (paged or dense), every query
+ * row of the round against tokens [0, valid_len[b]) (device [B], NULL = all the request's room;
+ * outside [0, room]: clamped, SS_DEV_BAD_VALID_LEN).  May be mixed with bf16 chunks in any order.
+ * The room must not exceed max_Lc (SS_ERR_SHAPE).  The split over the GPU follows the lengths on
+ * the device, so no host copy of them is taken and a captured call follows lengths that change
+ * between replays. */
+ss_status ss_verify_chunk8(ss_ctx* ctx, const ss_cache8* cache, const int32_t* valid_len, void* stream);
+
+/* Decoding: attention of Q [B, H_q, T_q, d] over the 8-bit cache alone in one launch, O and LSE as
+ * ss_verify_finalize writes them.  Every query sees all valid tokens, so a step with T_q = 1 is
+ * ss_kv8_write of the new token and ss_decode8; candidates that must not see one another go through
+ * a round (ss_verify_chunk8 + ss_verify_local).  SS_ERR_STATE while a round is open. */
+ss_status ss_decode8(ss_ctx* ctx, ss_tensor Q, int32_t B, int32_t T_q, float scale, const ss_cache8* cache,
+                     const int32_t* valid_len, void* O, float* LSE, void* stream);
+
 /* Read (and clear) the device status word after synchronising `stream`, waiting at most
  * timeout_ms (<= 0: wait without limit).  SS_OK, SS_ERR_DEVICE_FLAG (bits in *dev_bits if
  * non-NULL) or SS_ERR_TIMEOUT. */
@@ -553,9 +610,9 @@ ss_status ss_get_stats(ss_ctx* ctx, ss_stats* out);
 /* Number of kernels this context has launched since creation. */
 int64_t ss_launch_count(ss_ctx* ctx);
 /* "simt", "tcgen05" (rows on M), "tcgen05-keys" (keys on M), "tcgen05-round" / "tcgen05-keys-round"
- * (the same two over a list of chunks in one launch) or "simt-round" (a small round in one
- * launch): the chunk kernel the last chunk call, ss_verify_chunks or ss_verify_round used;
- * "none" before. */
+ * (the same two over a list of chunks in one launch), "simt-round" (a small round in one
+ * launch) or "kv8-simt" (8-bit cache): the chunk kernel the last chunk call,
+ * ss_verify_chunks, ss_verify_round or ss_decode8 used; "none" before. */
 const char* ss_last_chunk_kernel(ss_ctx* ctx);
 
 #ifdef __cplusplus

@@ -34,7 +34,7 @@ EXPORTS = ["ss_workspace_bytes", "ss_create", "ss_destroy", "ss_verify_begin", "
            "ss_tier_d2h_bytes", "ss_verify_chunk_paged", "ss_width_create", "ss_width_destroy",
            "ss_width_observe", "ss_width_next", "ss_width_estimate", "ss_cohort_build", "ss_probe_read",
            "ss_selftest_wait_expiry", "ss_verify_abort", "ss_cta_log_set", "ss_get_stats", "ss_verify_round", "ss_verify_chunks",
-           "ss_time_rounds"]
+           "ss_time_rounds", "ss_kv8_write", "ss_kv8_read", "ss_verify_chunk8", "ss_decode8"]
 
 
 class ss_stats(C.Structure):
@@ -106,6 +106,12 @@ class ss_chunk_desc(C.Structure):
                 ("valid_len_host", C.POINTER(C.c_int32))]
 
 
+class ss_cache8(C.Structure):
+    _fields_ = [("K", ss_tensor), ("V", ss_tensor), ("K_scale", ss_tensor), ("V_scale", ss_tensor),
+                ("n_pages", C.c_int32), ("page_size", C.c_int32), ("pages_per_req", C.c_int32),
+                ("page_table", C.c_void_p)]
+
+
 class ss_static_round(C.Structure):
     _fields_ = [("B", C.c_int32), ("H_q", C.c_int32), ("H_kv", C.c_int32), ("d", C.c_int32),
                 ("T_q", C.c_int32), ("T_loc", C.c_int32), ("L_c", C.c_int32), ("scale", C.c_float),
@@ -163,6 +169,15 @@ def load() -> C.CDLL:
     lib.ss_commit_gather.restype = C.c_int
     lib.ss_commit_gather.argtypes = [vp, ss_tensor, ss_tensor, i32, i32, vp, vp, ss_tensor,
                                      ss_tensor, i32, vp, vp]
+    c8 = C.POINTER(ss_cache8)
+    lib.ss_kv8_write.restype = C.c_int
+    lib.ss_kv8_write.argtypes = [vp, c8, ss_tensor, ss_tensor, i32, i32, vp, vp, vp, vp]
+    lib.ss_kv8_read.restype = C.c_int
+    lib.ss_kv8_read.argtypes = [vp, c8, ss_tensor, ss_tensor, i32, i32, vp, vp, vp]
+    lib.ss_verify_chunk8.restype = C.c_int
+    lib.ss_verify_chunk8.argtypes = [vp, c8, vp, vp]
+    lib.ss_decode8.restype = C.c_int
+    lib.ss_decode8.argtypes = [vp, ss_tensor, i32, i32, C.c_float, c8, vp, vp, vp, vp]
     lib.ss_poll_status.restype = C.c_int
     lib.ss_poll_status.argtypes = [vp, vp, i32, u32p]
     lib.ss_stream_round.restype = C.c_int
@@ -273,6 +288,38 @@ def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
 
 
+class Cache8:
+    """An 8-bit KV cache: codes K, V [n_pages, H_kv, page_size, d] with page_table int32
+    [B, pages_per_req], or [B, H_kv, tokens, d] without one, as uint8 (or float8_e4m3fn) tensors with d
+    contiguous, and K_scale, V_scale uint8 [.., H_kv, ..], one byte per row.  Holds the tensors; the
+    description is built once."""
+
+    def __init__(self, K: torch.Tensor, V: torch.Tensor, K_scale: torch.Tensor, V_scale: torch.Tensor,
+                 page_table: Optional[torch.Tensor] = None):
+        for t in (K, V):
+            assert t.dim() == 4 and t.element_size() == 1 and t.stride(3) == 1, (t.shape, t.dtype, t.stride())
+        for t in (K_scale, V_scale):
+            assert t.dtype == torch.uint8 and t.shape == K.shape[:3], (t.shape, t.dtype)
+        assert V.shape == K.shape
+        if page_table is not None:
+            assert page_table.dtype == torch.int32 and page_table.dim() == 2 and page_table.is_contiguous()
+        self.tensors = (K, V, K_scale, V_scale, page_table)
+        self.H_kv, self.d = K.shape[1], K.shape[3]
+        self.requests = K.shape[0] if page_table is None else page_table.shape[0]
+        t8 = lambda t: ss_tensor(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2))
+        self.desc = ss_cache8(t8(K), t8(V), t8(K_scale), t8(V_scale), K.shape[0], K.shape[2],
+                              1 if page_table is None else page_table.shape[1], _ptr(page_table))
+        self.ref = C.byref(self.desc)
+
+    @classmethod
+    def empty(cls, outer: int, H_kv: int, tokens: int, d: int, page_table: Optional[torch.Tensor] = None,
+              device="cuda:0") -> "Cache8":
+        """A cache of zeros: `outer` pages of `tokens` tokens, or `outer` requests with room for them."""
+        z = lambda *shape: torch.zeros(shape, dtype=torch.uint8, device=device)
+        s = (outer, H_kv, tokens)
+        return cls(z(*s, d), z(*s, d), z(*s), z(*s), page_table)
+
+
 class Context:
     """Owns an ss_ctx and its torch-allocated workspace.  Methods mirror the C entry points."""
 
@@ -290,6 +337,7 @@ class Context:
             raise SpecStreamError(st, "ss_create")
         self.H_q, self.H_kv, self.d = H_q, H_kv, d
         self._dev = device
+        self._B = 0   # requests of the open round
 
     def _sp(self, stream) -> int:
         """cudaStream_t of `stream`, else torch's current stream on this context's device."""
@@ -320,6 +368,7 @@ class Context:
         assert H_q == self.H_q and d == self.d
         self._check(self.lib.ss_verify_begin(self.handle, as_ss_tensor(Q), B, T_q, scale,
                                              self._sp(stream)), "ss_verify_begin")
+        self._B = B
 
     def ss_verify_chunk(self, K: torch.Tensor, V: torch.Tensor, valid_len: Optional[torch.Tensor] = None,
                         stream=None):
@@ -389,6 +438,49 @@ class Context:
                                               T_loc, accept_idx.data_ptr(), accept_cnt.data_ptr(),
                                               as_ss_tensor(K_dst), as_ss_tensor(V_dst), cap,
                                               dst_off.data_ptr(), self._sp(stream)), "ss_commit_gather")
+
+    def _cache8(self, cache: Cache8, B: int):
+        assert cache.H_kv == self.cfg.H_kv and cache.d == self.d and cache.requests >= B, "cache of another shape"
+        return cache.ref
+
+    @staticmethod
+    def _ints(shape, *tensors):
+        for t in tensors:
+            assert t is None or (t.dtype == torch.int32 and t.is_contiguous() and t.is_cuda and t.shape == shape)
+
+    def ss_kv8_write(self, cache: Cache8, K: torch.Tensor, V: torch.Tensor, dst_off=None, row_cnt=None,
+                     row_idx=None, stream=None):
+        """K, V [B, H_kv, T, d] bf16; dst_off, row_cnt int32 [B] and row_idx int32 [B, T] on the device or None."""
+        B, H, T, d = K.shape
+        assert V.shape == K.shape and H == self.cfg.H_kv and d == self.d
+        self._ints((B,), dst_off, row_cnt)
+        self._ints((B, T), row_idx)
+        self._check(self.lib.ss_kv8_write(self.handle, self._cache8(cache, B), as_ss_tensor(K), as_ss_tensor(V), B, T,
+                                          _ptr(row_idx), _ptr(row_cnt), _ptr(dst_off), self._sp(stream)), "ss_kv8_write")
+
+    def ss_kv8_read(self, cache: Cache8, K: torch.Tensor, V: torch.Tensor, src_off=None, row_cnt=None, stream=None):
+        """Tokens src_off[b] .. src_off[b] + row_cnt[b] of the cache into rows 0 .. of K, V [B, H_kv, T, d] bf16."""
+        B, H, T, d = K.shape
+        assert V.shape == K.shape and H == self.cfg.H_kv and d == self.d
+        self._ints((B,), src_off, row_cnt)
+        self._check(self.lib.ss_kv8_read(self.handle, self._cache8(cache, B), as_ss_tensor(K), as_ss_tensor(V), B, T,
+                                         _ptr(src_off), _ptr(row_cnt), self._sp(stream)), "ss_kv8_read")
+
+    def ss_verify_chunk8(self, cache: Cache8, valid_len: Optional[torch.Tensor] = None, stream=None):
+        """One chunk of the open round held in 8 bits."""
+        self._ints((self._B,), valid_len)
+        self._check(self.lib.ss_verify_chunk8(self.handle, self._cache8(cache, self._B), _ptr(valid_len),
+                                              self._sp(stream)), "ss_verify_chunk8")
+
+    def ss_decode8(self, Q: torch.Tensor, scale: float, cache: Cache8, valid_len: Optional[torch.Tensor],
+                   O: torch.Tensor, LSE: Optional[torch.Tensor] = None, stream=None):
+        """Q [B, H_q, T_q, d] over the first valid_len[b] tokens of the cache -> O (bf16), LSE (fp32 [B, H_q, T_q])."""
+        B, H_q, T_q, d = Q.shape
+        assert H_q == self.H_q and d == self.d and O.dtype == torch.bfloat16 and O.is_contiguous() and O.shape == Q.shape
+        assert LSE is None or (LSE.dtype == torch.float32 and LSE.is_contiguous() and LSE.shape == Q.shape[:3])
+        self._ints((B,), valid_len)
+        self._check(self.lib.ss_decode8(self.handle, as_ss_tensor(Q), B, T_q, scale, self._cache8(cache, B),
+                                        _ptr(valid_len), O.data_ptr(), _ptr(LSE), self._sp(stream)), "ss_decode8")
 
     def ss_poll_status(self, stream=None, timeout_ms: int = 0):
         """Returns (status, device_bits)."""

@@ -5,6 +5,7 @@
 #include <cstring>
 #include <new>
 
+#include "kv8.cuh"
 #include "ss_internal.h"
 
 struct ss_ctx {
@@ -68,6 +69,8 @@ struct ss_ctx {
   int hist_n[4];            // maps in use per slot (0 = empty)
   uint64_t hist_age[4];
   bool hist_pinned[4];      // the list was used under a stream capture: a graph may replay the launch, never evicted
+  unsigned int* tickets8;   // 8-bit cache: one ticket per unit of an attention launch (zero between launches)
+  float* scratch8;          // and the partial states of units cut by a share's end
   cudaEvent_t* ev_pool;     // timing events of the streamed round (SS_FLAG_STREAM_TIMING)
   int ev_pool_n;
 };
@@ -136,7 +139,8 @@ int slot_capacity_for(const ss_config* c) {
 
 constexpr int kHistSlots = 4;
 struct Layout {
-  size_t off_hist, off_ml, off_a, total;
+  size_t off_hist, off_ml, off_a, off_tickets8, off_scratch8, total;
+  size_t n_tickets8;
   int64_t set_stride_ml, set_stride_a;
   int R_stride;
 };
@@ -153,7 +157,11 @@ Layout layout_for(const ss_config* c) {
                ss::kRoundCounters * sizeof(unsigned int);   // status, trace region, round counters
   L.off_ml = L.off_hist + kHistSlots * 2 * ss::kMaxHistChunks * sizeof(CUtensorMap);  // lists of tensor maps
   L.off_a = align_up(L.off_ml + (size_t)sets * rows * sizeof(float2), 256);
-  L.total = align_up(L.off_a + (size_t)sets * rows * c->d * sizeof(float), 256);
+  L.off_tickets8 = align_up(L.off_a + (size_t)sets * rows * c->d * sizeof(float), 256);
+  L.n_tickets8 = (size_t)c->max_B * c->H_kv * ((L.R_stride + ss::kMinRows8 - 1) / ss::kMinRows8);
+  L.off_scratch8 = align_up(L.off_tickets8 + L.n_tickets8 * sizeof(unsigned int), 256);
+  const size_t rows8 = L.R_stride < ss::kRows8 ? L.R_stride : ss::kRows8;
+  L.total = align_up(L.off_scratch8 + 2 * ss::kCtas8 * rows8 * (c->d + 2) * sizeof(float), 256);
   return L;
 }
 
@@ -393,6 +401,8 @@ ss_status ss_create(ss_ctx** out, const ss_config* cfg, void* workspace, size_t 
   c->trace = (unsigned long long*)(c->ws + 256);
   c->round_counters = (unsigned int*)(c->ws + 256 + align_up(ss::kTraceWords * sizeof(unsigned long long), 256));
   c->hist_maps = (CUtensorMap*)(c->ws + L.off_hist);
+  c->tickets8 = (unsigned int*)(c->ws + L.off_tickets8);
+  c->scratch8 = (float*)(c->ws + L.off_scratch8);
   c->part_ml = (float2*)(c->ws + L.off_ml);
   c->part_a = (float*)(c->ws + L.off_a);
   c->set_stride_ml = L.set_stride_ml;
@@ -433,6 +443,7 @@ ss_status ss_create(ss_ctx** out, const ss_config* cfg, void* workspace, size_t 
   }
   e = cudaMemset(c->status, 0, 256);
   if (e == cudaSuccess) e = cudaMemset(c->round_counters, 0, ss::kRoundCounters * sizeof(unsigned int));
+  if (e == cudaSuccess) e = cudaMemset(c->tickets8, 0, L.n_tickets8 * sizeof(unsigned int));
   if (e != cudaSuccess) {
     delete c;
     return SS_ERR_CUDA;
@@ -1183,6 +1194,169 @@ ss_status ss_commit_gather(ss_ctx* c, ss_tensor K_loc, ss_tensor V_loc, int32_t 
   cudaError_t e = ss::launch_gather(p, (cudaStream_t)stream);
   if (e != cudaSuccess) return cuda_fail(c, e);
   ++c->launches;
+  return SS_OK;
+}
+
+// ---- 8-bit KV cache ---------------------------------------------------------------------------
+// The calls below run on the context's device whatever device is current, and leave it current.
+struct DeviceGuard {
+  int before = -1;
+  cudaError_t err;
+  explicit DeviceGuard(int dev) {
+    err = cudaGetDevice(&before);
+    if (err == cudaSuccess && before != dev) err = cudaSetDevice(dev);
+    else before = -1;
+  }
+  ~DeviceGuard() {
+    if (before >= 0) cudaSetDevice(before);
+  }
+};
+
+// Checks a cache for B requests and fills the kernels' view of it.
+static ss_status view8(const ss_ctx* c, const ss_cache8* k, int32_t B, ss::View8* v) {
+  if (!k || !k->K.ptr || !k->V.ptr || !k->K_scale.ptr || !k->V_scale.ptr) return SS_ERR_ARG;
+  if (k->n_pages <= 0 || k->page_size <= 0) return SS_ERR_ARG;
+  if (k->page_table && k->pages_per_req <= 0) return SS_ERR_ARG;
+  if (!k->page_table && B > k->n_pages) return SS_ERR_SHAPE;
+  const int64_t room = k->page_table ? (int64_t)k->page_size * k->pages_per_req : k->page_size;
+  if (room > 0x7fffffff - ss::kTok8) return SS_ERR_SHAPE;
+  for (const ss_tensor* t : {&k->K, &k->V})
+    if (!aligned16(t->ptr) || t->stride_b % 16 || t->stride_h % 16 || t->stride_t % 16) return SS_ERR_ALIGN;
+  if ((uintptr_t)k->page_table & 3) return SS_ERR_ALIGN;
+  memset(v, 0, sizeof(*v));
+  v->K = (uint8_t*)k->K.ptr;
+  v->V = (uint8_t*)k->V.ptr;
+  v->Ks = (uint8_t*)k->K_scale.ptr;
+  v->Vs = (uint8_t*)k->V_scale.ptr;
+  v->k_sb = k->K.stride_b, v->k_sh = k->K.stride_h, v->k_st = k->K.stride_t;
+  v->v_sb = k->V.stride_b, v->v_sh = k->V.stride_h, v->v_st = k->V.stride_t;
+  v->ks_sb = k->K_scale.stride_b, v->ks_sh = k->K_scale.stride_h, v->ks_st = k->K_scale.stride_t;
+  v->vs_sb = k->V_scale.stride_b, v->vs_sh = k->V_scale.stride_h, v->vs_st = k->V_scale.stride_t;
+  v->page_table = k->page_table;
+  v->n_outer = k->n_pages;
+  v->page_size = k->page_size;
+  v->pages_per_req = k->page_table ? k->pages_per_req : 1;
+  v->room = (int)room;
+  return SS_OK;
+}
+
+static ss_status copy8(ss_ctx* c, bool write, const ss_cache8* cache, ss_tensor K, ss_tensor V, int32_t B, int32_t T,
+                       const int32_t* idx, const int32_t* cnt, const int32_t* off, void* stream) {
+  if (!c || !K.ptr || !V.ptr || B <= 0 || T <= 0) return SS_ERR_ARG;
+  if (B > c->cfg.max_B || (int64_t)B * T * c->cfg.H_kv * 2 >= (1ll << 31)) return SS_ERR_SHAPE;
+  ss::Copy8Params p;
+  memset(&p, 0, sizeof(p));
+  const ss_status st = view8(c, cache, B, &p.kv);
+  if (st != SS_OK) return st;
+  if (!tensor_ok(K) || !tensor_ok(V)) return SS_ERR_ALIGN;
+  if (((uintptr_t)idx | (uintptr_t)cnt | (uintptr_t)off) & 3) return SS_ERR_ALIGN;
+  p.K = (uint16_t*)K.ptr;
+  p.V = (uint16_t*)V.ptr;
+  p.k_sb = K.stride_b, p.k_sh = K.stride_h, p.k_st = K.stride_t;
+  p.v_sb = V.stride_b, p.v_sh = V.stride_h, p.v_st = V.stride_t;
+  p.idx = idx;
+  p.cnt = cnt;
+  p.off = off;
+  p.B = B;
+  p.H_kv = c->cfg.H_kv;
+  p.T = T;
+  p.d = c->cfg.d;
+  p.status = c->status;
+  DeviceGuard on(c->cfg.device);
+  cudaError_t e = on.err;
+  if (e == cudaSuccess)
+    e = write ? ss::launch_kv8_write(p, (cudaStream_t)stream) : ss::launch_kv8_read(p, (cudaStream_t)stream);
+  if (e != cudaSuccess) return cuda_fail(c, e);
+  ++c->launches;
+  return SS_OK;
+}
+
+ss_status ss_kv8_write(ss_ctx* c, const ss_cache8* cache, ss_tensor K, ss_tensor V, int32_t B, int32_t T,
+                       const int32_t* row_idx, const int32_t* row_cnt, const int32_t* dst_off, void* stream) {
+  return copy8(c, true, cache, K, V, B, T, row_idx, row_cnt, dst_off, stream);
+}
+
+ss_status ss_kv8_read(ss_ctx* c, const ss_cache8* cache, ss_tensor K, ss_tensor V, int32_t B, int32_t T,
+                      const int32_t* src_off, const int32_t* row_cnt, void* stream) {
+  return copy8(c, false, cache, K, V, B, T, nullptr, row_cnt, src_off, stream);
+}
+
+// The attention launch that both entry points share; the caller has set where its result goes.
+static ss_status attn8(ss_ctx* c, const ss_tensor& Q, int32_t B, int32_t T_q, float scale, const ss_cache8* cache,
+                       const int32_t* valid_len, ss::Attn8Params* p, cudaStream_t s, bool pdl) {
+  const ss_status st = view8(c, cache, B, &p->kv);
+  if (st != SS_OK) return st;
+  if (p->kv.room > c->cfg.max_Lc) return SS_ERR_SHAPE;
+  if ((uintptr_t)valid_len & 3) return SS_ERR_ALIGN;
+  p->Q = (const __nv_bfloat16*)Q.ptr;
+  p->q_sb = Q.stride_b;
+  p->q_sh = Q.stride_h;
+  p->q_st = Q.stride_t;
+  p->valid_len = valid_len;
+  p->B = B;
+  p->H_kv = c->cfg.H_kv;
+  p->G = c->G;
+  p->T_q = T_q;
+  p->R = T_q * c->G;
+  p->d = c->cfg.d;
+  p->rows_per_tile = p->R < ss::kMinRows8 ? p->R : ss::kMinRows8;
+  p->row_tiles = (p->R + p->rows_per_tile - 1) / p->rows_per_tile;
+  p->scale_log2 = scale * 1.4426950408889634f;
+  p->min_tiles = 1;
+  p->scratch = c->scratch8;
+  p->tickets = c->tickets8;
+  p->status = c->status;
+  DeviceGuard on(c->cfg.device);
+  if (on.err != cudaSuccess) return cuda_fail(c, on.err);
+  const cudaError_t e = ss::launch_attn8_simt(*p, s, pdl);
+  if (e != cudaSuccess) return cuda_fail(c, e);
+  c->last_kernel = "kv8-simt";
+  ++c->launches;
+  ++c->stats.chunk_calls;
+  c->stats.kv_bytes += (int64_t)B * p->kv.room * c->cfg.H_kv * (c->cfg.d + 1) * 2;
+  return SS_OK;
+}
+
+ss_status ss_verify_chunk8(ss_ctx* c, const ss_cache8* cache, const int32_t* valid_len, void* stream) {
+  if (!c || !cache) return SS_ERR_ARG;
+  if (c->state != ss_ctx::OPEN || (cudaStream_t)stream != c->stream) return SS_ERR_STATE;
+  ss::Attn8Params p;
+  memset(&p, 0, sizeof(p));
+  ss_status st = view8(c, cache, c->B, &p.kv);  // (before a fold is enqueued)
+  if (st != SS_OK) return st;
+  if (c->n_sets == c->n_set_cap) {
+    const cudaError_t e = fold_sets(c, c->stream);
+    if (e != cudaSuccess) return cuda_fail(c, e);
+  }
+  // one partial state per row: the launch joins its own splits
+  p.part_ml = c->part_ml + (int64_t)c->n_sets * c->set_stride_ml;
+  p.part_a = c->part_a + (int64_t)c->n_sets * c->set_stride_a;
+  p.R_stride = c->R_stride;
+  st = attn8(c, c->Q, c->B, c->T_q, c->scale, cache, valid_len, &p, c->stream, use_pdl_first(c));
+  if (st != SS_OK) return st;
+  c->splits[c->n_sets] = 1;
+  memset(c->absent[c->n_sets], 0, sizeof(c->absent[0]));
+  ++c->n_sets;
+  c->first_launch = false;
+  return SS_OK;
+}
+
+ss_status ss_decode8(ss_ctx* c, ss_tensor Q, int32_t B, int32_t T_q, float scale, const ss_cache8* cache,
+                     const int32_t* valid_len, void* O, float* LSE, void* stream) {
+  if (!c || !Q.ptr || !cache || !O) return SS_ERR_ARG;
+  if (B <= 0 || T_q <= 0) return SS_ERR_ARG;
+  if (!(scale > 0.f) || !(scale < 3.0e38f)) return SS_ERR_ARG;
+  if (B > c->cfg.max_B || T_q > c->cfg.max_Tq) return SS_ERR_SHAPE;
+  if (!tensor_ok(Q) || !aligned16(O) || ((uintptr_t)LSE & 3)) return SS_ERR_ALIGN;
+  if (c->state != ss_ctx::IDLE) return SS_ERR_STATE;
+  ss::Attn8Params p;
+  memset(&p, 0, sizeof(p));
+  p.O = (__nv_bfloat16*)O;
+  p.LSE = LSE;
+  const ss_status st = attn8(c, Q, B, T_q, scale, cache, valid_len, &p, (cudaStream_t)stream, use_pdl_first(c));
+  if (st != SS_OK) return st;
+  ++c->stats.rounds;
+  c->stats.rows += (int64_t)B * c->cfg.H_q * T_q;
   return SS_OK;
 }
 
