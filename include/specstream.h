@@ -290,7 +290,8 @@ ss_status ss_commit_gather(ss_ctx* ctx, ss_tensor K_loc, ss_tensor V_loc, int32_
  * ss_cache8 describes a cache.  Paged (page_table not NULL): K, V are pools [n_pages, H_kv,
  * page_size, d] of codes, K_scale, V_scale [n_pages, H_kv, page_size] of bytes (stride_b = page
  * stride), page_table (device int32 [B, pages_per_req]) lists a request's pages, which hold
- * page_size * pages_per_req tokens.  Dense (page_table NULL): [B, H_kv, page_size, d], n_pages =
+ * page_size * pages_per_req tokens; attention runs on the tensor cores for pages of 8, 16, 32, 64 or
+ * a multiple of 128 tokens and on the CUDA cores, many times slower, for others.  Dense (page_table NULL): [B, H_kv, page_size, d], n_pages =
  * requests in the buffer (>= the call's B), pages_per_req ignored.  Strides are in bytes; for the
  * codes d is contiguous and base and strides are multiples of 16; the scales' strides and base are
  * free.  Table entries of pages that a call does not touch may hold anything. */
@@ -611,7 +612,7 @@ ss_status ss_get_stats(ss_ctx* ctx, ss_stats* out);
 int64_t ss_launch_count(ss_ctx* ctx);
 /* "simt", "tcgen05" (rows on M), "tcgen05-keys" (keys on M), "tcgen05-round" / "tcgen05-keys-round"
  * (the same two over a list of chunks in one launch), "simt-round" (a small round in one
- * launch) or "kv8-simt" (8-bit cache): the chunk kernel the last chunk call,
+ * launch), "kv8-tcgen05" or "kv8-simt" (8-bit cache): the chunk kernel the last chunk call,
  * ss_verify_chunks, ss_verify_round or ss_decode8 used; "none" before. */
 const char* ss_last_chunk_kernel(ss_ctx* ctx);
 

@@ -175,7 +175,26 @@ ss_status cuda_fail(ss_ctx* c, cudaError_t e) {
   return SS_ERR_CUDA;
 }
 
-// Tensor map over K or V [B, H_kv, L_c, d] with a [box_tokens][64 d] box and 128-byte swizzle.
+// Tensor map over K or V [B, H_kv, L_c, d] with a [box_tokens][64 d] box and 128-byte swizzle; for the
+// codes of an 8-bit cache (elem = 1 byte) a [box_tokens][d] box, swizzled over the d bytes of its rows.
+bool encode_map(const ss_ctx* c, const ss_tensor& t, int B, int L_c, int box_tokens, int elem, CUtensorMap* m) {
+  if (!g_encode) return false;
+  const int H_kv = c->cfg.H_kv, d = c->cfg.d;
+  cuuint64_t dims[4] = {(cuuint64_t)d, (cuuint64_t)L_c, (cuuint64_t)H_kv, (cuuint64_t)B};
+  // unused outer strides still have to be positive multiples of 16 bytes
+  const int64_t st = t.stride_t, sh = (H_kv > 1 || t.stride_h > 0) ? t.stride_h : (int64_t)L_c * st;
+  const int64_t sb = (B > 1 || t.stride_b > 0) ? t.stride_b : (int64_t)H_kv * sh;
+  if (st <= 0 || sh <= 0 || sb <= 0) return false;
+  cuuint64_t strides[3] = {(cuuint64_t)st * elem, (cuuint64_t)sh * elem, (cuuint64_t)sb * elem};
+  cuuint32_t box[4] = {elem == 2 ? 64u : (cuuint32_t)d, (cuuint32_t)box_tokens, 1, 1};
+  cuuint32_t estr[4] = {1, 1, 1, 1};
+  return g_encode(m, elem == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_UINT8, 4,
+                  const_cast<void*>(t.ptr), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  elem == 1 && d == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,
+                  CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// The map of a bf16 tensor, from the context's list of maps when it is there.
 bool get_tensor_map(ss_ctx* c, const ss_tensor& t, int B, int L_c, int box_tokens, CUtensorMap* out) {
   for (int i = 0; i < c->tm_n; ++i) {
     ss_ctx::TmEntry& e = c->tm[i];
@@ -186,22 +205,8 @@ bool get_tensor_map(ss_ctx* c, const ss_tensor& t, int B, int L_c, int box_token
       return true;
     }
   }
-  if (!g_encode) return false;
-  const int H_kv = c->cfg.H_kv, d = c->cfg.d;
-  cuuint64_t dims[4] = {(cuuint64_t)d, (cuuint64_t)L_c, (cuuint64_t)H_kv, (cuuint64_t)B};
-  // unused outer strides still have to be positive multiples of 16 bytes
-  const int64_t st = t.stride_t, sh = (H_kv > 1 || t.stride_h > 0) ? t.stride_h : (int64_t)L_c * st;
-  const int64_t sb = (B > 1 || t.stride_b > 0) ? t.stride_b : (int64_t)H_kv * sh;
-  if (st <= 0 || sh <= 0 || sb <= 0) return false;
-  cuuint64_t strides[3] = {(cuuint64_t)st * 2, (cuuint64_t)sh * 2, (cuuint64_t)sb * 2};
-  cuuint32_t box[4] = {64, (cuuint32_t)box_tokens, 1, 1};
-  cuuint32_t estr[4] = {1, 1, 1, 1};
   CUtensorMap m;
-  CUresult r = g_encode(&m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(t.ptr), dims,
-                        strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                        CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                        CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-  if (r != CUDA_SUCCESS) return false;
+  if (!encode_map(c, t, B, L_c, box_tokens, 2, &m)) return false;
   int slot = c->tm_n;
   if (c->tm_n < 64) {
     ++c->tm_n;
@@ -436,6 +441,7 @@ ss_status ss_create(ss_ctx** out, const ss_config* cfg, void* workspace, size_t 
   if (c->tc_ok) {
     e = ss::chunk_tc_prepare();
     if (e == cudaSuccess) e = ss::chunk_tc_keys_prepare();
+    if (e == cudaSuccess) e = ss::attn8_tc_prepare();
     if (e != cudaSuccess) {
       delete c;
       return SS_ERR_CUDA;
@@ -1299,8 +1305,20 @@ static ss_status attn8(ss_ctx* c, const ss_tensor& Q, int32_t B, int32_t T_q, fl
   p->T_q = T_q;
   p->R = T_q * c->G;
   p->d = c->cfg.d;
-  p->rows_per_tile = p->R < ss::kMinRows8 ? p->R : ss::kMinRows8;
-  p->row_tiles = (p->R + p->rows_per_tile - 1) / p->rows_per_tile;
+  // Tensor cores: a tile of 128 tokens is a dense range, part of a page, or a whole number of pages of 8
+  // tokens and more (a swizzle atom has 8 rows); other page sizes, and strides that a tensor map cannot
+  // hold, take the CUDA cores.
+  const int ps = cache->page_size;
+  bool tc = c->tc_ok && (!cache->page_table || ps % ss::kTok8 == 0 || (ps >= 8 && ss::kTok8 % ps == 0));
+  CUtensorMap tmK, tmV;
+  if (tc) {
+    const int box = cache->page_table && ps < ss::kTok8 ? ps : ss::kTok8;
+    tc = encode_map(c, cache->K, cache->n_pages, ps, box, 1, &tmK) &&
+         encode_map(c, cache->V, cache->n_pages, ps, box, 1, &tmV);
+  }
+  const int most = tc ? ss::kRows8 : ss::kMinRows8;  // rows per unit, evenly spread
+  p->row_tiles = (p->R + most - 1) / most;
+  p->rows_per_tile = (p->R + p->row_tiles - 1) / p->row_tiles;
   p->scale_log2 = scale * 1.4426950408889634f;
   p->min_tiles = 1;
   p->scratch = c->scratch8;
@@ -1308,9 +1326,9 @@ static ss_status attn8(ss_ctx* c, const ss_tensor& Q, int32_t B, int32_t T_q, fl
   p->status = c->status;
   DeviceGuard on(c->cfg.device);
   if (on.err != cudaSuccess) return cuda_fail(c, on.err);
-  const cudaError_t e = ss::launch_attn8_simt(*p, s, pdl);
+  const cudaError_t e = tc ? ss::launch_attn8_tc(*p, tmK, tmV, s, pdl) : ss::launch_attn8_simt(*p, s, pdl);
   if (e != cudaSuccess) return cuda_fail(c, e);
-  c->last_kernel = "kv8-simt";
+  c->last_kernel = tc ? "kv8-tcgen05" : "kv8-simt";
   ++c->launches;
   ++c->stats.chunk_calls;
   c->stats.kv_bytes += (int64_t)B * p->kv.room * c->cfg.H_kv * (c->cfg.d + 1) * 2;

@@ -69,6 +69,8 @@ struct Copy8Params {          // write (bf16 -> cache) and read (cache -> bf16)
 cudaError_t launch_kv8_write(const Copy8Params& p, cudaStream_t s);
 cudaError_t launch_kv8_read(const Copy8Params& p, cudaStream_t s);
 cudaError_t launch_attn8_simt(const Attn8Params& p, cudaStream_t s, bool pdl);
+cudaError_t launch_attn8_tc(const Attn8Params& p, const CUtensorMap& tmK, const CUtensorMap& tmV, cudaStream_t s, bool pdl);
+cudaError_t attn8_tc_prepare();  // one-time function attributes
 
 // ---- device side ---------------------------------------------------------------------------
 __device__ __forceinline__ float pow2_8(int e) { return __int_as_float((e + 127) << 23); }  // |e| <= 126

@@ -602,3 +602,16 @@ def test_a_generation_as_it_would_run():
         assert np.array_equal(Vr[b, :, :lens[b]].double().cpu().numpy(), want[b][1])
         assert (Kr[b, :, lens[b]:] == 0).all()
     ctx.close()
+
+
+@pytest.mark.parametrize("page,kernel", [(0, "kv8-tcgen05"), (8, "kv8-tcgen05"), (64, "kv8-tcgen05"), (256, "kv8-tcgen05"),
+                                         (4, "kv8-simt"), (24, "kv8-simt"), (192, "kv8-simt")])
+def test_which_kernel_runs(page, kernel):
+    ssb = _ssb()
+    cache = make_cache(ssb, 1, 2, 64, page, 500, 1)
+    Q = torch.randn(1, 4, 1, 64, generator=_gen(1)).bfloat16().to(DEV)
+    ctx = ssb.Context(1, 4, 2, 64, 1, 1, 1024)
+    O, LSE = decode(ssb, cache, Q, [500], ctx=ctx)
+    assert ctx.last_chunk_kernel() == kernel
+    check_attention(Q, O, LSE, lambda b: history(cache, b, 500), 64 ** -0.5)
+    ctx.close()
