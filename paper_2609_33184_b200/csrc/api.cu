@@ -1289,7 +1289,7 @@ ss_status ss_kv8_read(ss_ctx* c, const ss_cache8* cache, ss_tensor K, ss_tensor 
 
 // The attention launch that both entry points share; the caller has set where its result goes.
 static ss_status attn8(ss_ctx* c, const ss_tensor& Q, int32_t B, int32_t T_q, float scale, const ss_cache8* cache,
-                       const int32_t* valid_len, ss::Attn8Params* p, cudaStream_t s, bool pdl) {
+                       const int32_t* valid_len, ss::Attn8Params* p, cudaStream_t s) {
   const ss_status st = view8(c, cache, B, &p->kv);
   if (st != SS_OK) return st;
   if (p->kv.room > c->cfg.max_Lc) return SS_ERR_SHAPE;
@@ -1326,6 +1326,9 @@ static ss_status attn8(ss_ctx* c, const ss_tensor& Q, int32_t B, int32_t T_q, fl
   p->status = c->status;
   DeviceGuard on(c->cfg.device);
   if (on.err != cudaSuccess) return cuda_fail(c, on.err);
+  // Both kernels wait for the one in front of them before they touch anything, so they can always be
+  // launched under programmatic stream serialization (only launch and set-up overlap).
+  const bool pdl = !c->no_overlap;
   const cudaError_t e = tc ? ss::launch_attn8_tc(*p, tmK, tmV, s, pdl) : ss::launch_attn8_simt(*p, s, pdl);
   if (e != cudaSuccess) return cuda_fail(c, e);
   c->last_kernel = tc ? "kv8-tcgen05" : "kv8-simt";
@@ -1350,7 +1353,7 @@ ss_status ss_verify_chunk8(ss_ctx* c, const ss_cache8* cache, const int32_t* val
   p.part_ml = c->part_ml + (int64_t)c->n_sets * c->set_stride_ml;
   p.part_a = c->part_a + (int64_t)c->n_sets * c->set_stride_a;
   p.R_stride = c->R_stride;
-  st = attn8(c, c->Q, c->B, c->T_q, c->scale, cache, valid_len, &p, c->stream, use_pdl_first(c));
+  st = attn8(c, c->Q, c->B, c->T_q, c->scale, cache, valid_len, &p, c->stream);
   if (st != SS_OK) return st;
   c->splits[c->n_sets] = 1;
   memset(c->absent[c->n_sets], 0, sizeof(c->absent[0]));
@@ -1371,7 +1374,7 @@ ss_status ss_decode8(ss_ctx* c, ss_tensor Q, int32_t B, int32_t T_q, float scale
   memset(&p, 0, sizeof(p));
   p.O = (__nv_bfloat16*)O;
   p.LSE = LSE;
-  const ss_status st = attn8(c, Q, B, T_q, scale, cache, valid_len, &p, (cudaStream_t)stream, use_pdl_first(c));
+  const ss_status st = attn8(c, Q, B, T_q, scale, cache, valid_len, &p, (cudaStream_t)stream);
   if (st != SS_OK) return st;
   ++c->stats.rounds;
   c->stats.rows += (int64_t)B * c->cfg.H_q * T_q;

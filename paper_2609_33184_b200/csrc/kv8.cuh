@@ -244,7 +244,10 @@ __device__ __forceinline__ float* slot8(const Attn8Params& p, const Share8& s, l
 
 // By 128 threads, after each has stored its part of this CTA's state in its slot: takes the unit's
 // ticket and, for the last CTA, joins all states.  *flag is shared memory.
+constexpr int kJoin = 16;  // states of a row in flight
+template <int D>
 __device__ __forceinline__ void join8(const Attn8Params& p, const Share8& s, const Seg8& g, int tid, int* flag) {
+  constexpr int CPL = D / 32;
   const int i0 = share_of8(s.total, s.ctas, g.start), i1 = share_of8(s.total, s.ctas, g.start + g.n - 1);
   __threadfence();
   bar8(128);
@@ -256,25 +259,63 @@ __device__ __forceinline__ void join8(const Attn8Params& p, const Share8& s, con
   bar8(128);
   if (!*flag) return;
   __threadfence();
-  const int d = p.d, c = tid % d, r_step = 128 / d;
-  for (int r = tid / d; r < g.nrows; r += r_step) {
-    float m = -INFINITY, l = 0.f, a = 0.f;
-    for (int i = i0; i <= i1; ++i) {
-      const float2 st = __ldcg(reinterpret_cast<const float2*>(slot8(p, s, g.start, i)) + r);
-      if (st.y == 0.f) continue;
-      m = fmaxf(m, st.x);
+  // One warp per row: the states' (m, l) one per lane, their a[] in wide loads, many in flight (a
+  // state is a read of L2; one after the other they took 120 us for 37 states of 4 rows).
+  const int lane = tid & 31, n = i1 - i0 + 1;
+  for (int r = tid >> 5; r < g.nrows; r += 4) {
+    float m = -INFINITY;
+    for (int i = lane; i < n; i += 32) {
+      const float2 st = __ldcg(reinterpret_cast<const float2*>(slot8(p, s, g.start, i0 + i)) + r);
+      if (st.y != 0.f) m = fmaxf(m, st.x);
     }
-    for (int i = i0; i <= i1; ++i) {
-      const float* slot = slot8(p, s, g.start, i);
-      const float2 st = __ldcg(reinterpret_cast<const float2*>(slot) + r);
-      const float x = __ldcg(slot + 2 * p.rows_per_tile + r * d + c);
-      if (st.y == 0.f) continue;
-      const float w = st.x == m ? 1.f : exp2f(st.x - m);
-      l = fmaf(w, st.y, l);
-      a = fmaf(w, x, a);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    float l = 0.f, a[CPL];
+#pragma unroll
+    for (int c = 0; c < CPL; ++c) a[c] = 0.f;
+    for (int base = 0; base < n; base += 32) {
+      float w = 0.f;
+      if (base + lane < n) {
+        const float2 st = __ldcg(reinterpret_cast<const float2*>(slot8(p, s, g.start, i0 + base + lane)) + r);
+        if (st.y != 0.f) {  // (else an empty state, whose a[] is not read)
+          w = st.x == m ? 1.f : exp2f(st.x - m);
+          l = fmaf(w, st.y, l);
+        }
+      }
+      const int cnt = min(32, n - base);
+#pragma unroll 1
+      for (int j0 = 0; j0 < cnt; j0 += kJoin) {
+        float wj[kJoin], v[kJoin][CPL];
+#pragma unroll
+        for (int u = 0; u < kJoin; ++u) {
+          wj[u] = __shfl_sync(0xffffffffu, w, (j0 + u) & 31);
+#pragma unroll
+          for (int c = 0; c < CPL; ++c) v[u][c] = 0.f;
+          if (j0 + u < cnt && wj[u] != 0.f) {
+            const float* x = slot8(p, s, g.start, i0 + base + j0 + u) + 2 * p.rows_per_tile + r * (CPL * 32) + lane * CPL;
+            const float2 lo = __ldcg(reinterpret_cast<const float2*>(x));
+            v[u][0] = lo.x;
+            v[u][1] = lo.y;
+            if (CPL == 4) {
+              const float2 hi = __ldcg(reinterpret_cast<const float2*>(x + 2));
+              v[u][CPL - 2] = hi.x;
+              v[u][CPL - 1] = hi.y;
+            }
+          } else {
+            wj[u] = 0.f;
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < kJoin; ++u)
+#pragma unroll
+          for (int c = 0; c < CPL; ++c) a[c] = fmaf(wj[u], v[u][c], a[c]);
+      }
     }
-    if (c == 0) put_ml8(p, g, r, m, l);
-    put_a8(p, g, r, c, l, a);
+#pragma unroll
+    for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+    if (lane == 0) put_ml8(p, g, r, m, l);
+#pragma unroll
+    for (int c = 0; c < CPL; ++c) put_a8(p, g, r, lane * CPL + c, l, a[c]);
   }
 }
 

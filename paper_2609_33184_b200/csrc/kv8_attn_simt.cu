@@ -177,7 +177,7 @@ __global__ void __launch_bounds__(128) attn8_simt_kernel(const __grid_constant__
         slot[2 * p.rows_per_tile + r * D + c] = A;
       }
     }
-    if (!whole) join8(p, share, g, tid, &flag);
+    if (!whole) join8<D>(p, share, g, tid, &flag);
   }
 }
 

@@ -605,7 +605,7 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
         }
       }
       tc_fence_before();
-      if (!whole) join8(p, share, done, tid, &ctl->last);
+      if (!whole) join8<D>(p, share, done, tid, &ctl->last);
       bar8(128);  // sums, references and Q may be written anew
     }
   }
