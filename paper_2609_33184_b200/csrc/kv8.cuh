@@ -233,7 +233,10 @@ __device__ __forceinline__ void put_empty8(const Attn8Params& p, int tid, int n)
   }
 }
 
-__device__ __forceinline__ void bar8(int n) { asm volatile("bar.sync 1, %0;" ::"r"(n) : "memory"); }
+template <int N>
+__device__ __forceinline__ void bar8() {
+  asm volatile("bar.sync 1, %0;" ::"n"(N) : "memory");
+}
 
 // Slot of CTA i's state of the unit that begins at tile `start` (first CTA i0): the first segment of a
 // share uses the CTA's even slot, a later one (always the last) the odd slot.
@@ -242,80 +245,108 @@ __device__ __forceinline__ float* slot8(const Attn8Params& p, const Share8& s, l
   return p.scratch + (int64_t)(2 * i + odd) * p.rows_per_tile * (p.d + 2);
 }
 
-// By 128 threads, after each has stored its part of this CTA's state in its slot: takes the unit's
-// ticket and, for the last CTA, joins all states.  *flag is shared memory.
-constexpr int kJoin = 16;  // states of a row in flight
-template <int D>
-__device__ __forceinline__ void join8(const Attn8Params& p, const Share8& s, const Seg8& g, int tid, int* flag) {
-  constexpr int CPL = D / 32;
+// sum over the unit's n states of weight * a[c] for ROWS rows from r on, ROWS * STATES loads in flight
+template <int D, int ROWS, int STATES, int STEP>
+__device__ __forceinline__ void join_rows8(const Attn8Params& p, const Seg8& g, const float* first, const float* rest,
+                                           const float2* w, int block, int r0, int r, int n, int c) {
+  const int64_t slot = (int64_t)p.rows_per_tile * (D + 2);
+  float a[ROWS];
+#pragma unroll
+  for (int k = 0; k < ROWS; ++k) a[k] = 0.f;
+#pragma unroll 1
+  for (int j0 = 0; j0 < n; j0 += STATES) {
+    float v[STATES][ROWS], f[STATES][ROWS];
+#pragma unroll
+    for (int j = 0; j < STATES; ++j) {
+#pragma unroll
+      for (int k = 0; k < ROWS; ++k) {
+        const int row = r + k * STEP;
+        f[j][k] = (j0 + j < n && row < block) ? w[(j0 + j) * block + row].x : 0.f;
+        v[j][k] = 0.f;
+        if (f[j][k] != 0.f) {  // (a state of weight 0 may be unwritten)
+          const float* src = j0 + j == 0 ? first : rest + (int64_t)(j0 + j - 1) * 2 * slot;
+          v[j][k] = __ldcg(src + 2 * p.rows_per_tile + (r0 + row) * D + c);
+        }
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < STATES; ++j)
+#pragma unroll
+      for (int k = 0; k < ROWS; ++k) a[k] = fmaf(f[j][k], v[j][k], a[k]);
+  }
+#pragma unroll
+  for (int k = 0; k < ROWS; ++k) {
+    const int row = r + k * STEP;
+    if (row < block) put_a8(p, g, r0 + row, c, w[n * block + row].y, a[k]);
+  }
+}
+
+// By N threads (128 or 256), after each has stored its part of this CTA's state in its slot: takes the
+// unit's ticket and, for the last CTA, joins all states.  *flag and buf (kJoinBuf8 pairs) are shared
+// memory.  A read of another CTA's state is a read of L2, so all of a block of rows' (m, l) are fetched at once,
+// then their a[] with 2048 loads in flight: one row and state after the other, the join
+// took 120 us for 37 states of 4 rows.
+constexpr int kJoinBuf8 = 512;
+static_assert(kCtas8 + 1 <= kJoinBuf8, "a row's states fit the buffer");
+template <int D, int N>
+__device__ __noinline__ void join8(const Attn8Params& p, const Share8& s, const Seg8& g, int tid, int* flag, float2* buf) {
   const int i0 = share_of8(s.total, s.ctas, g.start), i1 = share_of8(s.total, s.ctas, g.start + g.n - 1);
   __threadfence();
-  bar8(128);
+  bar8<N>();
   if (tid == 0) {
     const int last = atomicAdd(&p.tickets[g.unit], 1u) == (unsigned)(i1 - i0);
     if (last) p.tickets[g.unit] = 0;  // nobody else touches it any more in this launch
     *flag = last;
   }
-  bar8(128);
+  bar8<N>();
   if (!*flag) return;
   __threadfence();
-  // One warp per row: the states' (m, l) one per lane, their a[] in wide loads, many in flight (a
-  // state is a read of L2; one after the other they took 120 us for 37 states of 4 rows).
-  const int lane = tid & 31, n = i1 - i0 + 1;
-  for (int r = tid >> 5; r < g.nrows; r += 4) {
-    float m = -INFINITY;
-    for (int i = lane; i < n; i += 32) {
-      const float2 st = __ldcg(reinterpret_cast<const float2*>(slot8(p, s, g.start, i0 + i)) + r);
-      if (st.y != 0.f) m = fmaxf(m, st.x);
+  const int n = i1 - i0 + 1;               // >= 2: the unit is cut
+  const float* first = slot8(p, s, g.start, i0);
+  const float* rest = slot8(p, s, g.start, i0 + 1);   // those after the first are the CTAs' even slots
+  const int64_t slot = (int64_t)p.rows_per_tile * (D + 2);
+  const int most = kJoinBuf8 / (n + 1);  // rows at a time, >= 1: n <= kCtas8
+  for (int r0 = 0; r0 < g.nrows; r0 += most) {
+    const int block = min(most, g.nrows - r0);
+    for (int f = tid; f < n * block; f += N) {
+      const int j = f / block, r = f - j * block;
+      const float* src = j == 0 ? first : rest + (int64_t)(j - 1) * 2 * slot;
+      buf[f] = __ldcg(reinterpret_cast<const float2*>(src) + r0 + r);
     }
-#pragma unroll
-    for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    float l = 0.f, a[CPL];
-#pragma unroll
-    for (int c = 0; c < CPL; ++c) a[c] = 0.f;
-    for (int base = 0; base < n; base += 32) {
-      float w = 0.f;
-      if (base + lane < n) {
-        const float2 st = __ldcg(reinterpret_cast<const float2*>(slot8(p, s, g.start, i0 + base + lane)) + r);
-        if (st.y != 0.f) {  // (else an empty state, whose a[] is not read)
-          w = st.x == m ? 1.f : exp2f(st.x - m);
-          l = fmaf(w, st.y, l);
-        }
+    bar8<N>();
+    // eight lanes per row: maximum, weights, sum (left in entry n of the row)
+    for (int rr = tid >> 3; rr < (block + N / 8 - 1) / (N / 8) * (N / 8); rr += N / 8) {
+      const int r = min(rr, block - 1), part = tid & 7;
+      const bool mine = rr < block;
+      float m = -INFINITY, l = 0.f;
+      for (int j = part; j < n; j += 8) {
+        const float2 st = buf[j * block + r];
+        if (st.y != 0.f) m = fmaxf(m, st.x);
       }
-      const int cnt = min(32, n - base);
-#pragma unroll 1
-      for (int j0 = 0; j0 < cnt; j0 += kJoin) {
-        float wj[kJoin], v[kJoin][CPL];
 #pragma unroll
-        for (int u = 0; u < kJoin; ++u) {
-          wj[u] = __shfl_sync(0xffffffffu, w, (j0 + u) & 31);
+      for (int o = 4; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+      for (int j = part; j < n; j += 8) {
+        const float2 st = buf[j * block + r];
+        const float w = st.y == 0.f ? 0.f : st.x == m ? 1.f : exp2f(st.x - m);  // (an empty state's a[] is not read)
+        l = fmaf(w, st.y, l);
+        if (mine) buf[j * block + r].x = w;
+      }
 #pragma unroll
-          for (int c = 0; c < CPL; ++c) v[u][c] = 0.f;
-          if (j0 + u < cnt && wj[u] != 0.f) {
-            const float* x = slot8(p, s, g.start, i0 + base + j0 + u) + 2 * p.rows_per_tile + r * (CPL * 32) + lane * CPL;
-            const float2 lo = __ldcg(reinterpret_cast<const float2*>(x));
-            v[u][0] = lo.x;
-            v[u][1] = lo.y;
-            if (CPL == 4) {
-              const float2 hi = __ldcg(reinterpret_cast<const float2*>(x + 2));
-              v[u][CPL - 2] = hi.x;
-              v[u][CPL - 1] = hi.y;
-            }
-          } else {
-            wj[u] = 0.f;
-          }
-        }
-#pragma unroll
-        for (int u = 0; u < kJoin; ++u)
-#pragma unroll
-          for (int c = 0; c < CPL; ++c) a[c] = fmaf(wj[u], v[u][c], a[c]);
+      for (int o = 4; o; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+      if (mine && part == 0) {
+        buf[n * block + r].y = l;
+        put_ml8(p, g, r0 + r, m, l);
       }
     }
-#pragma unroll
-    for (int o = 16; o; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
-    if (lane == 0) put_ml8(p, g, r, m, l);
-#pragma unroll
-    for (int c = 0; c < CPL; ++c) put_a8(p, g, r, lane * CPL + c, l, a[c]);
+    bar8<N>();
+    constexpr int G = N / D;  // rows side by side
+    const int c = tid % D, r = tid / D;
+    if (block <= 4 * G) {
+      join_rows8<D, 4, 2048 / N / 4, G>(p, g, first, rest, buf, block, r0, r, n, c);
+    } else {
+      for (int k = r; k < block; k += 8 * G) join_rows8<D, 8, 2048 / N / 8, G>(p, g, first, rest, buf, block, r0, k, n, c);
+    }
+    bar8<N>();
   }
 }
 

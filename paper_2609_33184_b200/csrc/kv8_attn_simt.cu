@@ -36,7 +36,8 @@ template <int D>
 __global__ void __launch_bounds__(128) attn8_simt_kernel(const __grid_constant__ Attn8Params p) {
   constexpr int CPL = D / 32;  // head dims per lane in the output
   __shared__ __align__(16) float q_s[kRT][D];
-  __shared__ float w_s[4][32][kRT];
+  __shared__ __align__(16) float w_s[4][32][kRT];  // (also the join's buffer)
+  static_assert(sizeof(w_s) >= kJoinBuf8 * sizeof(float2), "join buffer");
   __shared__ float2 ml_s[4][kRT];
   __shared__ float a_s[4][kRT][D];
   __shared__ int flag;
@@ -177,7 +178,7 @@ __global__ void __launch_bounds__(128) attn8_simt_kernel(const __grid_constant__
         slot[2 * p.rows_per_tile + r * D + c] = A;
       }
     }
-    if (!whole) join8<D>(p, share, g, tid, &flag);
+    if (!whole) join8<D, 128>(p, share, g, tid, &flag, reinterpret_cast<float2*>(w_s));
   }
 }
 

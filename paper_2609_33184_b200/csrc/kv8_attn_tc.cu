@@ -5,23 +5,26 @@
 //   O^T = V^T P^T  M = 128 head dims,        N = rows, K = 128 keys  (4 steps, e4m3 x e5m2)
 //
 // as in the bf16 kernel with the keys on M; tcgen05.mma kind::f8f6f4 takes both operands in 8 bits, so
-// Q and P are split into terms of 8 bits that stand side by side on the N axis (tensor work is not
-// what bounds this kernel: an MMA reads its 4 KB of A in 32 cycles and needs fewer for the maths):
-//  * Q row * 2^-eq (maximum in [128, 256)) = hi + lo / 16, both e4m3.  bf16 has 8 significant bits
-//    and a term holds 4, so the split is exact down to 2^-14 of the row's maximum, off by at most
-//    2^-22 of it below.  The score is (S_hi + S_lo / 16) * 2^eq * 2^ek * scale: all factors powers of two
-//    but the caller's, the sums in fp32.
+// Q and P are split into terms of 8 bits whose products add up in the accumulators (tensor work is not
+// what bounds this kernel):
+//  * Q row * 2^-eq (maximum in (224, 448]) = hi + lo, both e4m3.  bf16 has 8 significant bits and a term
+//    holds 4, so the split is exact down to 2^-13 of the row's maximum, off by at most 2^-17 of it below.
+//    The score is S * 2^eq * 2^ek * scale: all factors powers of two but the caller's, the sums in fp32.
 //  * weights.  x = s2 + ev - M + 7 with s2 the score in base 2, ev the key's value exponent, M the row's
-//    reference; P = 2^x multiplies the codes of V directly.  P as f16 is cut into hi + mid / 8 + lo / 64
-//    of e5m2, three bits each (the upper byte of an f16 IS an e5m2: the cut is a byte permutation, the
-//    rest an exact f16 subtraction), relative error <= 2^-9 like a bf16 P.  e5m2 and not e4m3 for its
-//    range: a weight keeps its 9 bits down to 2^-21 of the row's reference and vanishes below 2^-30, so
-//    a sink token of large weight does not swallow the 10^5 small ones whose weights add up.
+//    reference; P = 2^x multiplies the codes of V directly.  P as f16 is cut into hi + mid / 8 + lo / 64 of
+//    e5m2, three bits each (the upper byte of an f16 IS an e5m2: the cut is a byte permutation, the rest
+//    an exact f16 subtraction), relative error <= 2^-9.  e5m2 and not e4m3 for its range: a weight keeps
+//    its 9 bits down to 2^-21 of the row's reference and is off by at most 2^-30 of it below, so a sink
+//    token of large weight does not swallow the 10^5 small ones whose weights add up.
 //  * the row sum adds P * 2^-ev, unrounded, in fp32 (ev in [-32, 80], see kv8.cuh).
-// M is raised lazily (exact maximum of the first tile; later only when some x exceeds 15, so P <= 2^15).
+// The terms of P stand side by side on the N axis (one pass of the MMA over V); those of Q too for up to
+// 8 rows, and for more rows as further steps along K (the scores then take half the registers).
+// M is raised lazily (exact maximum of the first tile; later only when some x exceeds 15, so P <= 2^15:
+// eight binades of room, since one raise stops all rows of the CTA; with two binades - and unscaled terms, one
+// instruction less per weight - every second tile of a 32-row round raised, 281 -> 438 us).
 //
-// A CTA walks its share of the tiles (kv8.cuh): 4 softmax warps (thread = key of the tile in the
-// scores, head dim in the output), one TMA producer warp, one MMA issuer warp.  The producer runs
+// A CTA walks its share of the tiles (kv8.cuh): 4 softmax warps per 16 rows (thread = key of the tile in
+// the scores, head dim in the output), one TMA producer warp, one MMA issuer warp.  The producer runs
 // ahead across segment ends, so a new segment finds its first tiles in shared memory.  Two CTAs per
 // SM (at most 110 KB shared memory, 256 TMEM columns each) hide each other's segment ends.
 // Every wait is bounded; on expiry the CTA raises SS_DEV_WAIT_EXPIRED and leaves its tickets in order.
@@ -45,17 +48,24 @@ struct alignas(16) Ctl8 {
   volatile uint32_t abort;
   volatile uint32_t flag[3];
   int last;
+  int has[2];                     // the softmax warps' current and next segment (in use by turns)
+  Seg8 seg[2];
+  Share8 share;
   alignas(16) float nm[NR];       // bias - M
   alignas(16) float qf[NR];       // 2^eq * scale * log2(e)
   alignas(16) float smax[4][NR];  // per warp: maxima of a tile; at a segment's end the row sums
 };
 
-template <int NR, int D>
+// NR = rows, WG = softmax warpgroups (each takes NR / WG rows), D = head dim.
+template <int NR, int WG, int D>
 struct Cfg8 {
+  static constexpr int kSoft = 128 * WG, kThreads = kSoft + 64;
+  static constexpr int RT = NR / WG;                       // rows per softmax thread
+  static constexpr bool kSideBySide = NR == 8;             // Q's terms on the N axis
   static constexpr int kUnitBytes = kTok8 * D;             // one K or V tile
-  static constexpr int NS = 2 * NR;                        // score columns
+  static constexpr int NS = kSideBySide ? 2 * NR : NR;     // score columns
   static constexpr int NP = (3 * NR + 15) / 16 * 16;       // weight columns
-  static constexpr int kQBytes = NS * D;
+  static constexpr int kQBytes = 2 * NR * D;
   static constexpr int kPBytes = kTok8 * NP;
   static constexpr int kCtlBytes = (sizeof(Ctl8<NR>) + 127) / 128 * 128;
   static constexpr int kRest = (kQBytes + 1023) / 1024 * 1024 + kPBytes + kCtlBytes;
@@ -71,10 +81,9 @@ struct Cfg8 {
   static constexpr int kCols = 2 * NS + NP;
   static constexpr uint32_t kTmemCols = kCols <= 64 ? 64 : kCols <= 128 ? 128 : 256;
   static constexpr uint32_t kColO = 2 * NS;
-  static_assert(kUnits >= 4 && kCols <= 256, "shape");
+  static_assert(kUnits >= 4 && kCols <= 256 && RT % 8 == 0, "shape");
+  static_assert(kPBytes >= (int)(kJoinBuf8 * sizeof(float2)), "the join's buffer lies over the weights");
 };
-
-constexpr int kThreads8 = 192;
 
 __device__ __forceinline__ void mma8(uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
@@ -110,23 +119,52 @@ __device__ __forceinline__ float redux_max(float v) {
 __device__ __forceinline__ uint32_t h2_bits(__half2 h) { return *reinterpret_cast<uint32_t*>(&h); }
 __device__ __forceinline__ __half2 bits_h2(uint32_t u) { return *reinterpret_cast<__half2*>(&u); }
 
-// Two values of a weight pair's residue: (w - cut) * 8 with cut = w's upper bytes, exact in f16.
+// What a pair of weights leaves when its upper bytes are cut off, times 8, exact in f16.
 __device__ __forceinline__ uint32_t residue(uint32_t w) {
   return h2_bits(__hmul2(__hsub2(bits_h2(w), bits_h2(w & 0xff00ff00u)), __float2half2_rn(8.f)));
 }
+// Bounded wait: one try in line, the loop out of line.  A wait that gives up (or finds that another has)
+// returns like one that succeeded: what follows works on whatever is there, inside the CTA's own memory,
+// and only waits, tickets and barriers matter until the CTA leaves.
+__device__ __noinline__ void wait_slow(uint64_t* bar, uint32_t parity, volatile uint32_t* abort, uint32_t* status) {
+  if (*abort == 0) mbar_wait_abortable(bar, parity, abort, status);
+}
+__device__ __forceinline__ void wait8(uint64_t* bar, uint32_t parity, volatile uint32_t* abort, uint32_t* status) {
+  if (!mbar_try_wait(bar, parity)) wait_slow(bar, parity, abort, status);
+  __syncwarp();
+}
 
-template <int NR, int D>
-__global__ void __launch_bounds__(kThreads8, 2)
+// columns [col, col + N) of the calling warp's TMEM lanes
+template <int N>
+__device__ __forceinline__ void tmem_ld(uint32_t taddr, uint32_t* r) {
+  static_assert(N == 8 || N == 16, "columns");
+  if (N == 16) {
+    tmem_ld16(taddr, *reinterpret_cast<uint32_t(*)[16]>(r));
+  } else {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                 : "r"(taddr)
+                 : "memory");
+  }
+}
+template <int N>
+__device__ __forceinline__ void tmem_st(uint32_t taddr, const uint32_t* r) {
+  if (N == 16) tmem_st16(taddr, *reinterpret_cast<const uint32_t(*)[16]>(r));
+  else tmem_st8(taddr, *reinterpret_cast<const uint32_t(*)[8]>(r));
+}
+
+template <int NR, int WG, int D>
+__global__ void __launch_bounds__(Cfg8<NR, WG, D>::kThreads, 2)
 attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ CUtensorMap tmK,
                 const __grid_constant__ CUtensorMap tmV) {
-  using C = Cfg8<NR, D>;
-  constexpr int UNITS = C::kUnits, NS = C::NS, NP = C::NP;
+  using C = Cfg8<NR, WG, D>;
+  constexpr int UNITS = C::kUnits, NS = C::NS, NP = C::NP, RT = C::RT, SOFT = C::kSoft;
   extern __shared__ __align__(1024) uint8_t smem[];
   Ctl8<NR>* ctl = reinterpret_cast<Ctl8<NR>*>(smem + C::kOffCtl);
   uint8_t* q_s = smem + C::kOffQ;
   uint8_t* p_s = smem + C::kOffP;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  constexpr int kProducerWarp = 4, kMmaWarp = 5;
+  constexpr int kProducerWarp = 4 * WG, kMmaWarp = 4 * WG + 1;
 
   if (warp == kProducerWarp) {
     if (lane == 0) {
@@ -138,9 +176,9 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
       }
       mbar_init(&ctl->sfull[0], 1);
       mbar_init(&ctl->sfull[1], 1);
-      mbar_init(&ctl->pready, 128);
+      mbar_init(&ctl->pready, SOFT);
       mbar_init(&ctl->pfree, 1);
-      mbar_init(&ctl->qfull, 128);
+      mbar_init(&ctl->qfull, SOFT);
       ctl->abort = 0;
       ctl->flag[0] = ctl->flag[1] = ctl->flag[2] = 0;
       fence_barrier_init();
@@ -156,17 +194,22 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
                  : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
-  const Share8 share = find_share8(p);
+  if (warp == 0) {
+    const Share8 share = find_share8(p);
+    if (lane == 0) {
+      long long base;
+      ctl->share = share;
+      ctl->has[0] = seg_first8(p, share, &base, &ctl->seg[0]);
+    }
+  }
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = ctl->tmem_base;
+  const Share8& share = ctl->share;
   auto mwait = [&](uint64_t* bar, uint32_t parity) {
     return mbar_wait_abortable(bar, parity, &ctl->abort, p.status);
   };
-  long long base;
-  Seg8 g;
-  bool more = seg_first8(p, share, &base, &g);
 
   if (warp == kProducerWarp) {
     // ===== TMA producer =====
@@ -180,7 +223,9 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
     const bool mine = lane < kTok8 / ps;
     int j = 0;
     bool ok = true;
-    for (; more && ok; more = seg_next8(p, share, &base, &g)) {
+    long long base;
+    Seg8 g;
+    for (bool more = seg_first8(p, share, &base, &g); more && ok; more = seg_next8(p, share, &base, &g)) {
       int inner = 0, outer = 0;
       auto look = [&](int t) {  // this lane's page of tile t
         const int tok = t * kTok8 + lane * ps;
@@ -221,7 +266,9 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
     const uint32_t ring = smem_u32(smem), q_addr = smem_u32(q_s), p_addr = smem_u32(p_s);
     int it0 = 0, seg = 0;  // tiles and segments before this one
     bool ok = true;
-    for (; more && ok; more = seg_next8(p, share, &base, &g), ++seg) {
+    long long base;
+    Seg8 g;
+    for (bool more = seg_first8(p, share, &base, &g); more && ok; more = seg_next8(p, share, &base, &g), ++seg) {
       const int n = g.t1 - g.t0;
       int qi = 0, pi = 0;
       bool q_there = false;
@@ -237,8 +284,11 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
             const uint32_t k_addr = ring + (jk % UNITS) * C::kUnitBytes;
             if (leader) {
 #pragma unroll
-              for (int kk = 0; kk < D / 32; ++kk)
-                mma8(tmem + (it & 1) * NS, desc8<D>(k_addr + kk * 32, 16), desc8<D>(q_addr + kk * 32, 16), idesc_qk, kk > 0);
+              for (int term = 0; term < (C::kSideBySide ? 1 : 2); ++term)
+#pragma unroll
+                for (int kk = 0; kk < D / 32; ++kk)
+                  mma8(tmem + (it & 1) * NS, desc8<D>(k_addr + kk * 32, 16),
+                       desc8<D>(q_addr + term * NR * D + kk * 32, 16), idesc_qk, term > 0 || kk > 0);
               tc_commit(&ctl->uempty[jk % UNITS]);
               tc_commit(&ctl->sfull[it & 1]);
             }
@@ -249,6 +299,10 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
         }
         if (pi < qi) {
           const int it = it0 + pi, jv = 2 * it + 1;
+          // with the scores two tiles ahead nothing but this can go: sleep on it instead of polling
+          if (qi == n || qi == pi + 2) ok = mwait(&ctl->pready, it & 1) && mwait(&ctl->ufull[jv % UNITS], (jv / UNITS) & 1);
+          ok = __all_sync(0xffffffffu, ok);
+          if (!ok) break;
           if (__all_sync(0xffffffffu, mbar_test(&ctl->pready, it & 1) &&
                                           mbar_test(&ctl->ufull[jv % UNITS], (jv / UNITS) & 1))) {
             tc_fence_after();
@@ -285,18 +339,14 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
     }
   } else {
     // ===== softmax warps =====
-    // A wait that gives up makes the warp `dead`: it keeps walking the segments, barriers and tickets,
-    // so nobody is left waiting, and touches nothing else.
-    const uint32_t lane_off = (uint32_t)(warp * 32) << 16;
-    bool dead = false;
-    auto wait = [&](uint64_t* bar, uint32_t parity) {
-      if (!dead && !mwait(bar, parity)) dead = true;
-      dead = __any_sync(0xffffffffu, dead);
-    };
-    put_empty8(p, tid, 128);
+    const int quad = warp & 3, key = quad * 32 + lane;       // TMEM lane: key of a tile, head dim of the output
+    const int c0 = (warp >> 2) * RT;                         // this thread's rows: [c0, c0 + RT)
+    const uint32_t lane_off = (uint32_t)(quad * 32) << 16;
+    auto wait = [&](uint64_t* bar, uint32_t parity) { wait8(bar, parity, &ctl->abort, p.status); };
+    put_empty8(p, tid, SOFT);
 
-    // Q: 128 / NR threads per row, kE values each
-    constexpr int TPR = 128 / NR, kE = D / TPR, kQL = kE / 4;
+    // Q: SOFT / NR threads per row, kE values each
+    constexpr int TPR = SOFT / NR, kE = D / TPR, kQL = kE / 4;
     const int q_row = tid / TPR, q_part = tid % TPR;
     uint2 q_raw[kQL];
     auto q_load = [&](const Seg8& s) {
@@ -307,227 +357,241 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
         q_raw[i] = q_row < s.nrows ? *reinterpret_cast<const uint2*>(src + i * 4) : make_uint2(0, 0);
     };
     auto q_store = [&]() {
-      uint32_t w[2 * kQL], top = 0;
-#pragma unroll
-      for (int i = 0; i < kQL; ++i) {
-        w[2 * i] = q_raw[i].x;
-        w[2 * i + 1] = q_raw[i].y;
-      }
+      uint32_t top = 0;
 #pragma unroll
       for (int i = 0; i < 2 * kQL; ++i) {
-        const uint32_t a = w[i] & 0x7fffu, b = (w[i] >> 16) & 0x7fffu;
+        const uint32_t w = i & 1 ? q_raw[i / 2].y : q_raw[i / 2].x, a = w & 0x7fffu, b = (w >> 16) & 0x7fffu;
         if (a < 0x7f80u) top = max(top, a);
         if (b < 0x7f80u) top = max(top, b);
       }
 #pragma unroll
       for (int o = TPR / 2; o; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
-      const int eq = max(-100, min(119, (int)(top >> 7) - 127 - 7));  // |q| * 2^-eq < 256
+      // smallest eq with |q| <= 448 * 2^eq
+      const int eq = max(-100, min(119, (int)(top >> 7) - 127 - 8 + ((top & 127u) > 96u ? 1 : 0)));
       const float inv = pow2_8(-eq);
-      uint32_t hi[kE / 4], lo[kE / 4];
 #pragma unroll
       for (int i = 0; i < kE / 4; ++i) {
-        uint32_t h4 = 0, l4 = 0;
+        uint32_t term[2] = {0, 0};
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-          const uint32_t two = w[2 * i + k];
-          // (an infinite or NaN query makes its scores NaN)
+          const uint32_t two = k ? q_raw[i].y : q_raw[i].x;
           float2 v = make_float2(__uint_as_float(two << 16) * inv, __uint_as_float(two & 0xffff0000u) * inv);
+          // (an infinite or NaN query makes its scores NaN)
           if ((two & 0x7f80u) == 0x7f80u) v.x = __int_as_float(0x7fffffff);
           if ((two & 0x7f800000u) == 0x7f800000u) v.y = __int_as_float(0x7fffffff);
           const uint32_t c = __nv_cvt_float2_to_fp8x2(v, __NV_SATFINITE, __NV_E4M3);
           const __half2_raw hr = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)c, __NV_E4M3);
           const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&hr));
-          const uint32_t r = __nv_cvt_float2_to_fp8x2(make_float2((v.x - back.x) * 16.f, (v.y - back.y) * 16.f),
-                                                      __NV_SATFINITE, __NV_E4M3);
-          h4 |= c << (16 * k);
-          l4 |= r << (16 * k);
+          term[0] |= c << (16 * k);
+          term[1] |= (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(v.x - back.x, v.y - back.y), __NV_SATFINITE, __NV_E4M3)
+                     << (16 * k);
         }
-        hi[i] = h4;
-        lo[i] = l4;
-      }
-      // operand row n, 16-byte piece c at n * D + ((c ^ swizzle(n)) * 16); rows r and r + 8 of a group of
-      // 16 hold hi and lo of the same query row
-      const int n = 16 * (q_row / 8) + q_row % 8;
+        // operand row nn, 16-byte piece c at nn * D + ((c ^ swizzle(nn)) * 16); the lo rows follow the hi rows
 #pragma unroll
-      for (int term = 0; term < 2; ++term) {
-        const int nn = n + 8 * term;
-        const int sw = D == 128 ? (nn & 7) : ((nn >> 1) & 3);
-#pragma unroll
-        for (int i = 0; i < kE / 4; ++i) {
-          const int byte = q_part * kE + i * 4;
-          *reinterpret_cast<uint32_t*>(q_s + nn * D + (((byte >> 4) ^ sw) << 4) + (byte & 15)) = term ? lo[i] : hi[i];
+        for (int k = 0; k < 2; ++k) {
+          const int nn = q_row + k * NR, sw = D == 128 ? (nn & 7) : ((nn >> 1) & 3), byte = q_part * kE + i * 4;
+          *reinterpret_cast<uint32_t*>(q_s + nn * D + (((byte >> 4) ^ sw) << 4) + (byte & 15)) = term[k];
         }
       }
-      if (q_part == 0) ctl->qf[q_row] = pow2_8(eq) * p.scale_log2;
+      if (q_part == 0) {
+        ctl->qf[q_row] = pow2_8(eq) * p.scale_log2;
+        ctl->nm[q_row] = 0.f;
+      }
       fence_proxy_async();
       mbar_arrive(&ctl->qfull);
     };
 
-    // Scale bytes of this thread's key, fetched a tile ahead (and its page id two tiles ahead).
-    struct Ahead {
-      int outer, inner;      // where the key of the tile after next lives
-      uint32_t ek, ev;       // bytes of the next tile's key
-    } ah;
+    // Scale bytes of this thread's key, fetched a tile ahead (and its page id two tiles ahead).  Small
+    // pages: the key's place in its page is the same in every tile.
+    const bool paged = p.kv.page_table != nullptr, small = paged && p.kv.page_size < kTok8;
+    const int per_tile = small ? kTok8 / p.kv.page_size : 1;             // pages per tile
+    const int page_tiles = paged && !small ? p.kv.page_size / kTok8 : 1; // tiles per page
+    const int key_page = small ? key / p.kv.page_size : 0, key_in = small ? key % p.kv.page_size : key;
+    int ah_id = -1, ah_inner = 0;      // page (dense: request) of the key of the tile after next, as loaded
+    int ah_page = 0, ah_sub = 0;       // large pages: page of that tile, its tile within the page
+    uint32_t ah_ek = 127, ah_ev = 127; // bytes of the next tile's key
     auto ah_look = [&](const Seg8& s, int t) {
-      const int tok = t * kTok8 + tid;
-      ah.outer = -1;
-      ah.inner = 0;
-      if (t < s.t1 && tok < s.len) ah.outer = outer8(p.kv, s.b, tok, &ah.inner);
-    };
-    auto ah_fetch = [&](const Seg8& s) {
-      ah.ek = ah.ev = 127;   // (a key that is not there, or in a page outside the pool: value 0)
-      if (ah.outer >= 0) {
-        ah.ek = p.kv.Ks[ah.outer * p.kv.ks_sb + s.kvh * p.kv.ks_sh + ah.inner * p.kv.ks_st];
-        ah.ev = p.kv.Vs[ah.outer * p.kv.vs_sb + s.kvh * p.kv.vs_sh + ah.inner * p.kv.vs_st];
+      ah_id = -1;
+      if (t < s.t1 && t * kTok8 + key < s.len) {
+        if (!paged) {
+          ah_id = s.b;
+          ah_inner = t * kTok8 + key;
+        } else {
+          const int pg = small ? t * per_tile + key_page : ah_page;
+          ah_inner = small ? key_in : ah_sub * kTok8 + key;
+          ah_id = p.kv.page_table[(int64_t)s.b * p.kv.pages_per_req + pg];
+        }
+      }
+      if (++ah_sub == page_tiles) {
+        ah_sub = 0;
+        ++ah_page;
       }
     };
-    if (more) {
-      ah_look(g, g.t0);
-      q_load(g);
-      ah_fetch(g);
-      ah_look(g, g.t0 + 1);
-    }
+    auto ah_fetch = [&](const Seg8& s) {
+      ah_ek = ah_ev = 127;   // (a key that is not there, or in a page outside the pool: value 0)
+      if ((uint32_t)ah_id < (uint32_t)p.kv.n_outer) {
+        ah_ek = p.kv.Ks[ah_id * p.kv.ks_sb + s.kvh * p.kv.ks_sh + ah_inner * p.kv.ks_st];
+        ah_ev = p.kv.Vs[ah_id * p.kv.vs_sb + s.kvh * p.kv.vs_sh + ah_inner * p.kv.vs_st];
+      }
+    };
+    auto seg_fetch = [&](const Seg8& s) {
+      ah_page = s.t0 / page_tiles;
+      ah_sub = s.t0 - ah_page * page_tiles;
+      ah_look(s, s.t0);
+      q_load(s);
+      ah_fetch(s);
+      ah_look(s, s.t0 + 1);
+    };
+    if (ctl->has[0]) seg_fetch(ctl->seg[0]);
+    long long base = share.base0;  // (thread 0: tiles before the request of the segment it looks up)
+    auto top4 = [&](int r) {
+      return fmaxf(fmaxf(ctl->smax[0][r], ctl->smax[1][r]), fmaxf(ctl->smax[2][r], ctl->smax[3][r]));
+    };
 
     int it = 0;
-    while (more) {
+    for (int k_seg = 0; ctl->has[k_seg & 1]; ++k_seg) {
+      const Seg8& g = ctl->seg[k_seg & 1];
+      const int t0 = g.t0, t1 = g.t1, len = g.len;
+      if (tid == 0) {  // the next segment, read by everybody after this one's tiles
+        Seg8 s = g;
+        ctl->has[(k_seg + 1) & 1] = seg_next8(p, share, &base, &s);
+        ctl->seg[(k_seg + 1) & 1] = s;
+      }
       q_store();
-      float2 lsum[NR / 2];
+      bar8<SOFT>();  // (factors and references)
+      float2 lsum[RT / 2];
 #pragma unroll
-      for (int r = 0; r < NR / 2; ++r) lsum[r] = make_float2(0.f, 0.f);
-      for (int t = g.t0; t < g.t1; ++t, ++it) {
-        const float kf = scale8(ah.ek), evf = (float)(int)ah.ev - 127.f, vinv = scale8(254u - ah.ev);
+      for (int r = 0; r < RT / 2; ++r) lsum[r] = make_float2(0.f, 0.f);
+      for (int t = t0; t < t1; ++t, ++it) {
+        const float kf = scale8(ah_ek), evf = (float)(int)ah_ev - 127.f, vinv = scale8(254u - ah_ev);
         ah_fetch(g);
         ah_look(g, t + 2);
-        const int n_valid = min(kTok8, g.len - t * kTok8);
-        const bool key_ok = tid < n_valid;
+        const int n_valid = min(kTok8, len - t * kTok8);
+        const bool key_ok = key < n_valid, first = t == t0;
         wait(&ctl->sfull[it & 1], (it >> 1) & 1);
         tc_fence_after();
         if (n_valid < kTok8) {
           // tokens past the length may hold anything; their weights are 0, so V must be finite there
           const int jv = 2 * it + 1;
           wait(&ctl->ufull[jv % UNITS], (jv / UNITS) & 1);
-          if (!dead) {
-            uint4* v = reinterpret_cast<uint4*>(smem + (jv % UNITS) * C::kUnitBytes);
-            for (int i = n_valid * (D / 16) + tid; i < kTok8 * (D / 16); i += 128) v[i] = make_uint4(0, 0, 0, 0);
-          }
+          uint4* v = reinterpret_cast<uint4*>(smem + (jv % UNITS) * C::kUnitBytes);
+          for (int i = n_valid * (D / 16) + tid; i < kTok8 * (D / 16); i += SOFT) v[i] = make_uint4(0, 0, 0, 0);
         }
-        // x[r] = s2 + ev (first tile) or s2 + ev - M + bias
-        float x[NR];
-        const bool first = t == g.t0;
-        if (!dead) {
+        // x[r] = s2 + ev - M + bias (in the segment's first tile s2 + ev)
+        float2 x[RT / 2];
+        {
+          const float2 kf2 = make_float2(kf, kf), ev2 = make_float2(evf, evf);
+          const uint32_t t_s = tmem + lane_off + (it & 1) * NS + c0;
 #pragma unroll
-          for (int q = 0; q < NR / 8; ++q) {
+          for (int r0 = 0; r0 < RT; r0 += 16) {
             uint32_t raw[16];
-            tmem_ld16(tmem + lane_off + (it & 1) * NS + q * 16, raw);
+            if (C::kSideBySide || RT >= 16) tmem_ld<16>(t_s + r0, raw);
+            else tmem_ld<8>(t_s, raw);
             tc_wait_ld();
 #pragma unroll
-            for (int c = 0; c < 8; c += 4) {
-              const float4 qf = *reinterpret_cast<const float4*>(&ctl->qf[q * 8 + c]);
-              float4 nm = make_float4(0.f, 0.f, 0.f, 0.f);
-              if (!first) nm = *reinterpret_cast<const float4*>(&ctl->nm[q * 8 + c]);
-              const float qs[4] = {qf.x, qf.y, qf.z, qf.w}, ns[4] = {nm.x, nm.y, nm.z, nm.w};
-#pragma unroll
-              for (int k = 0; k < 4; k += 2) {
-                const float2 hi = make_float2(__uint_as_float(raw[c + k]), __uint_as_float(raw[c + k + 1]));
-                const float2 lo = make_float2(__uint_as_float(raw[8 + c + k]), __uint_as_float(raw[8 + c + k + 1]));
-                const float2 s = mul2_f(fma2_f(lo, make_float2(0.0625f, 0.0625f), hi), make_float2(qs[k], qs[k + 1]));
-                const float2 y = fma2_f(s, make_float2(kf, kf), add2_f(make_float2(ns[k], ns[k + 1]), make_float2(evf, evf)));
-                x[q * 8 + c + k] = y.x;
-                x[q * 8 + c + k + 1] = y.y;
+            for (int r = r0; r < RT && r < r0 + 16; r += 4) {
+              const float4 qf = *reinterpret_cast<const float4*>(&ctl->qf[c0 + r]);
+              const float4 nm = *reinterpret_cast<const float4*>(&ctl->nm[c0 + r]);
+              float2 s0 = make_float2(__uint_as_float(raw[r - r0]), __uint_as_float(raw[r - r0 + 1]));
+              float2 s1 = make_float2(__uint_as_float(raw[r - r0 + 2]), __uint_as_float(raw[r - r0 + 3]));
+              if (C::kSideBySide) {
+                s0 = add2_f(s0, make_float2(__uint_as_float(raw[8 + r]), __uint_as_float(raw[8 + r + 1])));
+                s1 = add2_f(s1, make_float2(__uint_as_float(raw[8 + r + 2]), __uint_as_float(raw[8 + r + 3])));
               }
+              x[r / 2] = fma2_f(mul2_f(s0, make_float2(qf.x, qf.y)), kf2, add2_f(make_float2(nm.x, nm.y), ev2));
+              x[r / 2 + 1] = fma2_f(mul2_f(s1, make_float2(qf.z, qf.w)), kf2, add2_f(make_float2(nm.z, nm.w), ev2));
             }
           }
         }
-        auto tile_max = [&]() {  // exact maxima of x over the tile's keys, all four warps
-          if (!dead) {
-            float mine = -INFINITY;
-#pragma unroll
-            for (int r = 0; r < NR; ++r) {
-              const float m = redux_max(key_ok ? x[r] : -INFINITY);
-              if (lane == r) mine = m;
-            }
-            if (lane < NR) ctl->smax[warp][lane] = mine;
-          }
-          bar8(128);
-        };
-        auto top4 = [&](int r) {
-          return fmaxf(fmaxf(ctl->smax[0][r], ctl->smax[1][r]), fmaxf(ctl->smax[2][r], ctl->smax[3][r]));
-        };
-        if (first) {
-          tile_max();
-          if (!dead) {
-#pragma unroll
-            for (int r = 0; r < NR; ++r) x[r] += kBias - top4(r);
-            if (tid < NR) ctl->nm[tid] = kBias - top4(tid);  // (read from the next tile on)
-          }
-          if (tid == 0) ctl->flag[(it + 1) % 3] = 0;
-          bar8(128);
-        } else {
+        {
           float mx = -INFINITY;
-          if (!dead) {
 #pragma unroll
-            for (int r = 0; r < NR; r += 2) mx = max3_f(mx, x[r], x[r + 1]);
-          }
+          for (int r = 0; r < RT / 2; ++r) mx = max3_f(mx, x[r].x, x[r].y);
           if (tid == 0) ctl->flag[(it + 1) % 3] = 0;
           if (__any_sync(0xffffffffu, key_ok && mx > kOver) && lane == 0) ctl->flag[it % 3] = 1;
-          bar8(128);
-          if (ctl->flag[it % 3]) {
-            // ---- raise the references to the exact maxima: rescale O^T and the row sums (rare) ----
-            tile_max();
+        }
+        bar8<SOFT>();
+        if (first || ctl->flag[it % 3]) {
+          // ---- set the references to the exact maxima; later in a segment (rare) raise them, which
+          // rescales O^T and the row sums ----
+          float mine = -INFINITY;
+#pragma unroll
+          for (int r = 0; r < RT; ++r) {
+            const float m = redux_max(key_ok ? (r & 1 ? x[r / 2].y : x[r / 2].x) : -INFINITY);
+            if (lane == r) mine = m;
+          }
+          if (lane < RT) ctl->smax[quad][c0 + lane] = mine;
+          bar8<SOFT>();
+          // M rises by this much (in the first tile, from 0 to the maximum - bias)
+          auto rise = [&](int r) { return first ? top4(r) - kBias : fmaxf(0.f, top4(r) - kBias); };
+          if (!first) {
             wait(&ctl->pfree, (it - 1) & 1);  // the output MMAs of the tile before have retired
             tc_fence_after();
-            if (!dead) {
-#pragma unroll
-              for (int r = 0; r < NR; ++r) {
-                const float up = fmaxf(0.f, top4(r) - kBias);  // M rises by this much
-                x[r] -= up;
-                if (r & 1) lsum[r / 2].y *= ex2_ftz(-up);
-                else lsum[r / 2].x *= ex2_ftz(-up);
-              }
-#pragma unroll
-              for (int q = 0; q < NP / 16; ++q) {
-                uint32_t o[16];
-                tmem_ld16(tmem + lane_off + C::kColO + q * 16, o);
+#pragma unroll 1
+            for (int k = 0; k < 3; ++k) {     // the three terms' accumulators of this thread's rows
+#pragma unroll 1
+              for (int r = 0; r < RT; r += 8) {
+                uint32_t o[8];
+                const uint32_t at = tmem + lane_off + C::kColO + k * NR + c0 + r;
+                tmem_ld<8>(at, o);
                 tc_wait_ld();
 #pragma unroll
-                for (int c = 0; c < 16; ++c)
-                  o[c] = __float_as_uint(__uint_as_float(o[c]) * ex2_ftz(-fmaxf(0.f, top4((q * 16 + c) % NR) - kBias)));
-                tmem_st16(tmem + lane_off + C::kColO + q * 16, o);
+                for (int c = 0; c < 8; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * ex2_ftz(-rise(c0 + r + c)));
+                tmem_st<8>(at, o);
               }
-              tc_wait_st();
             }
-            bar8(128);
-            if (tid < NR && !dead) ctl->nm[tid] -= fmaxf(0.f, top4(tid) - kBias);
-            bar8(128);
+            tc_wait_st();
           }
+#pragma unroll
+          for (int r = 0; r < RT / 2; ++r) {
+            const float2 up = make_float2(rise(c0 + 2 * r), rise(c0 + 2 * r + 1));
+            x[r] = add2_f(x[r], make_float2(-up.x, -up.y));
+            if (!first) lsum[r] = mul2_f(lsum[r], make_float2(ex2_ftz(-up.x), ex2_ftz(-up.y)));
+          }
+          bar8<SOFT>();
+          if (tid < NR) ctl->nm[tid] -= rise(tid);
+          bar8<SOFT>();
         }
-        if (it > 0 && !first) wait(&ctl->pfree, (it - 1) & 1);  // P^T has been consumed
-        if (!dead) {
-          uint32_t w[NR / 2];
+        if (!first) wait(&ctl->pfree, (it - 1) & 1);  // P^T has been consumed
+        {
+          const float2 vinv2 = make_float2(vinv, vinv);
+          // columns term * NR + row, 16 to a 16-byte piece per key
 #pragma unroll
-          for (int r = 0; r < NR; r += 2) {
-            float2 e = make_float2(ex2_ftz(x[r]), ex2_ftz(x[r + 1]));
-            if (n_valid < kTok8) e = key_ok ? e : make_float2(0.f, 0.f);
-            lsum[r / 2] = fma2_f(e, make_float2(vinv, vinv), lsum[r / 2]);
-            w[r / 2] = h2_bits(__float22half2_rn(e));
+          for (int r = 0; r < RT; r += 16) {
+            constexpr int W = RT < 16 ? RT / 4 : 4;  // words of 4 rows
+            uint32_t piece[3][4];
+#pragma unroll
+            for (int q = 0; q < W; ++q) {
+              uint32_t w[2];
+#pragma unroll
+              for (int k = 0; k < 2; ++k) {
+                const int i = r / 2 + 2 * q + k;
+                float2 e = make_float2(ex2_ftz(x[i].x), ex2_ftz(x[i].y));
+                if (n_valid < kTok8) e = key_ok ? e : make_float2(0.f, 0.f);
+                lsum[i] = fma2_f(e, vinv2, lsum[i]);
+                w[k] = h2_bits(__float22half2_rn(e));
+              }
+              const uint32_t a1 = residue(w[0]), b1 = residue(w[1]);
+              piece[0][q] = __byte_perm(w[0], w[1], 0x7531);
+              piece[1][q] = __byte_perm(a1, b1, 0x7531);
+              // (the last term rounds)
+              piece[2][q] = __byte_perm(residue(a1) + 0x00800080u, residue(b1) + 0x00800080u, 0x7531);
+            }
+            if (RT >= 16) {
+#pragma unroll
+              for (int k = 0; k < 3; ++k)
+                *reinterpret_cast<uint4*>(p_s + (k * NR + c0 + r) / 16 * (kTok8 * 16) + key * 16) =
+                    make_uint4(piece[k][0], piece[k][1], piece[k][2], piece[k][3]);
+            } else if (NR == 8) {  // hi | mid, lo | nothing
+              *reinterpret_cast<uint4*>(p_s + key * 16) = make_uint4(piece[0][0], piece[0][1], piece[1][0], piece[1][1]);
+              *reinterpret_cast<uint4*>(p_s + kTok8 * 16 + key * 16) = make_uint4(piece[2][0], piece[2][1], 0, 0);
+            } else {
+#pragma unroll
+              for (int k = 0; k < 3; ++k)
+                *reinterpret_cast<uint2*>(p_s + (k * NR + c0) / 16 * (kTok8 * 16) + key * 16 + (k * NR + c0) % 16) =
+                    make_uint2(piece[k][0], piece[k][1]);
+            }
           }
-          // columns term * NR + r, 16 to a 16-byte piece per key
-          uint32_t piece[NP / 4];
-#pragma unroll
-          for (int c = 0; c < NP / 4; ++c) piece[c] = 0;
-#pragma unroll
-          for (int r = 0; r < NR; r += 4) {
-            const uint32_t a = w[r / 2], b = w[r / 2 + 1];
-            const uint32_t a1 = residue(a), b1 = residue(b);
-            const uint32_t a2 = residue(a1) + 0x00800080u, b2 = residue(b1) + 0x00800080u;  // (the last term rounds)
-            piece[r / 4] = __byte_perm(a, b, 0x7531);
-            piece[(NR + r) / 4] = __byte_perm(a1, b1, 0x7531);
-            piece[(2 * NR + r) / 4] = __byte_perm(a2, b2, 0x7531);
-          }
-#pragma unroll
-          for (int q = 0; q < NP / 16; ++q)
-            *reinterpret_cast<uint4*>(p_s + q * (kTok8 * 16) + tid * 16) =
-                make_uint4(piece[4 * q], piece[4 * q + 1], piece[4 * q + 2], piece[4 * q + 3]);
           fence_proxy_async();
           tc_fence_before();
         }
@@ -535,27 +599,21 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
       }
 
       // ---- the segment's end: what the next one needs is fetched first ----
-      const Seg8 done = g;
-      more = seg_next8(p, share, &base, &g);
-      if (more) {
-        ah_look(g, g.t0);
-        q_load(g);
-        ah_fetch(g);
-        ah_look(g, g.t0 + 1);
-      }
-      // row sums: halve the rows a lane holds at every step, lane / (32 / NR) is the row in the end
+      const Seg8& done = g;
+      if (ctl->has[(k_seg + 1) & 1]) seg_fetch(ctl->seg[(k_seg + 1) & 1]);
+      // row sums: halve the rows a lane holds at every step, lane / (32 / RT) is the row in the end
       {
-        float v[NR];
+        float v[RT];
 #pragma unroll
-        for (int r = 0; r < NR; ++r) v[r] = (r & 1) ? lsum[r / 2].y : lsum[r / 2].x;
-        int n = NR;
+        for (int r = 0; r < RT; ++r) v[r] = (r & 1) ? lsum[r / 2].y : lsum[r / 2].x;
+        int n = RT;
 #pragma unroll
         for (int o = 16; o; o >>= 1) {
           if (n > 1) {
             n /= 2;
             const bool up = lane & o;
 #pragma unroll
-            for (int i = 0; i < NR / 2; ++i) {
+            for (int i = 0; i < RT / 2; ++i) {
               if (i < n) {
                 const float send = up ? v[i] : v[i + n], keep = up ? v[i + n] : v[i];
                 v[i] = keep + __shfl_xor_sync(0xffffffffu, send, o);
@@ -565,48 +623,42 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
             v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
           }
         }
-        bar8(128);  // (every thread is done with smax as maxima)
-        if (lane % (32 / NR) == 0) ctl->smax[warp][lane / (32 / NR)] = v[0];
+        bar8<SOFT>();  // (every thread is done with smax as maxima)
+        if (lane % (32 / RT) == 0) ctl->smax[quad][c0 + lane / (32 / RT)] = v[0];
       }
       wait(&ctl->pfree, (it - 1) & 1);
       tc_fence_after();
-      bar8(128);
+      bar8<SOFT>();
       const bool whole = done.t0 == 0 && done.t1 == done.n;
       float* slot = slot8(p, share, done.start, blockIdx.x);
-      const float (*sums)[NR] = ctl->smax;
-      auto row_l = [&](int r) { return (sums[0][r] + sums[1][r]) + (sums[2][r] + sums[3][r]); };
-      if (!dead) {
+      auto row_l = [&](int r) { return (ctl->smax[0][r] + ctl->smax[1][r]) + (ctl->smax[2][r] + ctl->smax[3][r]); };
+      {
         if (tid < done.nrows) {
           const float m = -ctl->nm[tid], l = row_l(tid);  // the sums are of 2^(s2 - M + bias)
           if (whole) put_ml8(p, done, tid, m, l);
           else reinterpret_cast<float2*>(slot)[tid] = make_float2(m, l);
         }
-#pragma unroll
-        for (int q = 0; q < NR / 8; ++q) {
+#pragma unroll 1
+        for (int q = 0; q < RT; q += 8) {
           uint32_t o[3][8];
 #pragma unroll
-          for (int k = 0; k < 3; ++k)
-            asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                         : "=r"(o[k][0]), "=r"(o[k][1]), "=r"(o[k][2]), "=r"(o[k][3]), "=r"(o[k][4]), "=r"(o[k][5]),
-                           "=r"(o[k][6]), "=r"(o[k][7])
-                         : "r"(tmem + lane_off + C::kColO + k * NR + q * 8)
-                         : "memory");
+          for (int k = 0; k < 3; ++k) tmem_ld<8>(tmem + lane_off + C::kColO + k * NR + c0 + q, o[k]);
           tc_wait_ld();
 #pragma unroll
           for (int c = 0; c < 8; ++c) {
-            const int r = q * 8 + c;
-            if (r < done.nrows && tid < D) {
+            const int r = c0 + q + c;
+            if (r < done.nrows && key < D) {
               const float a = fmaf(__uint_as_float(o[2][c]), 1.f / 64.f,
                                    fmaf(__uint_as_float(o[1][c]), 0.125f, __uint_as_float(o[0][c])));
-              if (whole) put_a8(p, done, r, tid, row_l(r), a);
-              else slot[2 * p.rows_per_tile + r * D + tid] = a;
+              if (whole) put_a8(p, done, r, key, row_l(r), a);
+              else slot[2 * p.rows_per_tile + r * D + key] = a;
             }
           }
         }
       }
       tc_fence_before();
-      if (!whole) join8<D>(p, share, done, tid, &ctl->last);
-      bar8(128);  // sums, references and Q may be written anew
+      if (!whole) join8<D, SOFT>(p, share, done, tid, &ctl->last, reinterpret_cast<float2*>(p_s));
+      bar8<SOFT>();  // sums, references and Q may be written anew
     }
   }
 
@@ -616,34 +668,37 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(C::kTmemCols) : "memory");
 }
 
-template <int NR, int D>
+template <int NR, int WG, int D>
 cudaError_t prepare8() {
-  return cudaFuncSetAttribute(attn8_tc_kernel<NR, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg8<NR, D>::kSmem);
+  return cudaFuncSetAttribute(attn8_tc_kernel<NR, WG, D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              Cfg8<NR, WG, D>::kSmem);
 }
-template <int NR, int D>
+template <int NR, int WG, int D>
 cudaError_t launch8(const Attn8Params& p, const CUtensorMap& tmK, const CUtensorMap& tmV, cudaStream_t s, bool pdl) {
-  return launch_kernel(attn8_tc_kernel<NR, D>, dim3(kCtas8), dim3(kThreads8), Cfg8<NR, D>::kSmem, s, pdl, p, tmK, tmV);
+  using C = Cfg8<NR, WG, D>;
+  return launch_kernel(attn8_tc_kernel<NR, WG, D>, dim3(kCtas8), dim3(C::kThreads), C::kSmem, s, pdl, p, tmK, tmV);
+}
+template <int D>
+cudaError_t launch_rows(const Attn8Params& p, const CUtensorMap& tmK, const CUtensorMap& tmV, cudaStream_t s, bool pdl) {
+  if (p.rows_per_tile <= 8) return launch8<8, 1, D>(p, tmK, tmV, s, pdl);
+  if (p.rows_per_tile <= 16) return launch8<16, 1, D>(p, tmK, tmV, s, pdl);
+  return launch8<32, 1, D>(p, tmK, tmV, s, pdl);
 }
 
 }  // namespace
 
 cudaError_t attn8_tc_prepare() {
-  cudaError_t e = prepare8<8, 128>();
-  if (e == cudaSuccess) e = prepare8<16, 128>();
-  if (e == cudaSuccess) e = prepare8<32, 128>();
-  if (e == cudaSuccess) e = prepare8<8, 64>();
-  if (e == cudaSuccess) e = prepare8<16, 64>();
-  if (e == cudaSuccess) e = prepare8<32, 64>();
+  cudaError_t e = prepare8<8, 1, 128>();
+  if (e == cudaSuccess) e = prepare8<16, 1, 128>();
+  if (e == cudaSuccess) e = prepare8<32, 1, 128>();
+  if (e == cudaSuccess) e = prepare8<8, 1, 64>();
+  if (e == cudaSuccess) e = prepare8<16, 1, 64>();
+  if (e == cudaSuccess) e = prepare8<32, 1, 64>();
   return e;
 }
 
 cudaError_t launch_attn8_tc(const Attn8Params& p, const CUtensorMap& tmK, const CUtensorMap& tmV, cudaStream_t s, bool pdl) {
-  const int rows = p.rows_per_tile;
-  if (p.d == 128)
-    return rows <= 8 ? launch8<8, 128>(p, tmK, tmV, s, pdl)
-                     : rows <= 16 ? launch8<16, 128>(p, tmK, tmV, s, pdl) : launch8<32, 128>(p, tmK, tmV, s, pdl);
-  return rows <= 8 ? launch8<8, 64>(p, tmK, tmV, s, pdl)
-                   : rows <= 16 ? launch8<16, 64>(p, tmK, tmV, s, pdl) : launch8<32, 64>(p, tmK, tmV, s, pdl);
+  return p.d == 128 ? launch_rows<128>(p, tmK, tmV, s, pdl) : launch_rows<64>(p, tmK, tmV, s, pdl);
 }
 
 }  // namespace ss
