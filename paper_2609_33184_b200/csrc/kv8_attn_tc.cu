@@ -104,13 +104,6 @@ __device__ __forceinline__ uint64_t desc8(uint32_t saddr, uint32_t lbo) {
   return (uint64_t)((saddr >> 4) & 0x3FFF) | ((uint64_t)(lbo >> 4) << 16) | ((uint64_t)((8 * D) >> 4) << 32) |
          (1ull << 46) | ((D == 128 ? 2ull : 4ull) << 61);
 }
-__device__ __forceinline__ float2 mul2_f(float2 a, float2 b) {
-  uint64_t d;
-  asm("mul.rn.f32x2 %0, %1, %2;"
-      : "=l"(d)
-      : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)));
-  return reinterpret_cast<float2&>(d);
-}
 __device__ __forceinline__ float redux_max(float v) {
   float r;
   asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
@@ -495,20 +488,26 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
               float2 s0 = make_float2(__uint_as_float(raw[r - r0]), __uint_as_float(raw[r - r0 + 1]));
               float2 s1 = make_float2(__uint_as_float(raw[r - r0 + 2]), __uint_as_float(raw[r - r0 + 3]));
               if (C::kSideBySide) {
-                s0 = add2_f(s0, make_float2(__uint_as_float(raw[8 + r]), __uint_as_float(raw[8 + r + 1])));
-                s1 = add2_f(s1, make_float2(__uint_as_float(raw[8 + r + 2]), __uint_as_float(raw[8 + r + 3])));
+                s0 = __fadd2_rn(s0, make_float2(__uint_as_float(raw[8 + r]), __uint_as_float(raw[8 + r + 1])));
+                s1 = __fadd2_rn(s1, make_float2(__uint_as_float(raw[8 + r + 2]), __uint_as_float(raw[8 + r + 3])));
               }
-              x[r / 2] = fma2_f(mul2_f(s0, make_float2(qf.x, qf.y)), kf2, add2_f(make_float2(nm.x, nm.y), ev2));
-              x[r / 2 + 1] = fma2_f(mul2_f(s1, make_float2(qf.z, qf.w)), kf2, add2_f(make_float2(nm.z, nm.w), ev2));
+              x[r / 2] = __ffma2_rn(__fmul2_rn(s0, make_float2(qf.x, qf.y)), kf2, __fadd2_rn(make_float2(nm.x, nm.y), ev2));
+              x[r / 2 + 1] = __ffma2_rn(__fmul2_rn(s1, make_float2(qf.z, qf.w)), kf2, __fadd2_rn(make_float2(nm.z, nm.w), ev2));
             }
           }
+        }
+        if (n_valid < kTok8) {
+          __syncwarp();  // (kept a branch: as selects it costs every tile an instruction per score)
+#pragma unroll
+          for (int r = 0; r < RT / 2; ++r)
+            if (!key_ok) x[r] = make_float2(-INFINITY, -INFINITY);
         }
         {
           float mx = -INFINITY;
 #pragma unroll
           for (int r = 0; r < RT / 2; ++r) mx = max3_f(mx, x[r].x, x[r].y);
           if (tid == 0) ctl->flag[(it + 1) % 3] = 0;
-          if (__any_sync(0xffffffffu, key_ok && mx > kOver) && lane == 0) ctl->flag[it % 3] = 1;
+          if (__any_sync(0xffffffffu, mx > kOver) && lane == 0) ctl->flag[it % 3] = 1;
         }
         bar8<SOFT>();
         if (first || ctl->flag[it % 3]) {
@@ -517,7 +516,7 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
           float mine = -INFINITY;
 #pragma unroll
           for (int r = 0; r < RT; ++r) {
-            const float m = redux_max(key_ok ? (r & 1 ? x[r / 2].y : x[r / 2].x) : -INFINITY);
+            const float m = redux_max(r & 1 ? x[r / 2].y : x[r / 2].x);
             if (lane == r) mine = m;
           }
           if (lane < RT) ctl->smax[quad][c0 + lane] = mine;
@@ -545,8 +544,8 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
 #pragma unroll
           for (int r = 0; r < RT / 2; ++r) {
             const float2 up = make_float2(rise(c0 + 2 * r), rise(c0 + 2 * r + 1));
-            x[r] = add2_f(x[r], make_float2(-up.x, -up.y));
-            if (!first) lsum[r] = mul2_f(lsum[r], make_float2(ex2_ftz(-up.x), ex2_ftz(-up.y)));
+            x[r] = __fadd2_rn(x[r], make_float2(-up.x, -up.y));
+            if (!first) lsum[r] = __fmul2_rn(lsum[r], make_float2(ex2_ftz(-up.x), ex2_ftz(-up.y)));
           }
           bar8<SOFT>();
           if (tid < NR) ctl->nm[tid] -= rise(tid);
@@ -566,9 +565,8 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
 #pragma unroll
               for (int k = 0; k < 2; ++k) {
                 const int i = r / 2 + 2 * q + k;
-                float2 e = make_float2(ex2_ftz(x[i].x), ex2_ftz(x[i].y));
-                if (n_valid < kTok8) e = key_ok ? e : make_float2(0.f, 0.f);
-                lsum[i] = fma2_f(e, vinv2, lsum[i]);
+                const float2 e = make_float2(ex2_ftz(x[i].x), ex2_ftz(x[i].y));
+                lsum[i] = __ffma2_rn(e, vinv2, lsum[i]);
                 w[k] = h2_bits(__float22half2_rn(e));
               }
               const uint32_t a1 = residue(w[0]), b1 = residue(w[1]);
