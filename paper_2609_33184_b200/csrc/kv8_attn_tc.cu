@@ -46,7 +46,6 @@ struct alignas(16) Ctl8 {
   uint64_t sfull[2], pready, pfree, qfull;
   uint32_t tmem_base;
   volatile uint32_t abort;
-  volatile uint32_t flag[3];
   int last;
   int has[2];                     // the softmax warps' current and next segment (in use by turns)
   Seg8 seg[2];
@@ -85,11 +84,15 @@ struct Cfg8 {
   static_assert(kPBytes >= (int)(kJoinBuf8 * sizeof(float2)), "the join's buffer lies over the weights");
 };
 
-__device__ __forceinline__ void mma8(uint32_t d_tmem, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+// A descriptor's low word holds the address / 16 (and the LBO above it), so the operands of the steps of
+// a tile differ by an addition there; the high word is the same for all.
+__device__ __forceinline__ void mma8(uint32_t d_tmem, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi,
+                                     uint32_t idesc, uint32_t accumulate) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
-      "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+      "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+      "mov.b64 a, {%1, %2};\n\tmov.b64 b, {%3, %4};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], a, b, %5, p;\n\t}" ::"r"(d_tmem),
+      "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate)
       : "memory");
 }
 // kind::f8f6f4 -> fp32: format 0 = e4m3, 1 = e5m2
@@ -108,6 +111,18 @@ __device__ __forceinline__ float redux_max(float v) {
   float r;
   asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
   return r;
+}
+// Barrier of the softmax warps that also ORs a flag over their threads.
+template <int N>
+__device__ __forceinline__ bool bar_or8(bool mine) {
+  uint32_t any;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 q, %1, 0;\n\t"
+      "bar.red.or.pred p, 1, %2, q;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(any)
+      : "r"((uint32_t)mine), "n"(N)
+      : "memory");
+  return any != 0;
 }
 __device__ __forceinline__ uint32_t h2_bits(__half2 h) { return *reinterpret_cast<uint32_t*>(&h); }
 __device__ __forceinline__ __half2 bits_h2(uint32_t u) { return *reinterpret_cast<__half2*>(&u); }
@@ -173,7 +188,6 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
       mbar_init(&ctl->pfree, 1);
       mbar_init(&ctl->qfull, SOFT);
       ctl->abort = 0;
-      ctl->flag[0] = ctl->flag[1] = ctl->flag[2] = 0;
       fence_barrier_init();
     }
   }
@@ -214,7 +228,8 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
     const bool small = p.kv.page_table && p.kv.page_size < kTok8;
     const int ps = small ? p.kv.page_size : kTok8;
     const bool mine = lane < kTok8 / ps;
-    int j = 0;
+    int j = 0, u = 0;      // units filled so far, the next one's place in the ring
+    uint32_t ph = 1;       // parity of its release
     bool ok = true;
     long long base;
     Seg8 g;
@@ -232,16 +247,22 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
       look(g.t0);
       for (int t = g.t0; t < g.t1 && ok; ++t) {
         for (int kv = 0; kv < 2; ++kv, ++j) {
-          const int u = j % UNITS;
           int go = 1;
           if (lane == 0) {
-            go = mwait(&ctl->uempty[u], ((j / UNITS) & 1) ^ 1);
+            go = mwait(&ctl->uempty[u], ph);
             if (go) mbar_expect_tx(&ctl->ufull[u], C::kUnitBytes);
           }
           ok = __shfl_sync(0xffffffffu, go, 0);  // (also orders the arming before the copies)
           if (!ok) break;
           const uint32_t dst = smem_u32(smem + u * C::kUnitBytes) + lane * ps * D;
-          if (mine) tma_load_4d(dst, kv ? &tmV : &tmK, 0, inner, g.kvh, outer, &ctl->ufull[u], pol);
+          if (mine) {
+            if (kv) tma_load_4d(dst, &tmV, 0, inner, g.kvh, outer, &ctl->ufull[u], pol);
+            else tma_load_4d(dst, &tmK, 0, inner, g.kvh, outer, &ctl->ufull[u], pol);
+          }
+          if (++u == UNITS) {
+            u = 0;
+            ph ^= 1;
+          }
         }
         look(t + 1);
       }
@@ -256,7 +277,21 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
     // ===== MMA issuer: polls for whichever of its two next operations can go =====
     constexpr uint32_t idesc_qk = idesc8(NS, 0, false), idesc_pv = idesc8(NP, 1, true);
     const bool leader = elect_one();
-    const uint32_t ring = smem_u32(smem), q_addr = smem_u32(q_s), p_addr = smem_u32(p_s);
+    const uint64_t k_desc = desc8<D>(smem_u32(smem), 16), v_desc = desc8<D>(smem_u32(smem), C::kUnitBytes),
+                   q_desc = desc8<D>(smem_u32(q_s), 16), p_desc = desc_mnmajor_plain(smem_u32(p_s), 128, kTok8 * 16);
+    const uint32_t k_lo = (uint32_t)k_desc, v_lo = (uint32_t)v_desc, q_lo = (uint32_t)q_desc, p_lo = (uint32_t)p_desc;
+    const uint32_t k_hi = (uint32_t)(k_desc >> 32), v_hi = (uint32_t)(v_desc >> 32), q_hi = (uint32_t)(q_desc >> 32),
+                   p_hi = (uint32_t)(p_desc >> 32);
+    // ring positions of the next score MMAs' K and of the next output MMAs' V, with their phases
+    int uk = 0, uv = 1;
+    uint32_t phk = 0, phv = 0;
+    auto step = [&](int& u, uint32_t& ph) {
+      u += 2;
+      if (u >= UNITS) {
+        u -= UNITS;
+        ph ^= 1;
+      }
+    };
     int it0 = 0, seg = 0;  // tiles and segments before this one
     bool ok = true;
     long long base;
@@ -270,45 +305,49 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
       while (pi < n) {
         bool did = false;
         if (qi < n && qi < pi + 2) {
-          const int it = it0 + qi, jk = 2 * it;
+          const int it = it0 + qi;
           if (!q_there) q_there = __all_sync(0xffffffffu, mbar_test(&ctl->qfull, seg & 1));
-          if (q_there && __all_sync(0xffffffffu, mbar_test(&ctl->ufull[jk % UNITS], (jk / UNITS) & 1))) {
+          if (q_there && __all_sync(0xffffffffu, mbar_test(&ctl->ufull[uk], phk))) {
             tc_fence_after();
-            const uint32_t k_addr = ring + (jk % UNITS) * C::kUnitBytes;
             if (leader) {
+              const uint32_t a = k_lo + uk * (C::kUnitBytes / 16), d_s = tmem + (it & 1) * NS;
 #pragma unroll
               for (int term = 0; term < (C::kSideBySide ? 1 : 2); ++term)
 #pragma unroll
                 for (int kk = 0; kk < D / 32; ++kk)
-                  mma8(tmem + (it & 1) * NS, desc8<D>(k_addr + kk * 32, 16),
-                       desc8<D>(q_addr + term * NR * D + kk * 32, 16), idesc_qk, term > 0 || kk > 0);
-              tc_commit(&ctl->uempty[jk % UNITS]);
+                  mma8(d_s, a + kk * 2, k_hi, q_lo + term * (NR * D / 16) + kk * 2, q_hi, idesc_qk, term > 0 || kk > 0);
+              tc_commit(&ctl->uempty[uk]);
               tc_commit(&ctl->sfull[it & 1]);
             }
             __syncwarp();
+            step(uk, phk);
             ++qi;
             did = true;
           }
         }
         if (pi < qi) {
-          const int it = it0 + pi, jv = 2 * it + 1;
+          const int it = it0 + pi;
           // with the scores two tiles ahead nothing but this can go: sleep on it instead of polling
-          if (qi == n || qi == pi + 2) ok = mwait(&ctl->pready, it & 1) && mwait(&ctl->ufull[jv % UNITS], (jv / UNITS) & 1);
-          ok = __all_sync(0xffffffffu, ok);
-          if (!ok) break;
-          if (__all_sync(0xffffffffu, mbar_test(&ctl->pready, it & 1) &&
-                                          mbar_test(&ctl->ufull[jv % UNITS], (jv / UNITS) & 1))) {
+          bool go = true;
+          if (qi == n || qi == pi + 2) {
+            ok = mwait(&ctl->pready, it & 1) && mwait(&ctl->ufull[uv], phv);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+          } else {
+            go = __all_sync(0xffffffffu, mbar_test(&ctl->pready, it & 1) && mbar_test(&ctl->ufull[uv], phv));
+          }
+          if (go) {
             tc_fence_after();
-            const uint32_t v_addr = ring + (jv % UNITS) * C::kUnitBytes;
             if (leader) {
+              const uint32_t a = v_lo + uv * (C::kUnitBytes / 16);
 #pragma unroll
               for (int kk = 0; kk < kTok8 / 32; ++kk)
-                mma8(tmem + C::kColO, desc8<D>(v_addr + kk * 32 * D, C::kUnitBytes),
-                     desc_mnmajor_plain(p_addr + kk * 512, 128, kTok8 * 16), idesc_pv, pi > 0 || kk > 0);
-              tc_commit(&ctl->uempty[jv % UNITS]);
+                mma8(tmem + C::kColO, a + kk * (2 * D), v_hi, p_lo + kk * 32, p_hi, idesc_pv, pi > 0 || kk > 0);
+              tc_commit(&ctl->uempty[uv]);
               tc_commit(&ctl->pfree);
             }
             __syncwarp();
+            step(uv, phv);
             ++pi;
             did = true;
           }
@@ -400,19 +439,20 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
     const int per_tile = small ? kTok8 / p.kv.page_size : 1;             // pages per tile
     const int page_tiles = paged && !small ? p.kv.page_size / kTok8 : 1; // tiles per page
     const int key_page = small ? key / p.kv.page_size : 0, key_in = small ? key % p.kv.page_size : key;
-    int ah_id = -1, ah_inner = 0;      // page (dense: request) of the key of the tile after next, as loaded
-    int ah_page = 0, ah_sub = 0;       // large pages: page of that tile, its tile within the page
-    uint32_t ah_ek = 127, ah_ev = 127; // bytes of the next tile's key
-    auto ah_look = [&](const Seg8& s, int t) {
-      ah_id = -1;
-      if (t < s.t1 && t * kTok8 + key < s.len) {
+    uint32_t ah_id = ~0u, ah_inner = 0; // page (dense: request) of the key of the tile after next, as loaded
+    int ah_page = 0, ah_sub = 0;        // large pages: page of that tile, its tile within the page
+    uint32_t ah_ek = 127, ah_ev = 127;  // bytes of the next tile's key
+    const int32_t* ah_table = nullptr;  // the request's row of the page table
+    const uint8_t *ah_ks = nullptr, *ah_vs = nullptr;  // the kv-head's scale bytes
+    auto ah_look = [&](int t, int t1, int len, uint32_t b) {
+      ah_id = ~0u;
+      if (t < t1 && t * kTok8 + key < len) {
         if (!paged) {
-          ah_id = s.b;
+          ah_id = b;
           ah_inner = t * kTok8 + key;
         } else {
-          const int pg = small ? t * per_tile + key_page : ah_page;
           ah_inner = small ? key_in : ah_sub * kTok8 + key;
-          ah_id = p.kv.page_table[(int64_t)s.b * p.kv.pages_per_req + pg];
+          ah_id = (uint32_t)ah_table[small ? t * per_tile + key_page : ah_page];
         }
       }
       if (++ah_sub == page_tiles) {
@@ -420,20 +460,23 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
         ++ah_page;
       }
     };
-    auto ah_fetch = [&](const Seg8& s) {
+    auto ah_fetch = [&]() {
       ah_ek = ah_ev = 127;   // (a key that is not there, or in a page outside the pool: value 0)
-      if ((uint32_t)ah_id < (uint32_t)p.kv.n_outer) {
-        ah_ek = p.kv.Ks[ah_id * p.kv.ks_sb + s.kvh * p.kv.ks_sh + ah_inner * p.kv.ks_st];
-        ah_ev = p.kv.Vs[ah_id * p.kv.vs_sb + s.kvh * p.kv.vs_sh + ah_inner * p.kv.vs_st];
+      if (ah_id < (uint32_t)p.kv.n_outer) {
+        ah_ek = ah_ks[(uint64_t)ah_id * (uint64_t)p.kv.ks_sb + (uint64_t)ah_inner * (uint64_t)p.kv.ks_st];
+        ah_ev = ah_vs[(uint64_t)ah_id * (uint64_t)p.kv.vs_sb + (uint64_t)ah_inner * (uint64_t)p.kv.vs_st];
       }
     };
     auto seg_fetch = [&](const Seg8& s) {
       ah_page = s.t0 / page_tiles;
       ah_sub = s.t0 - ah_page * page_tiles;
-      ah_look(s, s.t0);
+      ah_ks = p.kv.Ks + s.kvh * p.kv.ks_sh;
+      ah_vs = p.kv.Vs + s.kvh * p.kv.vs_sh;
+      if (paged) ah_table = p.kv.page_table + (int64_t)s.b * p.kv.pages_per_req;
+      ah_look(s.t0, s.t1, s.len, s.b);
       q_load(s);
-      ah_fetch(s);
-      ah_look(s, s.t0 + 1);
+      ah_fetch();
+      ah_look(s.t0 + 1, s.t1, s.len, s.b);
     };
     if (ctl->has[0]) seg_fetch(ctl->seg[0]);
     long long base = share.base0;  // (thread 0: tiles before the request of the segment it looks up)
@@ -444,7 +487,7 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
     int it = 0;
     for (int k_seg = 0; ctl->has[k_seg & 1]; ++k_seg) {
       const Seg8& g = ctl->seg[k_seg & 1];
-      const int t0 = g.t0, t1 = g.t1, len = g.len;
+      const int t0 = g.t0, t1 = g.t1, len = g.len, b = g.b;
       if (tid == 0) {  // the next segment, read by everybody after this one's tiles
         Seg8 s = g;
         ctl->has[(k_seg + 1) & 1] = seg_next8(p, share, &base, &s);
@@ -457,8 +500,8 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
       for (int r = 0; r < RT / 2; ++r) lsum[r] = make_float2(0.f, 0.f);
       for (int t = t0; t < t1; ++t, ++it) {
         const float kf = scale8(ah_ek), evf = (float)(int)ah_ev - 127.f, vinv = scale8(254u - ah_ev);
-        ah_fetch(g);
-        ah_look(g, t + 2);
+        ah_fetch();
+        ah_look(t + 2, t1, len, b);
         const int n_valid = min(kTok8, len - t * kTok8);
         const bool key_ok = key < n_valid, first = t == t0;
         wait(&ctl->sfull[it & 1], (it >> 1) & 1);
@@ -502,15 +545,10 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
           for (int r = 0; r < RT / 2; ++r)
             if (!key_ok) x[r] = make_float2(-INFINITY, -INFINITY);
         }
-        {
-          float mx = -INFINITY;
+        float mx = -INFINITY;
 #pragma unroll
-          for (int r = 0; r < RT / 2; ++r) mx = max3_f(mx, x[r].x, x[r].y);
-          if (tid == 0) ctl->flag[(it + 1) % 3] = 0;
-          if (__any_sync(0xffffffffu, mx > kOver) && lane == 0) ctl->flag[it % 3] = 1;
-        }
-        bar8<SOFT>();
-        if (first || ctl->flag[it % 3]) {
+        for (int r = 0; r < RT / 2; ++r) mx = max3_f(mx, x[r].x, x[r].y);
+        if (bar_or8<SOFT>(first || mx > kOver)) {
           // ---- set the references to the exact maxima; later in a segment (rare) raise them, which
           // rescales O^T and the row sums ----
           float mine = -INFINITY;
