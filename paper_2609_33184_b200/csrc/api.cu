@@ -161,7 +161,7 @@ Layout layout_for(const ss_config* c) {
   L.n_tickets8 = (size_t)c->max_B * c->H_kv * ((L.R_stride + ss::kMinRows8 - 1) / ss::kMinRows8);
   L.off_scratch8 = align_up(L.off_tickets8 + L.n_tickets8 * sizeof(unsigned int), 256);
   const size_t rows8 = L.R_stride < ss::kRows8 ? L.R_stride : ss::kRows8;
-  L.total = align_up(L.off_scratch8 + 2 * ss::kCtas8 * rows8 * (c->d + 2) * sizeof(float), 256);
+  L.total = align_up(L.off_scratch8 + 2 * ss::kCtas8 * rows8 * (c->d + 4) * sizeof(float), 256);
   return L;
 }
 
@@ -1243,6 +1243,13 @@ static ss_status view8(const ss_ctx* c, const ss_cache8* k, int32_t B, ss::View8
   v->page_size = k->page_size;
   v->pages_per_req = k->page_table ? k->pages_per_req : 1;
   v->room = (int)room;
+  v->page_shift = -1;
+  v->page_tiles = 1;
+  if (k->page_table && k->page_size < ss::kTok8) {
+    for (v->page_shift = 0; 1 << v->page_shift < k->page_size;) ++v->page_shift;
+  } else if (k->page_table) {
+    v->page_tiles = k->page_size / ss::kTok8;
+  }
   return SS_OK;
 }
 
@@ -1319,6 +1326,8 @@ static ss_status attn8(ss_ctx* c, const ss_tensor& Q, int32_t B, int32_t T_q, fl
   const int most = tc ? ss::kRows8 : ss::kMinRows8;  // rows per unit, evenly spread
   p->row_tiles = (p->R + most - 1) / most;
   p->rows_per_tile = (p->R + p->row_tiles - 1) / p->row_tiles;
+  // (the kernels number all tiles in 31 bits)
+  if ((int64_t)B * ((p->kv.room + ss::kTok8 - 1) / ss::kTok8) * p->H_kv * p->row_tiles >= (1ll << 31)) return SS_ERR_SHAPE;
   p->scale_log2 = scale * 1.4426950408889634f;
   p->min_tiles = 1;
   p->scratch = c->scratch8;

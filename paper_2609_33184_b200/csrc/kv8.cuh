@@ -36,6 +36,9 @@ struct View8 {
   const int32_t* page_table;  // null: dense, the outer index is the request
   int n_outer, page_size, pages_per_req;
   int room;                   // tokens a request can hold
+  // the same for the tensor-core kernel, which would spend a microsecond on the divisions
+  int page_shift;             // pages smaller than a tile: log2(page_size); else -1
+  int page_tiles;             // larger pages: tiles per page (1 for the rest)
 };
 
 struct Attn8Params {
@@ -47,7 +50,7 @@ struct Attn8Params {
   int row_tiles, rows_per_tile;
   float scale_log2;
   int min_tiles;              // a share holds at least this many tiles
-  float* scratch;             // 2 slots per CTA of rows_per_tile * (d + 2) floats
+  float* scratch;             // 2 slots per CTA of rows_per_tile * (d + 4) floats: (m, l) pairs, room, a[]
   unsigned int* tickets;      // one per unit, zero between launches
   __nv_bfloat16* O;           // either the finished output ...
   float* LSE;
@@ -97,48 +100,53 @@ __device__ __forceinline__ int outer8(const View8& kv, int b, int tok, int* inne
 }
 
 // One CTA's share of all tiles, and the walk through its segments (a segment = the part of one unit
-// that lies in the share).
+// that lies in the share).  Tiles are numbered in 32 bits: the host sees to it that all rooms together
+// hold fewer than 2^31.  The first `more` shares have q + 1 tiles, the others q.
 struct Share8 {
-  long long total, lo, hi;  // tiles of the launch; this CTA's range
-  int ctas;                 // CTAs that have a share
-  int b0;                   // request that holds tile `lo`, and the tiles before it
-  long long base0;
+  uint32_t total, lo, hi;   // tiles of the launch; this CTA's range
+  uint32_t ctas, q, more;   // CTAs that have a share
+  uint32_t b0, base0;       // request that holds tile `lo`, and the tiles before it
 };
-__device__ __forceinline__ long long share_lo8(long long total, int ctas, int i) { return total * i / ctas; }
-// The CTA whose share holds tile x: the largest i with floor(total * i / ctas) <= x.
-__device__ __forceinline__ int share_of8(long long total, int ctas, long long x) {
-  return (int)(((x + 1) * ctas - 1) / total);
+__device__ __forceinline__ uint32_t share_lo8(const Share8& s, uint32_t i) { return i * s.q + min(i, s.more); }
+// The CTA whose share holds tile x.
+__device__ __forceinline__ uint32_t share_of8(const Share8& s, uint32_t x) {
+  const uint32_t big = s.more * (s.q + 1);
+  return x < big ? x / (s.q + 1) : s.more + (x - big) / s.q;
 }
 
-// By one whole warp.  Lane 0 of CTA 0 also reports lengths that had to be clamped.
+// By one whole warp.  CTA 0 also reports lengths that had to be clamped.
 __device__ __forceinline__ Share8 find_share8(const Attn8Params& p) {
   const int lane = threadIdx.x & 31;
-  const long long units = (long long)p.H_kv * p.row_tiles;
-  Share8 s;
-  long long sum = 0;
+  const uint32_t units = (uint32_t)(p.H_kv * p.row_tiles);
+  Share8 s = {};
+  uint32_t sum = 0, n = 0;
   bool bad = false;
   for (int b = lane; b < p.B; b += 32) {
-    sum += tiles8(len8(p, b));
-    if (p.valid_len) bad |= p.valid_len[b] < 0 || p.valid_len[b] > p.kv.room;
+    int len = p.kv.room;
+    if (p.valid_len) {
+      len = p.valid_len[b];
+      bad |= len < 0 || len > p.kv.room;
+      len = max(0, min(len, p.kv.room));
+    }
+    n = units * tiles8(len);
+    sum += n;
   }
   if (blockIdx.x == 0 && __any_sync(0xffffffffu, bad) && lane == 0) atomicOr(p.status, SS_DEV_BAD_VALID_LEN);
-#pragma unroll
-  for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-  s.total = sum * units;
-  const long long want = (s.total + p.min_tiles - 1) / p.min_tiles;
-  s.ctas = (int)(want < gridDim.x ? (want > 0 ? want : 1) : gridDim.x);
-  s.lo = s.hi = 0;
-  s.b0 = 0;
-  s.base0 = 0;
-  if ((int)blockIdx.x >= s.ctas || s.total == 0) return s;
-  s.lo = share_lo8(s.total, s.ctas, blockIdx.x);
-  s.hi = share_lo8(s.total, s.ctas, blockIdx.x + 1);
-  long long base = 0;
+  s.total = __reduce_add_sync(0xffffffffu, sum);
+  const uint32_t want = (s.total + p.min_tiles - 1) / p.min_tiles;
+  s.ctas = want < gridDim.x ? max(want, 1u) : gridDim.x;
+  s.q = s.total / s.ctas;
+  s.more = s.total - s.q * s.ctas;
+  if (blockIdx.x >= s.ctas || s.total == 0) return s;
+  s.lo = share_lo8(s, blockIdx.x);
+  s.hi = share_lo8(s, blockIdx.x + 1);
+  uint32_t base = 0;
   for (int b = 0; b < p.B; b += 32) {
-    long long n = b + lane < p.B ? units * tiles8(len8(p, b + lane)) : 0, incl = n;
+    if (p.B > 32) n = b + lane < p.B ? units * tiles8(len8(p, b + lane)) : 0;  // (else still there)
+    uint32_t incl = n;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const long long up = __shfl_up_sync(0xffffffffu, incl, o);
+      const uint32_t up = __shfl_up_sync(0xffffffffu, incl, o);
       if (lane >= o) incl += up;
     }
     const unsigned past = __ballot_sync(0xffffffffu, base + incl > s.lo);
@@ -154,48 +162,45 @@ __device__ __forceinline__ Share8 find_share8(const Attn8Params& p) {
 }
 
 struct Seg8 {
-  int b, kvh, rt, unit;     // unit = number of the unit among all B * H_kv * row_tiles
+  int b, kvh, unit;         // unit = number of the unit among all B * H_kv * row_tiles
   int t0, t1, n;            // tiles [t0, t1) of the unit's n
   int len;                  // tokens of the request
-  long long start;          // the unit's first tile among all
-  long long pos;            // the segment's end among all tiles
+  uint32_t base, start, pos;  // tiles before the request, before the unit, before the segment's end
   int row0, nrows;
 };
-__device__ __forceinline__ void seg_set8(const Attn8Params& p, const Share8& s, long long base, Seg8* g) {
+__device__ __forceinline__ void seg_set8(const Attn8Params& p, const Share8& s, Seg8* g) {
   // (within a request a unit is (kv-head, row tile), row tile fastest: neighbours read the same K/V)
-  const int u = (int)((g->pos - base) / g->n);
-  g->kvh = u / p.row_tiles;
-  g->rt = u - g->kvh * p.row_tiles;
-  g->unit = (g->b * p.H_kv + g->kvh) * p.row_tiles + g->rt;
-  g->start = base + (long long)u * g->n;
+  const uint32_t u = (g->pos - g->base) / (uint32_t)g->n;
+  const int kvh = p.row_tiles == 1 ? u : u / (uint32_t)p.row_tiles, rt = u - kvh * p.row_tiles;
+  g->kvh = kvh;
+  g->unit = (g->b * p.H_kv + kvh) * p.row_tiles + rt;
+  g->start = g->base + u * g->n;
   g->t0 = (int)(g->pos - g->start);
-  const long long end = g->start + g->n < s.hi ? g->start + g->n : s.hi;
-  g->t1 = (int)(end - g->start);
-  g->pos = end;
-  g->row0 = g->rt * p.rows_per_tile;
+  g->pos = min(g->start + g->n, s.hi);
+  g->t1 = (int)(g->pos - g->start);
+  g->row0 = rt * p.rows_per_tile;
   g->nrows = min(p.rows_per_tile, p.R - g->row0);
 }
-// Walk: `base` is the number of tiles before request g->b.
-__device__ __forceinline__ bool seg_first8(const Attn8Params& p, const Share8& s, long long* base, Seg8* g) {
+__device__ __forceinline__ bool seg_first8(const Attn8Params& p, const Share8& s, Seg8* g) {
   if (s.lo >= s.hi) return false;
   g->b = s.b0;
   g->len = len8(p, g->b);
   g->n = tiles8(g->len);
   g->pos = s.lo;
-  *base = s.base0;
-  seg_set8(p, s, *base, g);
+  g->base = s.base0;
+  seg_set8(p, s, g);
   return true;
 }
-__device__ __forceinline__ bool seg_next8(const Attn8Params& p, const Share8& s, long long* base, Seg8* g) {
+__device__ __forceinline__ bool seg_next8(const Attn8Params& p, const Share8& s, Seg8* g) {
   if (g->pos >= s.hi) return false;
-  const long long units = (long long)p.H_kv * p.row_tiles;
-  while (g->pos >= *base + units * g->n) {  // the next request with tokens (there is one: pos < hi <= total)
-    *base += units * g->n;
+  const uint32_t units = (uint32_t)(p.H_kv * p.row_tiles);
+  while (g->pos >= g->base + units * g->n) {  // the next request with tokens (there is one: pos < hi <= total)
+    g->base += units * g->n;
     ++g->b;
     g->len = len8(p, g->b);
     g->n = tiles8(g->len);
   }
-  seg_set8(p, s, *base, g);
+  seg_set8(p, s, g);
   return true;
 }
 
@@ -216,6 +221,16 @@ __device__ __forceinline__ void put_a8(const Attn8Params& p, const Seg8& g, int 
     p.O[(((int64_t)g.b * p.H_kv + g.kvh) * p.R + g.row0 + r) * p.d + c] = __float2bfloat16_rn(a * inv);
   } else {
     p.part_a[(((int64_t)g.b * p.H_kv + g.kvh) * p.R_stride + g.row0 + r) * p.d + c] = a;
+  }
+}
+__device__ __forceinline__ void put_a8x4(const Attn8Params& p, const Seg8& g, int r, int c, float l, float4 a) {
+  if (p.O) {
+    const float inv = (l > 0.f || l != l) ? 1.f / l : 0.f;
+    const __nv_bfloat162 lo = __floats2bfloat162_rn(a.x * inv, a.y * inv), hi = __floats2bfloat162_rn(a.z * inv, a.w * inv);
+    *reinterpret_cast<uint2*>(p.O + (((int64_t)g.b * p.H_kv + g.kvh) * p.R + g.row0 + r) * p.d + c) =
+        make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+  } else {
+    *reinterpret_cast<float4*>(p.part_a + (((int64_t)g.b * p.H_kv + g.kvh) * p.R_stride + g.row0 + r) * p.d + c) = a;
   }
 }
 // Requests without a visible token, by `n` threads of every CTA.
@@ -240,78 +255,85 @@ __device__ __forceinline__ void bar8() {
 
 // Slot of CTA i's state of the unit that begins at tile `start` (first CTA i0): the first segment of a
 // share uses the CTA's even slot, a later one (always the last) the odd slot.
-__device__ __forceinline__ float* slot8(const Attn8Params& p, const Share8& s, long long start, int i) {
-  const int odd = share_lo8(s.total, s.ctas, i) < start ? 1 : 0;
-  return p.scratch + (int64_t)(2 * i + odd) * p.rows_per_tile * (p.d + 2);
+__device__ __forceinline__ float* slot8(const Attn8Params& p, const Share8& s, uint32_t start, uint32_t i) {
+  const int odd = share_lo8(s, i) < start ? 1 : 0;
+  return p.scratch + (int64_t)(2 * i + odd) * p.rows_per_tile * (p.d + 4);
 }
 
-// sum over the unit's n states of weight * a[c] for ROWS rows from r on, ROWS * STATES loads in flight
+// Four head dims c .. c + 3 of rows r, r + STEP, ..: the sum over the unit's n states of weight * a, with
+// ROWS * STATES loads of 16 bytes in flight (weights of the block's row k in w[state * block + k].x, the
+// row's sum in w[n * block + k].y).
 template <int D, int ROWS, int STATES, int STEP>
 __device__ __forceinline__ void join_rows8(const Attn8Params& p, const Seg8& g, const float* first, const float* rest,
                                            const float2* w, int block, int r0, int r, int n, int c) {
-  const int64_t slot = (int64_t)p.rows_per_tile * (D + 2);
-  float a[ROWS];
+  const int64_t slot = (int64_t)p.rows_per_tile * (D + 4);
+  float4 a[ROWS];
 #pragma unroll
-  for (int k = 0; k < ROWS; ++k) a[k] = 0.f;
+  for (int k = 0; k < ROWS; ++k) a[k] = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 1
   for (int j0 = 0; j0 < n; j0 += STATES) {
-    float v[STATES][ROWS], f[STATES][ROWS];
+    float4 v[STATES][ROWS];
+#pragma unroll
+    for (int j = 0; j < STATES; ++j) {
+      const int i = min(j0 + j, n - 1);
+      const float* src = (i == 0 ? first : rest + (int64_t)(i - 1) * 2 * slot) + 4 * p.rows_per_tile + c;
+#pragma unroll
+      for (int k = 0; k < ROWS; ++k)
+        v[j][k] = __ldcg(reinterpret_cast<const float4*>(src + (r0 + min(r + k * STEP, block - 1)) * D));
+    }
 #pragma unroll
     for (int j = 0; j < STATES; ++j) {
 #pragma unroll
       for (int k = 0; k < ROWS; ++k) {
-        const int row = r + k * STEP;
-        f[j][k] = (j0 + j < n && row < block) ? w[(j0 + j) * block + row].x : 0.f;
-        v[j][k] = 0.f;
-        if (f[j][k] != 0.f) {  // (a state of weight 0 may be unwritten)
-          const float* src = j0 + j == 0 ? first : rest + (int64_t)(j0 + j - 1) * 2 * slot;
-          v[j][k] = __ldcg(src + 2 * p.rows_per_tile + (r0 + row) * D + c);
-        }
+        const float f = j0 + j < n ? w[(j0 + j) * block + min(r + k * STEP, block - 1)].x : 0.f;
+        a[k].x = fmaf(f, v[j][k].x, a[k].x);
+        a[k].y = fmaf(f, v[j][k].y, a[k].y);
+        a[k].z = fmaf(f, v[j][k].z, a[k].z);
+        a[k].w = fmaf(f, v[j][k].w, a[k].w);
       }
     }
-#pragma unroll
-    for (int j = 0; j < STATES; ++j)
-#pragma unroll
-      for (int k = 0; k < ROWS; ++k) a[k] = fmaf(f[j][k], v[j][k], a[k]);
   }
 #pragma unroll
   for (int k = 0; k < ROWS; ++k) {
     const int row = r + k * STEP;
-    if (row < block) put_a8(p, g, r0 + row, c, w[n * block + row].y, a[k]);
+    if (row < block) put_a8x4(p, g, r0 + row, c, w[n * block + row].y, a[k]);
   }
 }
 
 // By N threads (128 or 256), after each has stored its part of this CTA's state in its slot: takes the
 // unit's ticket and, for the last CTA, joins all states.  *flag and buf (kJoinBuf8 pairs) are shared
 // memory.  A read of another CTA's state is a read of L2, so all of a block of rows' (m, l) are fetched at once,
-// then their a[] with 2048 loads in flight: one row and state after the other, the join
-// took 120 us for 37 states of 4 rows.
+// then their a[] with 16 loads of a thread in flight: one row and state after the other, the
+// join took 120 us for 37 states of 4 rows.
 constexpr int kJoinBuf8 = 512;
 static_assert(kCtas8 + 1 <= kJoinBuf8, "a row's states fit the buffer");
 template <int D, int N>
 __device__ __noinline__ void join8(const Attn8Params& p, const Share8& s, const Seg8& g, int tid, int* flag, float2* buf) {
-  const int i0 = share_of8(s.total, s.ctas, g.start), i1 = share_of8(s.total, s.ctas, g.start + g.n - 1);
-  __threadfence();
+  const int i0 = share_of8(s, g.start), i1 = share_of8(s, g.start + g.n - 1);
   bar8<N>();
   if (tid == 0) {
-    const int last = atomicAdd(&p.tickets[g.unit], 1u) == (unsigned)(i1 - i0);
+    // released after all the CTA's stores (the barrier), acquired before the loads of the others' states
+    uint32_t before;
+    asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], 1;" : "=r"(before) : "l"(&p.tickets[g.unit]) : "memory");
+    const int last = before == (uint32_t)(i1 - i0);
     if (last) p.tickets[g.unit] = 0;  // nobody else touches it any more in this launch
     *flag = last;
   }
   bar8<N>();
   if (!*flag) return;
-  __threadfence();
   const int n = i1 - i0 + 1;               // >= 2: the unit is cut
   const float* first = slot8(p, s, g.start, i0);
   const float* rest = slot8(p, s, g.start, i0 + 1);   // those after the first are the CTAs' even slots
-  const int64_t slot = (int64_t)p.rows_per_tile * (D + 2);
+  const int64_t slot = (int64_t)p.rows_per_tile * (D + 4);
   const int most = kJoinBuf8 / (n + 1);  // rows at a time, >= 1: n <= kCtas8
   for (int r0 = 0; r0 < g.nrows; r0 += most) {
     const int block = min(most, g.nrows - r0);
-    for (int f = tid; f < n * block; f += N) {
-      const int j = f / block, r = f - j * block;
-      const float* src = j == 0 ? first : rest + (int64_t)(j - 1) * 2 * slot;
-      buf[f] = __ldcg(reinterpret_cast<const float2*>(src) + r0 + r);
+    if ((tid & 31) < block) {
+#pragma unroll 4
+      for (int j = tid >> 5; j < n; j += N / 32) {
+        const float* src = j == 0 ? first : rest + (int64_t)(j - 1) * 2 * slot;
+        buf[j * block + (tid & 31)] = __ldcg(reinterpret_cast<const float2*>(src) + r0 + (tid & 31));
+      }
     }
     bar8<N>();
     // eight lanes per row: maximum, weights, sum (left in entry n of the row)
@@ -339,12 +361,14 @@ __device__ __noinline__ void join8(const Attn8Params& p, const Share8& s, const 
       }
     }
     bar8<N>();
-    constexpr int G = N / D;  // rows side by side
-    const int c = tid % D, r = tid / D;
-    if (block <= 4 * G) {
-      join_rows8<D, 4, 2048 / N / 4, G>(p, g, first, rest, buf, block, r0, r, n, c);
+    constexpr int kLanes = D / 4, G = N / kLanes;  // lanes per row, rows side by side
+    const int c = tid % kLanes * 4, r = tid / kLanes;
+    if (block <= G) {
+      join_rows8<D, 1, 16, G>(p, g, first, rest, buf, block, r0, r, n, c);
+    } else if (n <= 4) {
+      for (int k = r; k < block; k += 4 * G) join_rows8<D, 4, 4, G>(p, g, first, rest, buf, block, r0, k, n, c);
     } else {
-      for (int k = r; k < block; k += 8 * G) join_rows8<D, 8, 2048 / N / 8, G>(p, g, first, rest, buf, block, r0, k, n, c);
+      for (int k = r; k < block; k += 2 * G) join_rows8<D, 2, 8, G>(p, g, first, rest, buf, block, r0, k, n, c);
     }
     bar8<N>();
   }

@@ -45,10 +45,8 @@ __global__ void __launch_bounds__(128) attn8_simt_kernel(const __grid_constant__
   pdl_wait_prior();
   pdl_launch_dependents();
   const Share8 share = find_share8(p);
-  put_empty8(p, tid, 128);
-  long long base;
   Seg8 g;
-  for (bool more = seg_first8(p, share, &base, &g); more; more = seg_next8(p, share, &base, &g)) {
+  for (bool more = seg_first8(p, share, &g); more; more = seg_next8(p, share, &g)) {
     __syncthreads();  // the previous segment's shared memory has been read
     for (int i = tid; i < kRT * D; i += 128) {
       const int r = i / D, c = i % D;
@@ -175,11 +173,12 @@ __global__ void __launch_bounds__(128) attn8_simt_kernel(const __grid_constant__
         put_a8(p, g, r, c, L, A);
       } else {
         if (c == 0) reinterpret_cast<float2*>(slot)[r] = make_float2(M, L);
-        slot[2 * p.rows_per_tile + r * D + c] = A;
+        slot[4 * p.rows_per_tile + r * D + c] = A;
       }
     }
     if (!whole) join8<D, 128>(p, share, g, tid, &flag, reinterpret_cast<float2*>(w_s));
   }
+  put_empty8(p, tid, 128);
 }
 
 }  // namespace

@@ -204,9 +204,8 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
   if (warp == 0) {
     const Share8 share = find_share8(p);
     if (lane == 0) {
-      long long base;
       ctl->share = share;
-      ctl->has[0] = seg_first8(p, share, &base, &ctl->seg[0]);
+      ctl->has[0] = seg_first8(p, share, &ctl->seg[0]);
     }
   }
   tc_fence_before();
@@ -225,23 +224,29 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
     // side by side have the layout of one.  The swizzle atom (8 rows) is also why other page sizes
     // take the CUDA-core kernel.  Pages past the request's last token are not looked up.
     const uint64_t pol = p.row_tiles > 1 ? l2_evict_normal_policy() : l2_evict_first_policy();
-    const bool small = p.kv.page_table && p.kv.page_size < kTok8;
+    const bool small = p.kv.page_shift >= 0;
     const int ps = small ? p.kv.page_size : kTok8;
-    const bool mine = lane < kTok8 / ps;
+    const bool mine = lane * ps < kTok8;
     int j = 0, u = 0;      // units filled so far, the next one's place in the ring
     uint32_t ph = 1;       // parity of its release
     bool ok = true;
-    long long base;
     Seg8 g;
-    for (bool more = seg_first8(p, share, &base, &g); more && ok; more = seg_next8(p, share, &base, &g)) {
+    for (bool more = seg_first8(p, share, &g); more && ok; more = seg_next8(p, share, &g)) {
       int inner = 0, outer = 0;
       auto look = [&](int t) {  // this lane's page of tile t
         const int tok = t * kTok8 + lane * ps;
         outer = p.kv.n_outer;   // outside the tensor: reads as zeros
         inner = 0;
         if (!mine || t >= g.t1 || tok >= g.len) return;
-        const int id = outer8(p.kv, g.b, tok, &inner);
-        if (id >= 0) outer = id;
+        int id = g.b;
+        if (!p.kv.page_table) {
+          inner = tok;
+        } else {
+          const int pg = small ? tok >> p.kv.page_shift : p.kv.page_tiles == 1 ? t : t / p.kv.page_tiles;
+          if (!small) inner = tok - pg * p.kv.page_size;
+          id = p.kv.page_table[(int64_t)g.b * p.kv.pages_per_req + pg];
+        }
+        if (id >= 0 && id < p.kv.n_outer) outer = id;
         else atomicOr(p.status, SS_DEV_BAD_PAGE);
       };
       look(g.t0);
@@ -294,9 +299,8 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
     };
     int it0 = 0, seg = 0;  // tiles and segments before this one
     bool ok = true;
-    long long base;
     Seg8 g;
-    for (bool more = seg_first8(p, share, &base, &g); more && ok; more = seg_next8(p, share, &base, &g), ++seg) {
+    for (bool more = seg_first8(p, share, &g); more && ok; more = seg_next8(p, share, &g), ++seg) {
       const int n = g.t1 - g.t0;
       int qi = 0, pi = 0;
       bool q_there = false;
@@ -375,8 +379,6 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
     const int c0 = (warp >> 2) * RT;                         // this thread's rows: [c0, c0 + RT)
     const uint32_t lane_off = (uint32_t)(quad * 32) << 16;
     auto wait = [&](uint64_t* bar, uint32_t parity) { wait8(bar, parity, &ctl->abort, p.status); };
-    put_empty8(p, tid, SOFT);
-
     // Q: SOFT / NR threads per row, kE values each
     constexpr int TPR = SOFT / NR, kE = D / TPR, kQL = kE / 4;
     const int q_row = tid / TPR, q_part = tid % TPR;
@@ -435,10 +437,8 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
 
     // Scale bytes of this thread's key, fetched a tile ahead (and its page id two tiles ahead).  Small
     // pages: the key's place in its page is the same in every tile.
-    const bool paged = p.kv.page_table != nullptr, small = paged && p.kv.page_size < kTok8;
-    const int per_tile = small ? kTok8 / p.kv.page_size : 1;             // pages per tile
-    const int page_tiles = paged && !small ? p.kv.page_size / kTok8 : 1; // tiles per page
-    const int key_page = small ? key / p.kv.page_size : 0, key_in = small ? key % p.kv.page_size : key;
+    const bool paged = p.kv.page_table != nullptr, small = p.kv.page_shift >= 0;
+    const int page_tiles = p.kv.page_tiles;
     uint32_t ah_id = ~0u, ah_inner = 0; // page (dense: request) of the key of the tile after next, as loaded
     int ah_page = 0, ah_sub = 0;        // large pages: page of that tile, its tile within the page
     uint32_t ah_ek = 127, ah_ev = 127;  // bytes of the next tile's key
@@ -451,8 +451,9 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
           ah_id = b;
           ah_inner = t * kTok8 + key;
         } else {
-          ah_inner = small ? key_in : ah_sub * kTok8 + key;
-          ah_id = (uint32_t)ah_table[small ? t * per_tile + key_page : ah_page];
+          const int tok = t * kTok8 + key;
+          ah_inner = small ? tok & (p.kv.page_size - 1) : ah_sub * kTok8 + key;
+          ah_id = (uint32_t)ah_table[small ? tok >> p.kv.page_shift : ah_page];
         }
       }
       if (++ah_sub == page_tiles) {
@@ -468,18 +469,15 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
       }
     };
     auto seg_fetch = [&](const Seg8& s) {
-      ah_page = s.t0 / page_tiles;
+      ah_page = page_tiles == 1 ? s.t0 : s.t0 / page_tiles;
       ah_sub = s.t0 - ah_page * page_tiles;
       ah_ks = p.kv.Ks + s.kvh * p.kv.ks_sh;
       ah_vs = p.kv.Vs + s.kvh * p.kv.vs_sh;
       if (paged) ah_table = p.kv.page_table + (int64_t)s.b * p.kv.pages_per_req;
       ah_look(s.t0, s.t1, s.len, s.b);
       q_load(s);
-      ah_fetch();
-      ah_look(s.t0 + 1, s.t1, s.len, s.b);
     };
     if (ctl->has[0]) seg_fetch(ctl->seg[0]);
-    long long base = share.base0;  // (thread 0: tiles before the request of the segment it looks up)
     auto top4 = [&](int r) {
       return fmaxf(fmaxf(ctl->smax[0][r], ctl->smax[1][r]), fmaxf(ctl->smax[2][r], ctl->smax[3][r]));
     };
@@ -490,10 +488,12 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
       const int t0 = g.t0, t1 = g.t1, len = g.len, b = g.b;
       if (tid == 0) {  // the next segment, read by everybody after this one's tiles
         Seg8 s = g;
-        ctl->has[(k_seg + 1) & 1] = seg_next8(p, share, &base, &s);
+        ctl->has[(k_seg + 1) & 1] = seg_next8(p, share, &s);
         ctl->seg[(k_seg + 1) & 1] = s;
       }
       q_store();
+      ah_fetch();    // (its page id has arrived by now)
+      ah_look(t0 + 1, t1, len, b);
       bar8<SOFT>();  // (factors and references)
       float2 lsum[RT / 2];
 #pragma unroll
@@ -687,7 +687,7 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
               const float a = fmaf(__uint_as_float(o[2][c]), 1.f / 64.f,
                                    fmaf(__uint_as_float(o[1][c]), 0.125f, __uint_as_float(o[0][c])));
               if (whole) put_a8(p, done, r, key, row_l(r), a);
-              else slot[2 * p.rows_per_tile + r * D + key] = a;
+              else slot[4 * p.rows_per_tile + r * D + key] = a;
             }
           }
         }
@@ -696,6 +696,7 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
       if (!whole) join8<D, SOFT>(p, share, done, tid, &ctl->last, reinterpret_cast<float2*>(p_s));
       bar8<SOFT>();  // sums, references and Q may be written anew
     }
+    put_empty8(p, tid, SOFT);
   }
 
   tc_fence_before();
