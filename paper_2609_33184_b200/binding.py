@@ -266,8 +266,9 @@ class SpecStreamError(RuntimeError):
 
 def as_ss_tensor(t: torch.Tensor) -> ss_tensor:
     """[B, H, T, d] bf16 torch tensor -> ss_tensor (strides in elements)."""
-    assert t.dim() == 4 and t.dtype == torch.bfloat16 and t.stride(3) == 1, (t.shape, t.dtype, t.stride())
-    return ss_tensor(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2))
+    s = t.stride()
+    assert len(s) == 4 and t.dtype is torch.bfloat16 and s[3] == 1, (t.shape, t.dtype, s)
+    return ss_tensor(t.data_ptr(), s[0], s[1], s[2])
 
 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
@@ -439,48 +440,74 @@ class Context:
                                               as_ss_tensor(K_dst), as_ss_tensor(V_dst), cap,
                                               dst_off.data_ptr(), self._sp(stream)), "ss_commit_gather")
 
+    # The calls on the 8-bit cache are made once per step and layer, on small batches with more host
+    # than device time: their checks are few and flat.
     def _cache8(self, cache: Cache8, B: int):
-        assert cache.H_kv == self.cfg.H_kv and cache.d == self.d and cache.requests >= B, "cache of another shape"
+        if cache.H_kv != self.cfg.H_kv or cache.d != self.d or cache.requests < B:
+            raise AssertionError("cache of another shape")
         return cache.ref
 
     @staticmethod
-    def _ints(shape, *tensors):
-        for t in tensors:
-            assert t is None or (t.dtype == torch.int32 and t.is_contiguous() and t.is_cuda and t.shape == shape)
+    def _i32(t, n):
+        """Device pointer of an int32 tensor of n contiguous elements, or None."""
+        if t is None:
+            return None
+        if t.dtype is not torch.int32 or t.numel() != n or not (t.is_cuda and t.is_contiguous()):
+            raise AssertionError("int32 device tensor expected", t.shape, t.dtype)
+        return t.data_ptr()
+
+    @staticmethod
+    def _rows(t, shape):
+        """[B, H, T, d] bf16 tensor of this shape, d contiguous -> ss_tensor."""
+        s = t.stride()
+        if t.dtype is not torch.bfloat16 or t.shape != shape or s[3] != 1 or not t.is_cuda:
+            raise AssertionError("bf16 device tensor expected", t.shape, t.dtype, s)
+        return ss_tensor(t.data_ptr(), s[0], s[1], s[2])
 
     def ss_kv8_write(self, cache: Cache8, K: torch.Tensor, V: torch.Tensor, dst_off=None, row_cnt=None,
                      row_idx=None, stream=None):
         """K, V [B, H_kv, T, d] bf16; dst_off, row_cnt int32 [B] and row_idx int32 [B, T] on the device or None."""
-        B, H, T, d = K.shape
-        assert V.shape == K.shape and H == self.cfg.H_kv and d == self.d
-        self._ints((B,), dst_off, row_cnt)
-        self._ints((B, T), row_idx)
-        self._check(self.lib.ss_kv8_write(self.handle, self._cache8(cache, B), as_ss_tensor(K), as_ss_tensor(V), B, T,
-                                          _ptr(row_idx), _ptr(row_cnt), _ptr(dst_off), self._sp(stream)), "ss_kv8_write")
+        shape = K.shape
+        B, H, T, d = shape
+        i32, rows = self._i32, self._rows
+        st = self.lib.ss_kv8_write(self.handle, self._cache8(cache, B), rows(K, (B, cache.H_kv, T, self.d)),
+                                   rows(V, shape), B, T, i32(row_idx, B * T), i32(row_cnt, B), i32(dst_off, B),
+                                   self._sp(stream))
+        if st:
+            self._check(st, "ss_kv8_write")
 
     def ss_kv8_read(self, cache: Cache8, K: torch.Tensor, V: torch.Tensor, src_off=None, row_cnt=None, stream=None):
         """Tokens src_off[b] .. src_off[b] + row_cnt[b] of the cache into rows 0 .. of K, V [B, H_kv, T, d] bf16."""
-        B, H, T, d = K.shape
-        assert V.shape == K.shape and H == self.cfg.H_kv and d == self.d
-        self._ints((B,), src_off, row_cnt)
-        self._check(self.lib.ss_kv8_read(self.handle, self._cache8(cache, B), as_ss_tensor(K), as_ss_tensor(V), B, T,
-                                         _ptr(src_off), _ptr(row_cnt), self._sp(stream)), "ss_kv8_read")
+        shape = K.shape
+        B, H, T, d = shape
+        i32, rows = self._i32, self._rows
+        st = self.lib.ss_kv8_read(self.handle, self._cache8(cache, B), rows(K, (B, cache.H_kv, T, self.d)),
+                                  rows(V, shape), B, T, i32(src_off, B), i32(row_cnt, B), self._sp(stream))
+        if st:
+            self._check(st, "ss_kv8_read")
 
     def ss_verify_chunk8(self, cache: Cache8, valid_len: Optional[torch.Tensor] = None, stream=None):
         """One chunk of the open round held in 8 bits."""
-        self._ints((self._B,), valid_len)
-        self._check(self.lib.ss_verify_chunk8(self.handle, self._cache8(cache, self._B), _ptr(valid_len),
-                                              self._sp(stream)), "ss_verify_chunk8")
+        st = self.lib.ss_verify_chunk8(self.handle, self._cache8(cache, self._B), self._i32(valid_len, self._B),
+                                       self._sp(stream))
+        if st:
+            self._check(st, "ss_verify_chunk8")
 
     def ss_decode8(self, Q: torch.Tensor, scale: float, cache: Cache8, valid_len: Optional[torch.Tensor],
                    O: torch.Tensor, LSE: Optional[torch.Tensor] = None, stream=None):
         """Q [B, H_q, T_q, d] over the first valid_len[b] tokens of the cache -> O (bf16), LSE (fp32 [B, H_q, T_q])."""
-        B, H_q, T_q, d = Q.shape
-        assert H_q == self.H_q and d == self.d and O.dtype == torch.bfloat16 and O.is_contiguous() and O.shape == Q.shape
-        assert LSE is None or (LSE.dtype == torch.float32 and LSE.is_contiguous() and LSE.shape == Q.shape[:3])
-        self._ints((B,), valid_len)
-        self._check(self.lib.ss_decode8(self.handle, as_ss_tensor(Q), B, T_q, scale, self._cache8(cache, B),
-                                        _ptr(valid_len), O.data_ptr(), _ptr(LSE), self._sp(stream)), "ss_decode8")
+        shape = Q.shape
+        B, H, T, d = shape
+        if O.dtype is not torch.bfloat16 or O.shape != shape or not (O.is_contiguous() and O.is_cuda):
+            raise AssertionError("O: contiguous bf16 of Q's shape expected", O.shape, O.dtype)
+        if LSE is not None and (LSE.dtype is not torch.float32 or LSE.shape != shape[:3] or
+                                not (LSE.is_contiguous() and LSE.is_cuda)):
+            raise AssertionError("LSE: contiguous fp32 [B, H_q, T_q] expected", LSE.shape, LSE.dtype)
+        st = self.lib.ss_decode8(self.handle, self._rows(Q, (B, self.H_q, T, self.d)), B, T, scale,
+                                 self._cache8(cache, B), self._i32(valid_len, B), O.data_ptr(),
+                                 None if LSE is None else LSE.data_ptr(), self._sp(stream))
+        if st:
+            self._check(st, "ss_decode8")
 
     def ss_poll_status(self, stream=None, timeout_ms: int = 0):
         """Returns (status, device_bits)."""

@@ -1243,13 +1243,11 @@ static ss_status view8(const ss_ctx* c, const ss_cache8* k, int32_t B, ss::View8
   v->page_size = k->page_size;
   v->pages_per_req = k->page_table ? k->pages_per_req : 1;
   v->room = (int)room;
-  v->page_shift = -1;
-  v->page_tiles = 1;
-  if (k->page_table && k->page_size < ss::kTok8) {
-    for (v->page_shift = 0; 1 << v->page_shift < k->page_size;) ++v->page_shift;
-  } else if (k->page_table) {
-    v->page_tiles = k->page_size / ss::kTok8;
-  }
+  v->page_log2 = -1;
+  if ((k->page_size & (k->page_size - 1)) == 0)
+    for (v->page_log2 = 0; 1 << v->page_log2 < k->page_size;) ++v->page_log2;
+  v->page_shift = k->page_table && k->page_size < ss::kTok8 ? v->page_log2 : -1;
+  v->page_tiles = k->page_table && k->page_size > ss::kTok8 ? k->page_size / ss::kTok8 : 1;
   return SS_OK;
 }
 
@@ -1278,7 +1276,7 @@ static ss_status copy8(ss_ctx* c, bool write, const ss_cache8* cache, ss_tensor 
   DeviceGuard on(c->cfg.device);
   cudaError_t e = on.err;
   if (e == cudaSuccess)
-    e = write ? ss::launch_kv8_write(p, (cudaStream_t)stream) : ss::launch_kv8_read(p, (cudaStream_t)stream);
+    e = write ? ss::launch_kv8_write(p, (cudaStream_t)stream, true) : ss::launch_kv8_read(p, (cudaStream_t)stream, true);
   if (e != cudaSuccess) return cuda_fail(c, e);
   ++c->launches;
   return SS_OK;

@@ -36,6 +36,7 @@ struct View8 {
   const int32_t* page_table;  // null: dense, the outer index is the request
   int n_outer, page_size, pages_per_req;
   int room;                   // tokens a request can hold
+  int page_log2;              // log2(page_size), -1 when it is no power of two
   // the same for the tensor-core kernel, which would spend a microsecond on the divisions
   int page_shift;             // pages smaller than a tile: log2(page_size); else -1
   int page_tiles;             // larger pages: tiles per page (1 for the rest)
@@ -69,8 +70,8 @@ struct Copy8Params {          // write (bf16 -> cache) and read (cache -> bf16)
   uint32_t* status;
 };
 
-cudaError_t launch_kv8_write(const Copy8Params& p, cudaStream_t s);
-cudaError_t launch_kv8_read(const Copy8Params& p, cudaStream_t s);
+cudaError_t launch_kv8_write(const Copy8Params& p, cudaStream_t s, bool pdl);
+cudaError_t launch_kv8_read(const Copy8Params& p, cudaStream_t s, bool pdl);
 cudaError_t launch_attn8_simt(const Attn8Params& p, cudaStream_t s, bool pdl);
 cudaError_t launch_attn8_tc(const Attn8Params& p, const CUtensorMap& tmK, const CUtensorMap& tmV, cudaStream_t s, bool pdl);
 cudaError_t attn8_tc_prepare();  // one-time function attributes

@@ -1,7 +1,8 @@
 // Rows into the 8-bit KV cache and back.
 //
-// A row of d values is handled by d / 16 neighbouring lanes, 16 values each: two 16-byte loads of
-// bf16 and one 16-byte store of codes (write), or the reverse (read).  The row's exponent comes
+// A row of d values is handled by d / 16 neighbouring lanes, twice 8 values each, half a row apart: 16-byte
+// accesses of bf16 and 8-byte accesses of codes, each contiguous over the lanes (32 contiguous bytes a
+// lane would leave every access with half of each sector).  The row's exponent comes
 // from an integer maximum over the bf16 bit patterns (a shuffle reduction over the lanes), so the
 // only floating-point steps are an exact multiplication by a power of two and one rounding to
 // e4m3; reading back is exact (4 significant bits times 2^e).  Memory bound: 3 d + 1 bytes per row.
@@ -13,73 +14,97 @@ namespace ss {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kUnroll = 2;   // rows in flight per thread
+constexpr int kUnroll = 4;   // rows in flight per thread (128 bytes each way at most)
 
-// Unsigned division by a launch constant: q = (mulhi(n, m) + n) >> s for n < 2^31.
-struct Div {
-  uint32_t d, m, s;
-};
-Div make_div(uint32_t d) {
-  uint32_t s = 0;
-  while ((1ull << s) < d) ++s;
-  const uint64_t m = ((1ull << 32) * ((1ull << s) - d)) / d + 1;
-  return {d, (uint32_t)m, s};
-}
-__device__ __forceinline__ uint32_t quot(const Div& v, uint32_t n) {
-  return (uint32_t)(((uint64_t)__umulhi(n, v.m) + n) >> v.s);
-}
-
-struct RowAt {
-  int64_t b16;      // element offset on the bf16 side
-  int64_t c8, sc;   // byte offsets of the codes and of the scale byte
-  bool v, live;
-  bool zero;        // (read) page outside the pool: the row reads as zeros
+// A block takes kUnroll * kThreads / (d / 16) rows: 2^shift consecutive tokens (T of them for short calls) of
+// as many (K|V, head) pairs of one request as that makes, so the request, its count and its offset are
+// the block's and a row's place costs shifts.  (Rows numbered through and divided down took 183 us for
+// 102,000 prompt tokens of 8 heads instead of the time below.)
+struct Plan {
+  int shift;                   // log2 of the tokens of a block
+  int token_blocks, pair_blocks;
 };
 
-// Row number -> addresses.  Rows are numbered (request, K|V, head, row), the row fastest.
+struct Block {
+  int b, k0, pair0, n;   // request, first row, first pair, rows that the call covers
+  int64_t off;
+};
 template <bool WRITE>
-__device__ __forceinline__ RowAt row_at(const Copy8Params& p, const Div& dT, const Div& dH, uint32_t row, bool report) {
-  RowAt a;
-  uint32_t x = quot(dT, row);
-  const int k = (int)(row - x * dT.d);
-  const uint32_t y = quot(dH, x);
-  const int h = (int)(x - y * dH.d);
-  a.v = y & 1;
-  const int b = (int)(y >> 1);
-  const bool first = report && h == 0 && !a.v;  // one row of its kind reports
-  a.live = false;
-  a.zero = false;
-  int n = p.cnt ? p.cnt[b] : p.T;
-  if (n < 0 || n > p.T) {
-    if (first && k == 0) atomicOr(p.status, WRITE ? SS_DEV_BAD_ACCEPT : SS_DEV_BAD_VALID_LEN);
-    n = max(0, min(n, p.T));
+__device__ __forceinline__ Block block_at(const Copy8Params& p, const Plan& plan) {
+  Block w;
+  int x = blockIdx.x;
+  const int tb = x % plan.token_blocks;
+  x /= plan.token_blocks;
+  const int pb = x % plan.pair_blocks;
+  w.b = x / plan.pair_blocks;
+  w.k0 = tb << plan.shift;
+  w.pair0 = pb * ((kUnroll * kThreads * 16 / p.d) >> plan.shift);
+  w.n = p.cnt ? p.cnt[w.b] : p.T;
+  w.off = p.off ? (int64_t)p.off[w.b] : 0;
+  if (w.n < 0 || w.n > p.T) {
+    if (threadIdx.x == 0 && tb == 0 && pb == 0) atomicOr(p.status, WRITE ? SS_DEV_BAD_ACCEPT : SS_DEV_BAD_VALID_LEN);
+    w.n = max(0, min(w.n, p.T));
   }
-  if (k >= n) return a;
-  int src = k;
+  return w;
+}
+
+// One (K|V, head) pair of a request: where its rows are on both sides.
+struct Pair {
+  uint16_t* rows;        // bf16 row 0
+  uint8_t *codes, *scales;   // outer index 0, token 0
+  uint64_t row_st, code_sb, code_st, scale_sb, scale_st;
+};
+__device__ __forceinline__ Pair pair_at(const Copy8Params& p, int b, int pair) {
+  const bool v = pair >= p.H_kv;
+  const int h = v ? pair - p.H_kv : pair;
+  Pair a;
+  a.rows = v ? p.V + b * p.v_sb + h * p.v_sh : p.K + b * p.k_sb + h * p.k_sh;
+  a.codes = v ? p.kv.V + h * p.kv.v_sh : p.kv.K + h * p.kv.k_sh;
+  a.scales = v ? p.kv.Vs + h * p.kv.vs_sh : p.kv.Ks + h * p.kv.ks_sh;
+  a.row_st = v ? p.v_st : p.k_st;
+  a.code_sb = v ? p.kv.v_sb : p.kv.k_sb;
+  a.code_st = v ? p.kv.v_st : p.kv.k_st;
+  a.scale_sb = v ? p.kv.vs_sb : p.kv.ks_sb;
+  a.scale_st = v ? p.kv.vs_st : p.kv.ks_st;
+  return a;
+}
+
+// Row k of the call: its row on the bf16 side (src) and its place in the cache.
+struct Place {
+  uint32_t src, outer, inner;
+  bool live, zero;       // zero: (read) in a page outside the pool, reads as zeros
+};
+template <bool WRITE>
+__device__ __forceinline__ Place place_of(const Copy8Params& p, const Block& w, int k, bool report) {
+  Place a = {(uint32_t)k, 0, 0, false, false};
+  if (k >= w.n) return a;
   if (WRITE && p.idx) {
-    src = p.idx[(int64_t)b * p.T + k];
+    const int src = p.idx[(int64_t)w.b * p.T + k];
     if (src < 0 || src >= p.T) {
-      if (first) atomicOr(p.status, SS_DEV_BAD_ACCEPT);
+      if (report) atomicOr(p.status, SS_DEV_BAD_ACCEPT);
       return a;
     }
+    a.src = src;
   }
-  const int64_t tok = (p.off ? (int64_t)p.off[b] : 0) + k;
+  const int64_t tok = w.off + k;
   if (tok < 0 || tok >= p.kv.room) {
-    if (first) atomicOr(p.status, WRITE ? SS_DEV_DST_OVERFLOW : SS_DEV_BAD_VALID_LEN);
+    if (report) atomicOr(p.status, WRITE ? SS_DEV_DST_OVERFLOW : SS_DEV_BAD_VALID_LEN);
     return a;
   }
-  int inner, outer = outer8(p.kv, b, (int)tok, &inner);
-  if (outer < 0) {
-    if (first) atomicOr(p.status, SS_DEV_BAD_PAGE);
-    if (WRITE) return a;
-    a.zero = true;
-    outer = 0;
-  }
   a.live = true;
-  a.b16 = b * (a.v ? p.v_sb : p.k_sb) + h * (a.v ? p.v_sh : p.k_sh) + src * (a.v ? p.v_st : p.k_st);
-  a.c8 = outer * (a.v ? p.kv.v_sb : p.kv.k_sb) + h * (a.v ? p.kv.v_sh : p.kv.k_sh) + inner * (a.v ? p.kv.v_st : p.kv.k_st);
-  a.sc = outer * (a.v ? p.kv.vs_sb : p.kv.ks_sb) + h * (a.v ? p.kv.vs_sh : p.kv.ks_sh) +
-         inner * (a.v ? p.kv.vs_st : p.kv.ks_st);
+  a.outer = w.b;
+  a.inner = (uint32_t)tok;
+  if (p.kv.page_table) {
+    const uint32_t t = (uint32_t)tok, pg = p.kv.page_log2 >= 0 ? t >> p.kv.page_log2 : t / (uint32_t)p.kv.page_size;
+    a.inner = t - pg * p.kv.page_size;
+    a.outer = (uint32_t)p.kv.page_table[(int64_t)w.b * p.kv.pages_per_req + pg];
+    if (a.outer >= (uint32_t)p.kv.n_outer) {
+      if (report) atomicOr(p.status, SS_DEV_BAD_PAGE);
+      a.live = !WRITE;
+      a.zero = true;
+      a.outer = 0;
+    }
+  }
   return a;
 }
 
@@ -90,109 +115,142 @@ __device__ __forceinline__ uint32_t top_of(uint32_t two, uint32_t top) {
   if (hi < 0x7f80u) top = max(top, hi);
   return top;
 }
-__device__ __forceinline__ uint32_t codes_of(uint32_t two, float inv) {
-  const float2 v = make_float2(__uint_as_float(two << 16) * inv, __uint_as_float(two & 0xffff0000u) * inv);
+__device__ __forceinline__ uint32_t codes_of(uint32_t two, float2 inv) {
+  const float2 v = __fmul2_rn(make_float2(__uint_as_float(two << 16), __uint_as_float(two & 0xffff0000u)), inv);
   return __nv_cvt_float2_to_fp8x2(v, __NV_SATFINITE, __NV_E4M3);
 }
-__device__ __forceinline__ uint32_t bf16_of(uint32_t two, float scale) {
+__device__ __forceinline__ uint32_t bf16_of(uint32_t two, float2 scale) {
   const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)two, __NV_E4M3);
-  const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&h));
-  const __nv_bfloat162 o = __floats2bfloat162_rn(v.x * scale, v.y * scale);
+  const float2 v = __fmul2_rn(__half22float2(*reinterpret_cast<const __half2*>(&h)), scale);
+  const __nv_bfloat162 o = __floats2bfloat162_rn(v.x, v.y);
   return *reinterpret_cast<const uint32_t*>(&o);
 }
 
-template <int D>
-__global__ void __launch_bounds__(kThreads) write8_kernel(const __grid_constant__ Copy8Params p, const Div dT,
-                                                          const Div dH, const uint32_t rows) {
+// ONE: all rows of the block belong to one pair (calls of many rows), whose addresses are the block's.
+template <int D, bool ONE>
+__global__ void __launch_bounds__(kThreads) write8_kernel(const __grid_constant__ Copy8Params p, const Plan plan) {
   constexpr int LPR = D / 16, RPB = kThreads / LPR;
   const int part = threadIdx.x % LPR;
-  const uint32_t row0 = blockIdx.x * (RPB * kUnroll) + threadIdx.x / LPR;
-  RowAt at[kUnroll];
+  pdl_wait_prior();
+  pdl_launch_dependents();
+  const Block w = block_at<true>(p, plan);
+  if (w.k0 >= w.n) return;
+  Pair one;
+  if (ONE) one = pair_at(p, w.b, w.pair0);
+  Place at[kUnroll];
   uint4 raw[kUnroll][2];
 #pragma unroll
   for (int u = 0; u < kUnroll; ++u) {
-    const uint32_t row = row0 + u * RPB;
-    at[u].live = false;
-    if (row < rows) at[u] = row_at<true>(p, dT, dH, row, part == 0);
+    const int i = threadIdx.x / LPR + u * RPB;
+    const int pair = ONE ? w.pair0 : w.pair0 + (i >> plan.shift), k = w.k0 + (ONE ? i : i & ((1 << plan.shift) - 1));
+    at[u] = place_of<true>(p, w, pair < 2 * p.H_kv ? k : w.n, part == 0 && pair == 0);
     raw[u][0] = raw[u][1] = make_uint4(0, 0, 0, 0);
     if (at[u].live) {
-      const uint4* src = reinterpret_cast<const uint4*>((at[u].v ? p.V : p.K) + at[u].b16 + part * 16);
+      const Pair a = ONE ? one : pair_at(p, w.b, pair);
+      const uint4* src = reinterpret_cast<const uint4*>(a.rows + at[u].src * a.row_st) + part;
       raw[u][0] = __ldcs(src);
-      raw[u][1] = __ldcs(src + 1);
+      raw[u][1] = __ldcs(src + LPR);
     }
   }
 #pragma unroll
   for (int u = 0; u < kUnroll; ++u) {
-    const uint32_t w[8] = {raw[u][0].x, raw[u][0].y, raw[u][0].z, raw[u][0].w,
+    const uint32_t x[8] = {raw[u][0].x, raw[u][0].y, raw[u][0].z, raw[u][0].w,
                            raw[u][1].x, raw[u][1].y, raw[u][1].z, raw[u][1].w};
-    uint32_t top = 0;
+    uint32_t top2 = 0;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) top = top_of(w[j], top);
+    for (int j = 0; j < 8; ++j) top2 = __vmaxu2(top2, x[j] & 0x7fff7fffu);
+    uint32_t top = max(top2 & 0xffffu, top2 >> 16);
+    if (__any_sync(0xffffffffu, top >= 0x7f80u)) {  // infinities and NaN do not count
+      top = 0;
+#pragma unroll 1
+      for (int j = 0; j < 8; ++j) top = top_of(x[j], top);
+    }
 #pragma unroll
     for (int o = LPR / 2; o; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
     // top = (1 + f / 128) 2^(E - 127) against 448 = (1 + 96 / 128) 2^8
-    const int e = max(kMinExp8, min(kMaxExp8, (int)(top >> 7) - 127 - 8 + ((top & 127u) > 96u ? 1 : 0)));
-    const float inv = pow2_8(-e);
+    const int e = max(kMinExp8, min(kMaxExp8, (int)((top + 31u) >> 7) - 127 - 8));
+    const float2 inv = make_float2(pow2_8(-e), pow2_8(-e));
     if (!at[u].live) continue;
     uint32_t c[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) c[j] = codes_of(w[2 * j], inv) | (codes_of(w[2 * j + 1], inv) << 16);
-    *reinterpret_cast<uint4*>((at[u].v ? p.kv.V : p.kv.K) + at[u].c8 + part * 16) = make_uint4(c[0], c[1], c[2], c[3]);
-    if (part == 0) (at[u].v ? p.kv.Vs : p.kv.Ks)[at[u].sc] = (uint8_t)(e + 127);
+    for (int j = 0; j < 4; ++j) c[j] = codes_of(x[2 * j], inv) | (codes_of(x[2 * j + 1], inv) << 16);
+    const int pair = ONE ? w.pair0 : w.pair0 + ((threadIdx.x / LPR + u * RPB) >> plan.shift);
+    const Pair a = ONE ? one : pair_at(p, w.b, pair);
+    uint2* dst = reinterpret_cast<uint2*>(a.codes + at[u].outer * a.code_sb + at[u].inner * a.code_st) + part;
+    dst[0] = make_uint2(c[0], c[1]);
+    dst[LPR] = make_uint2(c[2], c[3]);
+    if (part == 0) a.scales[at[u].outer * a.scale_sb + at[u].inner * a.scale_st] = (uint8_t)(e + 127);
   }
 }
 
-template <int D>
-__global__ void __launch_bounds__(kThreads) read8_kernel(const __grid_constant__ Copy8Params p, const Div dT,
-                                                         const Div dH, const uint32_t rows) {
+template <int D, bool ONE>
+__global__ void __launch_bounds__(kThreads) read8_kernel(const __grid_constant__ Copy8Params p, const Plan plan) {
   constexpr int LPR = D / 16, RPB = kThreads / LPR;
   const int part = threadIdx.x % LPR;
-  const uint32_t row0 = blockIdx.x * (RPB * kUnroll) + threadIdx.x / LPR;
-  RowAt at[kUnroll];
-  uint4 raw[kUnroll];
+  pdl_wait_prior();
+  pdl_launch_dependents();
+  const Block w = block_at<false>(p, plan);
+  if (w.k0 >= w.n) return;
+  Pair one;
+  if (ONE) one = pair_at(p, w.b, w.pair0);
+  uint16_t* to[kUnroll];
+  uint2 raw[kUnroll][2];
   uint32_t sc[kUnroll];
 #pragma unroll
   for (int u = 0; u < kUnroll; ++u) {
-    const uint32_t row = row0 + u * RPB;
-    at[u].live = false;
-    if (row < rows) at[u] = row_at<false>(p, dT, dH, row, part == 0);
-    raw[u] = make_uint4(0, 0, 0, 0);
+    const int i = threadIdx.x / LPR + u * RPB;
+    const int pair = ONE ? w.pair0 : w.pair0 + (i >> plan.shift), k = w.k0 + (ONE ? i : i & ((1 << plan.shift) - 1));
+    const Place at = place_of<false>(p, w, pair < 2 * p.H_kv ? k : w.n, part == 0 && pair == 0);
+    to[u] = nullptr;
+    raw[u][0] = raw[u][1] = make_uint2(0, 0);
     sc[u] = 127;
-    if (at[u].live && !at[u].zero) {
-      raw[u] = __ldcs(reinterpret_cast<const uint4*>((at[u].v ? p.kv.V : p.kv.K) + at[u].c8 + part * 16));
-      sc[u] = (at[u].v ? p.kv.Vs : p.kv.Ks)[at[u].sc];
+    if (at.live) {
+      const Pair a = ONE ? one : pair_at(p, w.b, pair);
+      to[u] = a.rows + at.src * a.row_st;
+      if (!at.zero) {
+        const uint2* src = reinterpret_cast<const uint2*>(a.codes + at.outer * a.code_sb + at.inner * a.code_st) + part;
+        raw[u][0] = __ldcs(src);
+        raw[u][1] = __ldcs(src + LPR);
+        sc[u] = a.scales[at.outer * a.scale_sb + at.inner * a.scale_st];
+      }
     }
   }
 #pragma unroll
   for (int u = 0; u < kUnroll; ++u) {
-    if (!at[u].live) continue;
-    const float scale = scale8(sc[u]);
-    const uint32_t w[4] = {raw[u].x, raw[u].y, raw[u].z, raw[u].w};
+    if (!to[u]) continue;
+    const float2 scale = make_float2(scale8(sc[u]), scale8(sc[u]));
+    const uint32_t x[4] = {raw[u][0].x, raw[u][0].y, raw[u][1].x, raw[u][1].y};
     uint32_t o[8];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      o[2 * j] = bf16_of(w[j] & 0xffffu, scale);
-      o[2 * j + 1] = bf16_of(w[j] >> 16, scale);
+      o[2 * j] = bf16_of(x[j] & 0xffffu, scale);
+      o[2 * j + 1] = bf16_of(x[j] >> 16, scale);
     }
-    uint4* dst = reinterpret_cast<uint4*>((at[u].v ? p.V : p.K) + at[u].b16 + part * 16);
+    uint4* dst = reinterpret_cast<uint4*>(to[u]) + part;
     dst[0] = make_uint4(o[0], o[1], o[2], o[3]);
-    dst[1] = make_uint4(o[4], o[5], o[6], o[7]);
+    dst[LPR] = make_uint4(o[4], o[5], o[6], o[7]);
   }
 }
 
 template <bool WRITE>
-cudaError_t launch_copy(const Copy8Params& p, cudaStream_t s) {
-  const uint32_t rows = (uint32_t)p.B * p.T * p.H_kv * 2;  // below 2^31 (checked by the caller)
-  const uint32_t per = kThreads / (p.d / 16) * kUnroll;
-  const dim3 grid((rows + per - 1) / per), block(kThreads);
-  const Div dT = make_div(p.T), dH = make_div(p.H_kv);
-  if (p.d == 128) return launch_kernel(WRITE ? write8_kernel<128> : read8_kernel<128>, grid, block, 0, s, false, p, dT, dH, rows);
-  return launch_kernel(WRITE ? write8_kernel<64> : read8_kernel<64>, grid, block, 0, s, false, p, dT, dH, rows);
+cudaError_t launch_copy(const Copy8Params& p, cudaStream_t s, bool pdl) {
+  const int rows = kUnroll * kThreads * 16 / p.d;
+  Plan plan = {0, 0, 0};
+  while (1 << plan.shift < p.T && 1 << plan.shift < rows) ++plan.shift;
+  const int pairs = rows >> plan.shift;
+  plan.token_blocks = (p.T + (1 << plan.shift) - 1) >> plan.shift;
+  plan.pair_blocks = (2 * p.H_kv + pairs - 1) / pairs;
+  const dim3 grid((unsigned)plan.token_blocks * plan.pair_blocks * p.B), block(kThreads);  // below 2^31: see the caller
+  auto kernel = p.d == 128 ? pairs == 1 ? (WRITE ? write8_kernel<128, true> : read8_kernel<128, true>)
+                                        : (WRITE ? write8_kernel<128, false> : read8_kernel<128, false>)
+                           : pairs == 1 ? (WRITE ? write8_kernel<64, true> : read8_kernel<64, true>)
+                                        : (WRITE ? write8_kernel<64, false> : read8_kernel<64, false>);
+  return launch_kernel(kernel, grid, block, 0, s, pdl, p, plan);
 }
 
 }  // namespace
 
-cudaError_t launch_kv8_write(const Copy8Params& p, cudaStream_t s) { return launch_copy<true>(p, s); }
-cudaError_t launch_kv8_read(const Copy8Params& p, cudaStream_t s) { return launch_copy<false>(p, s); }
+cudaError_t launch_kv8_write(const Copy8Params& p, cudaStream_t s, bool pdl) { return launch_copy<true>(p, s, pdl); }
+cudaError_t launch_kv8_read(const Copy8Params& p, cudaStream_t s, bool pdl) { return launch_copy<false>(p, s, pdl); }
 
 }  // namespace ss
