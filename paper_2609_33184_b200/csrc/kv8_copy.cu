@@ -14,14 +14,18 @@ namespace ss {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kUnroll = 4;   // rows in flight per thread (128 bytes each way at most)
 
-// A block takes kUnroll * kThreads / (d / 16) rows: 2^shift consecutive tokens (T of them for short calls) of
+// U rows in flight per thread: 4 for calls that fill the GPU, 1 for small ones, which want short
+// threads and many blocks (102,000 prompt tokens of 8 heads: 110 us with 4, 118 with 2, 158 with 1; 32
+// requests' accepted tokens: 4.4, 2.8 and 2.4 us).
+//
+// A block takes U * kThreads / (d / 16) rows: 2^shift consecutive tokens (T of them for short calls) of
 // as many (K|V, head) pairs of one request as that makes, so the request, its count and its offset are
 // the block's and a row's place costs shifts.  (Rows numbered through and divided down took 183 us for
 // 102,000 prompt tokens of 8 heads instead of the time below.)
 struct Plan {
   int shift;                   // log2 of the tokens of a block
+  int pairs;                   // pairs of a block
   int token_blocks, pair_blocks;
 };
 
@@ -38,7 +42,7 @@ __device__ __forceinline__ Block block_at(const Copy8Params& p, const Plan& plan
   const int pb = x % plan.pair_blocks;
   w.b = x / plan.pair_blocks;
   w.k0 = tb << plan.shift;
-  w.pair0 = pb * ((kUnroll * kThreads * 16 / p.d) >> plan.shift);
+  w.pair0 = pb * plan.pairs;
   w.n = p.cnt ? p.cnt[w.b] : p.T;
   w.off = p.off ? (int64_t)p.off[w.b] : 0;
   if (w.n < 0 || w.n > p.T) {
@@ -127,7 +131,7 @@ __device__ __forceinline__ uint32_t bf16_of(uint32_t two, float2 scale) {
 }
 
 // ONE: all rows of the block belong to one pair (calls of many rows), whose addresses are the block's.
-template <int D, bool ONE>
+template <int D, bool ONE, int U>
 __global__ void __launch_bounds__(kThreads) write8_kernel(const __grid_constant__ Copy8Params p, const Plan plan) {
   constexpr int LPR = D / 16, RPB = kThreads / LPR;
   const int part = threadIdx.x % LPR;
@@ -137,10 +141,10 @@ __global__ void __launch_bounds__(kThreads) write8_kernel(const __grid_constant_
   if (w.k0 >= w.n) return;
   Pair one;
   if (ONE) one = pair_at(p, w.b, w.pair0);
-  Place at[kUnroll];
-  uint4 raw[kUnroll][2];
+  Place at[U];
+  uint4 raw[U][2];
 #pragma unroll
-  for (int u = 0; u < kUnroll; ++u) {
+  for (int u = 0; u < U; ++u) {
     const int i = threadIdx.x / LPR + u * RPB;
     const int pair = ONE ? w.pair0 : w.pair0 + (i >> plan.shift), k = w.k0 + (ONE ? i : i & ((1 << plan.shift) - 1));
     at[u] = place_of<true>(p, w, pair < 2 * p.H_kv ? k : w.n, part == 0 && pair == 0);
@@ -153,7 +157,7 @@ __global__ void __launch_bounds__(kThreads) write8_kernel(const __grid_constant_
     }
   }
 #pragma unroll
-  for (int u = 0; u < kUnroll; ++u) {
+  for (int u = 0; u < U; ++u) {
     const uint32_t x[8] = {raw[u][0].x, raw[u][0].y, raw[u][0].z, raw[u][0].w,
                            raw[u][1].x, raw[u][1].y, raw[u][1].z, raw[u][1].w};
     uint32_t top2 = 0;
@@ -162,7 +166,7 @@ __global__ void __launch_bounds__(kThreads) write8_kernel(const __grid_constant_
     uint32_t top = max(top2 & 0xffffu, top2 >> 16);
     if (__any_sync(0xffffffffu, top >= 0x7f80u)) {  // infinities and NaN do not count
       top = 0;
-#pragma unroll 1
+#pragma unroll
       for (int j = 0; j < 8; ++j) top = top_of(x[j], top);
     }
 #pragma unroll
@@ -183,7 +187,7 @@ __global__ void __launch_bounds__(kThreads) write8_kernel(const __grid_constant_
   }
 }
 
-template <int D, bool ONE>
+template <int D, bool ONE, int U>
 __global__ void __launch_bounds__(kThreads) read8_kernel(const __grid_constant__ Copy8Params p, const Plan plan) {
   constexpr int LPR = D / 16, RPB = kThreads / LPR;
   const int part = threadIdx.x % LPR;
@@ -193,11 +197,11 @@ __global__ void __launch_bounds__(kThreads) read8_kernel(const __grid_constant__
   if (w.k0 >= w.n) return;
   Pair one;
   if (ONE) one = pair_at(p, w.b, w.pair0);
-  uint16_t* to[kUnroll];
-  uint2 raw[kUnroll][2];
-  uint32_t sc[kUnroll];
+  uint16_t* to[U];
+  uint2 raw[U][2];
+  uint32_t sc[U];
 #pragma unroll
-  for (int u = 0; u < kUnroll; ++u) {
+  for (int u = 0; u < U; ++u) {
     const int i = threadIdx.x / LPR + u * RPB;
     const int pair = ONE ? w.pair0 : w.pair0 + (i >> plan.shift), k = w.k0 + (ONE ? i : i & ((1 << plan.shift) - 1));
     const Place at = place_of<false>(p, w, pair < 2 * p.H_kv ? k : w.n, part == 0 && pair == 0);
@@ -216,7 +220,7 @@ __global__ void __launch_bounds__(kThreads) read8_kernel(const __grid_constant__
     }
   }
 #pragma unroll
-  for (int u = 0; u < kUnroll; ++u) {
+  for (int u = 0; u < U; ++u) {
     if (!to[u]) continue;
     const float2 scale = make_float2(scale8(sc[u]), scale8(sc[u]));
     const uint32_t x[4] = {raw[u][0].x, raw[u][0].y, raw[u][1].x, raw[u][1].y};
@@ -232,20 +236,25 @@ __global__ void __launch_bounds__(kThreads) read8_kernel(const __grid_constant__
   }
 }
 
+template <bool WRITE, int D, int U>
+cudaError_t launch_rows8(const Copy8Params& p, cudaStream_t s, bool pdl) {
+  constexpr int kRows = U * kThreads * 16 / D;
+  Plan plan = {0, 0, 0, 0};
+  while (1 << plan.shift < p.T && 1 << plan.shift < kRows) ++plan.shift;
+  plan.pairs = kRows >> plan.shift;
+  plan.token_blocks = (p.T + (1 << plan.shift) - 1) >> plan.shift;
+  plan.pair_blocks = (2 * p.H_kv + plan.pairs - 1) / plan.pairs;
+  const dim3 grid((unsigned)plan.token_blocks * plan.pair_blocks * p.B), block(kThreads);  // below 2^31: see the caller
+  auto kernel = plan.pairs == 1 ? (WRITE ? write8_kernel<D, true, U> : read8_kernel<D, true, U>)
+                                : (WRITE ? write8_kernel<D, false, U> : read8_kernel<D, false, U>);
+  return launch_kernel(kernel, grid, block, 0, s, pdl, p, plan);
+}
 template <bool WRITE>
 cudaError_t launch_copy(const Copy8Params& p, cudaStream_t s, bool pdl) {
-  const int rows = kUnroll * kThreads * 16 / p.d;
-  Plan plan = {0, 0, 0};
-  while (1 << plan.shift < p.T && 1 << plan.shift < rows) ++plan.shift;
-  const int pairs = rows >> plan.shift;
-  plan.token_blocks = (p.T + (1 << plan.shift) - 1) >> plan.shift;
-  plan.pair_blocks = (2 * p.H_kv + pairs - 1) / pairs;
-  const dim3 grid((unsigned)plan.token_blocks * plan.pair_blocks * p.B), block(kThreads);  // below 2^31: see the caller
-  auto kernel = p.d == 128 ? pairs == 1 ? (WRITE ? write8_kernel<128, true> : read8_kernel<128, true>)
-                                        : (WRITE ? write8_kernel<128, false> : read8_kernel<128, false>)
-                           : pairs == 1 ? (WRITE ? write8_kernel<64, true> : read8_kernel<64, true>)
-                                        : (WRITE ? write8_kernel<64, false> : read8_kernel<64, false>);
-  return launch_kernel(kernel, grid, block, 0, s, pdl, p, plan);
+  // large: more rows than one block per SM would take with four in flight per thread
+  const bool large = (int64_t)p.B * p.T * p.H_kv * 2 > (int64_t)kNumSM * 4 * kThreads * 16 / p.d;
+  if (p.d == 128) return large ? launch_rows8<WRITE, 128, 4>(p, s, pdl) : launch_rows8<WRITE, 128, 1>(p, s, pdl);
+  return large ? launch_rows8<WRITE, 64, 4>(p, s, pdl) : launch_rows8<WRITE, 64, 1>(p, s, pdl);
 }
 
 }  // namespace
