@@ -383,10 +383,10 @@ ss_status ss_create(ss_ctx** out, const ss_config* cfg, void* workspace, size_t 
   if ((uintptr_t)workspace & 255) return SS_ERR_ALIGN;
   const Layout L = layout_for(cfg);
   if (workspace_bytes < L.total) return SS_ERR_CAPACITY;
-  cudaDeviceProp prop;
-  cudaError_t e = cudaGetDeviceProperties(&prop, cfg->device);
+  int major = 0;  // (one attribute: all properties of the device take milliseconds to collect)
+  cudaError_t e = cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, cfg->device);
   if (e != cudaSuccess) return SS_ERR_CUDA;
-  if (prop.major != 10) return SS_ERR_UNSUPPORTED;
+  if (major != 10) return SS_ERR_UNSUPPORTED;
   e = cudaSetDevice(cfg->device);
   if (e != cudaSuccess) return SS_ERR_CUDA;
 
