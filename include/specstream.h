@@ -329,7 +329,7 @@ ss_status ss_kv8_read(ss_ctx* ctx, const ss_cache8* cache, ss_tensor K, ss_tenso
  * between replays. */
 ss_status ss_verify_chunk8(ss_ctx* ctx, const ss_cache8* cache, const int32_t* valid_len, void* stream);
 
-/* Decoding: attention of Q [B, H_q, T_q, d] over the 8-bit cache alone in one launch, O and LSE as
+/* Decoding: attention of Q [B, H_q, T_q, d] over the 8-bit cache alone, O and LSE as
  * ss_verify_finalize writes them.  Every query sees all valid tokens, so a step with T_q = 1 is
  * ss_kv8_write of the new token and ss_decode8; candidates that must not see one another go through
  * a round (ss_verify_chunk8 + ss_verify_local).  SS_ERR_STATE while a round is open. */

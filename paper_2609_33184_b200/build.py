@@ -10,7 +10,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libspecstream.so")
 SOURCES = ["api.cu", "chunk_simt.cu", "chunk_tc.cu", "chunk_tc_keys.cu", "local_finalize.cu", "stream_round.cu", "static_round.cu", "tier.cu", "width.cu", "cohort.cu", "probe.cu",
-           "kv8_copy.cu", "kv8_attn_simt.cu", "kv8_attn_tc.cu"]
+           "kv8_copy.cu", "kv8_attn_simt.cu", "kv8_attn_tc.cu", "kv8_join.cu"]
 
 
 def _newest_source_mtime() -> float:

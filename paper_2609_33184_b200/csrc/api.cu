@@ -69,8 +69,7 @@ struct ss_ctx {
   int hist_n[4];            // maps in use per slot (0 = empty)
   uint64_t hist_age[4];
   bool hist_pinned[4];      // the list was used under a stream capture: a graph may replay the launch, never evicted
-  unsigned int* tickets8;   // 8-bit cache: one ticket per unit of an attention launch (zero between launches)
-  float* scratch8;          // and the partial states of units cut by a share's end
+  float* scratch8;          // 8-bit cache: partial states of units cut by a share's end
   cudaEvent_t* ev_pool;     // timing events of the streamed round (SS_FLAG_STREAM_TIMING)
   int ev_pool_n;
 };
@@ -139,8 +138,7 @@ int slot_capacity_for(const ss_config* c) {
 
 constexpr int kHistSlots = 4;
 struct Layout {
-  size_t off_hist, off_ml, off_a, off_tickets8, off_scratch8, total;
-  size_t n_tickets8;
+  size_t off_hist, off_ml, off_a, off_scratch8, total;
   int64_t set_stride_ml, set_stride_a;
   int R_stride;
 };
@@ -157,9 +155,7 @@ Layout layout_for(const ss_config* c) {
                ss::kRoundCounters * sizeof(unsigned int);   // status, trace region, round counters
   L.off_ml = L.off_hist + kHistSlots * 2 * ss::kMaxHistChunks * sizeof(CUtensorMap);  // lists of tensor maps
   L.off_a = align_up(L.off_ml + (size_t)sets * rows * sizeof(float2), 256);
-  L.off_tickets8 = align_up(L.off_a + (size_t)sets * rows * c->d * sizeof(float), 256);
-  L.n_tickets8 = (size_t)c->max_B * c->H_kv * ((L.R_stride + ss::kMinRows8 - 1) / ss::kMinRows8);
-  L.off_scratch8 = align_up(L.off_tickets8 + L.n_tickets8 * sizeof(unsigned int), 256);
+  L.off_scratch8 = align_up(L.off_a + (size_t)sets * rows * c->d * sizeof(float), 256);
   const size_t rows8 = L.R_stride < ss::kRows8 ? L.R_stride : ss::kRows8;
   L.total = align_up(L.off_scratch8 + 2 * ss::kCtas8 * rows8 * (c->d + 4) * sizeof(float), 256);
   return L;
@@ -406,7 +402,6 @@ ss_status ss_create(ss_ctx** out, const ss_config* cfg, void* workspace, size_t 
   c->trace = (unsigned long long*)(c->ws + 256);
   c->round_counters = (unsigned int*)(c->ws + 256 + align_up(ss::kTraceWords * sizeof(unsigned long long), 256));
   c->hist_maps = (CUtensorMap*)(c->ws + L.off_hist);
-  c->tickets8 = (unsigned int*)(c->ws + L.off_tickets8);
   c->scratch8 = (float*)(c->ws + L.off_scratch8);
   c->part_ml = (float2*)(c->ws + L.off_ml);
   c->part_a = (float*)(c->ws + L.off_a);
@@ -449,7 +444,6 @@ ss_status ss_create(ss_ctx** out, const ss_config* cfg, void* workspace, size_t 
   }
   e = cudaMemset(c->status, 0, 256);
   if (e == cudaSuccess) e = cudaMemset(c->round_counters, 0, ss::kRoundCounters * sizeof(unsigned int));
-  if (e == cudaSuccess) e = cudaMemset(c->tickets8, 0, L.n_tickets8 * sizeof(unsigned int));
   if (e != cudaSuccess) {
     delete c;
     return SS_ERR_CUDA;
@@ -1329,17 +1323,21 @@ static ss_status attn8(ss_ctx* c, const ss_tensor& Q, int32_t B, int32_t T_q, fl
   p->scale_log2 = scale * 1.4426950408889634f;
   p->min_tiles = 1;
   p->scratch = c->scratch8;
-  p->tickets = c->tickets8;
   p->status = c->status;
   DeviceGuard on(c->cfg.device);
   if (on.err != cudaSuccess) return cuda_fail(c, on.err);
   // Both kernels wait for the one in front of them before they touch anything, so they can always be
   // launched under programmatic stream serialization (only launch and set-up overlap).
   const bool pdl = !c->no_overlap;
-  const cudaError_t e = tc ? ss::launch_attn8_tc(*p, tmK, tmV, s, pdl) : ss::launch_attn8_simt(*p, s, pdl);
+  cudaError_t e = tc ? ss::launch_attn8_tc(*p, tmK, tmV, s, pdl) : ss::launch_attn8_simt(*p, s, pdl);
   if (e != cudaSuccess) return cuda_fail(c, e);
   c->last_kernel = tc ? "kv8-tcgen05" : "kv8-simt";
   ++c->launches;
+  if (p->kv.room > ss::kTok8) {  // (a unit of one tile is never cut)
+    e = ss::launch_attn8_join(*p, s, pdl);
+    if (e != cudaSuccess) return cuda_fail(c, e);
+    ++c->launches;
+  }
   ++c->stats.chunk_calls;
   c->stats.kv_bytes += (int64_t)B * p->kv.room * c->cfg.H_kv * (c->cfg.d + 1) * 2;
   return SS_OK;

@@ -13,8 +13,8 @@
 // on the device) are given to the CTAs in equal shares, so a long request is split over many CTAs
 // and short ones are gathered in one, whatever the batch looks like and without the host knowing
 // the lengths.  A unit inside one share is finished by its CTA; a unit cut by a share's end leaves
-// one partial state (m, l, a[d]) per CTA in the scratch area, and the CTA that finishes last (a
-// ticket per unit) joins them in CTA order, so the result does not depend on which one that is.
+// one partial state (m, l, a[d]) per CTA in the scratch area, and a second kernel joins them in CTA order
+// (kv8_join.cu), so results do not depend on timing.
 #pragma once
 #include <cuda_fp16.h>
 
@@ -52,7 +52,6 @@ struct Attn8Params {
   float scale_log2;
   int min_tiles;              // a share holds at least this many tiles
   float* scratch;             // 2 slots per CTA of rows_per_tile * (d + 4) floats: (m, l) pairs, room, a[]
-  unsigned int* tickets;      // one per unit, zero between launches
   __nv_bfloat16* O;           // either the finished output ...
   float* LSE;
   float2* part_ml;            // ... or (O null) one partial state per row, as the chunk kernels leave them
@@ -74,6 +73,7 @@ cudaError_t launch_kv8_write(const Copy8Params& p, cudaStream_t s, bool pdl);
 cudaError_t launch_kv8_read(const Copy8Params& p, cudaStream_t s, bool pdl);
 cudaError_t launch_attn8_simt(const Attn8Params& p, cudaStream_t s, bool pdl);
 cudaError_t launch_attn8_tc(const Attn8Params& p, const CUtensorMap& tmK, const CUtensorMap& tmV, cudaStream_t s, bool pdl);
+cudaError_t launch_attn8_join(const Attn8Params& p, cudaStream_t s, bool pdl);
 cudaError_t attn8_tc_prepare();  // one-time function attributes
 
 // ---- device side ---------------------------------------------------------------------------
@@ -115,6 +115,14 @@ __device__ __forceinline__ uint32_t share_of8(const Share8& s, uint32_t x) {
   return x < big ? x / (s.q + 1) : s.more + (x - big) / s.q;
 }
 
+// From the number of tiles to the shares of a launch of at most `grid` CTAs.
+__device__ __forceinline__ void set_shares8(const Attn8Params& p, uint32_t grid, Share8* s) {
+  const uint32_t want = (s->total + p.min_tiles - 1) / p.min_tiles;
+  s->ctas = min(max(want, 1u), grid);
+  s->q = s->total / s->ctas;
+  s->more = s->total - s->q * s->ctas;
+}
+
 // By one whole warp.  CTA 0 also reports lengths that had to be clamped.
 __device__ __forceinline__ Share8 find_share8(const Attn8Params& p) {
   const int lane = threadIdx.x & 31;
@@ -134,10 +142,7 @@ __device__ __forceinline__ Share8 find_share8(const Attn8Params& p) {
   }
   if (blockIdx.x == 0 && __any_sync(0xffffffffu, bad) && lane == 0) atomicOr(p.status, SS_DEV_BAD_VALID_LEN);
   s.total = __reduce_add_sync(0xffffffffu, sum);
-  const uint32_t want = (s.total + p.min_tiles - 1) / p.min_tiles;
-  s.ctas = want < gridDim.x ? max(want, 1u) : gridDim.x;
-  s.q = s.total / s.ctas;
-  s.more = s.total - s.q * s.ctas;
+  set_shares8(p, gridDim.x, &s);
   if (blockIdx.x >= s.ctas || s.total == 0) return s;
   s.lo = share_lo8(s, blockIdx.x);
   s.hi = share_lo8(s, blockIdx.x + 1);
@@ -163,7 +168,7 @@ __device__ __forceinline__ Share8 find_share8(const Attn8Params& p) {
 }
 
 struct Seg8 {
-  int b, kvh, unit;         // unit = number of the unit among all B * H_kv * row_tiles
+  int b, kvh;
   int t0, t1, n;            // tiles [t0, t1) of the unit's n
   int len;                  // tokens of the request
   uint32_t base, start, pos;  // tiles before the request, before the unit, before the segment's end
@@ -174,7 +179,6 @@ __device__ __forceinline__ void seg_set8(const Attn8Params& p, const Share8& s, 
   const uint32_t u = (g->pos - g->base) / (uint32_t)g->n;
   const int kvh = p.row_tiles == 1 ? u : u / (uint32_t)p.row_tiles, rt = u - kvh * p.row_tiles;
   g->kvh = kvh;
-  g->unit = (g->b * p.H_kv + kvh) * p.row_tiles + rt;
   g->start = g->base + u * g->n;
   g->t0 = (int)(g->pos - g->start);
   g->pos = min(g->start + g->n, s.hi);
@@ -224,16 +228,6 @@ __device__ __forceinline__ void put_a8(const Attn8Params& p, const Seg8& g, int 
     p.part_a[(((int64_t)g.b * p.H_kv + g.kvh) * p.R_stride + g.row0 + r) * p.d + c] = a;
   }
 }
-__device__ __forceinline__ void put_a8x4(const Attn8Params& p, const Seg8& g, int r, int c, float l, float4 a) {
-  if (p.O) {
-    const float inv = (l > 0.f || l != l) ? 1.f / l : 0.f;
-    const __nv_bfloat162 lo = __floats2bfloat162_rn(a.x * inv, a.y * inv), hi = __floats2bfloat162_rn(a.z * inv, a.w * inv);
-    *reinterpret_cast<uint2*>(p.O + (((int64_t)g.b * p.H_kv + g.kvh) * p.R + g.row0 + r) * p.d + c) =
-        make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
-  } else {
-    *reinterpret_cast<float4*>(p.part_a + (((int64_t)g.b * p.H_kv + g.kvh) * p.R_stride + g.row0 + r) * p.d + c) = a;
-  }
-}
 // Requests without a visible token, by `n` threads of every CTA.
 __device__ __forceinline__ void put_empty8(const Attn8Params& p, int tid, int n) {
   for (int b = blockIdx.x; b < p.B; b += gridDim.x) {
@@ -249,130 +243,11 @@ __device__ __forceinline__ void put_empty8(const Attn8Params& p, int tid, int n)
   }
 }
 
-template <int N>
-__device__ __forceinline__ void bar8() {
-  asm volatile("bar.sync 1, %0;" ::"n"(N) : "memory");
-}
-
 // Slot of CTA i's state of the unit that begins at tile `start` (first CTA i0): the first segment of a
 // share uses the CTA's even slot, a later one (always the last) the odd slot.
 __device__ __forceinline__ float* slot8(const Attn8Params& p, const Share8& s, uint32_t start, uint32_t i) {
   const int odd = share_lo8(s, i) < start ? 1 : 0;
   return p.scratch + (int64_t)(2 * i + odd) * p.rows_per_tile * (p.d + 4);
-}
-
-// Four head dims c .. c + 3 of rows r, r + STEP, ..: the sum over the unit's n states of weight * a, with
-// ROWS * STATES loads of 16 bytes in flight (weights of the block's row k in w[state * block + k].x, the
-// row's sum in w[n * block + k].y).
-template <int D, int ROWS, int STATES, int STEP>
-__device__ __forceinline__ void join_rows8(const Attn8Params& p, const Seg8& g, const float* first, const float* rest,
-                                           const float2* w, int block, int r0, int r, int n, int c) {
-  const int64_t slot = (int64_t)p.rows_per_tile * (D + 4);
-  float4 a[ROWS];
-#pragma unroll
-  for (int k = 0; k < ROWS; ++k) a[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 1
-  for (int j0 = 0; j0 < n; j0 += STATES) {
-    float4 v[STATES][ROWS];
-#pragma unroll
-    for (int j = 0; j < STATES; ++j) {
-      const int i = min(j0 + j, n - 1);
-      const float* src = (i == 0 ? first : rest + (int64_t)(i - 1) * 2 * slot) + 4 * p.rows_per_tile + c;
-#pragma unroll
-      for (int k = 0; k < ROWS; ++k)
-        v[j][k] = __ldcg(reinterpret_cast<const float4*>(src + (r0 + min(r + k * STEP, block - 1)) * D));
-    }
-#pragma unroll
-    for (int j = 0; j < STATES; ++j) {
-#pragma unroll
-      for (int k = 0; k < ROWS; ++k) {
-        const float f = j0 + j < n ? w[(j0 + j) * block + min(r + k * STEP, block - 1)].x : 0.f;
-        a[k].x = fmaf(f, v[j][k].x, a[k].x);
-        a[k].y = fmaf(f, v[j][k].y, a[k].y);
-        a[k].z = fmaf(f, v[j][k].z, a[k].z);
-        a[k].w = fmaf(f, v[j][k].w, a[k].w);
-      }
-    }
-  }
-#pragma unroll
-  for (int k = 0; k < ROWS; ++k) {
-    const int row = r + k * STEP;
-    if (row < block) put_a8x4(p, g, r0 + row, c, w[n * block + row].y, a[k]);
-  }
-}
-
-// By N threads (128 or 256), after each has stored its part of this CTA's state in its slot: takes the
-// unit's ticket and, for the last CTA, joins all states.  *flag and buf (kJoinBuf8 pairs) are shared
-// memory.  A read of another CTA's state is a read of L2, so all of a block of rows' (m, l) are fetched at once,
-// then their a[] with 16 loads of a thread in flight: one row and state after the other, the
-// join took 120 us for 37 states of 4 rows.
-constexpr int kJoinBuf8 = 512;
-static_assert(kCtas8 + 1 <= kJoinBuf8, "a row's states fit the buffer");
-template <int D, int N>
-__device__ __noinline__ void join8(const Attn8Params& p, const Share8& s, const Seg8& g, int tid, int* flag, float2* buf) {
-  const int i0 = share_of8(s, g.start), i1 = share_of8(s, g.start + g.n - 1);
-  bar8<N>();
-  if (tid == 0) {
-    // released after all the CTA's stores (the barrier), acquired before the loads of the others' states
-    uint32_t before;
-    asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], 1;" : "=r"(before) : "l"(&p.tickets[g.unit]) : "memory");
-    const int last = before == (uint32_t)(i1 - i0);
-    if (last) p.tickets[g.unit] = 0;  // nobody else touches it any more in this launch
-    *flag = last;
-  }
-  bar8<N>();
-  if (!*flag) return;
-  const int n = i1 - i0 + 1;               // >= 2: the unit is cut
-  const float* first = slot8(p, s, g.start, i0);
-  const float* rest = slot8(p, s, g.start, i0 + 1);   // those after the first are the CTAs' even slots
-  const int64_t slot = (int64_t)p.rows_per_tile * (D + 4);
-  const int most = kJoinBuf8 / (n + 1);  // rows at a time, >= 1: n <= kCtas8
-  for (int r0 = 0; r0 < g.nrows; r0 += most) {
-    const int block = min(most, g.nrows - r0);
-    if ((tid & 31) < block) {
-#pragma unroll 4
-      for (int j = tid >> 5; j < n; j += N / 32) {
-        const float* src = j == 0 ? first : rest + (int64_t)(j - 1) * 2 * slot;
-        buf[j * block + (tid & 31)] = __ldcg(reinterpret_cast<const float2*>(src) + r0 + (tid & 31));
-      }
-    }
-    bar8<N>();
-    // eight lanes per row: maximum, weights, sum (left in entry n of the row)
-    for (int rr = tid >> 3; rr < (block + N / 8 - 1) / (N / 8) * (N / 8); rr += N / 8) {
-      const int r = min(rr, block - 1), part = tid & 7;
-      const bool mine = rr < block;
-      float m = -INFINITY, l = 0.f;
-      for (int j = part; j < n; j += 8) {
-        const float2 st = buf[j * block + r];
-        if (st.y != 0.f) m = fmaxf(m, st.x);
-      }
-#pragma unroll
-      for (int o = 4; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-      for (int j = part; j < n; j += 8) {
-        const float2 st = buf[j * block + r];
-        const float w = st.y == 0.f ? 0.f : st.x == m ? 1.f : exp2f(st.x - m);  // (an empty state's a[] is not read)
-        l = fmaf(w, st.y, l);
-        if (mine) buf[j * block + r].x = w;
-      }
-#pragma unroll
-      for (int o = 4; o; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
-      if (mine && part == 0) {
-        buf[n * block + r].y = l;
-        put_ml8(p, g, r0 + r, m, l);
-      }
-    }
-    bar8<N>();
-    constexpr int kLanes = D / 4, G = N / kLanes;  // lanes per row, rows side by side
-    const int c = tid % kLanes * 4, r = tid / kLanes;
-    if (block <= G) {
-      join_rows8<D, 1, 16, G>(p, g, first, rest, buf, block, r0, r, n, c);
-    } else if (n <= 4) {
-      for (int k = r; k < block; k += 4 * G) join_rows8<D, 4, 4, G>(p, g, first, rest, buf, block, r0, k, n, c);
-    } else {
-      for (int k = r; k < block; k += 2 * G) join_rows8<D, 2, 8, G>(p, g, first, rest, buf, block, r0, k, n, c);
-    }
-    bar8<N>();
-  }
 }
 
 }  // namespace ss

@@ -36,11 +36,9 @@ template <int D>
 __global__ void __launch_bounds__(128) attn8_simt_kernel(const __grid_constant__ Attn8Params p) {
   constexpr int CPL = D / 32;  // head dims per lane in the output
   __shared__ __align__(16) float q_s[kRT][D];
-  __shared__ __align__(16) float w_s[4][32][kRT];  // (also the join's buffer)
-  static_assert(sizeof(w_s) >= kJoinBuf8 * sizeof(float2), "join buffer");
+  __shared__ __align__(16) float w_s[4][32][kRT];
   __shared__ float2 ml_s[4][kRT];
   __shared__ float a_s[4][kRT][D];
-  __shared__ int flag;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   pdl_wait_prior();
   pdl_launch_dependents();
@@ -176,7 +174,6 @@ __global__ void __launch_bounds__(128) attn8_simt_kernel(const __grid_constant__
         slot[4 * p.rows_per_tile + r * D + c] = A;
       }
     }
-    if (!whole) join8<D, 128>(p, share, g, tid, &flag, reinterpret_cast<float2*>(w_s));
   }
   put_empty8(p, tid, 128);
 }

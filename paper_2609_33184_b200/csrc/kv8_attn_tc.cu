@@ -27,7 +27,7 @@
 // the scores, head dim in the output), one TMA producer warp, one MMA issuer warp.  The producer runs
 // ahead across segment ends, so a new segment finds its first tiles in shared memory.  Two CTAs per
 // SM (at most 110 KB shared memory, 256 TMEM columns each) hide each other's segment ends.
-// Every wait is bounded; on expiry the CTA raises SS_DEV_WAIT_EXPIRED and leaves its tickets in order.
+// Every wait is bounded; on expiry the CTA raises SS_DEV_WAIT_EXPIRED and returns.
 #include <cuda_fp8.h>
 
 #include "kv8.cuh"
@@ -46,7 +46,6 @@ struct alignas(16) Ctl8 {
   uint64_t sfull[2], pready, pfree, qfull;
   uint32_t tmem_base;
   volatile uint32_t abort;
-  int last;
   int has[2];                     // the softmax warps' current and next segment (in use by turns)
   Seg8 seg[2];
   Share8 share;
@@ -81,7 +80,6 @@ struct Cfg8 {
   static constexpr uint32_t kTmemCols = kCols <= 64 ? 64 : kCols <= 128 ? 128 : 256;
   static constexpr uint32_t kColO = 2 * NS;
   static_assert(kUnits >= 4 && kCols <= 256 && RT % 8 == 0, "shape");
-  static_assert(kPBytes >= (int)(kJoinBuf8 * sizeof(float2)), "the join's buffer lies over the weights");
 };
 
 // A descriptor's low word holds the address / 16 (and the LBO above it), so the operands of the steps of
@@ -106,6 +104,10 @@ template <int D>
 __device__ __forceinline__ uint64_t desc8(uint32_t saddr, uint32_t lbo) {
   return (uint64_t)((saddr >> 4) & 0x3FFF) | ((uint64_t)(lbo >> 4) << 16) | ((uint64_t)((8 * D) >> 4) << 32) |
          (1ull << 46) | ((D == 128 ? 2ull : 4ull) << 61);
+}
+template <int N>
+__device__ __forceinline__ void bar8() {
+  asm volatile("bar.sync 1, %0;" ::"n"(N) : "memory");
 }
 __device__ __forceinline__ float redux_max(float v) {
   float r;
@@ -132,8 +134,8 @@ __device__ __forceinline__ uint32_t residue(uint32_t w) {
   return h2_bits(__hmul2(__hsub2(bits_h2(w), bits_h2(w & 0xff00ff00u)), __float2half2_rn(8.f)));
 }
 // Bounded wait: one try in line, the loop out of line.  A wait that gives up (or finds that another has)
-// returns like one that succeeded: what follows works on whatever is there, inside the CTA's own memory,
-// and only waits, tickets and barriers matter until the CTA leaves.
+// returns like one that succeeded: what follows works on whatever is there, inside the CTA's own memory
+// and its own slots, until the CTA leaves.
 __device__ __noinline__ void wait_slow(uint64_t* bar, uint32_t parity, volatile uint32_t* abort, uint32_t* status) {
   if (*abort == 0) mbar_wait_abortable(bar, parity, abort, status);
 }
@@ -693,7 +695,6 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
         }
       }
       tc_fence_before();
-      if (!whole) join8<D, SOFT>(p, share, done, tid, &ctl->last, reinterpret_cast<float2*>(p_s));
       bar8<SOFT>();  // sums, references and Q may be written anew
     }
     put_empty8(p, tid, SOFT);
