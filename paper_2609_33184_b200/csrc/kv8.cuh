@@ -130,6 +130,7 @@ __device__ __forceinline__ Share8 find_share8(const Attn8Params& p) {
   Share8 s = {};
   uint32_t sum = 0, n = 0;
   bool bad = false;
+#pragma unroll 1
   for (int b = lane; b < p.B; b += 32) {
     int len = p.kv.room;
     if (p.valid_len) {
@@ -147,6 +148,7 @@ __device__ __forceinline__ Share8 find_share8(const Attn8Params& p) {
   s.lo = share_lo8(s, blockIdx.x);
   s.hi = share_lo8(s, blockIdx.x + 1);
   uint32_t base = 0;
+#pragma unroll 1
   for (int b = 0; b < p.B; b += 32) {
     if (p.B > 32) n = b + lane < p.B ? units * tiles8(len8(p, b + lane)) : 0;  // (else still there)
     uint32_t incl = n;
@@ -199,6 +201,7 @@ __device__ __forceinline__ bool seg_first8(const Attn8Params& p, const Share8& s
 __device__ __forceinline__ bool seg_next8(const Attn8Params& p, const Share8& s, Seg8* g) {
   if (g->pos >= s.hi) return false;
   const uint32_t units = (uint32_t)(p.H_kv * p.row_tiles);
+#pragma unroll 1
   while (g->pos >= g->base + units * g->n) {  // the next request with tokens (there is one: pos < hi <= total)
     g->base += units * g->n;
     ++g->b;
@@ -228,18 +231,23 @@ __device__ __forceinline__ void put_a8(const Attn8Params& p, const Seg8& g, int 
     p.part_a[(((int64_t)g.b * p.H_kv + g.kvh) * p.R_stride + g.row0 + r) * p.d + c] = a;
   }
 }
-// Requests without a visible token, by `n` threads of every CTA.
-__device__ __forceinline__ void put_empty8(const Attn8Params& p, int tid, int n) {
+// Requests without a visible token, by `n` threads of every CTA.  (Out of line, not unrolled: what a
+// kernel seldom runs should not stand between the parts that it always runs.)
+static __device__ __noinline__ void put_empty8(const Attn8Params& p, int tid, int n) {
+#pragma unroll 1
   for (int b = blockIdx.x; b < p.B; b += gridDim.x) {
     if (len8(p, b) > 0) continue;
-    for (int i = tid; i < p.H_kv * p.R; i += n) {
+    const int rows = p.H_kv * p.R;
+#pragma unroll 1
+    for (int i = tid; i < rows; i += n) {
       const int kvh = i / p.R, r = i - kvh * p.R;
       if (!p.O) p.part_ml[((int64_t)b * p.H_kv + kvh) * p.R_stride + r] = make_float2(-INFINITY, 0.f);
-      else if (p.LSE) p.LSE[((int64_t)b * p.H_kv + kvh) * p.R + r] = -INFINITY;
+      else if (p.LSE) p.LSE[(int64_t)b * rows + i] = -INFINITY;
     }
-    if (p.O)
-      for (int64_t i = tid; i < (int64_t)p.H_kv * p.R * p.d; i += n)
-        p.O[(int64_t)b * p.H_kv * p.R * p.d + i] = __float2bfloat16_rn(0.f);
+    if (!p.O) continue;
+    uint4* o = reinterpret_cast<uint4*>(p.O + (int64_t)b * rows * p.d);  // 8 values of bf16 zeros
+#pragma unroll 1
+    for (int i = tid; i < rows * (p.d / 8); i += n) o[i] = make_uint4(0, 0, 0, 0);
   }
 }
 

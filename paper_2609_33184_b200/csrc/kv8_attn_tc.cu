@@ -136,8 +136,8 @@ __device__ __forceinline__ uint32_t residue(uint32_t w) {
 // Bounded wait: one try in line, the loop out of line.  A wait that gives up (or finds that another has)
 // returns like one that succeeded: what follows works on whatever is there, inside the CTA's own memory
 // and its own slots, until the CTA leaves.
-__device__ __noinline__ void wait_slow(uint64_t* bar, uint32_t parity, volatile uint32_t* abort, uint32_t* status) {
-  if (*abort == 0) mbar_wait_abortable(bar, parity, abort, status);
+__device__ __noinline__ bool wait_slow(uint64_t* bar, uint32_t parity, volatile uint32_t* abort, uint32_t* status) {
+  return *abort == 0 && mbar_wait_abortable(bar, parity, abort, status);
 }
 __device__ __forceinline__ void wait8(uint64_t* bar, uint32_t parity, volatile uint32_t* abort, uint32_t* status) {
   if (!mbar_try_wait(bar, parity)) wait_slow(bar, parity, abort, status);
@@ -216,7 +216,7 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
   const uint32_t tmem = ctl->tmem_base;
   const Share8& share = ctl->share;
   auto mwait = [&](uint64_t* bar, uint32_t parity) {
-    return mbar_wait_abortable(bar, parity, &ctl->abort, p.status);
+    return mbar_try_wait(bar, parity) || wait_slow(bar, parity, &ctl->abort, p.status);
   };
 
   if (warp == kProducerWarp) {
@@ -513,6 +513,7 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
           const int jv = 2 * it + 1;
           wait(&ctl->ufull[jv % UNITS], (jv / UNITS) & 1);
           uint4* v = reinterpret_cast<uint4*>(smem + (jv % UNITS) * C::kUnitBytes);
+#pragma unroll 1
           for (int i = n_valid * (D / 16) + tid; i < kTok8 * (D / 16); i += SOFT) v[i] = make_uint4(0, 0, 0, 0);
         }
         // x[r] = s2 + ev - M + bias (in the segment's first tile s2 + ev)
@@ -667,29 +668,36 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
       wait(&ctl->pfree, (it - 1) & 1);
       tc_fence_after();
       bar8<SOFT>();
+      // the unit's result when it is whole, this CTA's state of it when it is cut
       const bool whole = done.t0 == 0 && done.t1 == done.n;
       float* slot = slot8(p, share, done.start, blockIdx.x);
       auto row_l = [&](int r) { return (ctl->smax[0][r] + ctl->smax[1][r]) + (ctl->smax[2][r] + ctl->smax[3][r]); };
-      {
-        if (tid < done.nrows) {
-          const float m = -ctl->nm[tid], l = row_l(tid);  // the sums are of 2^(s2 - M + bias)
-          if (whole) put_ml8(p, done, tid, m, l);
-          else reinterpret_cast<float2*>(slot)[tid] = make_float2(m, l);
-        }
+      if (tid < done.nrows) {
+        const float m = -ctl->nm[tid], l = row_l(tid);  // the sums are of 2^(s2 - M + bias)
+        if (whole) put_ml8(p, done, tid, m, l);
+        else reinterpret_cast<float2*>(slot)[tid] = make_float2(m, l);
+      }
+      const int64_t pair = (int64_t)done.b * p.H_kv + done.kvh;
+      const bool to_o = whole && p.O;
+      __nv_bfloat16* o_row = p.O + (pair * p.R + done.row0) * D + key;
+      float* a_row = (whole ? p.part_a + (pair * p.R_stride + done.row0) * D : slot + 4 * p.rows_per_tile) + key;
 #pragma unroll 1
-        for (int q = 0; q < RT; q += 8) {
-          uint32_t o[3][8];
+      for (int q = c0; q < c0 + RT && q < done.nrows; q += 8) {
+        uint32_t o[3][8];
 #pragma unroll
-          for (int k = 0; k < 3; ++k) tmem_ld<8>(tmem + lane_off + C::kColO + k * NR + c0 + q, o[k]);
-          tc_wait_ld();
+        for (int k = 0; k < 3; ++k) tmem_ld<8>(tmem + lane_off + C::kColO + k * NR + q, o[k]);
+        tc_wait_ld();
+        const int n = key < D ? done.nrows - q : 0;
 #pragma unroll
-          for (int c = 0; c < 8; ++c) {
-            const int r = c0 + q + c;
-            if (r < done.nrows && key < D) {
-              const float a = fmaf(__uint_as_float(o[2][c]), 1.f / 64.f,
-                                   fmaf(__uint_as_float(o[1][c]), 0.125f, __uint_as_float(o[0][c])));
-              if (whole) put_a8(p, done, r, key, row_l(r), a);
-              else slot[4 * p.rows_per_tile + r * D + key] = a;
+        for (int c = 0; c < 8; ++c) {
+          const float a = fmaf(__uint_as_float(o[2][c]), 1.f / 64.f,
+                               fmaf(__uint_as_float(o[1][c]), 0.125f, __uint_as_float(o[0][c])));
+          if (c < n) {
+            if (to_o) {
+              const float l = row_l(q + c);
+              o_row[(q + c) * D] = __float2bfloat16_rn(l > 0.f || l != l ? a * (1.f / l) : 0.f);
+            } else {
+              a_row[(q + c) * D] = a;
             }
           }
         }
