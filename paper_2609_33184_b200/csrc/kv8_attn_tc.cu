@@ -51,6 +51,7 @@ struct alignas(16) Ctl8 {
   Share8 share;
   alignas(16) float nm[NR];       // bias - M
   alignas(16) float qf[NR];       // 2^eq * scale * log2(e)
+  alignas(16) float up[NR];       // rise of the references; at a segment's end 1 / row sum
   alignas(16) float smax[4][NR];  // per warp: maxima of a tile; at a segment's end the row sums
 };
 
@@ -480,10 +481,6 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
       q_load(s);
     };
     if (ctl->has[0]) seg_fetch(ctl->seg[0]);
-    auto top4 = [&](int r) {
-      return fmaxf(fmaxf(ctl->smax[0][r], ctl->smax[1][r]), fmaxf(ctl->smax[2][r], ctl->smax[3][r]));
-    };
-
     int it = 0;
     for (int k_seg = 0; ctl->has[k_seg & 1]; ++k_seg) {
       const Seg8& g = ctl->seg[k_seg & 1];
@@ -562,8 +559,13 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
           }
           if (lane < RT) ctl->smax[quad][c0 + lane] = mine;
           bar8<SOFT>();
-          // M rises by this much (in the first tile, from 0 to the maximum - bias)
-          auto rise = [&](int r) { return first ? top4(r) - kBias : fmaxf(0.f, top4(r) - kBias); };
+          if (tid < NR) {  // M rises by this much (in the first tile, from 0 to the maximum - bias)
+            const float top = fmaxf(fmaxf(ctl->smax[0][tid], ctl->smax[1][tid]), fmaxf(ctl->smax[2][tid], ctl->smax[3][tid]));
+            const float up = first ? top - kBias : fmaxf(0.f, top - kBias);
+            ctl->up[tid] = up;
+            ctl->nm[tid] -= up;
+          }
+          bar8<SOFT>();
           if (!first) {
             wait(&ctl->pfree, (it - 1) & 1);  // the output MMAs of the tile before have retired
             tc_fence_after();
@@ -576,7 +578,7 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
                 tmem_ld<8>(at, o);
                 tc_wait_ld();
 #pragma unroll
-                for (int c = 0; c < 8; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * ex2_ftz(-rise(c0 + r + c)));
+                for (int c = 0; c < 8; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * ex2_ftz(-ctl->up[c0 + r + c]));
                 tmem_st<8>(at, o);
               }
             }
@@ -584,13 +586,10 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
           }
 #pragma unroll
           for (int r = 0; r < RT / 2; ++r) {
-            const float2 up = make_float2(rise(c0 + 2 * r), rise(c0 + 2 * r + 1));
+            const float2 up = *reinterpret_cast<const float2*>(&ctl->up[c0 + 2 * r]);
             x[r] = __fadd2_rn(x[r], make_float2(-up.x, -up.y));
             if (!first) lsum[r] = __fmul2_rn(lsum[r], make_float2(ex2_ftz(-up.x), ex2_ftz(-up.y)));
           }
-          bar8<SOFT>();
-          if (tid < NR) ctl->nm[tid] -= rise(tid);
-          bar8<SOFT>();
         }
         if (!first) wait(&ctl->pfree, (it - 1) & 1);  // P^T has been consumed
         {
@@ -671,12 +670,14 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
       // the unit's result when it is whole, this CTA's state of it when it is cut
       const bool whole = done.t0 == 0 && done.t1 == done.n;
       float* slot = slot8(p, share, done.start, blockIdx.x);
-      auto row_l = [&](int r) { return (ctl->smax[0][r] + ctl->smax[1][r]) + (ctl->smax[2][r] + ctl->smax[3][r]); };
       if (tid < done.nrows) {
-        const float m = -ctl->nm[tid], l = row_l(tid);  // the sums are of 2^(s2 - M + bias)
+        // (the sums are of 2^(s2 - M + bias))
+        const float m = -ctl->nm[tid], l = (ctl->smax[0][tid] + ctl->smax[1][tid]) + (ctl->smax[2][tid] + ctl->smax[3][tid]);
         if (whole) put_ml8(p, done, tid, m, l);
         else reinterpret_cast<float2*>(slot)[tid] = make_float2(m, l);
+        ctl->up[tid] = l > 0.f || l != l ? 1.f / l : 0.f;
       }
+      bar8<SOFT>();
       const int64_t pair = (int64_t)done.b * p.H_kv + done.kvh;
       const bool to_o = whole && p.O;
       __nv_bfloat16* o_row = p.O + (pair * p.R + done.row0) * D + key;
@@ -694,8 +695,7 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
                                fmaf(__uint_as_float(o[1][c]), 0.125f, __uint_as_float(o[0][c])));
           if (c < n) {
             if (to_o) {
-              const float l = row_l(q + c);
-              o_row[(q + c) * D] = __float2bfloat16_rn(l > 0.f || l != l ? a * (1.f / l) : 0.f);
+              o_row[(q + c) * D] = __float2bfloat16_rn(a * ctl->up[q + c]);
             } else {
               a_row[(q + c) * D] = a;
             }
