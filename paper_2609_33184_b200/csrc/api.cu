@@ -1350,6 +1350,10 @@ ss_status ss_verify_chunk8(ss_ctx* c, const ss_cache8* cache, const int32_t* val
   memset(&p, 0, sizeof(p));
   ss_status st = view8(c, cache, c->B, &p.kv);  // (before a fold is enqueued)
   if (st != SS_OK) return st;
+  if (p.kv.room > c->cfg.max_Lc) return SS_ERR_SHAPE;
+  if ((uintptr_t)valid_len & 3) return SS_ERR_ALIGN;
+  DeviceGuard on(c->cfg.device);
+  if (on.err != cudaSuccess) return cuda_fail(c, on.err);
   if (c->n_sets == c->n_set_cap) {
     const cudaError_t e = fold_sets(c, c->stream);
     if (e != cudaSuccess) return cuda_fail(c, e);

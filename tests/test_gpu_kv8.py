@@ -619,3 +619,130 @@ def test_which_kernel_runs(page, kernel):
     assert ctx.last_chunk_kernel() == kernel
     check_attention(Q, O, LSE, lambda b: history(cache, b, 500), 64 ** -0.5)
     ctx.close()
+
+
+MORE = [
+    # B, H_q, H_kv, d, T_q, lens, page, order, pad
+    (2, 8, 2, 128, 3, [5000, 131], 64, (0, 1, 2), 0),                    # 12 rows
+    (2, 16, 2, 128, 4, [2600, 999], 16, (0, 2, 1), 0),                   # 32 rows
+    (2, 10, 2, 128, 8, [1300, 700], 8, (0, 1, 2), 16),                   # 40 rows in two tiles
+    (1, 8, 1, 128, 1, [40001], 128, (0, 1, 2), 0),                       # more CTAs than 128-token pages per share
+    (1, 16, 1, 64, 2, [70000], 64, (0, 1, 2), 0),
+    (3, 6, 3, 128, 1, [1152, 700, 384], 384, (0, 1, 2), 0),              # pages of three tiles
+    (2, 4, 2, 64, 1, [1025, 1024], 0, (0, 2, 1), 16),                    # dense, tokens interleaved with heads
+    (40, 4, 4, 128, 1, [1 + (b * 53) % 300 for b in range(40)], 32, (0, 1, 2), 0),
+    (33, 5, 1, 64, 7, [0 if b % 3 else 200 + b for b in range(33)], 16, (0, 1, 2), 0),
+]
+
+
+@pytest.mark.parametrize("case", MORE, ids=lambda c: f"B{c[0]}_{c[1]}x{c[2]}_d{c[3]}_T{c[4]}_p{c[6]}")
+def test_attention_on_the_tensor_cores(case):
+    ssb = _ssb()
+    B, H_q, H_kv, d, T, lens, page, order, pad = case
+    cache = make_cache(ssb, B, H_kv, d, page, max(lens) + 30, B + d, order, pad)
+    poison(cache, lens)
+    Q = torch.randn(B, H_q, T, d, generator=_gen(6)).bfloat16().to(DEV)
+    ctx = ssb.Context(B, H_q, H_kv, d, T, 1, cache.desc.page_size * cache.desc.pages_per_req)
+    O, LSE = decode(ssb, cache, Q, lens, ctx=ctx)
+    assert ctx.last_chunk_kernel() == "kv8-tcgen05"
+    check_attention(Q, O, LSE, lambda b: history(cache, b, lens[b]), d ** -0.5)
+    vl = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    ctx.ss_decode8(Q, d ** -0.5, cache, vl, O.zero_(), None)             # LSE is optional
+    again, _ = decode(ssb, cache, Q, lens, ctx=ctx)
+    assert torch.equal(O.view(torch.int16), again.view(torch.int16))
+    ctx.close()
+
+
+def test_calls_back_to_back_on_one_context():
+    """Large and small batches (units cut and whole, with and without a join) in one stream without a wait between
+    them: every result as when it is computed alone."""
+    ssb = _ssb()
+    H_q, H_kv, d = 8, 2, 128
+    ctx = ssb.Context(6, H_q, H_kv, d, 4, 4, 8192, flags=ssb.SS_FLAG_OVERLAP_CHUNKS)
+    jobs = []
+    for k, (B, T, page, lens) in enumerate([(1, 1, 64, [8000]), (6, 1, 16, [3, 90, 128, 1, 17, 60]), (2, 4, 64, [5000, 1]),
+                                            (1, 1, 128, [100]), (6, 3, 32, [700] * 6), (3, 1, 0, [0, 0, 129])]):
+        cache = make_cache(ssb, B, H_kv, d, page, max(lens) + 1, 40 + k)
+        Q = torch.randn(B, H_q, T, d, generator=_gen(k)).bfloat16().to(DEV)
+        vl = torch.tensor(lens, dtype=torch.int32, device=DEV)
+        alone = decode(ssb, cache, Q, lens, ctx=ctx)
+        check_attention(Q, *alone, lambda b: history(cache, b, lens[b]), d ** -0.5)
+        jobs.append((cache, Q, vl, alone))
+    outs = []
+    for turn in range(5):
+        for k in np.random.RandomState(turn).permutation(len(jobs)):
+            cache, Q, vl, alone = jobs[k]
+            O, LSE = torch.empty_like(alone[0]), torch.empty_like(alone[1])
+            ctx.ss_decode8(Q, d ** -0.5, cache, vl, O, LSE)
+            outs.append((k, O, LSE))
+    torch.cuda.synchronize()
+    assert ctx.ss_poll_status() == (0, 0)
+    for k, O, LSE in outs:
+        assert torch.equal(O.view(torch.int16), jobs[k][3][0].view(torch.int16)) and torch.equal(LSE, jobs[k][3][1]), k
+    ctx.close()
+
+
+def test_a_query_that_is_not_finite_spoils_its_own_row_only():
+    ssb = _ssb()
+    H_q, H_kv, d, n = 8, 2, 128, 500
+    cache = make_cache(ssb, 1, H_kv, d, 16, n, 3)
+    Q = torch.randn(1, H_q, 2, d, generator=_gen(1)).bfloat16().to(DEV)
+    bad = Q.clone()
+    bad[0, 1, 0, 7], bad[0, 6, 1, 100] = float("nan"), float("inf")
+    good, gl = decode(ssb, cache, Q, [n])
+    O, LSE = decode(ssb, cache, bad, [n])
+    hit = torch.zeros(1, H_q, 2, dtype=torch.bool, device=DEV)
+    hit[0, 1, 0] = hit[0, 6, 1] = True
+    assert torch.isnan(O[hit]).all() and torch.isnan(LSE[hit]).all()
+    assert torch.equal(O[~hit], good[~hit]) and torch.equal(LSE[~hit], gl[~hit])
+
+
+def test_state_of_an_8_bit_chunk_can_be_exported():
+    """The chunk's merged state leaves one round and enters another as any partial state does."""
+    ssb = _ssb()
+    B, H_q, H_kv, d, T = 2, 8, 2, 128, 3
+    lens = [900, 140]
+    cache = make_cache(ssb, B, H_kv, d, 64, 1000, 4)
+    poison(cache, lens)
+    vl = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    Q = torch.randn(B, H_q, T, d, generator=_gen(2)).bfloat16().to(DEV)
+    ctx = ssb.Context(B, H_q, H_kv, d, T, T, 1024)
+    rows = B * H_q * T
+    ml, a = torch.empty(rows, 2, device=DEV), torch.empty(rows, d, device=DEV)
+    O, LSE = torch.empty_like(Q), torch.empty(B, H_q, T, device=DEV)
+    ctx.ss_verify_begin(Q, 0.1)
+    ctx.ss_verify_chunk8(cache, vl)
+    ctx.ss_verify_export_state(ml, a)
+    ctx.ss_verify_abort()
+    ctx.ss_verify_begin(Q, 0.1)
+    ctx.ss_verify_import_state(ml, a)
+    ctx.ss_verify_finalize(O, LSE)
+    assert ctx.ss_poll_status() == (0, 0)
+    check_attention(Q, O, LSE, lambda b: history(cache, b, lens[b]), 0.1)
+    ctx.close()
+
+
+@pytest.mark.parametrize("T", [64, 65, 130, 700])
+def test_writes_across_block_sizes(T):
+    """Rows that end inside a block of either size, small and large calls, counts and offsets of their own."""
+    ssb = _ssb()
+    for B, H_kv, d in ((3, 2, 64), (24, 8, 128)):
+        ctx = ssb.Context(B, H_kv, H_kv, d, 1, 1, 64)
+        cache = make_cache(ssb, B, H_kv, d, 16, T + 40, T + B)
+        g = _gen(T)
+        K, V = (torch.randn(B, H_kv, T, d, generator=g).bfloat16() for _ in range(2))
+        cnt = torch.tensor([(T * (b + 1)) // B for b in range(B)], dtype=torch.int32, device=DEV)
+        off = torch.tensor([(7 * b) % 41 for b in range(B)], dtype=torch.int32, device=DEV)
+        ctx.ss_kv8_write(cache, K.to(DEV), V.to(DEV), off, cnt)
+        Kr, Vr = (torch.full((B, H_kv, T, d), 3.0, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+        ctx.ss_kv8_read(cache, Kr, Vr, off, cnt)
+        assert ctx.ss_poll_status() == (0, 0)
+        for b in range(0, B, 5):
+            n = int(cnt[b])
+            for src, got in ((K, Kr), (V, Vr)):
+                for h in range(H_kv):
+                    for r in {0, n // 2, n - 1}:
+                        want = kv8.decode(*kv8.encode_row(src[b, h, r].double().numpy()))
+                        assert np.array_equal(got[b, h, r].double().cpu().numpy(), want), (b, h, r)
+                assert (got[b, :, n:] == 3.0).all()
+        ctx.close()
