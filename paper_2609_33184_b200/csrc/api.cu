@@ -70,6 +70,9 @@ struct ss_ctx {
   uint64_t hist_age[4];
   bool hist_pinned[4];      // the list was used under a stream capture: a graph may replay the launch, never evicted
   float* scratch8;          // 8-bit cache: partial states of units cut by a share's end
+  uint32_t* plan8;          // and the tiles before each request that the launch went by
+  bool pend8;               // the open round's 8-bit chunk is not joined yet: its launch is ...
+  ss::Attn8Params last8;    // ... this one
   cudaEvent_t* ev_pool;     // timing events of the streamed round (SS_FLAG_STREAM_TIMING)
   int ev_pool_n;
 };
@@ -138,7 +141,7 @@ int slot_capacity_for(const ss_config* c) {
 
 constexpr int kHistSlots = 4;
 struct Layout {
-  size_t off_hist, off_ml, off_a, off_scratch8, total;
+  size_t off_hist, off_ml, off_a, off_scratch8, off_plan8, total;
   int64_t set_stride_ml, set_stride_a;
   int R_stride;
 };
@@ -157,7 +160,8 @@ Layout layout_for(const ss_config* c) {
   L.off_a = align_up(L.off_ml + (size_t)sets * rows * sizeof(float2), 256);
   L.off_scratch8 = align_up(L.off_a + (size_t)sets * rows * c->d * sizeof(float), 256);
   const size_t rows8 = L.R_stride < ss::kRows8 ? L.R_stride : ss::kRows8;
-  L.total = align_up(L.off_scratch8 + 2 * ss::kCtas8 * rows8 * (c->d + 4) * sizeof(float), 256);
+  L.off_plan8 = align_up(L.off_scratch8 + 2 * ss::kCtas8 * rows8 * (c->d + 4) * sizeof(float), 256);
+  L.total = align_up(L.off_plan8 + ((size_t)c->max_B + 1) * sizeof(uint32_t), 256);
   return L;
 }
 
@@ -261,14 +265,44 @@ void fill_merge(ss_ctx* c, ss::MergeParams* m) {
   memcpy(m->absent, c->absent, sizeof(m->absent));
 }
 
+// The calls on the 8-bit cache run on the context's device whatever device is current, and leave that current.
+struct DeviceGuard {
+  int before = -1;
+  cudaError_t err;
+  explicit DeviceGuard(int dev) {
+    err = cudaGetDevice(&before);
+    if (err == cudaSuccess && before != dev) err = cudaSetDevice(dev);
+    else before = -1;
+  }
+  ~DeviceGuard() {
+    if (before >= 0) cudaSetDevice(before);
+  }
+};
+
+// Joins what the round's last 8-bit chunk call has left in pieces: before anything but the round's own end
+// reads its set, and before the scratch area is used again.
+cudaError_t settle8(ss_ctx* c) {
+  if (!c->pend8) return cudaSuccess;
+  DeviceGuard on(c->cfg.device);
+  if (on.err != cudaSuccess) return on.err;
+  const cudaError_t e = ss::launch_attn8_join(c->last8, true, c->stream, !c->no_overlap);
+  if (e != cudaSuccess) return e;
+  c->pend8 = false;
+  ++c->launches;
+  c->first_launch = true;  // the next kernel must not overlap it
+  return cudaSuccess;
+}
+
 // All partial sets in use: fold them into set 0 (Eq. 14 is associative).
 cudaError_t fold_sets(ss_ctx* c, cudaStream_t s) {
+  cudaError_t e = settle8(c);
+  if (e != cudaSuccess) return e;
   ss::MergeParams m;
   fill_merge(c, &m);
   m.has_local = 0;
   m.fold_ml = c->part_ml;
   m.fold_a = c->part_a;
-  cudaError_t e = ss::launch_fold(m, s);
+  e = ss::launch_fold(m, s);
   if (e != cudaSuccess) return e;
   ++c->launches;
   c->n_sets = 1;
@@ -403,6 +437,7 @@ ss_status ss_create(ss_ctx** out, const ss_config* cfg, void* workspace, size_t 
   c->round_counters = (unsigned int*)(c->ws + 256 + align_up(ss::kTraceWords * sizeof(unsigned long long), 256));
   c->hist_maps = (CUtensorMap*)(c->ws + L.off_hist);
   c->scratch8 = (float*)(c->ws + L.off_scratch8);
+  c->plan8 = (uint32_t*)(c->ws + L.off_plan8);
   c->part_ml = (float2*)(c->ws + L.off_ml);
   c->part_a = (float*)(c->ws + L.off_a);
   c->set_stride_ml = L.set_stride_ml;
@@ -475,6 +510,7 @@ ss_status ss_verify_begin(ss_ctx* c, ss_tensor Q, int32_t B, int32_t T_q, float 
   c->scale = scale;
   c->n_sets = 0;
   c->has_local = false;
+  c->pend8 = false;
   c->first_launch = true;
   c->stream = (cudaStream_t)stream;
   c->state = ss_ctx::OPEN;
@@ -705,11 +741,13 @@ ss_status ss_verify_export_state(ss_ctx* c, float* ml, float* a, void* stream) {
   if (!c || !ml || !a) return SS_ERR_ARG;
   if (((uintptr_t)ml & 7) || !aligned16(a)) return SS_ERR_ALIGN;
   if (c->state != ss_ctx::OPEN || (cudaStream_t)stream != c->stream) return SS_ERR_STATE;
+  cudaError_t e = settle8(c);
+  if (e != cudaSuccess) return cuda_fail(c, e);
   ss::MergeParams m;
   fill_merge(c, &m);
   m.fold_ml = (float2*)ml;
   m.fold_a = a;
-  cudaError_t e = ss::launch_export(m, c->stream);
+  e = ss::launch_export(m, c->stream);
   if (e != cudaSuccess) return cuda_fail(c, e);
   ++c->launches;
   c->first_launch = true;  // reads every partial: the next kernel must not overlap it
@@ -744,11 +782,25 @@ ss_status ss_verify_finalize(ss_ctx* c, void* O, float* LSE, void* stream) {
   if (!c || !O) return SS_ERR_ARG;
   if (!aligned16(O) || (LSE && ((uintptr_t)LSE & 3))) return SS_ERR_ALIGN;
   if (c->state != ss_ctx::OPEN || (cudaStream_t)stream != c->stream) return SS_ERR_STATE;
-  ss::MergeParams m;
-  fill_merge(c, &m);
-  m.O = (__nv_bfloat16*)O;
-  m.LSE = LSE;
-  cudaError_t e = ss::launch_finalize(m, c->stream, use_pdl(c));
+  cudaError_t e;
+  if (c->pend8 && c->n_sets == 1) {
+    // the history was one 8-bit chunk: its pieces and the local segment straight to the output (the kernel
+    // waits for the one in front of it before it reads anything)
+    const int64_t loc = c->has_local ? c->n_set_cap : -1;
+    const ss::Final8 out = {loc < 0 ? nullptr : c->part_ml + loc * c->set_stride_ml,
+                            loc < 0 ? nullptr : c->part_a + loc * c->set_stride_a, (__nv_bfloat16*)O, LSE};
+    DeviceGuard on(c->cfg.device);
+    e = on.err;
+    if (e == cudaSuccess) e = ss::launch_attn8_finalize(c->last8, out, c->stream, !c->no_overlap);
+    c->pend8 = false;
+  } else {
+    e = settle8(c);
+    ss::MergeParams m;
+    fill_merge(c, &m);
+    m.O = (__nv_bfloat16*)O;
+    m.LSE = LSE;
+    if (e == cudaSuccess) e = ss::launch_finalize(m, c->stream, use_pdl(c));
+  }
   if (e != cudaSuccess) return cuda_fail(c, e);
   ++c->launches;
   ++c->stats.rounds;
@@ -1151,6 +1203,7 @@ ss_status ss_verify_abort(ss_ctx* c) {
   c->Q.ptr = nullptr;
   c->n_sets = 0;
   c->has_local = false;
+  c->pend8 = false;
   return SS_OK;
 }
 
@@ -1198,20 +1251,6 @@ ss_status ss_commit_gather(ss_ctx* c, ss_tensor K_loc, ss_tensor V_loc, int32_t 
 }
 
 // ---- 8-bit KV cache ---------------------------------------------------------------------------
-// The calls below run on the context's device whatever device is current, and leave it current.
-struct DeviceGuard {
-  int before = -1;
-  cudaError_t err;
-  explicit DeviceGuard(int dev) {
-    err = cudaGetDevice(&before);
-    if (err == cudaSuccess && before != dev) err = cudaSetDevice(dev);
-    else before = -1;
-  }
-  ~DeviceGuard() {
-    if (before >= 0) cudaSetDevice(before);
-  }
-};
-
 // Checks a cache for B requests and fills the kernels' view of it.
 static ss_status view8(const ss_ctx* c, const ss_cache8* k, int32_t B, ss::View8* v) {
   if (!k || !k->K.ptr || !k->V.ptr || !k->K_scale.ptr || !k->V_scale.ptr) return SS_ERR_ARG;
@@ -1321,8 +1360,8 @@ static ss_status attn8(ss_ctx* c, const ss_tensor& Q, int32_t B, int32_t T_q, fl
   // (the kernels number all tiles in 31 bits)
   if ((int64_t)B * ((p->kv.room + ss::kTok8 - 1) / ss::kTok8) * p->H_kv * p->row_tiles >= (1ll << 31)) return SS_ERR_SHAPE;
   p->scale_log2 = scale * 1.4426950408889634f;
-  p->min_tiles = 1;
   p->scratch = c->scratch8;
+  p->plan = p->O ? nullptr : c->plan8;
   p->status = c->status;
   DeviceGuard on(c->cfg.device);
   if (on.err != cudaSuccess) return cuda_fail(c, on.err);
@@ -1333,8 +1372,8 @@ static ss_status attn8(ss_ctx* c, const ss_tensor& Q, int32_t B, int32_t T_q, fl
   if (e != cudaSuccess) return cuda_fail(c, e);
   c->last_kernel = tc ? "kv8-tcgen05" : "kv8-simt";
   ++c->launches;
-  if (p->kv.room > ss::kTok8) {  // (a unit of one tile is never cut)
-    e = ss::launch_attn8_join(*p, s, pdl);
+  if (p->O && p->kv.room > ss::kTok8) {  // (a unit of one tile is never cut; a round joins later)
+    e = ss::launch_attn8_join(*p, false, s, pdl);
     if (e != cudaSuccess) return cuda_fail(c, e);
     ++c->launches;
   }
@@ -1354,11 +1393,10 @@ ss_status ss_verify_chunk8(ss_ctx* c, const ss_cache8* cache, const int32_t* val
   if ((uintptr_t)valid_len & 3) return SS_ERR_ALIGN;
   DeviceGuard on(c->cfg.device);
   if (on.err != cudaSuccess) return cuda_fail(c, on.err);
-  if (c->n_sets == c->n_set_cap) {
-    const cudaError_t e = fold_sets(c, c->stream);
-    if (e != cudaSuccess) return cuda_fail(c, e);
-  }
-  // one partial state per row: the launch joins its own splits
+  cudaError_t e = settle8(c);
+  if (e == cudaSuccess && c->n_sets == c->n_set_cap) e = fold_sets(c, c->stream);
+  if (e != cudaSuccess) return cuda_fail(c, e);
+  // one partial state per row, once the pieces are joined
   p.part_ml = c->part_ml + (int64_t)c->n_sets * c->set_stride_ml;
   p.part_a = c->part_a + (int64_t)c->n_sets * c->set_stride_a;
   p.R_stride = c->R_stride;
@@ -1366,6 +1404,8 @@ ss_status ss_verify_chunk8(ss_ctx* c, const ss_cache8* cache, const int32_t* val
   if (st != SS_OK) return st;
   c->splits[c->n_sets] = 1;
   memset(c->absent[c->n_sets], 0, sizeof(c->absent[0]));
+  c->pend8 = true;
+  c->last8 = p;
   ++c->n_sets;
   c->first_launch = false;
   return SS_OK;

@@ -50,14 +50,21 @@ struct Attn8Params {
   int B, H_kv, G, T_q, R, d;
   int row_tiles, rows_per_tile;
   float scale_log2;
-  int min_tiles;              // a share holds at least this many tiles
   float* scratch;             // 2 slots per CTA of rows_per_tile * (d + 4) floats: (m, l) pairs, room, a[]
+  uint32_t* plan;             // [B + 1] or null: receives the tiles before each request (all units), and their total
   __nv_bfloat16* O;           // either the finished output ...
   float* LSE;
   float2* part_ml;            // ... or (O null) one partial state per row, as the chunk kernels leave them
   float* part_a;
   int R_stride;
   uint32_t* status;
+};
+
+struct Final8 {               // end of a round
+  const float2* loc_ml;       // the local segment's states, null without one
+  const float* loc_a;
+  __nv_bfloat16* O;
+  float* LSE;                 // may be null
 };
 
 struct Copy8Params {          // write (bf16 -> cache) and read (cache -> bf16)
@@ -73,7 +80,8 @@ cudaError_t launch_kv8_write(const Copy8Params& p, cudaStream_t s, bool pdl);
 cudaError_t launch_kv8_read(const Copy8Params& p, cudaStream_t s, bool pdl);
 cudaError_t launch_attn8_simt(const Attn8Params& p, cudaStream_t s, bool pdl);
 cudaError_t launch_attn8_tc(const Attn8Params& p, const CUtensorMap& tmK, const CUtensorMap& tmV, cudaStream_t s, bool pdl);
-cudaError_t launch_attn8_join(const Attn8Params& p, cudaStream_t s, bool pdl);
+cudaError_t launch_attn8_join(const Attn8Params& p, bool from_plan, cudaStream_t s, bool pdl);
+cudaError_t launch_attn8_finalize(const Attn8Params& p, const Final8& out, cudaStream_t s, bool pdl);
 cudaError_t attn8_tc_prepare();  // one-time function attributes
 
 // ---- device side ---------------------------------------------------------------------------
@@ -116,9 +124,8 @@ __device__ __forceinline__ uint32_t share_of8(const Share8& s, uint32_t x) {
 }
 
 // From the number of tiles to the shares of a launch of at most `grid` CTAs.
-__device__ __forceinline__ void set_shares8(const Attn8Params& p, uint32_t grid, Share8* s) {
-  const uint32_t want = (s->total + p.min_tiles - 1) / p.min_tiles;
-  s->ctas = min(max(want, 1u), grid);
+__device__ __forceinline__ void set_shares8(uint32_t grid, Share8* s) {
+  s->ctas = min(max(s->total, 1u), grid);
   s->q = s->total / s->ctas;
   s->more = s->total - s->q * s->ctas;
 }
@@ -143,7 +150,7 @@ __device__ __forceinline__ Share8 find_share8(const Attn8Params& p) {
   }
   if (blockIdx.x == 0 && __any_sync(0xffffffffu, bad) && lane == 0) atomicOr(p.status, SS_DEV_BAD_VALID_LEN);
   s.total = __reduce_add_sync(0xffffffffu, sum);
-  set_shares8(p, gridDim.x, &s);
+  set_shares8(gridDim.x, &s);
   if (blockIdx.x >= s.ctas || s.total == 0) return s;
   s.lo = share_lo8(s, blockIdx.x);
   s.hi = share_lo8(s, blockIdx.x + 1);
@@ -249,6 +256,28 @@ static __device__ __noinline__ void put_empty8(const Attn8Params& p, int tid, in
 #pragma unroll 1
     for (int i = tid; i < rows * (p.d / 8); i += n) o[i] = make_uint4(0, 0, 0, 0);
   }
+}
+
+// The record of the lengths that this launch went by, for a join that runs later: by one warp of the
+// last CTA (the one with the least to do).
+static __device__ __noinline__ void put_plan8(const Attn8Params& p) {
+  if (!p.plan || blockIdx.x != gridDim.x - 1) return;
+  const int lane = threadIdx.x & 31;
+  const uint32_t units = (uint32_t)(p.H_kv * p.row_tiles);
+  uint32_t base = 0;
+#pragma unroll 1
+  for (int b = 0; b < p.B; b += 32) {
+    const uint32_t n = b + lane < p.B ? units * tiles8(len8(p, b + lane)) : 0;
+    uint32_t incl = n;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t up = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += up;
+    }
+    if (b + lane < p.B) p.plan[b + lane] = base + incl - n;
+    base += __shfl_sync(0xffffffffu, incl, 31);
+  }
+  if (lane == 0) p.plan[p.B] = base;
 }
 
 // Slot of CTA i's state of the unit that begins at tile `start` (first CTA i0): the first segment of a

@@ -706,6 +706,7 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
       bar8<SOFT>();  // sums, references and Q may be written anew
     }
     put_empty8(p, tid, SOFT);
+    if (warp == 0) put_plan8(p);
   }
 
   tc_fence_before();

@@ -3,9 +3,10 @@
 // a ticket: one launch less and slower everywhere, 9.8 against 7.9 us for one request of 1024 tokens, 52
 // against 48 for 131071, 55 against 29 for a round of 2 x 6909 tokens and 40 rows per kv-head.)
 //
-// The warp works the shares out again from the lengths.  It does so before it waits for the attention
-// kernel: that kernel let this one start only after everything in front of it, the lengths' producer too,
-// was complete.  Bound by two dependent reads of L2.
+// Directly behind the attention kernel (decoding) a warp works the shares out again from the lengths, and
+// does so before it waits: the attention kernel let this one start only after everything in front of it, the
+// lengths' producer too, was complete.  At a round's end, when the lengths' buffer may have been written
+// anew, it reads the attention kernel's own record of them.  Bound by dependent reads of L2.
 #include "kv8.cuh"
 
 namespace ss {
@@ -14,71 +15,90 @@ namespace {
 constexpr int kWarps = 4;
 constexpr int kFlight = 16;  // states in flight
 
-template <int D>
-__global__ void __launch_bounds__(kWarps * 32) attn8_join_kernel(const __grid_constant__ Attn8Params p) {
-  constexpr int CPL = D / 32;
-  pdl_launch_dependents();
-  const int lane = threadIdx.x & 31;
-  const int64_t row = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);  // (request, kv-head, row)
-  if (row >= (int64_t)p.B * p.H_kv * p.R) return;  // (the block's first warp has a row)
+// A query row and where its unit's states are: n of them, the first at `first`, the others two slots apart
+// from `rest`; n = 0: empty request, n = 1: finished by one CTA, not in the scratch area.
+struct Row8 {
   Seg8 g;
-  const int pair = (int)(row / p.R), rr = (int)(row - (int64_t)pair * p.R);
+  int r, rr;                // row in its unit, in its kv-head
+  int n;
+  const float *first, *rest;
+};
+template <bool PLAN>
+__device__ __forceinline__ Row8 row8(const Attn8Params& p, int64_t row, int lane) {
+  Row8 w;
+  Seg8& g = w.g;
+  const int pair = (int)(row / p.R);
+  w.rr = (int)(row - (int64_t)pair * p.R);
   g.b = pair / p.H_kv;
   g.kvh = pair - g.b * p.H_kv;
-  const int rt = rr / p.rows_per_tile, r = rr - rt * p.rows_per_tile;
+  const int rt = w.rr / p.rows_per_tile;
+  w.r = w.rr - rt * p.rows_per_tile;
   g.row0 = rt * p.rows_per_tile;
   g.nrows = min(p.rows_per_tile, p.R - g.row0);
-  g.n = tiles8(len8(p, g.b));
   const uint32_t units = (uint32_t)(p.H_kv * p.row_tiles);
-  uint32_t sum = 0, before = 0;  // tiles of all requests, of those before g.b
-  for (int b = lane; b < p.B; b += 32) {
-    const uint32_t n = units * tiles8(len8(p, b));
-    sum += n;
-    if (b < g.b) before += n;
-  }
   Share8 s = {};
-  s.total = __reduce_add_sync(0xffffffffu, sum);
-  before = __reduce_add_sync(0xffffffffu, before);
-  int i0 = 0, n = 0;
-  const float *first = nullptr, *rest = nullptr;
-  if (g.n > 0) {
-    set_shares8(p, kCtas8, &s);
-    g.start = before + (uint32_t)(g.kvh * p.row_tiles + rt) * g.n;
-    i0 = min((int)share_of8(s, g.start), kCtas8 - 1);  // (no address depends on more than these two)
-    n = min((int)share_of8(s, g.start + g.n - 1), kCtas8 - 1) - i0 + 1;
-    first = slot8(p, s, g.start, i0);
-    rest = slot8(p, s, g.start, i0 + 1);
+  uint32_t before = 0;  // tiles of the requests before this one
+  if (PLAN) {
+    before = __ldcg(&p.plan[g.b]);
+    g.n = (int)((__ldcg(&p.plan[g.b + 1]) - before) / units);
+    s.total = __ldcg(&p.plan[p.B]);
+  } else {
+    g.n = tiles8(len8(p, g.b));
+    uint32_t sum = 0;
+    for (int b = lane; b < p.B; b += 32) {
+      const uint32_t n = units * tiles8(len8(p, b));
+      sum += n;
+      if (b < g.b) before += n;
+    }
+    s.total = __reduce_add_sync(0xffffffffu, sum);
+    before = __reduce_add_sync(0xffffffffu, before);
   }
-  const int64_t slot = (int64_t)p.rows_per_tile * (D + 4);
-  // Every warp waits, those with nothing to join too: this grid must not be complete before the other is.
-  pdl_wait_prior();
-  if (n < 2) return;  // an empty request, or a unit that one CTA finished: written by the attention kernel
+  w.n = 0;
+  w.first = w.rest = nullptr;
+  if (g.n > 0) {
+    set_shares8(kCtas8, &s);
+    g.start = before + (uint32_t)(g.kvh * p.row_tiles + rt) * g.n;
+    const int i0 = min((int)share_of8(s, g.start), kCtas8 - 1);  // (no address depends on more than these two)
+    w.n = min((int)share_of8(s, g.start + g.n - 1), kCtas8 - 1) - i0 + 1;
+    w.first = slot8(p, s, g.start, i0);
+    w.rest = slot8(p, s, g.start, i0 + 1);
+  }
+  return w;
+}
 
-  float m = -INFINITY, l = 0.f, a[CPL];
-#pragma unroll
-  for (int c = 0; c < CPL; ++c) a[c] = 0.f;
+template <int CPL>
+__device__ __forceinline__ void load_a(const float* x, float (&v)[CPL]) {
+  if (CPL == 4) {
+    const float4 q = __ldcg(reinterpret_cast<const float4*>(x));
+    v[0] = q.x;
+    v[1] = q.y;
+    v[CPL - 2] = q.z;
+    v[CPL - 1] = q.w;
+  } else {
+    const float2 q = __ldcg(reinterpret_cast<const float2*>(x));
+    v[0] = q.x;
+    v[1] = q.y;
+  }
+}
+
+// Adds the row's n states to (m, l, a); a lane holds D / 32 head dims.
+template <int D>
+__device__ __forceinline__ void add_states(const Attn8Params& p, const Row8& w, int lane, float& m, float& l,
+                                           float (&a)[D / 32]) {
+  constexpr int CPL = D / 32;
+  const int64_t slot = (int64_t)p.rows_per_tile * (D + 4);
 #pragma unroll 1
-  for (int j0 = 0; j0 < n; j0 += kFlight) {
+  for (int j0 = 0; j0 < w.n; j0 += kFlight) {
     // (m, l) one state per lane, a[] all lanes of one state after the other
     const int own = j0 + (lane & (kFlight - 1));
     float2 st = make_float2(-INFINITY, 0.f);
-    if (own < n) st = __ldcg(reinterpret_cast<const float2*>(own == 0 ? first : rest + (int64_t)(own - 1) * 2 * slot) + r);
+    if (own < w.n)
+      st = __ldcg(reinterpret_cast<const float2*>(own == 0 ? w.first : w.rest + (int64_t)(own - 1) * 2 * slot) + w.r);
     float v[kFlight][CPL];
 #pragma unroll
     for (int j = 0; j < kFlight; ++j) {
-      const int i = min(j0 + j, n - 1);
-      const float* x = (i == 0 ? first : rest + (int64_t)(i - 1) * 2 * slot) + 4 * p.rows_per_tile + r * D + lane * CPL;
-      if (CPL == 4) {
-        const float4 q = __ldcg(reinterpret_cast<const float4*>(x));
-        v[j][0] = q.x;
-        v[j][1] = q.y;
-        v[j][CPL - 2] = q.z;
-        v[j][CPL - 1] = q.w;
-      } else {
-        const float2 q = __ldcg(reinterpret_cast<const float2*>(x));
-        v[j][0] = q.x;
-        v[j][1] = q.y;
-      }
+      const int i = min(j0 + j, w.n - 1);
+      load_a<CPL>((i == 0 ? w.first : w.rest + (int64_t)(i - 1) * 2 * slot) + 4 * p.rows_per_tile + w.r * D + lane * CPL, v[j]);
     }
     float top = st.y != 0.f ? st.x : -INFINITY;  // (l = 0: an empty state)
 #pragma unroll
@@ -86,8 +106,8 @@ __global__ void __launch_bounds__(kWarps * 32) attn8_join_kernel(const __grid_co
     top = fmaxf(top, m);
     const float f = m == top ? 1.f : exp2f(m - top);
     m = top;
-    const float w = st.y == 0.f ? 0.f : st.x == top ? 1.f : exp2f(st.x - top);
-    float lw = w * st.y;
+    const float wt = st.y == 0.f ? 0.f : st.x == top ? 1.f : exp2f(st.x - top);
+    float lw = wt * st.y;
 #pragma unroll
     for (int o = kFlight / 2; o; o >>= 1) lw += __shfl_xor_sync(0xffffffffu, lw, o);
     l = fmaf(l, f, lw);
@@ -95,24 +115,102 @@ __global__ void __launch_bounds__(kWarps * 32) attn8_join_kernel(const __grid_co
     for (int c = 0; c < CPL; ++c) a[c] *= f;
 #pragma unroll
     for (int j = 0; j < kFlight; ++j) {
-      const float wj = __shfl_sync(0xffffffffu, w, j);
-      if (j0 + j < n) {
+      const float wj = __shfl_sync(0xffffffffu, wt, j);
+      if (j0 + j < w.n) {
 #pragma unroll
         for (int c = 0; c < CPL; ++c) a[c] = fmaf(wj, v[j][c], a[c]);
       }
     }
   }
-  if (lane == 0) put_ml8(p, g, r, m, l);
+}
+
+template <int D, bool PLAN>
+__global__ void __launch_bounds__(kWarps * 32) attn8_join_kernel(const __grid_constant__ Attn8Params p) {
+  constexpr int CPL = D / 32;
+  pdl_launch_dependents();
+  const int lane = threadIdx.x & 31;
+  const int64_t row = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);  // (request, kv-head, row)
+  if (row >= (int64_t)p.B * p.H_kv * p.R) return;  // (the block's first warp has a row)
+  if (PLAN) pdl_wait_prior();
+  const Row8 w = row8<PLAN>(p, row, lane);
+  // Every warp waits, those with nothing to join too: this grid must not be complete before the other is.
+  if (!PLAN) pdl_wait_prior();
+  if (w.n < 2) return;  // written by the attention kernel
+  float m = -INFINITY, l = 0.f, a[CPL];
 #pragma unroll
-  for (int c = 0; c < CPL; ++c) put_a8(p, g, r, lane * CPL + c, l, a[c]);
+  for (int c = 0; c < CPL; ++c) a[c] = 0.f;
+  add_states<D>(p, w, lane, m, l, a);
+  if (lane == 0) put_ml8(p, w.g, w.r, m, l);
+#pragma unroll
+  for (int c = 0; c < CPL; ++c) put_a8(p, w.g, w.r, lane * CPL + c, l, a[c]);
+}
+
+// End of a round whose history is one 8-bit chunk: its states, joined or not, and the local segment's
+// straight to O and LSE.
+template <int D>
+__global__ void __launch_bounds__(kWarps * 32) attn8_finalize_kernel(const __grid_constant__ Attn8Params p,
+                                                                     const Final8 out) {
+  constexpr int CPL = D / 32;
+  pdl_launch_dependents();
+  const int lane = threadIdx.x & 31;
+  const int64_t row = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
+  if (row >= (int64_t)p.B * p.H_kv * p.R) return;
+  pdl_wait_prior();
+  const int64_t pair = row / p.R, at = pair * p.R_stride + (row - pair * p.R);
+  float m = -INFINITY, l = 0.f, a[CPL];
+#pragma unroll
+  for (int c = 0; c < CPL; ++c) a[c] = 0.f;
+  // the local segment's state (fetched while the unit's place is worked out)
+  float2 ml = make_float2(-INFINITY, 0.f);
+  float v[CPL];
+  if (out.loc_ml) {
+    ml = __ldcg(out.loc_ml + at);
+    load_a<CPL>(out.loc_a + at * D + lane * CPL, v);
+  }
+  const Row8 w = row8<true>(p, row, lane);
+  if (ml.y != 0.f && ml.x != -INFINITY) {  // (an identity state's a[] is undefined)
+    m = ml.x;
+    l = ml.y;
+#pragma unroll
+    for (int c = 0; c < CPL; ++c) a[c] = v[c];
+  }
+  if (w.n >= 2) {
+    add_states<D>(p, w, lane, m, l, a);
+  } else if (w.n == 1) {
+    const float2 st = __ldcg(p.part_ml + at);
+    if (st.y != 0.f) {
+      load_a<CPL>(p.part_a + at * D + lane * CPL, v);
+      const float top = fmaxf(m, st.x), f = m == top ? 1.f : exp2f(m - top), wt = st.x == top ? 1.f : exp2f(st.x - top);
+      m = top;
+      l = fmaf(l, f, wt * st.y);
+#pragma unroll
+      for (int c = 0; c < CPL; ++c) a[c] = fmaf(wt, v[c], a[c] * f);
+    }
+  }
+  const bool some = l > 0.f || l != l;
+  const float inv = some ? 1.f / l : 0.f;
+  __nv_bfloat162* o = reinterpret_cast<__nv_bfloat162*>(out.O + row * D + lane * CPL);
+#pragma unroll
+  for (int c = 0; c < CPL / 2; ++c) o[c] = __floats2bfloat162_rn(a[2 * c] * inv, a[2 * c + 1] * inv);
+  if (out.LSE && lane == 0) out.LSE[row] = some ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+}
+
+dim3 join_grid(const Attn8Params& p) {
+  const int64_t rows = (int64_t)p.B * p.H_kv * p.R;  // below 2^31 (ss_create)
+  return dim3((unsigned)((rows + kWarps - 1) / kWarps));
 }
 
 }  // namespace
 
-cudaError_t launch_attn8_join(const Attn8Params& p, cudaStream_t s, bool pdl) {
-  const int64_t rows = (int64_t)p.B * p.H_kv * p.R;  // below 2^31 (ss_create)
-  const dim3 grid((unsigned)((rows + kWarps - 1) / kWarps)), block(kWarps * 32);
-  return launch_kernel(p.d == 128 ? attn8_join_kernel<128> : attn8_join_kernel<64>, grid, block, 0, s, pdl, p);
+cudaError_t launch_attn8_join(const Attn8Params& p, bool from_plan, cudaStream_t s, bool pdl) {
+  auto kernel = p.d == 128 ? (from_plan ? attn8_join_kernel<128, true> : attn8_join_kernel<128, false>)
+                           : (from_plan ? attn8_join_kernel<64, true> : attn8_join_kernel<64, false>);
+  return launch_kernel(kernel, join_grid(p), dim3(kWarps * 32), 0, s, pdl, p);
+}
+
+cudaError_t launch_attn8_finalize(const Attn8Params& p, const Final8& out, cudaStream_t s, bool pdl) {
+  return launch_kernel(p.d == 128 ? attn8_finalize_kernel<128> : attn8_finalize_kernel<64>, join_grid(p), dim3(kWarps * 32),
+                       0, s, pdl, p, out);
 }
 
 }  // namespace ss
