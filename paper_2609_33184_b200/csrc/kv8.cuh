@@ -259,9 +259,8 @@ static __device__ __noinline__ void put_empty8(const Attn8Params& p, int tid, in
 }
 
 // The record of the lengths that this launch went by, for a join that runs later: by one warp of the
-// last CTA (the one with the least to do).
+// last CTA, which has the least to do.
 static __device__ __noinline__ void put_plan8(const Attn8Params& p) {
-  if (!p.plan || blockIdx.x != gridDim.x - 1) return;
   const int lane = threadIdx.x & 31;
   const uint32_t units = (uint32_t)(p.H_kv * p.row_tiles);
   uint32_t base = 0;

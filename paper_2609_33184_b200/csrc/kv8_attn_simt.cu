@@ -175,8 +175,8 @@ __global__ void __launch_bounds__(128) attn8_simt_kernel(const __grid_constant__
       }
     }
   }
-  put_empty8(p, tid, 128);
-  if (warp == 0) put_plan8(p);
+  if ((int)blockIdx.x < p.B) put_empty8(p, tid, 128);
+  if (p.plan && warp == 0 && blockIdx.x == gridDim.x - 1) put_plan8(p);
 }
 
 }  // namespace

@@ -705,8 +705,8 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
       tc_fence_before();
       bar8<SOFT>();  // sums, references and Q may be written anew
     }
-    put_empty8(p, tid, SOFT);
-    if (warp == 0) put_plan8(p);
+    if ((int)blockIdx.x < p.B) put_empty8(p, tid, SOFT);
+    if (p.plan && warp == 0 && blockIdx.x == gridDim.x - 1) put_plan8(p);
   }
 
   tc_fence_before();
