@@ -323,8 +323,9 @@ ss_status ss_kv8_read(ss_ctx* ctx, const ss_cache8* cache, ss_tensor K, ss_tenso
 
 /* A history chunk that is held in 8 bits: like ss_verify_chunk_paged (paged or dense), every query
  * row of the round against tokens [0, valid_len[b]) (device [B], NULL = all the request's room;
- * outside [0, room]: clamped, SS_DEV_BAD_VALID_LEN).  May be mixed with bf16 chunks in any order.
- * The room must not exceed max_Lc (SS_ERR_SHAPE).  The split over the GPU follows the lengths on
+ * outside [0, room]: clamped, SS_DEV_BAD_VALID_LEN).  May be mixed with bf16 chunks in any order, and
+ * called several times.  The room must not exceed max_Lc (SS_ERR_SHAPE).  A query value that is not
+ * finite makes its row NaN.  The split over the GPU follows the lengths on
  * the device, so no host copy of them is taken and a captured call follows lengths that change
  * between replays. */
 ss_status ss_verify_chunk8(ss_ctx* ctx, const ss_cache8* cache, const int32_t* valid_len, void* stream);
@@ -555,7 +556,7 @@ const char* ss_strerror(ss_status s);
 size_t ss_sizeof_stream_desc(void);
 /* Last CUDA error code seen by this context (cudaError_t as int), 0 if none. */
 int32_t ss_last_cuda_error(ss_ctx* ctx);
-/* Tracing.  While enabled, CTA (0,0,0) of every tensor-core chunk kernel stamps the SM clock
+/* Tracing.  While enabled, CTA (0,0,0) of every bf16 tensor-core chunk kernel stamps the SM clock
  * at fixed points of its tile loop into a region of the workspace: words
  * [role][tile < 32][event < 8], role 0 = TMA producer, 1 = MMA issuer, 2 = softmax lane 0;
  * event 0 is the role's first stamp for that tile (the softmax thread reaching the tile, the
