@@ -516,27 +516,33 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
         // x[r] = s2 + ev - M + bias (in the segment's first tile s2 + ev)
         float2 x[RT / 2];
         {
+          // 16 rows at a time; the factors are formed while the scores are on their way
           const float2 kf2 = make_float2(kf, kf), ev2 = make_float2(evf, evf);
           const uint32_t t_s = tmem + lane_off + (it & 1) * NS + c0;
+          constexpr int H = RT < 16 ? RT : 16;
+          uint32_t raw[16];
+          if (C::kSideBySide || RT >= 16) tmem_ld<16>(t_s, raw);
+          else tmem_ld<8>(t_s, raw);
 #pragma unroll
-          for (int r0 = 0; r0 < RT; r0 += 16) {
-            uint32_t raw[16];
-            if (C::kSideBySide || RT >= 16) tmem_ld<16>(t_s + r0, raw);
-            else tmem_ld<8>(t_s, raw);
+          for (int r0 = 0; r0 < RT; r0 += H) {
+            float2 f[H / 2], e[H / 2];
+#pragma unroll
+            for (int r = 0; r < H; r += 4) {
+              const float4 qf = *reinterpret_cast<const float4*>(&ctl->qf[c0 + r0 + r]);
+              const float4 nm = *reinterpret_cast<const float4*>(&ctl->nm[c0 + r0 + r]);
+              f[r / 2] = __fmul2_rn(make_float2(qf.x, qf.y), kf2);
+              f[r / 2 + 1] = __fmul2_rn(make_float2(qf.z, qf.w), kf2);
+              e[r / 2] = __fadd2_rn(make_float2(nm.x, nm.y), ev2);
+              e[r / 2 + 1] = __fadd2_rn(make_float2(nm.z, nm.w), ev2);
+            }
             tc_wait_ld();
 #pragma unroll
-            for (int r = r0; r < RT && r < r0 + 16; r += 4) {
-              const float4 qf = *reinterpret_cast<const float4*>(&ctl->qf[c0 + r]);
-              const float4 nm = *reinterpret_cast<const float4*>(&ctl->nm[c0 + r]);
-              float2 s0 = make_float2(__uint_as_float(raw[r - r0]), __uint_as_float(raw[r - r0 + 1]));
-              float2 s1 = make_float2(__uint_as_float(raw[r - r0 + 2]), __uint_as_float(raw[r - r0 + 3]));
-              if (C::kSideBySide) {
-                s0 = __fadd2_rn(s0, make_float2(__uint_as_float(raw[8 + r]), __uint_as_float(raw[8 + r + 1])));
-                s1 = __fadd2_rn(s1, make_float2(__uint_as_float(raw[8 + r + 2]), __uint_as_float(raw[8 + r + 3])));
-              }
-              x[r / 2] = __ffma2_rn(__fmul2_rn(s0, make_float2(qf.x, qf.y)), kf2, __fadd2_rn(make_float2(nm.x, nm.y), ev2));
-              x[r / 2 + 1] = __ffma2_rn(__fmul2_rn(s1, make_float2(qf.z, qf.w)), kf2, __fadd2_rn(make_float2(nm.z, nm.w), ev2));
+            for (int r = 0; r < H; r += 2) {
+              float2 sc = make_float2(__uint_as_float(raw[r]), __uint_as_float(raw[r + 1]));
+              if (C::kSideBySide) sc = __fadd2_rn(sc, make_float2(__uint_as_float(raw[8 + r]), __uint_as_float(raw[8 + r + 1])));
+              x[(r0 + r) / 2] = __ffma2_rn(sc, f[r / 2], e[r / 2]);
             }
+            if (r0 + H < RT) tmem_ld<16>(t_s + r0 + H, raw);
           }
         }
         if (n_valid < kTok8) {
