@@ -13,11 +13,13 @@
 namespace ss {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 128;
 
 // U rows in flight per thread: 4 for calls that fill the GPU, 1 for small ones, which want short
-// threads and many blocks (102,000 prompt tokens of 8 heads: 110 us with 4, 118 with 2, 158 with 1; 32
-// requests' accepted tokens: 4.4, 2.8 and 2.4 us).
+// threads and many blocks (102,000 prompt tokens of 8 heads, blocks of 256: 110 us with 4, 118 with 2, 158
+// with 1; 32 requests' accepted tokens: 4.4, 2.8 and 2.4 us).  Blocks of 128 threads: 99 us against 107 with
+// 256.  Stores go past L2's other contents (__stcs): 157 us against 191 for 165,000 tokens read back.  Both
+// large cases then run at the copy rate.
 //
 // A block takes U * kThreads / (d / 16) rows: 2^shift consecutive tokens (T of them for short calls) of
 // as many (K|V, head) pairs of one request as that makes, so the request, its count and its offset are
@@ -181,8 +183,8 @@ __global__ void __launch_bounds__(kThreads) write8_kernel(const __grid_constant_
     const int pair = ONE ? w.pair0 : w.pair0 + ((threadIdx.x / LPR + u * RPB) >> plan.shift);
     const Pair a = ONE ? one : pair_at(p, w.b, pair);
     uint2* dst = reinterpret_cast<uint2*>(a.codes + at[u].outer * a.code_sb + at[u].inner * a.code_st) + part;
-    dst[0] = make_uint2(c[0], c[1]);
-    dst[LPR] = make_uint2(c[2], c[3]);
+    __stcs(dst, make_uint2(c[0], c[1]));
+    __stcs(dst + LPR, make_uint2(c[2], c[3]));
     if (part == 0) a.scales[at[u].outer * a.scale_sb + at[u].inner * a.scale_st] = (uint8_t)(e + 127);
   }
 }
@@ -231,8 +233,8 @@ __global__ void __launch_bounds__(kThreads) read8_kernel(const __grid_constant__
       o[2 * j + 1] = bf16_of(x[j] >> 16, scale);
     }
     uint4* dst = reinterpret_cast<uint4*>(to[u]) + part;
-    dst[0] = make_uint4(o[0], o[1], o[2], o[3]);
-    dst[LPR] = make_uint4(o[4], o[5], o[6], o[7]);
+    __stcs(dst, make_uint4(o[0], o[1], o[2], o[3]));
+    __stcs(dst + LPR, make_uint4(o[4], o[5], o[6], o[7]));
   }
 }
 
