@@ -130,24 +130,39 @@ __device__ __forceinline__ void set_shares8(uint32_t grid, Share8* s) {
   s->more = s->total - s->q * s->ctas;
 }
 
+// Tiles (all units) of requests b0 + 4 * lane .. + 3: 128 requests per step of a warp, whose loads go out together.
+__device__ __forceinline__ uint32_t tiles_of_four8(const Attn8Params& p, int b0, uint32_t (&n)[4], bool* bad) {
+  const uint32_t units = (uint32_t)(p.H_kv * p.row_tiles);
+  const int b = b0 + 4 * (threadIdx.x & 31);
+  int len[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) len[j] = b + j >= p.B ? 0 : p.valid_len ? p.valid_len[b + j] : p.kv.room;
+  uint32_t sum = 0;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    *bad |= len[j] < 0 || len[j] > p.kv.room;
+    n[j] = units * tiles8(max(0, min(len[j], p.kv.room)));
+    sum += n[j];
+  }
+  return sum;
+}
+__device__ __forceinline__ uint32_t warp_scan8(uint32_t v) {  // inclusive
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint32_t up = __shfl_up_sync(0xffffffffu, v, o);
+    if ((threadIdx.x & 31) >= o) v += up;
+  }
+  return v;
+}
+
 // By one whole warp.  CTA 0 also reports lengths that had to be clamped.
 __device__ __forceinline__ Share8 find_share8(const Attn8Params& p) {
   const int lane = threadIdx.x & 31;
-  const uint32_t units = (uint32_t)(p.H_kv * p.row_tiles);
   Share8 s = {};
-  uint32_t sum = 0, n = 0;
+  uint32_t n[4], sum = 0, mine = 0;
   bool bad = false;
 #pragma unroll 1
-  for (int b = lane; b < p.B; b += 32) {
-    int len = p.kv.room;
-    if (p.valid_len) {
-      len = p.valid_len[b];
-      bad |= len < 0 || len > p.kv.room;
-      len = max(0, min(len, p.kv.room));
-    }
-    n = units * tiles8(len);
-    sum += n;
-  }
+  for (int b = 0; b < p.B; b += 128) sum += mine = tiles_of_four8(p, b, n, &bad);
   if (blockIdx.x == 0 && __any_sync(0xffffffffu, bad) && lane == 0) atomicOr(p.status, SS_DEV_BAD_VALID_LEN);
   s.total = __reduce_add_sync(0xffffffffu, sum);
   set_shares8(gridDim.x, &s);
@@ -156,19 +171,24 @@ __device__ __forceinline__ Share8 find_share8(const Attn8Params& p) {
   s.hi = share_lo8(s, blockIdx.x + 1);
   uint32_t base = 0;
 #pragma unroll 1
-  for (int b = 0; b < p.B; b += 32) {
-    if (p.B > 32) n = b + lane < p.B ? units * tiles8(len8(p, b + lane)) : 0;  // (else still there)
-    uint32_t incl = n;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const uint32_t up = __shfl_up_sync(0xffffffffu, incl, o);
-      if (lane >= o) incl += up;
-    }
+  for (int b = 0; b < p.B; b += 128) {
+    if (p.B > 128) mine = tiles_of_four8(p, b, n, &bad);  // (else still there)
+    const uint32_t incl = warp_scan8(mine);
     const unsigned past = __ballot_sync(0xffffffffu, base + incl > s.lo);
     if (past) {
+      // the first lane past the share's start, and which of its four requests
+      uint32_t before = base + incl - mine;
+      int j = 0;
+#pragma unroll
+      for (int k = 0; k < 3; ++k) {
+        if (j == k && before + n[k] <= s.lo) {
+          before += n[k];
+          ++j;
+        }
+      }
       const int at = __ffs(past) - 1;
-      s.b0 = b + at;
-      s.base0 = base + __shfl_sync(0xffffffffu, incl - n, at);
+      s.b0 = b + 4 * at + __shfl_sync(0xffffffffu, j, at);
+      s.base0 = __shfl_sync(0xffffffffu, before, at);
       break;
     }
     base += __shfl_sync(0xffffffffu, incl, 31);
@@ -262,18 +282,17 @@ static __device__ __noinline__ void put_empty8(const Attn8Params& p, int tid, in
 // last CTA, which has the least to do.
 static __device__ __noinline__ void put_plan8(const Attn8Params& p) {
   const int lane = threadIdx.x & 31;
-  const uint32_t units = (uint32_t)(p.H_kv * p.row_tiles);
-  uint32_t base = 0;
+  uint32_t base = 0, n[4];
+  bool bad = false;
 #pragma unroll 1
-  for (int b = 0; b < p.B; b += 32) {
-    const uint32_t n = b + lane < p.B ? units * tiles8(len8(p, b + lane)) : 0;
-    uint32_t incl = n;
+  for (int b = 0; b < p.B; b += 128) {
+    const uint32_t mine = tiles_of_four8(p, b, n, &bad), incl = warp_scan8(mine);
+    uint32_t before = base + incl - mine;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const uint32_t up = __shfl_up_sync(0xffffffffu, incl, o);
-      if (lane >= o) incl += up;
+    for (int j = 0; j < 4; ++j) {
+      if (b + 4 * lane + j < p.B) p.plan[b + 4 * lane + j] = before;
+      before += n[j];
     }
-    if (b + lane < p.B) p.plan[b + lane] = base + incl - n;
     base += __shfl_sync(0xffffffffu, incl, 31);
   }
   if (lane == 0) p.plan[p.B] = base;

@@ -746,3 +746,26 @@ def test_writes_across_block_sizes(T):
                         assert np.array_equal(got[b, h, r].double().cpu().numpy(), want), (b, h, r)
                 assert (got[b, :, n:] == 3.0).all()
         ctx.close()
+
+
+@pytest.mark.parametrize("B", [128, 131, 300])
+def test_large_batches(B):
+    """More requests than a warp looks up in one step, most of them empty or short; whole rounds too."""
+    ssb = _ssb()
+    H_q, H_kv, d, page = 4, 1, 64, 16
+    lens = [(0 if b % 5 == 2 else (b * 37) % 400 if b % 7 else 0) for b in range(B)]
+    cache = make_cache(ssb, B, H_kv, d, page, 416, B)
+    poison(cache, lens)
+    Q = torch.randn(B, H_q, 2, d, generator=_gen(B)).bfloat16().to(DEV)
+    ctx = ssb.Context(B, H_q, H_kv, d, 2, 2, 512)
+    O, LSE = decode(ssb, cache, Q, lens, ctx=ctx)
+    check_attention(Q, O, LSE, lambda b: history(cache, b, lens[b]), d ** -0.5)
+    vl = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    O2, LSE2 = torch.empty_like(O), torch.empty_like(LSE)
+    ctx.ss_verify_begin(Q, d ** -0.5)
+    ctx.ss_verify_chunk8(cache, vl)
+    vl.fill_(1)                                    # the round keeps to the lengths that the chunk went by
+    ctx.ss_verify_finalize(O2, LSE2)
+    assert ctx.ss_poll_status() == (0, 0)
+    check_attention(Q, O2, LSE2, lambda b: history(cache, b, lens[b]), d ** -0.5)
+    ctx.close()
