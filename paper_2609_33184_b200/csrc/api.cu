@@ -160,7 +160,9 @@ Layout layout_for(const ss_config* c) {
   L.off_a = align_up(L.off_ml + (size_t)sets * rows * sizeof(float2), 256);
   L.off_scratch8 = align_up(L.off_a + (size_t)sets * rows * c->d * sizeof(float), 256);
   const size_t rows8 = L.R_stride < ss::kRows8 ? L.R_stride : ss::kRows8;
-  L.off_plan8 = align_up(L.off_scratch8 + 2 * ss::kCtas8 * rows8 * (c->d + 4) * sizeof(float), 256);
+  const size_t few8 = L.R_stride < ss::kFew8 ? L.R_stride : ss::kFew8;
+  const size_t slots8 = 2 * (ss::kCtas8 * rows8 > ss::kCtasFew8 * few8 ? ss::kCtas8 * rows8 : ss::kCtasFew8 * few8);
+  L.off_plan8 = align_up(L.off_scratch8 + slots8 * (c->d + 4) * sizeof(float), 256);
   L.total = align_up(L.off_plan8 + ((size_t)c->max_B + 1) * sizeof(uint32_t), 256);
   return L;
 }
@@ -1359,6 +1361,7 @@ static ss_status attn8(ss_ctx* c, const ss_tensor& Q, int32_t B, int32_t T_q, fl
   p->rows_per_tile = (p->R + p->row_tiles - 1) / p->row_tiles;
   // (the kernels number all tiles in 31 bits)
   if ((int64_t)B * ((p->kv.room + ss::kTok8 - 1) / ss::kTok8) * p->H_kv * p->row_tiles >= (1ll << 31)) return SS_ERR_SHAPE;
+  p->max_ctas = tc && p->d == 64 && p->rows_per_tile <= ss::kFew8 ? ss::kCtasFew8 : ss::kCtas8;  // as many as are resident
   p->scale_log2 = scale * 1.4426950408889634f;
   p->scratch = c->scratch8;
   p->plan = p->O ? nullptr : c->plan8;

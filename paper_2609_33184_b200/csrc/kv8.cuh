@@ -23,7 +23,9 @@
 namespace ss {
 
 constexpr int kTok8 = 128;                 // tokens per tile
-constexpr int kCtas8 = 2 * kNumSM;         // most CTAs of an attention launch
+constexpr int kCtas8 = 2 * kNumSM;         // CTAs of an attention launch,
+constexpr int kCtasFew8 = 3 * kNumSM;      // and at head dim 64 with at most kFew8 rows per unit
+constexpr int kFew8 = 16;
 constexpr int kRows8 = 32;                 // most query rows per unit
 constexpr int kMinRows8 = 8;               // rows per unit of the CUDA-core kernel
 constexpr int kMinExp8 = -32, kMaxExp8 = 80;
@@ -50,6 +52,7 @@ struct Attn8Params {
   int B, H_kv, G, T_q, R, d;
   int row_tiles, rows_per_tile;
   float scale_log2;
+  int max_ctas;               // grid of the attention launch (more CTAs than tiles: the others do nothing)
   float* scratch;             // 2 slots per CTA of rows_per_tile * (d + 4) floats: (m, l) pairs, room, a[]
   uint32_t* plan;             // [B + 1] or null: receives the tiles before each request (all units), and their total
   __nv_bfloat16* O;           // either the finished output ...
@@ -165,7 +168,7 @@ __device__ __forceinline__ Share8 find_share8(const Attn8Params& p) {
   for (int b = 0; b < p.B; b += 128) sum += mine = tiles_of_four8(p, b, n, &bad);
   if (blockIdx.x == 0 && __any_sync(0xffffffffu, bad) && lane == 0) atomicOr(p.status, SS_DEV_BAD_VALID_LEN);
   s.total = __reduce_add_sync(0xffffffffu, sum);
-  set_shares8(gridDim.x, &s);
+  set_shares8(p.max_ctas, &s);
   if (blockIdx.x >= s.ctas || s.total == 0) return s;
   s.lo = share_lo8(s, blockIdx.x);
   s.hi = share_lo8(s, blockIdx.x + 1);

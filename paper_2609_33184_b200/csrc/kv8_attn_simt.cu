@@ -182,7 +182,7 @@ __global__ void __launch_bounds__(128) attn8_simt_kernel(const __grid_constant__
 }  // namespace
 
 cudaError_t launch_attn8_simt(const Attn8Params& p, cudaStream_t s, bool pdl) {
-  const dim3 grid(kCtas8), block(128);
+  const dim3 grid(p.max_ctas), block(128);
   return p.d == 128 ? launch_kernel(attn8_simt_kernel<128>, grid, block, 0, s, pdl, p)
                     : launch_kernel(attn8_simt_kernel<64>, grid, block, 0, s, pdl, p);
 }

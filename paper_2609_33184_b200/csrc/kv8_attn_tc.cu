@@ -25,8 +25,8 @@
 //
 // A CTA walks its share of the tiles (kv8.cuh): 4 softmax warps per 16 rows (thread = key of the tile in
 // the scores, head dim in the output), one TMA producer warp, one MMA issuer warp.  The producer runs
-// ahead across segment ends, so a new segment finds its first tiles in shared memory.  Two CTAs per
-// SM (at most 110 KB shared memory, 256 TMEM columns each) hide each other's segment ends.
+// ahead across segment ends, so a new segment finds its first tiles in shared memory.  Two or
+// three CTAs per SM hide each other's segment ends.
 // Every wait is bounded; on expiry the CTA raises SS_DEV_WAIT_EXPIRED and returns.
 #include <cuda_fp8.h>
 
@@ -70,8 +70,12 @@ struct Cfg8 {
   static constexpr int kRest = (kQBytes + 1023) / 1024 * 1024 + kPBytes + kCtlBytes;
   // head dim 64: the output MMA's upper 64 rows read one unit further on (results never used), the
   // last unit's inside this window too
-  static constexpr int kAfter = kRest > kUnitBytes ? kRest : kUnitBytes;
-  static constexpr int kUnits0 = (112 * 1024 - kAfter) / kUnitBytes;
+  static constexpr int kAfter = D == 64 && kRest < kUnitBytes ? kUnitBytes : kRest;
+  // Resident CTAs.  Head dim 64 has half the bytes per tile for the same chain of steps, so a third CTA pays (16 x
+  // 32768 tokens in pages of 16, 4 rows: 134 -> 107 us; 16 rows, pages of 64: 112 -> 97); at head dim 128 its shorter rings cost more than
+  // it gives (166 -> 170 us).
+  static constexpr int kPerSM = D == 64 && NR <= kFew8 ? 3 : 2;
+  static constexpr int kUnits0 = ((kPerSM == 3 ? 74 : 112) * 1024 - kAfter) / kUnitBytes;
   static constexpr int kUnits = kUnits0 > 12 ? 12 : kUnits0;
   static constexpr int kOffQ = kUnits * kUnitBytes;
   static constexpr int kOffP = kOffQ + (kQBytes + 1023) / 1024 * 1024;
@@ -165,7 +169,7 @@ __device__ __forceinline__ void tmem_st(uint32_t taddr, const uint32_t* r) {
 }
 
 template <int NR, int WG, int D>
-__global__ void __launch_bounds__(Cfg8<NR, WG, D>::kThreads, 2)
+__global__ void __launch_bounds__(Cfg8<NR, WG, D>::kThreads, Cfg8<NR, WG, D>::kPerSM)
 attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ CUtensorMap tmK,
                 const __grid_constant__ CUtensorMap tmV) {
   using C = Cfg8<NR, WG, D>;
@@ -729,7 +733,7 @@ cudaError_t prepare8() {
 template <int NR, int WG, int D>
 cudaError_t launch8(const Attn8Params& p, const CUtensorMap& tmK, const CUtensorMap& tmV, cudaStream_t s, bool pdl) {
   using C = Cfg8<NR, WG, D>;
-  return launch_kernel(attn8_tc_kernel<NR, WG, D>, dim3(kCtas8), dim3(C::kThreads), C::kSmem, s, pdl, p, tmK, tmV);
+  return launch_kernel(attn8_tc_kernel<NR, WG, D>, dim3(p.max_ctas), dim3(C::kThreads), C::kSmem, s, pdl, p, tmK, tmV);
 }
 template <int D>
 cudaError_t launch_rows(const Attn8Params& p, const CUtensorMap& tmK, const CUtensorMap& tmV, cudaStream_t s, bool pdl) {

@@ -56,10 +56,10 @@ __device__ __forceinline__ Row8 row8(const Attn8Params& p, int64_t row, int lane
   w.n = 0;
   w.first = w.rest = nullptr;
   if (g.n > 0) {
-    set_shares8(kCtas8, &s);
+    set_shares8(p.max_ctas, &s);
     g.start = before + (uint32_t)(g.kvh * p.row_tiles + rt) * g.n;
-    const int i0 = min((int)share_of8(s, g.start), kCtas8 - 1);  // (no address depends on more than these two)
-    w.n = min((int)share_of8(s, g.start + g.n - 1), kCtas8 - 1) - i0 + 1;
+    const int i0 = min((int)share_of8(s, g.start), p.max_ctas - 1);  // (no address depends on more than these two)
+    w.n = min((int)share_of8(s, g.start + g.n - 1), p.max_ctas - 1) - i0 + 1;
     w.first = slot8(p, s, g.start, i0);
     w.rest = slot8(p, s, g.start, i0 + 1);
   }
