@@ -1360,8 +1360,10 @@ static ss_status attn8(ss_ctx* c, const ss_tensor& Q, int32_t B, int32_t T_q, fl
   p->row_tiles = (p->R + most - 1) / most;
   p->rows_per_tile = (p->R + p->row_tiles - 1) / p->row_tiles;
   // (the kernels number all tiles in 31 bits)
-  if ((int64_t)B * ((p->kv.room + ss::kTok8 - 1) / ss::kTok8) * p->H_kv * p->row_tiles >= (1ll << 31)) return SS_ERR_SHAPE;
-  p->max_ctas = tc && p->d == 64 && p->rows_per_tile <= ss::kFew8 ? ss::kCtasFew8 : ss::kCtas8;  // as many as are resident
+  if ((int64_t)B * ((p->kv.room + ss::kTok8 - 1) / ss::kTok8) * p->H_kv >= (1ll << 31)) return SS_ERR_SHAPE;
+  // as many CTAs as are resident, and one for every row tile at least
+  p->shares = (tc && p->d == 64 && p->rows_per_tile <= ss::kFew8 ? ss::kCtasFew8 : ss::kCtas8) / p->row_tiles;
+  if (p->shares < 1) p->shares = 1;
   p->scale_log2 = scale * 1.4426950408889634f;
   p->scratch = c->scratch8;
   p->plan = p->O ? nullptr : c->plan8;

@@ -8,11 +8,13 @@
 // keeps the ratio of two scales below 2^112, so that sums of weights and of weights times scales
 // stay in fp32's range under one reference.
 //
-// Sharing out.  A unit is one tile of query rows of one (request, kv-head); its history is cut into
-// tiles of kTok8 tokens.  The tiles of all units laid end to end (request by request, lengths read
-// on the device) are given to the CTAs in equal shares, so a long request is split over many CTAs
-// and short ones are gathered in one, whatever the batch looks like and without the host knowing
-// the lengths.  A unit inside one share is finished by its CTA; a unit cut by a share's end leaves
+// Sharing out.  A unit is one (request, kv-head); its history is cut into tiles of kTok8 tokens.  The
+// tiles of all units laid end to end (request by request, lengths read on the device) are given to the
+// CTAs in equal shares, so a long request is split over many CTAs and short ones are gathered in one,
+// whatever the batch looks like and without the host knowing the lengths.  Where the rows of a unit take
+// several row tiles, as many CTAs side by side go through one share, a row tile each: they read the same
+// K/V at about the same time, from memory once (laid end to end as units of their own, each row tile
+// read it again: 16 x 16384 tokens with 64 rows 201 us against 186, a 320-row tree 960 against 825).  A unit inside one share is finished by its CTA; a unit cut by a share's end leaves
 // one partial state (m, l, a[d]) per CTA in the scratch area, and a second kernel joins them in CTA order
 // (kv8_join.cu), so results do not depend on timing.
 #pragma once
@@ -52,9 +54,9 @@ struct Attn8Params {
   int B, H_kv, G, T_q, R, d;
   int row_tiles, rows_per_tile;
   float scale_log2;
-  int max_ctas;               // grid of the attention launch (more CTAs than tiles: the others do nothing)
+  int shares;                 // most shares; the attention launch has shares * row_tiles CTAs
   float* scratch;             // 2 slots per CTA of rows_per_tile * (d + 4) floats: (m, l) pairs, room, a[]
-  uint32_t* plan;             // [B + 1] or null: receives the tiles before each request (all units), and their total
+  uint32_t* plan;             // [B + 1] or null: receives the tiles before each request (all kv-heads), and their total
   __nv_bfloat16* O;           // either the finished output ...
   float* LSE;
   float2* part_ml;            // ... or (O null) one partial state per row, as the chunk kernels leave them
@@ -116,7 +118,8 @@ __device__ __forceinline__ int outer8(const View8& kv, int b, int tok, int* inne
 // hold fewer than 2^31.  The first `more` shares have q + 1 tiles, the others q.
 struct Share8 {
   uint32_t total, lo, hi;   // tiles of the launch; this CTA's range
-  uint32_t ctas, q, more;   // CTAs that have a share
+  uint32_t ctas, q, more;   // shares
+  uint32_t idx, rt;         // this CTA's share and row tile
   uint32_t b0, base0;       // request that holds tile `lo`, and the tiles before it
 };
 __device__ __forceinline__ uint32_t share_lo8(const Share8& s, uint32_t i) { return i * s.q + min(i, s.more); }
@@ -126,16 +129,16 @@ __device__ __forceinline__ uint32_t share_of8(const Share8& s, uint32_t x) {
   return x < big ? x / (s.q + 1) : s.more + (x - big) / s.q;
 }
 
-// From the number of tiles to the shares of a launch of at most `grid` CTAs.
-__device__ __forceinline__ void set_shares8(uint32_t grid, Share8* s) {
-  s->ctas = min(max(s->total, 1u), grid);
+// From the number of tiles to at most `most` shares.
+__device__ __forceinline__ void set_shares8(uint32_t most, Share8* s) {
+  s->ctas = min(max(s->total, 1u), most);
   s->q = s->total / s->ctas;
   s->more = s->total - s->q * s->ctas;
 }
 
-// Tiles (all units) of requests b0 + 4 * lane .. + 3: 128 requests per step of a warp, whose loads go out together.
+// Tiles (all kv-heads) of requests b0 + 4 * lane .. + 3: 128 requests per step of a warp, whose loads go out together.
 __device__ __forceinline__ uint32_t tiles_of_four8(const Attn8Params& p, int b0, uint32_t (&n)[4], bool* bad) {
-  const uint32_t units = (uint32_t)(p.H_kv * p.row_tiles);
+  const uint32_t units = (uint32_t)p.H_kv;
   const int b = b0 + 4 * (threadIdx.x & 31);
   int len[4];
 #pragma unroll
@@ -168,10 +171,15 @@ __device__ __forceinline__ Share8 find_share8(const Attn8Params& p) {
   for (int b = 0; b < p.B; b += 128) sum += mine = tiles_of_four8(p, b, n, &bad);
   if (blockIdx.x == 0 && __any_sync(0xffffffffu, bad) && lane == 0) atomicOr(p.status, SS_DEV_BAD_VALID_LEN);
   s.total = __reduce_add_sync(0xffffffffu, sum);
-  set_shares8(p.max_ctas, &s);
-  if (blockIdx.x >= s.ctas || s.total == 0) return s;
-  s.lo = share_lo8(s, blockIdx.x);
-  s.hi = share_lo8(s, blockIdx.x + 1);
+  s.idx = blockIdx.x;
+  if (p.row_tiles > 1) {
+    s.idx /= (uint32_t)p.row_tiles;
+    s.rt = blockIdx.x - s.idx * p.row_tiles;
+  }
+  set_shares8(p.shares, &s);
+  if (s.idx >= s.ctas || s.total == 0) return s;
+  s.lo = share_lo8(s, s.idx);
+  s.hi = share_lo8(s, s.idx + 1);
   uint32_t base = 0;
 #pragma unroll 1
   for (int b = 0; b < p.B; b += 128) {
@@ -207,15 +215,13 @@ struct Seg8 {
   int row0, nrows;
 };
 __device__ __forceinline__ void seg_set8(const Attn8Params& p, const Share8& s, Seg8* g) {
-  // (within a request a unit is (kv-head, row tile), row tile fastest: neighbours read the same K/V)
   const uint32_t u = (g->pos - g->base) / (uint32_t)g->n;
-  const int kvh = p.row_tiles == 1 ? u : u / (uint32_t)p.row_tiles, rt = u - kvh * p.row_tiles;
-  g->kvh = kvh;
+  g->kvh = (int)u;
   g->start = g->base + u * g->n;
   g->t0 = (int)(g->pos - g->start);
   g->pos = min(g->start + g->n, s.hi);
   g->t1 = (int)(g->pos - g->start);
-  g->row0 = rt * p.rows_per_tile;
+  g->row0 = (int)s.rt * p.rows_per_tile;
   g->nrows = min(p.rows_per_tile, p.R - g->row0);
 }
 __device__ __forceinline__ bool seg_first8(const Attn8Params& p, const Share8& s, Seg8* g) {
@@ -230,7 +236,7 @@ __device__ __forceinline__ bool seg_first8(const Attn8Params& p, const Share8& s
 }
 __device__ __forceinline__ bool seg_next8(const Attn8Params& p, const Share8& s, Seg8* g) {
   if (g->pos >= s.hi) return false;
-  const uint32_t units = (uint32_t)(p.H_kv * p.row_tiles);
+  const uint32_t units = (uint32_t)p.H_kv;
 #pragma unroll 1
   while (g->pos >= g->base + units * g->n) {  // the next request with tokens (there is one: pos < hi <= total)
     g->base += units * g->n;
@@ -301,11 +307,11 @@ static __device__ __noinline__ void put_plan8(const Attn8Params& p) {
   if (lane == 0) p.plan[p.B] = base;
 }
 
-// Slot of CTA i's state of the unit that begins at tile `start` (first CTA i0): the first segment of a
-// share uses the CTA's even slot, a later one (always the last) the odd slot.
+// Slot of share i's state of the unit that begins at tile `start` (in row tile s.rt): the first segment
+// of a share uses the even slot of its CTA, a later one (always the last) the odd slot.
 __device__ __forceinline__ float* slot8(const Attn8Params& p, const Share8& s, uint32_t start, uint32_t i) {
   const int odd = share_lo8(s, i) < start ? 1 : 0;
-  return p.scratch + (int64_t)(2 * i + odd) * p.rows_per_tile * (p.d + 4);
+  return p.scratch + (int64_t)(2 * (i * p.row_tiles + s.rt) + odd) * p.rows_per_tile * (p.d + 4);
 }
 
 }  // namespace ss

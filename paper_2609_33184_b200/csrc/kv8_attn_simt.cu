@@ -152,7 +152,7 @@ __global__ void __launch_bounds__(128) attn8_simt_kernel(const __grid_constant__
     }
     __syncthreads();
     const bool whole = g.t0 == 0 && g.t1 == g.n;
-    float* slot = whole ? nullptr : slot8(p, share, g.start, blockIdx.x);
+    float* slot = whole ? nullptr : slot8(p, share, g.start, share.idx);
     for (int r = tid / D; r < g.nrows; r += 128 / D) {
       const int c = tid % D;
       float M = -INFINITY, L = 0.f, A = 0.f;
@@ -182,7 +182,7 @@ __global__ void __launch_bounds__(128) attn8_simt_kernel(const __grid_constant__
 }  // namespace
 
 cudaError_t launch_attn8_simt(const Attn8Params& p, cudaStream_t s, bool pdl) {
-  const dim3 grid(p.max_ctas), block(128);
+  const dim3 grid(p.shares * p.row_tiles), block(128);
   return p.d == 128 ? launch_kernel(attn8_simt_kernel<128>, grid, block, 0, s, pdl, p)
                     : launch_kernel(attn8_simt_kernel<64>, grid, block, 0, s, pdl, p);
 }

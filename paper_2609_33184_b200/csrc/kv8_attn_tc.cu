@@ -679,7 +679,7 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
       bar8<SOFT>();
       // the unit's result when it is whole, this CTA's state of it when it is cut
       const bool whole = done.t0 == 0 && done.t1 == done.n;
-      float* slot = slot8(p, share, done.start, blockIdx.x);
+      float* slot = slot8(p, share, done.start, share.idx);
       if (tid < done.nrows) {
         // (the sums are of 2^(s2 - M + bias))
         const float m = -ctl->nm[tid], l = (ctl->smax[0][tid] + ctl->smax[1][tid]) + (ctl->smax[2][tid] + ctl->smax[3][tid]);
@@ -733,7 +733,7 @@ cudaError_t prepare8() {
 template <int NR, int WG, int D>
 cudaError_t launch8(const Attn8Params& p, const CUtensorMap& tmK, const CUtensorMap& tmV, cudaStream_t s, bool pdl) {
   using C = Cfg8<NR, WG, D>;
-  return launch_kernel(attn8_tc_kernel<NR, WG, D>, dim3(p.max_ctas), dim3(C::kThreads), C::kSmem, s, pdl, p, tmK, tmV);
+  return launch_kernel(attn8_tc_kernel<NR, WG, D>, dim3(p.shares * p.row_tiles), dim3(C::kThreads), C::kSmem, s, pdl, p, tmK, tmV);
 }
 template <int D>
 cudaError_t launch_rows(const Attn8Params& p, const CUtensorMap& tmK, const CUtensorMap& tmV, cudaStream_t s, bool pdl) {

@@ -15,13 +15,14 @@ namespace {
 constexpr int kWarps = 4;
 constexpr int kFlight = 16;  // states in flight
 
-// A query row and where its unit's states are: n of them, the first at `first`, the others two slots apart
-// from `rest`; n = 0: empty request, n = 1: finished by one CTA, not in the scratch area.
+// A query row and where its unit's states are: n of them, the first at `first`, the others `step` floats
+// apart from `rest`; n = 0: empty request, n = 1: finished by one CTA, not in the scratch area.
 struct Row8 {
   Seg8 g;
   int r, rr;                // row in its unit, in its kv-head
   int n;
   const float *first, *rest;
+  int64_t step;
 };
 template <bool PLAN>
 __device__ __forceinline__ Row8 row8(const Attn8Params& p, int64_t row, int lane) {
@@ -35,7 +36,7 @@ __device__ __forceinline__ Row8 row8(const Attn8Params& p, int64_t row, int lane
   w.r = w.rr - rt * p.rows_per_tile;
   g.row0 = rt * p.rows_per_tile;
   g.nrows = min(p.rows_per_tile, p.R - g.row0);
-  const uint32_t units = (uint32_t)(p.H_kv * p.row_tiles);
+  const uint32_t units = (uint32_t)p.H_kv;
   Share8 s = {};
   uint32_t before = 0;  // tiles of the requests before this one
   if (PLAN) {
@@ -55,11 +56,13 @@ __device__ __forceinline__ Row8 row8(const Attn8Params& p, int64_t row, int lane
   }
   w.n = 0;
   w.first = w.rest = nullptr;
+  w.step = (int64_t)2 * p.row_tiles * p.rows_per_tile * (p.d + 4);
+  s.rt = (uint32_t)rt;
   if (g.n > 0) {
-    set_shares8(p.max_ctas, &s);
-    g.start = before + (uint32_t)(g.kvh * p.row_tiles + rt) * g.n;
-    const int i0 = min((int)share_of8(s, g.start), p.max_ctas - 1);  // (no address depends on more than these two)
-    w.n = min((int)share_of8(s, g.start + g.n - 1), p.max_ctas - 1) - i0 + 1;
+    set_shares8(p.shares, &s);
+    g.start = before + (uint32_t)g.kvh * g.n;
+    const int i0 = min((int)share_of8(s, g.start), p.shares - 1);  // (no address depends on more than these two)
+    w.n = min((int)share_of8(s, g.start + g.n - 1), p.shares - 1) - i0 + 1;
     w.first = slot8(p, s, g.start, i0);
     w.rest = slot8(p, s, g.start, i0 + 1);
   }
@@ -86,19 +89,18 @@ template <int D>
 __device__ __forceinline__ void add_states(const Attn8Params& p, const Row8& w, int lane, float& m, float& l,
                                            float (&a)[D / 32]) {
   constexpr int CPL = D / 32;
-  const int64_t slot = (int64_t)p.rows_per_tile * (D + 4);
 #pragma unroll 1
   for (int j0 = 0; j0 < w.n; j0 += kFlight) {
     // (m, l) one state per lane, a[] all lanes of one state after the other
     const int own = j0 + (lane & (kFlight - 1));
     float2 st = make_float2(-INFINITY, 0.f);
     if (own < w.n)
-      st = __ldcg(reinterpret_cast<const float2*>(own == 0 ? w.first : w.rest + (int64_t)(own - 1) * 2 * slot) + w.r);
+      st = __ldcg(reinterpret_cast<const float2*>(own == 0 ? w.first : w.rest + (own - 1) * w.step) + w.r);
     float v[kFlight][CPL];
 #pragma unroll
     for (int j = 0; j < kFlight; ++j) {
       const int i = min(j0 + j, w.n - 1);
-      load_a<CPL>((i == 0 ? w.first : w.rest + (int64_t)(i - 1) * 2 * slot) + 4 * p.rows_per_tile + w.r * D + lane * CPL, v[j]);
+      load_a<CPL>((i == 0 ? w.first : w.rest + (i - 1) * w.step) + 4 * p.rows_per_tile + w.r * D + lane * CPL, v[j]);
     }
     float top = st.y != 0.f ? st.x : -INFINITY;  // (l = 0: an empty state)
 #pragma unroll
