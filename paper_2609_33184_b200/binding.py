@@ -304,6 +304,9 @@ class Cache8:
         assert V.shape == K.shape
         if page_table is not None:
             assert page_table.dtype == torch.int32 and page_table.dim() == 2 and page_table.is_contiguous()
+        self.device = K.get_device()   # -1: the CPU
+        for t in (V, K_scale, V_scale, page_table):
+            assert t is None or t.get_device() == self.device, (t.device, K.device)
         self.tensors = (K, V, K_scale, V_scale, page_table)
         self.H_kv, self.d = K.shape[1], K.shape[3]
         self.requests = K.shape[0] if page_table is None else page_table.shape[0]
@@ -443,25 +446,23 @@ class Context:
     # The calls on the 8-bit cache are made once per step and layer, on small batches with more host
     # than device time: their checks are few and flat.
     def _cache8(self, cache: Cache8, B: int):
-        if cache.H_kv != self.cfg.H_kv or cache.d != self.d or cache.requests < B:
-            raise AssertionError("cache of another shape")
+        if cache.H_kv != self.cfg.H_kv or cache.d != self.d or cache.requests < B or cache.device != self._dev:
+            raise AssertionError("cache of another shape or device")
         return cache.ref
 
-    @staticmethod
-    def _i32(t, n):
+    def _i32(self, t, n):
         """Device pointer of an int32 tensor of n contiguous elements, or None."""
         if t is None:
             return None
-        if t.dtype is not torch.int32 or t.numel() != n or not (t.is_cuda and t.is_contiguous()):
-            raise AssertionError("int32 device tensor expected", t.shape, t.dtype)
+        if t.dtype is not torch.int32 or t.numel() != n or t.get_device() != self._dev or not t.is_contiguous():
+            raise AssertionError("int32 tensor on the context's device expected", t.shape, t.dtype, t.device)
         return t.data_ptr()
 
-    @staticmethod
-    def _rows(t, shape):
+    def _rows(self, t, shape):
         """[B, H, T, d] bf16 tensor of this shape, d contiguous -> ss_tensor."""
         s = t.stride()
-        if t.dtype is not torch.bfloat16 or t.shape != shape or s[3] != 1 or not t.is_cuda:
-            raise AssertionError("bf16 device tensor expected", t.shape, t.dtype, s)
+        if t.dtype is not torch.bfloat16 or t.shape != shape or s[3] != 1 or t.get_device() != self._dev:
+            raise AssertionError("bf16 tensor on the context's device expected", t.shape, t.dtype, s, t.device)
         return ss_tensor(t.data_ptr(), s[0], s[1], s[2])
 
     def ss_kv8_write(self, cache: Cache8, K: torch.Tensor, V: torch.Tensor, dst_off=None, row_cnt=None,
@@ -498,10 +499,10 @@ class Context:
         """Q [B, H_q, T_q, d] over the first valid_len[b] tokens of the cache -> O (bf16), LSE (fp32 [B, H_q, T_q])."""
         shape = Q.shape
         B, H, T, d = shape
-        if O.dtype is not torch.bfloat16 or O.shape != shape or not (O.is_contiguous() and O.is_cuda):
+        if O.dtype is not torch.bfloat16 or O.shape != shape or O.get_device() != self._dev or not O.is_contiguous():
             raise AssertionError("O: contiguous bf16 of Q's shape expected", O.shape, O.dtype)
         if LSE is not None and (LSE.dtype is not torch.float32 or LSE.shape != shape[:3] or
-                                not (LSE.is_contiguous() and LSE.is_cuda)):
+                                LSE.get_device() != self._dev or not LSE.is_contiguous()):
             raise AssertionError("LSE: contiguous fp32 [B, H_q, T_q] expected", LSE.shape, LSE.dtype)
         st = self.lib.ss_decode8(self.handle, self._rows(Q, (B, self.H_q, T, self.d)), B, T, scale,
                                  self._cache8(cache, B), self._i32(valid_len, B), O.data_ptr(),

@@ -769,3 +769,75 @@ def test_large_batches(B):
     assert ctx.ss_poll_status() == (0, 0)
     check_attention(Q, O2, LSE2, lambda b: history(cache, b, lens[b]), d ** -0.5)
     ctx.close()
+
+
+def test_tensors_on_another_device_are_refused():
+    ssb = _ssb()
+    B, H_kv, d = 2, 2, 64
+    ctx = ssb.Context(B, 4, H_kv, d, 2, 2, 64)
+    cache, there = ssb.Cache8.empty(B, H_kv, 64, d), ssb.Cache8.empty(B, H_kv, 64, d, device="cpu")
+    Q, x = torch.zeros(B, 4, 1, d, dtype=torch.bfloat16, device=DEV), torch.zeros(B, H_kv, 2, d, dtype=torch.bfloat16, device=DEV)
+    O, L, n = torch.empty_like(Q), torch.empty(B, 4, 1, device=DEV), torch.ones(B, dtype=torch.int32, device=DEV)
+    launches = ctx.launch_count()
+    for args in ((there, x, x), (cache, x.cpu(), x), (cache, x, x.cpu())):
+        for f in (ctx.ss_kv8_write, ctx.ss_kv8_read):
+            with pytest.raises(AssertionError):
+                f(*args)
+    for f in (ctx.ss_kv8_write, ctx.ss_kv8_read):
+        with pytest.raises(AssertionError):
+            f(cache, x, x, row_cnt=n.cpu())
+    for args in ((Q.cpu(), 1.0, cache, n, O, L), (Q, 1.0, there, n, O, L), (Q, 1.0, cache, n.cpu(), O, L),
+                 (Q, 1.0, cache, n, O.cpu(), L), (Q, 1.0, cache, n, O, L.cpu())):
+        with pytest.raises(AssertionError):
+            ctx.ss_decode8(*args)
+    with pytest.raises(AssertionError):
+        ssb.Cache8(cache.tensors[0], *there.tensors[1:4])
+    assert ctx.launch_count() == launches
+    ctx.close()
+
+
+def test_rows_and_pages_given_twice():
+    """A row may be a source several times, and requests may share pages that they only read."""
+    ssb = _ssb()
+    B, H_q, H_kv, d, page = 2, 4, 2, 128, 16
+    cache = ssb.Cache8.empty(8, H_kv, page, d, torch.tensor([[5, 2, 5, 7], [5, 2, 0, 1]], dtype=torch.int32, device=DEV))
+    ctx = ssb.Context(B, H_q, H_kv, d, 1, 1, 4 * page)
+    g = torch.Generator().manual_seed(3)
+    K, V = (torch.randn(B, H_kv, 4, d, generator=g).bfloat16().to(DEV) for _ in range(2))
+    idx = torch.tensor([[2, 2, 0, 2], [1, 1, 1, 1]], dtype=torch.int32, device=DEV)
+    off = torch.tensor([48, 40], dtype=torch.int32, device=DEV)     # pages 7 and 0
+    ctx.ss_kv8_write(cache, K, V, dst_off=off, row_idx=idx)
+    Kr, Vr = torch.empty_like(K), torch.empty_like(V)
+    ctx.ss_kv8_read(cache, Kr, Vr, src_off=off)
+    for b in range(B):
+        for k in range(4):
+            src = int(idx[b, k])
+            first = idx[b].tolist().index(src)
+            for got, rows in ((Kr, K), (Vr, V)):
+                assert torch.equal(got[b, :, k], got[b, :, first])
+                want = rows[b, :, src].double()
+                top = want.abs().amax(-1, keepdim=True)
+                # half a step of e4m3: 2^-4 of the value, or 2^-10 * 2^e with 2^e < 2 * top / 448
+                tol = torch.maximum(2.0 ** -4 * want.abs(), 2.0 ** -9 / 448 * top)
+                assert ((got[b, :, k].double() - want).abs() <= tol).all()
+    # page 5 twice in one request and in both
+    fill = torch.randn(1, H_kv, 32, d, generator=g).bfloat16().to(DEV)
+    ctx.ss_kv8_write(ssb.Cache8(*cache.tensors[:4], cache.tensors[4][:1].contiguous()), fill, fill)
+    Kr, Vr = (torch.empty(B, H_kv, 48, d, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    ctx.ss_kv8_read(cache, Kr, Vr)
+    assert torch.equal(Kr[0, :, :16], Kr[0, :, 32:]) and torch.equal(Kr[0, :, :32], Kr[1, :, :32])
+    Q = torch.randn(B, H_q, 1, d, generator=g).bfloat16().to(DEV)
+    O, L = torch.empty_like(Q), torch.empty(B, H_q, 1, device=DEV)
+    n = torch.tensor([48, 32], dtype=torch.int32, device=DEV)
+    ctx.ss_decode8(Q, d ** -0.5, cache, n, O, L)
+    for b in range(B):
+        for h in range(H_q):
+            rows = int(n[b])
+            k, v = (t[b, h // 2, :rows].double().cpu().numpy() for t in (Kr, Vr))
+            o, lse, A = kv8.attention(Q[b, h].double().cpu().numpy(), k, v, d ** -0.5)
+            err = np.abs(O[b, h].double().cpu().numpy() - o)
+            # bf16 output (2^-8 of the value) and weights of 9 bits (2^-9 of the sum of |w v|)
+            assert (err <= 2.0 ** -8 * np.abs(o) + 2.0 ** -8 * A).all()
+            assert abs(float(L[b, h, 0]) - lse[0]) < 1e-4
+    assert ctx.ss_poll_status()[0] == 0
+    ctx.close()
