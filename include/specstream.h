@@ -291,10 +291,16 @@ ss_status ss_commit_gather(ss_ctx* ctx, ss_tensor K_loc, ss_tensor V_loc, int32_
  * page_size, d] of codes, K_scale, V_scale [n_pages, H_kv, page_size] of bytes (stride_b = page
  * stride), page_table (device int32 [B, pages_per_req]) lists a request's pages, which hold
  * page_size * pages_per_req tokens; attention runs on the tensor cores for pages of 8, 16, 32, 64 or
- * a multiple of 128 tokens and on the CUDA cores, many times slower, for others.  Dense (page_table NULL): [B, H_kv, page_size, d], n_pages =
- * requests in the buffer (>= the call's B), pages_per_req ignored.  Strides are in bytes; for the
- * codes d is contiguous and base and strides are multiples of 16; the scales' strides and base are
- * free.  Table entries of pages that a call does not touch may hold anything. */
+ * a multiple of 128 tokens and on the CUDA cores, many times slower, for others.  Dense (page_table
+ * NULL): [B, H_kv, page_size, d], n_pages = requests in the buffer (>= the call's B), pages_per_req
+ * ignored.  Strides are in bytes; for the codes d is contiguous and base and strides are multiples of
+ * 16; the scales' strides and base are free.  Table entries of pages that a call does not touch may
+ * hold anything.
+ *
+ * Attention over the cache (ss_verify_chunk8, ss_decode8) keeps pieces of its result in the context's
+ * workspace: rounds and decoding steps of one context, replays of captured ones too, have to follow
+ * one another on the device (one stream, or streams ordered by events).  Give what is to run side by
+ * side a context each.  Writing and reading use no workspace. */
 typedef struct {
   ss_tensor K, V;               /* codes, device                                             */
   ss_tensor K_scale, V_scale;   /* one byte per row, device                                  */
@@ -325,9 +331,8 @@ ss_status ss_kv8_read(ss_ctx* ctx, const ss_cache8* cache, ss_tensor K, ss_tenso
  * row of the round against tokens [0, valid_len[b]) (device [B], NULL = all the request's room;
  * outside [0, room]: clamped, SS_DEV_BAD_VALID_LEN).  May be mixed with bf16 chunks in any order, and
  * called several times.  The room must not exceed max_Lc (SS_ERR_SHAPE).  A query value that is not
- * finite makes its row NaN.  The split over the GPU follows the lengths on
- * the device, so no host copy of them is taken and a captured call follows lengths that change
- * between replays. */
+ * finite makes its row NaN.  The split over the GPU follows the lengths on the device, so no host copy
+ * of them is taken and a captured call follows lengths that change between replays. */
 ss_status ss_verify_chunk8(ss_ctx* ctx, const ss_cache8* cache, const int32_t* valid_len, void* stream);
 
 /* Decoding: attention of Q [B, H_q, T_q, d] over the 8-bit cache alone, O and LSE as
