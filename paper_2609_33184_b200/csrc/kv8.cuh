@@ -14,9 +14,11 @@
 // whatever the batch looks like and without the host knowing the lengths.  Where the rows of a unit take
 // several row tiles, as many CTAs side by side go through one share, a row tile each: they read the same
 // K/V at about the same time, from memory once (laid end to end as units of their own, each row tile
-// read it again: 16 x 16384 tokens with 64 rows 201 us against 186, a 320-row tree 960 against 825).  A unit inside one share is finished by its CTA; a unit cut by a share's end leaves
-// one partial state (m, l, a[d]) per CTA in the scratch area, and a second kernel joins them in CTA order
-// (kv8_join.cu), so results do not depend on timing.
+// read it again: 16 x 16384 tokens with 64 rows 201 us against 186, a 320-row tree 960 against 825; 179
+// and 793 since).
+// A unit inside one share is finished by its CTA; a unit cut by a share's end leaves one partial state
+// (m, l, a[d]) per CTA in the scratch area, and a second kernel joins them in CTA order (kv8_join.cu), so
+// results do not depend on timing.
 #pragma once
 #include <cuda_fp16.h>
 
@@ -26,10 +28,10 @@ namespace ss {
 
 constexpr int kTok8 = 128;                 // tokens per tile
 constexpr int kCtas8 = 2 * kNumSM;         // CTAs of an attention launch,
-constexpr int kCtasFew8 = 3 * kNumSM;      // and at head dim 64 with at most kFew8 rows per unit
+constexpr int kCtasFew8 = 3 * kNumSM;      // and at head dim 64 with at most kFew8 rows per row tile
 constexpr int kFew8 = 16;
-constexpr int kRows8 = 32;                 // most query rows per unit
-constexpr int kMinRows8 = 8;               // rows per unit of the CUDA-core kernel
+constexpr int kRows8 = 32;                 // most rows of a row tile
+constexpr int kMinRows8 = 8;               // rows of a row tile in the CUDA-core kernel
 constexpr int kMinExp8 = -32, kMaxExp8 = 80;
 
 // A cache as the kernels address it; all strides in bytes.
@@ -93,7 +95,7 @@ cudaError_t attn8_tc_prepare();  // one-time function attributes
 __device__ __forceinline__ float pow2_8(int e) { return __int_as_float((e + 127) << 23); }  // |e| <= 126
 __device__ __forceinline__ float scale8(uint32_t byte) { return __int_as_float((int)(byte << 23)); }  // 2^(byte - 127)
 
-// Length of a request in tokens, flagged and clamped when it is outside [0, room].
+// Length of a request in tokens, clamped to [0, room] (find_share8 reports one outside).
 __device__ __forceinline__ int len8(const Attn8Params& p, int b) {
   if (!p.valid_len) return p.kv.room;
   const int v = p.valid_len[b];
@@ -113,7 +115,7 @@ __device__ __forceinline__ int outer8(const View8& kv, int b, int tok, int* inne
   return (id < 0 || id >= kv.n_outer) ? -1 : id;
 }
 
-// One CTA's share of all tiles, and the walk through its segments (a segment = the part of one unit
+// A CTA's share of all tiles, and the walk through its segments (a segment = the part of one unit
 // that lies in the share).  Tiles are numbered in 32 bits: the host sees to it that all rooms together
 // hold fewer than 2^31.  The first `more` shares have q + 1 tiles, the others q.
 struct Share8 {
@@ -123,7 +125,7 @@ struct Share8 {
   uint32_t b0, base0;       // request that holds tile `lo`, and the tiles before it
 };
 __device__ __forceinline__ uint32_t share_lo8(const Share8& s, uint32_t i) { return i * s.q + min(i, s.more); }
-// The CTA whose share holds tile x.
+// The share that holds tile x.
 __device__ __forceinline__ uint32_t share_of8(const Share8& s, uint32_t x) {
   const uint32_t big = s.more * (s.q + 1);
   return x < big ? x / (s.q + 1) : s.more + (x - big) / s.q;
@@ -136,7 +138,8 @@ __device__ __forceinline__ void set_shares8(uint32_t most, Share8* s) {
   s->more = s->total - s->q * s->ctas;
 }
 
-// Tiles (all kv-heads) of requests b0 + 4 * lane .. + 3: 128 requests per step of a warp, whose loads go out together.
+// Tiles (all kv-heads) of requests b0 + 4 * lane .. + 3: 128 requests per step of a warp, whose loads go
+// out together.
 __device__ __forceinline__ uint32_t tiles_of_four8(const Attn8Params& p, int b0, uint32_t (&n)[4], bool* bad) {
   const uint32_t units = (uint32_t)p.H_kv;
   const int b = b0 + 4 * (threadIdx.x & 31);

@@ -20,13 +20,13 @@
 // The terms of P stand side by side on the N axis (one pass of the MMA over V); those of Q too for up to
 // 8 rows, and for more rows as further steps along K (the scores then take half the registers).
 // M is raised lazily (exact maximum of the first tile; later only when some x exceeds 15, so P <= 2^15:
-// eight binades of room, since one raise stops all rows of the CTA; with two binades - and unscaled terms, one
-// instruction less per weight - every second tile of a 32-row round raised, 281 -> 438 us).
+// eight binades of room, since one raise stops all rows of the CTA; with two binades - and unscaled
+// terms, one instruction less per weight - every second tile of a 32-row round raised, 281 -> 438 us).
 //
-// A CTA walks its share of the tiles (kv8.cuh): 4 softmax warps per 16 rows (thread = key of the tile in
-// the scores, head dim in the output), one TMA producer warp, one MMA issuer warp.  The producer runs
-// ahead across segment ends, so a new segment finds its first tiles in shared memory.  Two or
-// three CTAs per SM hide each other's segment ends.
+// A CTA walks its share of the tiles (kv8.cuh): 4 softmax warps (thread = key of the tile in the
+// scores, head dim in the output; a second set of four for 32 rows spilled, 263 against 193 us), one TMA
+// producer warp, one MMA issuer warp.  The producer runs ahead across segment ends, so a new segment
+// finds its first tiles in shared memory.  Two or three CTAs per SM hide each other's segment ends.
 // Every wait is bounded; on expiry the CTA raises SS_DEV_WAIT_EXPIRED and returns.
 #include <cuda_fp8.h>
 
@@ -55,11 +55,10 @@ struct alignas(16) Ctl8 {
   alignas(16) float smax[4][NR];  // per warp: maxima of a tile; at a segment's end the row sums
 };
 
-// NR = rows, WG = softmax warpgroups (each takes NR / WG rows), D = head dim.
-template <int NR, int WG, int D>
+// NR = rows, D = head dim.
+template <int NR, int D>
 struct Cfg8 {
-  static constexpr int kSoft = 128 * WG, kThreads = kSoft + 64;
-  static constexpr int RT = NR / WG;                       // rows per softmax thread
+  static constexpr int kSoft = 128, kThreads = kSoft + 64; // softmax threads, all threads
   static constexpr bool kSideBySide = NR == 8;             // Q's terms on the N axis
   static constexpr int kUnitBytes = kTok8 * D;             // one K or V tile
   static constexpr int NS = kSideBySide ? 2 * NR : NR;     // score columns
@@ -71,9 +70,9 @@ struct Cfg8 {
   // head dim 64: the output MMA's upper 64 rows read one unit further on (results never used), the
   // last unit's inside this window too
   static constexpr int kAfter = D == 64 && kRest < kUnitBytes ? kUnitBytes : kRest;
-  // Resident CTAs.  Head dim 64 has half the bytes per tile for the same chain of steps, so a third CTA pays (16 x
-  // 32768 tokens in pages of 16, 4 rows: 134 -> 107 us; 16 rows, pages of 64: 112 -> 97); at head dim 128 its shorter rings cost more than
-  // it gives (166 -> 170 us).
+  // Resident CTAs.  Head dim 64 has half the bytes per tile for the same chain of steps, so a third CTA
+  // pays (16 x 32768 tokens in pages of 16, 4 rows: 134 -> 107 us; 16 rows, pages of 64: 112 -> 97); at
+  // head dim 128 its shorter rings cost more than it gives (166 -> 170 us).
   static constexpr int kPerSM = D == 64 && NR <= kFew8 ? 3 : 2;
   static constexpr int kUnits0 = ((kPerSM == 3 ? 74 : 112) * 1024 - kAfter) / kUnitBytes;
   static constexpr int kUnits = kUnits0 > 12 ? 12 : kUnits0;
@@ -84,7 +83,7 @@ struct Cfg8 {
   static constexpr int kCols = 2 * NS + NP;
   static constexpr uint32_t kTmemCols = kCols <= 64 ? 64 : kCols <= 128 ? 128 : 256;
   static constexpr uint32_t kColO = 2 * NS;
-  static_assert(kUnits >= 4 && kCols <= 256 && RT % 8 == 0, "shape");
+  static_assert(kUnits >= 4 && kCols <= 256 && NR % 8 == 0, "shape");
 };
 
 // A descriptor's low word holds the address / 16 (and the LBO above it), so the operands of the steps of
@@ -162,24 +161,19 @@ __device__ __forceinline__ void tmem_ld(uint32_t taddr, uint32_t* r) {
                  : "memory");
   }
 }
-template <int N>
-__device__ __forceinline__ void tmem_st(uint32_t taddr, const uint32_t* r) {
-  if (N == 16) tmem_st16(taddr, *reinterpret_cast<const uint32_t(*)[16]>(r));
-  else tmem_st8(taddr, *reinterpret_cast<const uint32_t(*)[8]>(r));
-}
 
-template <int NR, int WG, int D>
-__global__ void __launch_bounds__(Cfg8<NR, WG, D>::kThreads, Cfg8<NR, WG, D>::kPerSM)
+template <int NR, int D>
+__global__ void __launch_bounds__(Cfg8<NR, D>::kThreads, Cfg8<NR, D>::kPerSM)
 attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ CUtensorMap tmK,
                 const __grid_constant__ CUtensorMap tmV) {
-  using C = Cfg8<NR, WG, D>;
-  constexpr int UNITS = C::kUnits, NS = C::NS, NP = C::NP, RT = C::RT, SOFT = C::kSoft;
+  using C = Cfg8<NR, D>;
+  constexpr int UNITS = C::kUnits, NS = C::NS, NP = C::NP, SOFT = C::kSoft;
   extern __shared__ __align__(1024) uint8_t smem[];
   Ctl8<NR>* ctl = reinterpret_cast<Ctl8<NR>*>(smem + C::kOffCtl);
   uint8_t* q_s = smem + C::kOffQ;
   uint8_t* p_s = smem + C::kOffP;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  constexpr int kProducerWarp = 4 * WG, kMmaWarp = 4 * WG + 1;
+  constexpr int kProducerWarp = 4, kMmaWarp = 5;
 
   if (warp == kProducerWarp) {
     if (lane == 0) {
@@ -382,9 +376,8 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
     }
   } else {
     // ===== softmax warps =====
-    const int quad = warp & 3, key = quad * 32 + lane;       // TMEM lane: key of a tile, head dim of the output
-    const int c0 = (warp >> 2) * RT;                         // this thread's rows: [c0, c0 + RT)
-    const uint32_t lane_off = (uint32_t)(quad * 32) << 16;
+    const int key = tid;                                     // TMEM lane: key of a tile, head dim of the output
+    const uint32_t lane_off = (uint32_t)(warp * 32) << 16;
     auto wait = [&](uint64_t* bar, uint32_t parity) { wait8(bar, parity, &ctl->abort, p.status); };
     // Q: SOFT / NR threads per row, kE values each
     constexpr int TPR = SOFT / NR, kE = D / TPR, kQL = kE / 4;
@@ -498,9 +491,9 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
       ah_fetch();    // (its page id has arrived by now)
       ah_look(t0 + 1, t1, len, b);
       bar8<SOFT>();  // (factors and references)
-      float2 lsum[RT / 2];
+      float2 lsum[NR / 2];
 #pragma unroll
-      for (int r = 0; r < RT / 2; ++r) lsum[r] = make_float2(0.f, 0.f);
+      for (int r = 0; r < NR / 2; ++r) lsum[r] = make_float2(0.f, 0.f);
       for (int t = t0; t < t1; ++t, ++it) {
         const float kf = scale8(ah_ek), evf = (float)(int)ah_ev - 127.f, vinv = scale8(254u - ah_ev);
         ah_fetch();
@@ -518,22 +511,22 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
           for (int i = n_valid * (D / 16) + tid; i < kTok8 * (D / 16); i += SOFT) v[i] = make_uint4(0, 0, 0, 0);
         }
         // x[r] = s2 + ev - M + bias (in the segment's first tile s2 + ev)
-        float2 x[RT / 2];
+        float2 x[NR / 2];
         {
           // 16 rows at a time; the factors are formed while the scores are on their way
           const float2 kf2 = make_float2(kf, kf), ev2 = make_float2(evf, evf);
-          const uint32_t t_s = tmem + lane_off + (it & 1) * NS + c0;
-          constexpr int H = RT < 16 ? RT : 16;
+          const uint32_t t_s = tmem + lane_off + (it & 1) * NS;
+          constexpr int H = NR < 16 ? NR : 16;
           uint32_t raw[16];
-          if (C::kSideBySide || RT >= 16) tmem_ld<16>(t_s, raw);
+          if (C::kSideBySide || NR >= 16) tmem_ld<16>(t_s, raw);
           else tmem_ld<8>(t_s, raw);
 #pragma unroll
-          for (int r0 = 0; r0 < RT; r0 += H) {
+          for (int r0 = 0; r0 < NR; r0 += H) {
             float2 f[H / 2], e[H / 2];
 #pragma unroll
             for (int r = 0; r < H; r += 4) {
-              const float4 qf = *reinterpret_cast<const float4*>(&ctl->qf[c0 + r0 + r]);
-              const float4 nm = *reinterpret_cast<const float4*>(&ctl->nm[c0 + r0 + r]);
+              const float4 qf = *reinterpret_cast<const float4*>(&ctl->qf[r0 + r]);
+              const float4 nm = *reinterpret_cast<const float4*>(&ctl->nm[r0 + r]);
               f[r / 2] = __fmul2_rn(make_float2(qf.x, qf.y), kf2);
               f[r / 2 + 1] = __fmul2_rn(make_float2(qf.z, qf.w), kf2);
               e[r / 2] = __fadd2_rn(make_float2(nm.x, nm.y), ev2);
@@ -546,28 +539,28 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
               if (C::kSideBySide) sc = __fadd2_rn(sc, make_float2(__uint_as_float(raw[8 + r]), __uint_as_float(raw[8 + r + 1])));
               x[(r0 + r) / 2] = __ffma2_rn(sc, f[r / 2], e[r / 2]);
             }
-            if (r0 + H < RT) tmem_ld<16>(t_s + r0 + H, raw);
+            if (r0 + H < NR) tmem_ld<16>(t_s + r0 + H, raw);
           }
         }
         if (n_valid < kTok8) {
           __syncwarp();  // (kept a branch: as selects it costs every tile an instruction per score)
 #pragma unroll
-          for (int r = 0; r < RT / 2; ++r)
+          for (int r = 0; r < NR / 2; ++r)
             if (!key_ok) x[r] = make_float2(-INFINITY, -INFINITY);
         }
         float mx = -INFINITY;
 #pragma unroll
-        for (int r = 0; r < RT / 2; ++r) mx = max3_f(mx, x[r].x, x[r].y);
+        for (int r = 0; r < NR / 2; ++r) mx = max3_f(mx, x[r].x, x[r].y);
         if (bar_or8<SOFT>(first || mx > kOver)) {
           // ---- set the references to the exact maxima; later in a segment (rare) raise them, which
           // rescales O^T and the row sums ----
           float mine = -INFINITY;
 #pragma unroll
-          for (int r = 0; r < RT; ++r) {
+          for (int r = 0; r < NR; ++r) {
             const float m = redux_max(r & 1 ? x[r / 2].y : x[r / 2].x);
             if (lane == r) mine = m;
           }
-          if (lane < RT) ctl->smax[quad][c0 + lane] = mine;
+          if (lane < NR) ctl->smax[warp][lane] = mine;
           bar8<SOFT>();
           if (tid < NR) {  // M rises by this much (in the first tile, from 0 to the maximum - bias)
             const float top = fmaxf(fmaxf(ctl->smax[0][tid], ctl->smax[1][tid]), fmaxf(ctl->smax[2][tid], ctl->smax[3][tid]));
@@ -580,23 +573,23 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
             wait(&ctl->pfree, (it - 1) & 1);  // the output MMAs of the tile before have retired
             tc_fence_after();
 #pragma unroll 1
-            for (int k = 0; k < 3; ++k) {     // the three terms' accumulators of this thread's rows
+            for (int k = 0; k < 3; ++k) {     // the three terms' accumulators
 #pragma unroll 1
-              for (int r = 0; r < RT; r += 8) {
+              for (int r = 0; r < NR; r += 8) {
                 uint32_t o[8];
-                const uint32_t at = tmem + lane_off + C::kColO + k * NR + c0 + r;
+                const uint32_t at = tmem + lane_off + C::kColO + k * NR + r;
                 tmem_ld<8>(at, o);
                 tc_wait_ld();
 #pragma unroll
-                for (int c = 0; c < 8; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * ex2_ftz(-ctl->up[c0 + r + c]));
-                tmem_st<8>(at, o);
+                for (int c = 0; c < 8; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * ex2_ftz(-ctl->up[r + c]));
+                tmem_st8(at, o);
               }
             }
             tc_wait_st();
           }
 #pragma unroll
-          for (int r = 0; r < RT / 2; ++r) {
-            const float2 up = *reinterpret_cast<const float2*>(&ctl->up[c0 + 2 * r]);
+          for (int r = 0; r < NR / 2; ++r) {
+            const float2 up = *reinterpret_cast<const float2*>(&ctl->up[2 * r]);
             x[r] = __fadd2_rn(x[r], make_float2(-up.x, -up.y));
             if (!first) lsum[r] = __fmul2_rn(lsum[r], make_float2(ex2_ftz(-up.x), ex2_ftz(-up.y)));
           }
@@ -606,8 +599,8 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
           const float2 vinv2 = make_float2(vinv, vinv);
           // columns term * NR + row, 16 to a 16-byte piece per key
 #pragma unroll
-          for (int r = 0; r < RT; r += 16) {
-            constexpr int W = RT < 16 ? RT / 4 : 4;  // words of 4 rows
+          for (int r = 0; r < NR; r += 16) {
+            constexpr int W = NR < 16 ? NR / 4 : 4;  // words of 4 rows
             uint32_t piece[3][4];
 #pragma unroll
             for (int q = 0; q < W; ++q) {
@@ -625,19 +618,14 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
               // (the last term rounds)
               piece[2][q] = __byte_perm(residue(a1) + 0x00800080u, residue(b1) + 0x00800080u, 0x7531);
             }
-            if (RT >= 16) {
+            if (NR >= 16) {
 #pragma unroll
               for (int k = 0; k < 3; ++k)
-                *reinterpret_cast<uint4*>(p_s + (k * NR + c0 + r) / 16 * (kTok8 * 16) + key * 16) =
+                *reinterpret_cast<uint4*>(p_s + (k * NR + r) / 16 * (kTok8 * 16) + key * 16) =
                     make_uint4(piece[k][0], piece[k][1], piece[k][2], piece[k][3]);
-            } else if (NR == 8) {  // hi | mid, lo | nothing
+            } else {  // 8 rows: hi | mid, lo | nothing
               *reinterpret_cast<uint4*>(p_s + key * 16) = make_uint4(piece[0][0], piece[0][1], piece[1][0], piece[1][1]);
               *reinterpret_cast<uint4*>(p_s + kTok8 * 16 + key * 16) = make_uint4(piece[2][0], piece[2][1], 0, 0);
-            } else {
-#pragma unroll
-              for (int k = 0; k < 3; ++k)
-                *reinterpret_cast<uint2*>(p_s + (k * NR + c0) / 16 * (kTok8 * 16) + key * 16 + (k * NR + c0) % 16) =
-                    make_uint2(piece[k][0], piece[k][1]);
             }
           }
           fence_proxy_async();
@@ -649,19 +637,19 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
       // ---- the segment's end: what the next one needs is fetched first ----
       const Seg8& done = g;
       if (ctl->has[(k_seg + 1) & 1]) seg_fetch(ctl->seg[(k_seg + 1) & 1]);
-      // row sums: halve the rows a lane holds at every step, lane / (32 / RT) is the row in the end
+      // row sums: halve the rows a lane holds at every step, lane / (32 / NR) is the row in the end
       {
-        float v[RT];
+        float v[NR];
 #pragma unroll
-        for (int r = 0; r < RT; ++r) v[r] = (r & 1) ? lsum[r / 2].y : lsum[r / 2].x;
-        int n = RT;
+        for (int r = 0; r < NR; ++r) v[r] = (r & 1) ? lsum[r / 2].y : lsum[r / 2].x;
+        int n = NR;
 #pragma unroll
         for (int o = 16; o; o >>= 1) {
           if (n > 1) {
             n /= 2;
             const bool up = lane & o;
 #pragma unroll
-            for (int i = 0; i < RT / 2; ++i) {
+            for (int i = 0; i < NR / 2; ++i) {
               if (i < n) {
                 const float send = up ? v[i] : v[i + n], keep = up ? v[i + n] : v[i];
                 v[i] = keep + __shfl_xor_sync(0xffffffffu, send, o);
@@ -672,7 +660,7 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
           }
         }
         bar8<SOFT>();  // (every thread is done with smax as maxima)
-        if (lane % (32 / RT) == 0) ctl->smax[quad][c0 + lane / (32 / RT)] = v[0];
+        if (lane % (32 / NR) == 0) ctl->smax[warp][lane / (32 / NR)] = v[0];
       }
       wait(&ctl->pfree, (it - 1) & 1);
       tc_fence_after();
@@ -693,7 +681,7 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
       __nv_bfloat16* o_row = p.O + (pair * p.R + done.row0) * D + key;
       float* a_row = (whole ? p.part_a + (pair * p.R_stride + done.row0) * D : slot + 4 * p.rows_per_tile) + key;
 #pragma unroll 1
-      for (int q = c0; q < c0 + RT && q < done.nrows; q += 8) {
+      for (int q = 0; q < NR && q < done.nrows; q += 8) {
         uint32_t o[3][8];
 #pragma unroll
         for (int k = 0; k < 3; ++k) tmem_ld<8>(tmem + lane_off + C::kColO + k * NR + q, o[k]);
@@ -725,32 +713,32 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(C::kTmemCols) : "memory");
 }
 
-template <int NR, int WG, int D>
+template <int NR, int D>
 cudaError_t prepare8() {
-  return cudaFuncSetAttribute(attn8_tc_kernel<NR, WG, D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                              Cfg8<NR, WG, D>::kSmem);
+  return cudaFuncSetAttribute(attn8_tc_kernel<NR, D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              Cfg8<NR, D>::kSmem);
 }
-template <int NR, int WG, int D>
+template <int NR, int D>
 cudaError_t launch8(const Attn8Params& p, const CUtensorMap& tmK, const CUtensorMap& tmV, cudaStream_t s, bool pdl) {
-  using C = Cfg8<NR, WG, D>;
-  return launch_kernel(attn8_tc_kernel<NR, WG, D>, dim3(p.shares * p.row_tiles), dim3(C::kThreads), C::kSmem, s, pdl, p, tmK, tmV);
+  using C = Cfg8<NR, D>;
+  return launch_kernel(attn8_tc_kernel<NR, D>, dim3(p.shares * p.row_tiles), dim3(C::kThreads), C::kSmem, s, pdl, p, tmK, tmV);
 }
 template <int D>
 cudaError_t launch_rows(const Attn8Params& p, const CUtensorMap& tmK, const CUtensorMap& tmV, cudaStream_t s, bool pdl) {
-  if (p.rows_per_tile <= 8) return launch8<8, 1, D>(p, tmK, tmV, s, pdl);
-  if (p.rows_per_tile <= 16) return launch8<16, 1, D>(p, tmK, tmV, s, pdl);
-  return launch8<32, 1, D>(p, tmK, tmV, s, pdl);
+  if (p.rows_per_tile <= 8) return launch8<8, D>(p, tmK, tmV, s, pdl);
+  if (p.rows_per_tile <= 16) return launch8<16, D>(p, tmK, tmV, s, pdl);
+  return launch8<32, D>(p, tmK, tmV, s, pdl);
 }
 
 }  // namespace
 
 cudaError_t attn8_tc_prepare() {
-  cudaError_t e = prepare8<8, 1, 128>();
-  if (e == cudaSuccess) e = prepare8<16, 1, 128>();
-  if (e == cudaSuccess) e = prepare8<32, 1, 128>();
-  if (e == cudaSuccess) e = prepare8<8, 1, 64>();
-  if (e == cudaSuccess) e = prepare8<16, 1, 64>();
-  if (e == cudaSuccess) e = prepare8<32, 1, 64>();
+  cudaError_t e = prepare8<8, 128>();
+  if (e == cudaSuccess) e = prepare8<16, 128>();
+  if (e == cudaSuccess) e = prepare8<32, 128>();
+  if (e == cudaSuccess) e = prepare8<8, 64>();
+  if (e == cudaSuccess) e = prepare8<16, 64>();
+  if (e == cudaSuccess) e = prepare8<32, 64>();
   return e;
 }
 
