@@ -40,7 +40,7 @@ using namespace ss::tc;
 
 constexpr float kBias = 7.f, kOver = 15.f;
 
-template <int NR>
+template <int NQ>
 struct alignas(16) Ctl8 {
   uint64_t ufull[16], uempty[16];
   uint64_t sfull[2], pready, pfree, qfull;
@@ -49,10 +49,10 @@ struct alignas(16) Ctl8 {
   int has[2];                     // the softmax warps' current and next segment (in use by turns)
   Seg8 seg[2];
   Share8 share;
-  alignas(16) float nm[NR];       // bias - M
-  alignas(16) float qf[NR];       // 2^eq * scale * log2(e)
-  alignas(16) float up[NR];       // rise of the references; at a segment's end 1 / row sum
-  alignas(16) float smax[4][NR];  // per warp: maxima of a tile; at a segment's end the row sums
+  alignas(16) float nm[NQ];       // bias - M
+  alignas(16) float qf[NQ];       // 2^eq * scale * log2(e)
+  alignas(16) float up[NQ];       // rise of the references; at a segment's end 1 / row sum
+  alignas(16) float smax[4][NQ];  // per warp: maxima of a tile; at a segment's end the row sums
 };
 
 // NR = rows, D = head dim.
@@ -60,12 +60,13 @@ template <int NR, int D>
 struct Cfg8 {
   static constexpr int kSoft = 128, kThreads = kSoft + 64; // softmax threads, all threads
   static constexpr bool kSideBySide = NR == 8;             // Q's terms on the N axis
+  static constexpr int NQ = NR == 24 ? 32 : NR;            // rows of the Q operand (N has to be a multiple of 16)
   static constexpr int kUnitBytes = kTok8 * D;             // one K or V tile
-  static constexpr int NS = kSideBySide ? 2 * NR : NR;     // score columns
+  static constexpr int NS = kSideBySide ? 2 * NQ : NQ;     // score columns
   static constexpr int NP = (3 * NR + 15) / 16 * 16;       // weight columns
-  static constexpr int kQBytes = 2 * NR * D;
+  static constexpr int kQBytes = 2 * NQ * D;
   static constexpr int kPBytes = kTok8 * NP;
-  static constexpr int kCtlBytes = (sizeof(Ctl8<NR>) + 127) / 128 * 128;
+  static constexpr int kCtlBytes = (sizeof(Ctl8<NQ>) + 127) / 128 * 128;
   static constexpr int kRest = (kQBytes + 1023) / 1024 * 1024 + kPBytes + kCtlBytes;
   // head dim 64: the output MMA's upper 64 rows read one unit further on (results never used), the
   // last unit's inside this window too
@@ -167,9 +168,9 @@ __global__ void __launch_bounds__(Cfg8<NR, D>::kThreads, Cfg8<NR, D>::kPerSM)
 attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ CUtensorMap tmK,
                 const __grid_constant__ CUtensorMap tmV) {
   using C = Cfg8<NR, D>;
-  constexpr int UNITS = C::kUnits, NS = C::NS, NP = C::NP, SOFT = C::kSoft;
+  constexpr int UNITS = C::kUnits, NQ = C::NQ, NS = C::NS, NP = C::NP, SOFT = C::kSoft;
   extern __shared__ __align__(1024) uint8_t smem[];
-  Ctl8<NR>* ctl = reinterpret_cast<Ctl8<NR>*>(smem + C::kOffCtl);
+  Ctl8<C::NQ>* ctl = reinterpret_cast<Ctl8<C::NQ>*>(smem + C::kOffCtl);
   uint8_t* q_s = smem + C::kOffQ;
   uint8_t* p_s = smem + C::kOffP;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -320,7 +321,7 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
               for (int term = 0; term < (C::kSideBySide ? 1 : 2); ++term)
 #pragma unroll
                 for (int kk = 0; kk < D / 32; ++kk)
-                  mma8(d_s, a + kk * 2, k_hi, q_lo + term * (NR * D / 16) + kk * 2, q_hi, idesc_qk, term > 0 || kk > 0);
+                  mma8(d_s, a + kk * 2, k_hi, q_lo + term * (NQ * D / 16) + kk * 2, q_hi, idesc_qk, term > 0 || kk > 0);
               tc_commit(&ctl->uempty[uk]);
               tc_commit(&ctl->sfull[it & 1]);
             }
@@ -379,8 +380,8 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
     const int key = tid;                                     // TMEM lane: key of a tile, head dim of the output
     const uint32_t lane_off = (uint32_t)(warp * 32) << 16;
     auto wait = [&](uint64_t* bar, uint32_t parity) { wait8(bar, parity, &ctl->abort, p.status); };
-    // Q: SOFT / NR threads per row, kE values each
-    constexpr int TPR = SOFT / NR, kE = D / TPR, kQL = kE / 4;
+    // Q: SOFT / NQ threads per row, kE values each
+    constexpr int TPR = SOFT / NQ, kE = D / TPR, kQL = kE / 4;
     const int q_row = tid / TPR, q_part = tid % TPR;
     uint2 q_raw[kQL];
     auto q_load = [&](const Seg8& s) {
@@ -423,7 +424,7 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
         // operand row nn, 16-byte piece c at nn * D + ((c ^ swizzle(nn)) * 16); the lo rows follow the hi rows
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-          const int nn = q_row + k * NR, sw = D == 128 ? (nn & 7) : ((nn >> 1) & 3), byte = q_part * kE + i * 4;
+          const int nn = q_row + k * NQ, sw = D == 128 ? (nn & 7) : ((nn >> 1) & 3), byte = q_part * kE + i * 4;
           *reinterpret_cast<uint32_t*>(q_s + nn * D + (((byte >> 4) ^ sw) << 4) + (byte & 15)) = term[k];
         }
       }
@@ -524,7 +525,7 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
           for (int r0 = 0; r0 < NR; r0 += H) {
             float2 f[H / 2], e[H / 2];
 #pragma unroll
-            for (int r = 0; r < H; r += 4) {
+            for (int r = 0; r < H && r0 + r < NR; r += 4) {
               const float4 qf = *reinterpret_cast<const float4*>(&ctl->qf[r0 + r]);
               const float4 nm = *reinterpret_cast<const float4*>(&ctl->nm[r0 + r]);
               f[r / 2] = __fmul2_rn(make_float2(qf.x, qf.y), kf2);
@@ -534,12 +535,13 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
             }
             tc_wait_ld();
 #pragma unroll
-            for (int r = 0; r < H; r += 2) {
+            for (int r = 0; r < H && r0 + r < NR; r += 2) {
               float2 sc = make_float2(__uint_as_float(raw[r]), __uint_as_float(raw[r + 1]));
               if (C::kSideBySide) sc = __fadd2_rn(sc, make_float2(__uint_as_float(raw[8 + r]), __uint_as_float(raw[8 + r + 1])));
               x[(r0 + r) / 2] = __ffma2_rn(sc, f[r / 2], e[r / 2]);
             }
-            if (r0 + H < NR) tmem_ld<16>(t_s + r0 + H, raw);
+            if (r0 + 2 * H <= NR) tmem_ld<16>(t_s + r0 + H, raw);
+            else if (r0 + H < NR) tmem_ld<8>(t_s + r0 + H, raw);
           }
         }
         if (n_valid < kTok8) {
@@ -597,36 +599,41 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
         if (!first) wait(&ctl->pfree, (it - 1) & 1);  // P^T has been consumed
         {
           const float2 vinv2 = make_float2(vinv, vinv);
-          // columns term * NR + row, 16 to a 16-byte piece per key
+          // columns term * NR + row, 16 to a 16-byte piece per key, in words of 4
+          auto weights = [&](int r, uint32_t& hi, uint32_t& mid, uint32_t& lo) {
+            uint32_t w[2];
 #pragma unroll
-          for (int r = 0; r < NR; r += 16) {
-            constexpr int W = NR < 16 ? NR / 4 : 4;  // words of 4 rows
-            uint32_t piece[3][4];
-#pragma unroll
-            for (int q = 0; q < W; ++q) {
-              uint32_t w[2];
-#pragma unroll
-              for (int k = 0; k < 2; ++k) {
-                const int i = r / 2 + 2 * q + k;
-                const float2 e = make_float2(ex2_ftz(x[i].x), ex2_ftz(x[i].y));
-                lsum[i] = __ffma2_rn(e, vinv2, lsum[i]);
-                w[k] = h2_bits(__float22half2_rn(e));
-              }
-              const uint32_t a1 = residue(w[0]), b1 = residue(w[1]);
-              piece[0][q] = __byte_perm(w[0], w[1], 0x7531);
-              piece[1][q] = __byte_perm(a1, b1, 0x7531);
-              // (the last term rounds)
-              piece[2][q] = __byte_perm(residue(a1) + 0x00800080u, residue(b1) + 0x00800080u, 0x7531);
+            for (int k = 0; k < 2; ++k) {
+              const int i = r / 2 + k;
+              const float2 e = make_float2(ex2_ftz(x[i].x), ex2_ftz(x[i].y));
+              lsum[i] = __ffma2_rn(e, vinv2, lsum[i]);
+              w[k] = h2_bits(__float22half2_rn(e));
             }
-            if (NR >= 16) {
+            const uint32_t a1 = residue(w[0]), b1 = residue(w[1]);
+            hi = __byte_perm(w[0], w[1], 0x7531);
+            mid = __byte_perm(a1, b1, 0x7531);
+            // (the last term rounds)
+            lo = __byte_perm(residue(a1) + 0x00800080u, residue(b1) + 0x00800080u, 0x7531);
+          };
+          auto put = [&](int piece, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+            *reinterpret_cast<uint4*>(p_s + piece * (kTok8 * 16) + key * 16) = make_uint4(a, b, c, d);
+          };
+          if (NR % 16 == 0) {
 #pragma unroll
-              for (int k = 0; k < 3; ++k)
-                *reinterpret_cast<uint4*>(p_s + (k * NR + r) / 16 * (kTok8 * 16) + key * 16) =
-                    make_uint4(piece[k][0], piece[k][1], piece[k][2], piece[k][3]);
-            } else {  // 8 rows: hi | mid, lo | nothing
-              *reinterpret_cast<uint4*>(p_s + key * 16) = make_uint4(piece[0][0], piece[0][1], piece[1][0], piece[1][1]);
-              *reinterpret_cast<uint4*>(p_s + kTok8 * 16 + key * 16) = make_uint4(piece[2][0], piece[2][1], 0, 0);
+            for (int r = 0; r < NR; r += 16) {
+              uint32_t t[3][4];
+#pragma unroll
+              for (int q = 0; q < 4; ++q) weights((r + 4 * q) % NR, t[0][q], t[1][q], t[2][q]);
+#pragma unroll
+              for (int k = 0; k < 3; ++k) put((k * NR + r) / 16, t[k][0], t[k][1], t[k][2], t[k][3]);
             }
+          } else {  // the terms share pieces; what is behind them is nothing
+            constexpr int W = NR / 4;
+            uint32_t t[NP / 4] = {};
+#pragma unroll
+            for (int q = 0; q < W; ++q) weights(4 * q, t[q], t[W + q], t[2 * W + q]);
+#pragma unroll
+            for (int k = 0; k < NP / 16; ++k) put(k, t[4 * k], t[4 * k + 1], t[4 * k + 2], t[4 * k + 3]);
           }
           fence_proxy_async();
           tc_fence_before();
@@ -637,19 +644,19 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
       // ---- the segment's end: what the next one needs is fetched first ----
       const Seg8& done = g;
       if (ctl->has[(k_seg + 1) & 1]) seg_fetch(ctl->seg[(k_seg + 1) & 1]);
-      // row sums: halve the rows a lane holds at every step, lane / (32 / NR) is the row in the end
+      // row sums: halve the rows a lane holds at every step, lane / (32 / NQ) is the row in the end
       {
-        float v[NR];
+        float v[NQ];
 #pragma unroll
-        for (int r = 0; r < NR; ++r) v[r] = (r & 1) ? lsum[r / 2].y : lsum[r / 2].x;
-        int n = NR;
+        for (int r = 0; r < NQ; ++r) v[r] = r >= NR ? 0.f : (r & 1) ? lsum[r / 2].y : lsum[r / 2].x;
+        int n = NQ;
 #pragma unroll
         for (int o = 16; o; o >>= 1) {
           if (n > 1) {
             n /= 2;
             const bool up = lane & o;
 #pragma unroll
-            for (int i = 0; i < NR / 2; ++i) {
+            for (int i = 0; i < NQ / 2; ++i) {
               if (i < n) {
                 const float send = up ? v[i] : v[i + n], keep = up ? v[i + n] : v[i];
                 v[i] = keep + __shfl_xor_sync(0xffffffffu, send, o);
@@ -660,7 +667,7 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
           }
         }
         bar8<SOFT>();  // (every thread is done with smax as maxima)
-        if (lane % (32 / NR) == 0) ctl->smax[warp][lane / (32 / NR)] = v[0];
+        if (lane % (32 / NQ) == 0) ctl->smax[warp][lane / (32 / NQ)] = v[0];
       }
       wait(&ctl->pfree, (it - 1) & 1);
       tc_fence_after();
@@ -727,6 +734,7 @@ template <int D>
 cudaError_t launch_rows(const Attn8Params& p, const CUtensorMap& tmK, const CUtensorMap& tmV, cudaStream_t s, bool pdl) {
   if (p.rows_per_tile <= 8) return launch8<8, D>(p, tmK, tmV, s, pdl);
   if (p.rows_per_tile <= 16) return launch8<16, D>(p, tmK, tmV, s, pdl);
+  if (p.rows_per_tile <= 24) return launch8<24, D>(p, tmK, tmV, s, pdl);
   return launch8<32, D>(p, tmK, tmV, s, pdl);
 }
 
@@ -735,9 +743,11 @@ cudaError_t launch_rows(const Attn8Params& p, const CUtensorMap& tmK, const CUte
 cudaError_t attn8_tc_prepare() {
   cudaError_t e = prepare8<8, 128>();
   if (e == cudaSuccess) e = prepare8<16, 128>();
+  if (e == cudaSuccess) e = prepare8<24, 128>();
   if (e == cudaSuccess) e = prepare8<32, 128>();
   if (e == cudaSuccess) e = prepare8<8, 64>();
   if (e == cudaSuccess) e = prepare8<16, 64>();
+  if (e == cudaSuccess) e = prepare8<24, 64>();
   if (e == cudaSuccess) e = prepare8<32, 64>();
   return e;
 }

@@ -841,3 +841,35 @@ def test_rows_and_pages_given_twice():
             assert abs(float(L[b, h, 0]) - lse[0]) < 1e-4
     assert ctx.ss_poll_status()[0] == 0
     ctx.close()
+
+
+@pytest.mark.parametrize("rows", [12, 17, 24, 25, 32, 40, 48, 51])
+@pytest.mark.parametrize("kind", ["rising", "sink", "wide_v"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_uneven_values_with_many_rows(rows, kind, d):
+    """References raised in mid-stream, and scales far apart, for every number of rows per tile; a row's
+    scores grow at its own pace."""
+    ssb = _ssb()
+    B, H_kv, lens = 2, 2, [2900, 140]
+    n = max(lens)
+    cache = make_cache(ssb, B, H_kv, d, 32, n, 17)
+    g = _gen(rows)
+    K, V = torch.randn(B, H_kv, n, d, generator=g), torch.randn(B, H_kv, n, d, generator=g)
+    Q = torch.randn(B, H_kv * rows, 1, d, generator=g)
+    u = torch.sign(torch.randn(d, generator=g))
+    t = torch.arange(n).view(1, 1, n, 1) / n
+    pace = (torch.arange(H_kv * rows) % rows + 1).view(1, -1, 1, 1) / rows
+    if kind == "rising":
+        K, Q = K * 0.1 + u * t * 4, Q * 0.1 + u * 0.3 * pace
+    elif kind == "sink":
+        K, Q = K * 0.1, Q * 0.1 + u * 0.3 * pace
+        K[:, :, 0], V[:, :, 0] = 4 * u, V[:, :, 0] * 2.0 ** -6
+    else:
+        V = V * torch.exp2(torch.randint(-24, 60, (1, 1, n, 1), generator=g).float())
+    ctx = ssb.Context(B, H_kv * rows, H_kv, d, 1, 1, cache.desc.page_size * cache.desc.pages_per_req)
+    ctx.ss_kv8_write(cache, K.bfloat16().to(DEV), V.bfloat16().to(DEV))
+    Q = Q.bfloat16().to(DEV)
+    O, LSE = decode(ssb, cache, Q, lens, ctx=ctx)
+    assert ctx.last_chunk_kernel() == "kv8-tcgen05"
+    check_attention(Q, O, LSE, lambda b: history(cache, b, lens[b]), d ** -0.5)
+    ctx.close()
