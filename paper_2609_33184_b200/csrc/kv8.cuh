@@ -14,8 +14,8 @@
 // whatever the batch looks like and without the host knowing the lengths.  Where the rows of a unit take
 // several row tiles, as many CTAs side by side go through one share, a row tile each: they read the same
 // K/V at about the same time, from memory once (laid end to end as units of their own, each row tile
-// read it again: 16 x 16384 tokens with 64 rows 201 us against 186, a 320-row tree 960 against 825; 179
-// and 793 since).
+// read it again: 16 x 16384 tokens with 64 rows 201 us against 186, a 320-row tree 960 against 825;
+// today 174 and 772).
 // A unit inside one share is finished by its CTA; a unit cut by a share's end leaves one partial state
 // (m, l, a[d]) per CTA in the scratch area, and a second kernel joins them in CTA order (kv8_join.cu), so
 // results do not depend on timing.

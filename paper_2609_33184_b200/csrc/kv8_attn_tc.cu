@@ -17,16 +17,17 @@
 //    its 9 bits down to 2^-21 of the row's reference and is off by at most 2^-30 of it below, so a sink
 //    token of large weight does not swallow the 10^5 small ones whose weights add up.
 //  * the row sum adds P * 2^-ev, unrounded, in fp32 (ev in [-32, 80], see kv8.cuh).
-// The terms of P stand side by side on the N axis (one pass of the MMA over V); those of Q too for up to
-// 8 rows, and for more rows as further steps along K (the scores then take half the registers).
+// The terms of P stand side by side on the N axis (one pass of the MMA over V), and so do those of Q: as
+// further steps along K they spared additions, but K's tile was read from shared memory twice (40 rows,
+// 16 x 16384 tokens: 155 us against 149; 32 rows, 16 x 32768: 182.5 against 181).
 // M is raised lazily (exact maximum of the first tile; later only when some x exceeds 15, so P <= 2^15:
 // eight binades of room, since one raise stops all rows of the CTA; with two binades - and unscaled
 // terms, one instruction less per weight - every second tile of a 32-row round raised, 281 -> 438 us).
 //
 // A CTA walks its share of the tiles (kv8.cuh): 4 softmax warps (thread = key of the tile in the
-// scores, head dim in the output; a second set of four for 32 rows spilled, 263 against 193 us), one TMA
-// producer warp, one MMA issuer warp.  The producer runs ahead across segment ends, so a new segment
-// finds its first tiles in shared memory.  Two or three CTAs per SM hide each other's segment ends.
+// scores, head dim in the output; with a second set of four for 32 rows 64 rows took 185 us against 179),
+// one TMA producer warp, one MMA issuer warp.  The producer runs ahead across segment ends, so a new
+// segment finds its first tiles in shared memory.  Two or three CTAs per SM hide each other's segment ends.
 // Every wait is bounded; on expiry the CTA raises SS_DEV_WAIT_EXPIRED and returns.
 #include <cuda_fp8.h>
 
@@ -59,10 +60,9 @@ struct alignas(16) Ctl8 {
 template <int NR, int D>
 struct Cfg8 {
   static constexpr int kSoft = 128, kThreads = kSoft + 64; // softmax threads, all threads
-  static constexpr bool kSideBySide = NR == 8;             // Q's terms on the N axis
   static constexpr int NQ = NR == 24 ? 32 : NR;            // rows of the Q operand (N has to be a multiple of 16)
   static constexpr int kUnitBytes = kTok8 * D;             // one K or V tile
-  static constexpr int NS = kSideBySide ? 2 * NQ : NQ;     // score columns
+  static constexpr int NS = 2 * NQ;                    // score columns, hi and lo
   static constexpr int NP = (3 * NR + 15) / 16 * 16;       // weight columns
   static constexpr int kQBytes = 2 * NQ * D;
   static constexpr int kPBytes = kTok8 * NP;
@@ -318,10 +318,8 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
             if (leader) {
               const uint32_t a = k_lo + uk * (C::kUnitBytes / 16), d_s = tmem + (it & 1) * NS;
 #pragma unroll
-              for (int term = 0; term < (C::kSideBySide ? 1 : 2); ++term)
-#pragma unroll
-                for (int kk = 0; kk < D / 32; ++kk)
-                  mma8(d_s, a + kk * 2, k_hi, q_lo + term * (NQ * D / 16) + kk * 2, q_hi, idesc_qk, term > 0 || kk > 0);
+              for (int kk = 0; kk < D / 32; ++kk)
+                mma8(d_s, a + kk * 2, k_hi, q_lo + kk * 2, q_hi, idesc_qk, kk > 0);
               tc_commit(&ctl->uempty[uk]);
               tc_commit(&ctl->sfull[it & 1]);
             }
@@ -514,18 +512,24 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
         // x[r] = s2 + ev - M + bias (in the segment's first tile s2 + ev)
         float2 x[NR / 2];
         {
-          // 16 rows at a time; the factors are formed while the scores are on their way
+          // 8 rows at a time, hi and lo; the factors are formed while the scores are on their way
           const float2 kf2 = make_float2(kf, kf), ev2 = make_float2(evf, evf);
           const uint32_t t_s = tmem + lane_off + (it & 1) * NS;
-          constexpr int H = NR < 16 ? NR : 16;
           uint32_t raw[16];
-          if (C::kSideBySide || NR >= 16) tmem_ld<16>(t_s, raw);
-          else tmem_ld<8>(t_s, raw);
+          auto load = [&](int r0) {
+            if (NQ == 8) {
+              tmem_ld<16>(t_s, raw);
+            } else {
+              tmem_ld<8>(t_s + r0, raw);
+              tmem_ld<8>(t_s + NQ + r0, raw + 8);
+            }
+          };
+          load(0);
 #pragma unroll
-          for (int r0 = 0; r0 < NR; r0 += H) {
-            float2 f[H / 2], e[H / 2];
+          for (int r0 = 0; r0 < NR; r0 += 8) {
+            float2 f[4], e[4];
 #pragma unroll
-            for (int r = 0; r < H && r0 + r < NR; r += 4) {
+            for (int r = 0; r < 8; r += 4) {
               const float4 qf = *reinterpret_cast<const float4*>(&ctl->qf[r0 + r]);
               const float4 nm = *reinterpret_cast<const float4*>(&ctl->nm[r0 + r]);
               f[r / 2] = __fmul2_rn(make_float2(qf.x, qf.y), kf2);
@@ -535,13 +539,12 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
             }
             tc_wait_ld();
 #pragma unroll
-            for (int r = 0; r < H && r0 + r < NR; r += 2) {
-              float2 sc = make_float2(__uint_as_float(raw[r]), __uint_as_float(raw[r + 1]));
-              if (C::kSideBySide) sc = __fadd2_rn(sc, make_float2(__uint_as_float(raw[8 + r]), __uint_as_float(raw[8 + r + 1])));
+            for (int r = 0; r < 8; r += 2) {
+              const float2 sc = __fadd2_rn(make_float2(__uint_as_float(raw[r]), __uint_as_float(raw[r + 1])),
+                                           make_float2(__uint_as_float(raw[8 + r]), __uint_as_float(raw[9 + r])));
               x[(r0 + r) / 2] = __ffma2_rn(sc, f[r / 2], e[r / 2]);
             }
-            if (r0 + 2 * H <= NR) tmem_ld<16>(t_s + r0 + H, raw);
-            else if (r0 + H < NR) tmem_ld<8>(t_s + r0 + H, raw);
+            if (r0 + 8 < NR) load(r0 + 8);
           }
         }
         if (n_valid < kTok8) {
@@ -596,45 +599,34 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
             if (!first) lsum[r] = __fmul2_rn(lsum[r], make_float2(ex2_ftz(-up.x), ex2_ftz(-up.y)));
           }
         }
-        if (!first) wait(&ctl->pfree, (it - 1) & 1);  // P^T has been consumed
         {
+          // columns term * NR + row, 16 to a 16-byte piece per key, in words of 4; nothing behind them.
+          // All are formed before the wait: the output MMAs of the tile before run meanwhile (16 rows at
+          // a time behind it: 64 rows, 16 x 16384 tokens, 178 us against 174).
           const float2 vinv2 = make_float2(vinv, vinv);
-          // columns term * NR + row, 16 to a 16-byte piece per key, in words of 4
-          auto weights = [&](int r, uint32_t& hi, uint32_t& mid, uint32_t& lo) {
+          constexpr int W = NR / 4;
+          uint32_t word[NP / 4] = {};
+#pragma unroll
+          for (int q = 0; q < W; ++q) {
             uint32_t w[2];
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-              const int i = r / 2 + k;
+              const int i = 2 * q + k;
               const float2 e = make_float2(ex2_ftz(x[i].x), ex2_ftz(x[i].y));
               lsum[i] = __ffma2_rn(e, vinv2, lsum[i]);
               w[k] = h2_bits(__float22half2_rn(e));
             }
             const uint32_t a1 = residue(w[0]), b1 = residue(w[1]);
-            hi = __byte_perm(w[0], w[1], 0x7531);
-            mid = __byte_perm(a1, b1, 0x7531);
+            word[q] = __byte_perm(w[0], w[1], 0x7531);
+            word[W + q] = __byte_perm(a1, b1, 0x7531);
             // (the last term rounds)
-            lo = __byte_perm(residue(a1) + 0x00800080u, residue(b1) + 0x00800080u, 0x7531);
-          };
-          auto put = [&](int piece, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
-            *reinterpret_cast<uint4*>(p_s + piece * (kTok8 * 16) + key * 16) = make_uint4(a, b, c, d);
-          };
-          if (NR % 16 == 0) {
-#pragma unroll
-            for (int r = 0; r < NR; r += 16) {
-              uint32_t t[3][4];
-#pragma unroll
-              for (int q = 0; q < 4; ++q) weights((r + 4 * q) % NR, t[0][q], t[1][q], t[2][q]);
-#pragma unroll
-              for (int k = 0; k < 3; ++k) put((k * NR + r) / 16, t[k][0], t[k][1], t[k][2], t[k][3]);
-            }
-          } else {  // the terms share pieces; what is behind them is nothing
-            constexpr int W = NR / 4;
-            uint32_t t[NP / 4] = {};
-#pragma unroll
-            for (int q = 0; q < W; ++q) weights(4 * q, t[q], t[W + q], t[2 * W + q]);
-#pragma unroll
-            for (int k = 0; k < NP / 16; ++k) put(k, t[4 * k], t[4 * k + 1], t[4 * k + 2], t[4 * k + 3]);
+            word[2 * W + q] = __byte_perm(residue(a1) + 0x00800080u, residue(b1) + 0x00800080u, 0x7531);
           }
+          if (!first) wait(&ctl->pfree, (it - 1) & 1);  // P^T has been consumed
+#pragma unroll
+          for (int k = 0; k < NP / 16; ++k)
+            *reinterpret_cast<uint4*>(p_s + k * (kTok8 * 16) + key * 16) =
+                make_uint4(word[4 * k], word[4 * k + 1], word[4 * k + 2], word[4 * k + 3]);
           fence_proxy_async();
           tc_fence_before();
         }
@@ -732,6 +724,7 @@ cudaError_t launch8(const Attn8Params& p, const CUtensorMap& tmK, const CUtensor
 }
 template <int D>
 cudaError_t launch_rows(const Attn8Params& p, const CUtensorMap& tmK, const CUtensorMap& tmV, cudaStream_t s, bool pdl) {
+  // (24 rows as 32: 247 us against 242 for 8 x 98304 tokens; 40 rows as 2 x 32 against 2 x 24: 172 and 155)
   if (p.rows_per_tile <= 8) return launch8<8, D>(p, tmK, tmV, s, pdl);
   if (p.rows_per_tile <= 16) return launch8<16, D>(p, tmK, tmV, s, pdl);
   if (p.rows_per_tile <= 24) return launch8<24, D>(p, tmK, tmV, s, pdl);
