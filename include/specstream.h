@@ -285,7 +285,8 @@ ss_status ss_commit_gather(ss_ctx* ctx, ss_tensor K_loc, ss_tensor V_loc, int32_
  * least -32 and at most 80, a value is code * 2^e, and its code is x * 2^-e rounded to e4m3
  * (nearest even; infinities and what exceeds 448 * 2^80 saturate, NaN stays NaN).  So a value is
  * off by at most 2^-4 of itself or 2^-10 * 2^e, whichever is more, and a row read back and written
- * again keeps its values.
+ * again keeps its values.  A scale byte below 95 or above 207 counts as 95 or 207, so visible tokens of
+ * a zeroed buffer are rows of zeros (score 0, value 0) as those written as zeros are.
  *
  * ss_cache8 describes a cache.  Paged (page_table not NULL): K, V are pools [n_pages, H_kv,
  * page_size, d] of codes, K_scale, V_scale [n_pages, H_kv, page_size] of bytes (stride_b = page

@@ -2,7 +2,7 @@
 
 A row is d codes in e4m3 (sign, 4 exponent bits with bias 7, 3 fraction bits, no infinities, 0x7f and
 0xff are NaN) and one byte e + 127: a value is code * 2^e.  e is the smallest integer in [-32, 80] with
-max|x| <= 448 * 2^e over the row's finite values.
+max|x| <= 448 * 2^e over the row's finite values; a byte outside [95, 207] counts as the nearer end.
 """
 import numpy as np
 
@@ -46,7 +46,7 @@ def encode_row(row):
 
 def decode(codes, byte):
     """codes [.., d], byte [..] -> fp64 values."""
-    return VALUES[codes] * np.exp2(np.asarray(byte, dtype=np.float64) - 127.0)[..., None]
+    return VALUES[codes] * np.exp2(np.clip(np.asarray(byte, dtype=np.float64), 95.0, 207.0) - 127.0)[..., None]
 
 
 def attention(q, K, V, scale):

@@ -318,10 +318,11 @@ class Cache8:
     @classmethod
     def empty(cls, outer: int, H_kv: int, tokens: int, d: int, page_table: Optional[torch.Tensor] = None,
               device="cuda:0") -> "Cache8":
-        """A cache of zeros: `outer` pages of `tokens` tokens, or `outer` requests with room for them."""
-        z = lambda *shape: torch.zeros(shape, dtype=torch.uint8, device=device)
+        """A cache of rows of zeros as ss_kv8_write writes them: `outer` pages of `tokens` tokens, or `outer` requests
+        with room for them."""
+        fill = lambda value, *shape: torch.full(shape, value, dtype=torch.uint8, device=device)
         s = (outer, H_kv, tokens)
-        return cls(z(*s, d), z(*s, d), z(*s), z(*s), page_table)
+        return cls(fill(0, *s, d), fill(0, *s, d), fill(95, *s), fill(95, *s), page_table)   # 95: e = -32
 
 
 class Context:

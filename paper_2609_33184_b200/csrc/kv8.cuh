@@ -6,7 +6,8 @@
 // rounding is that to e4m3 (half a step: 2^-4 of the value, or 2^-10 * 2^e for the smallest);
 // since e4m3 is a float format nothing is lost by not using the exact maximum.  The range of e
 // keeps the ratio of two scales below 2^112, so that sums of weights and of weights times scales
-// stay in fp32's range under one reference.
+// stay in fp32's range under one reference.  A byte outside it (a buffer that nobody wrote) counts as the
+// nearer end: taken as it is, a row of zeros with byte 0 would enter a row sum with the factor 2^127.
 //
 // Sharing out.  A unit is one (request, kv-head); its history is cut into tiles of kTok8 tokens.  The
 // tiles of all units laid end to end (request by request, lengths read on the device) are given to the
@@ -94,6 +95,7 @@ cudaError_t attn8_tc_prepare();  // one-time function attributes
 // ---- device side ---------------------------------------------------------------------------
 __device__ __forceinline__ float pow2_8(int e) { return __int_as_float((e + 127) << 23); }  // |e| <= 126
 __device__ __forceinline__ float scale8(uint32_t byte) { return __int_as_float((int)(byte << 23)); }  // 2^(byte - 127)
+__device__ __forceinline__ uint32_t byte8(uint32_t byte) { return min(max(byte, (uint32_t)(kMinExp8 + 127)), (uint32_t)(kMaxExp8 + 127)); }
 
 // Length of a request in tokens, clamped to [0, room] (find_share8 reports one outside).
 __device__ __forceinline__ int len8(const Attn8Params& p, int b) {

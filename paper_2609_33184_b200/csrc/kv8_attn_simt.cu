@@ -94,8 +94,8 @@ __global__ void __launch_bounds__(128) attn8_simt_kernel(const __grid_constant__
         }
         const uint8_t ek = p.kv.Ks[outer * p.kv.ks_sb + g.kvh * p.kv.ks_sh + inner * p.kv.ks_st];
         const uint8_t ev = p.kv.Vs[outer * p.kv.vs_sb + g.kvh * p.kv.vs_sh + inner * p.kv.vs_st];
-        const float ks = scale8(ek) * p.scale_log2;
-        vs = scale8(ev);
+        const float ks = scale8(byte8(ek)) * p.scale_log2;
+        vs = scale8(byte8(ev));
 #pragma unroll
         for (int r = 0; r < kRT; ++r) s[r] *= ks;
       }

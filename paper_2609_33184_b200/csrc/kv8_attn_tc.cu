@@ -494,7 +494,9 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
 #pragma unroll
       for (int r = 0; r < NR / 2; ++r) lsum[r] = make_float2(0.f, 0.f);
       for (int t = t0; t < t1; ++t, ++it) {
-        const float kf = scale8(ah_ek), evf = (float)(int)ah_ev - 127.f, vinv = scale8(254u - ah_ev);
+        // (put into the format's range here, not where they are loaded: that would wait for them)
+        const uint32_t ek = byte8(ah_ek), ev = byte8(ah_ev);
+        const float kf = scale8(ek), evf = (float)(int)ev - 127.f, vinv = scale8(254u - ev);
         ah_fetch();
         ah_look(t + 2, t1, len, b);
         const int n_valid = min(kTok8, len - t * kTok8);

@@ -224,7 +224,8 @@ __global__ void __launch_bounds__(kThreads) read8_kernel(const __grid_constant__
 #pragma unroll
   for (int u = 0; u < U; ++u) {
     if (!to[u]) continue;
-    const float2 scale = make_float2(scale8(sc[u]), scale8(sc[u]));
+    const float one_scale = scale8(byte8(sc[u]));
+    const float2 scale = make_float2(one_scale, one_scale);
     const uint32_t x[4] = {raw[u][0].x, raw[u][0].y, raw[u][1].x, raw[u][1].y};
     uint32_t o[8];
 #pragma unroll

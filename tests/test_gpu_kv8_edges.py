@@ -1,0 +1,103 @@
+"""The 8-bit KV cache on the GPU where its inputs leave the ordinary: rows that nobody wrote, scale bytes outside the
+format."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import kv8
+from tests.test_gpu_kv8 import DEV, _gen, _ssb, check_attention, decode, history, make_cache, slots
+
+pytestmark = pytest.mark.gpu
+
+
+def whole_round(ctx, cache, Q, vl, scale, K_loc, V_loc):
+    O = torch.full(Q.shape, float("nan"), dtype=torch.bfloat16, device=DEV)
+    LSE = torch.full(Q.shape[:3], float("nan"), device=DEV)
+    ctx.ss_verify_begin(Q, scale)
+    ctx.ss_verify_chunk8(cache, vl)
+    ctx.ss_verify_local(K_loc, V_loc)
+    ctx.ss_verify_finalize(O, LSE)
+    assert ctx.ss_poll_status() == (0, 0)
+    return O, LSE
+
+
+@pytest.mark.parametrize("flags", [0, 1], ids=["auto", "simt"])
+@pytest.mark.parametrize("fill", ["empty", "zeros"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_visible_tokens_that_were_never_written(d, fill, flags):
+    """They are rows of zeros: score 0, value 0, in the row sum with weight e^0.  One request with none written, one with
+    a few, whose scores differ from 0 by several binades, and long enough to be cut."""
+    ssb = _ssb()
+    B, H_q, H_kv, T, page, lens = 3, 8, 2, 2, 16, [300, 2000, 1]
+    per = 128
+    cache = ssb.Cache8.empty(B * per, H_kv, page, d,
+                             torch.randperm(B * per, generator=_gen(1)).to(torch.int32).view(B, per).to(DEV))
+    if fill == "zeros":                        # a user's own buffers
+        for t in cache.tensors[2:4]:
+            t.zero_()
+    g = _gen(d)
+    K, V = (torch.randn(B, H_kv, 70, d, generator=g).bfloat16().to(DEV) for _ in range(2))
+    Q = torch.randn(B, H_q, T, d, generator=g).bfloat16().to(DEV)
+    K_loc, V_loc = (torch.randn(B, H_kv, T, d, generator=g).bfloat16().to(DEV) for _ in range(2))
+    scale = 4 * d ** -0.5                       # scores of the written tokens up to about 16
+    ctx = ssb.Context(B, H_q, H_kv, d, T, T, per * page, flags=flags)
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device=DEV)
+    ctx.ss_kv8_write(cache, K, V, i32(0, 777, 0), i32(0, 70, 0))
+    written = (torch.zeros(B, H_kv, 70, d, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    Kr, Vr = written
+    ctx.ss_kv8_read(cache, Kr, Vr, i32(0, 777, 0), i32(70, 70, 70))
+    assert (Kr[0] == 0).all() and (Vr[2] == 0).all()
+
+    def kv(b):
+        k, v = np.zeros((2, H_kv, lens[b], d))
+        if b == 1:
+            k[:, 777:847], v[:, 777:847] = Kr[1].double().cpu().numpy(), Vr[1].double().cpu().numpy()
+        return k, v
+    O, LSE = decode(ssb, cache, Q, lens, scale=scale, ctx=ctx)
+    assert ctx.last_chunk_kernel() == ("kv8-simt" if flags else "kv8-tcgen05")
+    check_attention(Q, O, LSE, kv, scale)
+    assert (O[0] == 0).all()
+    O, LSE = whole_round(ctx, cache, Q, i32(*lens), scale, K_loc, V_loc)
+    f = lambda t, b, n: t[b, :, :n].double().cpu().numpy()
+    for i in range(T):
+        near = lambda b: (np.concatenate([kv(b)[0], f(K_loc, b, i + 1)], 1), np.concatenate([kv(b)[1], f(V_loc, b, i + 1)], 1))
+        check_attention(Q[:, :, i:i + 1], O[:, :, i:i + 1], LSE[:, :, i:i + 1], near, scale)
+    ctx.close()
+
+
+@pytest.mark.parametrize("flags", [0, 1], ids=["auto", "simt"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_scale_bytes_outside_the_format_count_as_its_ends(d, flags):
+    """Bytes below 95 as 95, above 207 as 207, in attention and in reading back."""
+    ssb = _ssb()
+    B, H_q, H_kv, n = 2, 8, 2, 700
+    cache = make_cache(ssb, B, H_kv, d, 32, n, 9)
+    K, V, Ks, Vs, _ = cache.tensors
+    pick = lambda shape, bytes_, seed: torch.tensor(bytes_, dtype=torch.uint8)[
+        torch.randint(0, len(bytes_), shape, generator=_gen(seed))].to(DEV)
+    Ks.copy_(pick(Ks.shape, [0, 1, 94, 95, 118, 119], 1))
+    Vs.copy_(pick(Vs.shape, [0, 94, 95, 120, 200, 206, 207, 208, 254, 255], 2))
+
+    def clamped(b):
+        out = []
+        for k in (0, 1):
+            o, i = slots(cache, b, np.arange(n))
+            byte = np.clip(cache.tensors[2 + k].cpu().numpy()[o, :, i], 95, 207)
+            codes = cache.tensors[k].cpu().numpy()[o, :, i]
+            out.append((kv8.VALUES[codes] * np.exp2(byte.astype(np.float64) - 127.0)[..., None]).transpose(1, 0, 2))
+        return out
+    Q = torch.randn(B, H_q, 1, d, generator=_gen(3)).bfloat16().to(DEV)
+    ctx = ssb.Context(B, H_q, H_kv, d, 1, 1, 1024, flags=flags)
+    Kr, Vr = (torch.empty(B, H_kv, n, d, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    ctx.ss_kv8_read(cache, Vr, Kr)
+    ctx.ss_kv8_read(cache, Kr, Vr)
+    for b in range(B):
+        k, v = clamped(b)
+        assert np.array_equal(Kr[b].double().cpu().numpy(), k) and np.array_equal(Vr[b].double().cpu().numpy(), v)
+        hk, hv = history(cache, b, n)           # and so the oracle reads them
+        assert np.array_equal(hk, k) and np.array_equal(hv, v)
+    O, LSE = decode(ssb, cache, Q, [n, 130], ctx=ctx)
+    check_attention(Q, O, LSE, lambda b: [x[:, :[n, 130][b]] for x in clamped(b)], d ** -0.5)
+    ctx.close()
