@@ -324,7 +324,8 @@ ss_status ss_kv8_write(ss_ctx* ctx, const ss_cache8* cache, ss_tensor K, ss_tens
  * k < row_cnt[b]; rows from row_cnt[b] on are left as they are.  src_off NULL = 0, row_cnt NULL = T.
  * Exact: every value of the cache is a bf16 value.  A count outside [0, T] is clamped and a token
  * outside the request's room skipped (SS_DEV_BAD_VALID_LEN); tokens of a page id outside the pool
- * read as zeros (SS_DEV_BAD_PAGE).  Independent of the round state. */
+ * read as zeros (SS_DEV_BAD_PAGE).  Independent of the round state; inside an open round the rows may be
+ * the K/V of the very next chunk or local call, also under SS_FLAG_OVERLAP_CHUNKS. */
 ss_status ss_kv8_read(ss_ctx* ctx, const ss_cache8* cache, ss_tensor K, ss_tensor V, int32_t B, int32_t T,
                       const int32_t* src_off, const int32_t* row_cnt, void* stream);
 

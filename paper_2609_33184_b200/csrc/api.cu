@@ -1314,6 +1314,9 @@ static ss_status copy8(ss_ctx* c, bool write, const ss_cache8* cache, ss_tensor 
     e = write ? ss::launch_kv8_write(p, (cudaStream_t)stream, true) : ss::launch_kv8_read(p, (cudaStream_t)stream, true);
   if (e != cudaSuccess) return cuda_fail(c, e);
   ++c->launches;
+  // The read lets its successor start before its rows are stored, and a chunk or local kernel in the middle of a
+  // round loads K and V without waiting: the next one has to, it may take these rows.
+  if (!write && c->state == ss_ctx::OPEN) c->first_launch = true;
   return SS_OK;
 }
 

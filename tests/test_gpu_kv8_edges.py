@@ -101,3 +101,49 @@ def test_scale_bytes_outside_the_format_count_as_its_ends(d, flags):
     O, LSE = decode(ssb, cache, Q, [n, 130], ctx=ctx)
     check_attention(Q, O, LSE, lambda b: [x[:, :[n, 130][b]] for x in clamped(b)], d ** -0.5)
     ctx.close()
+
+
+@pytest.mark.parametrize("first", ["chunk8", "chunk"])
+def test_rows_read_back_inside_a_round_are_the_next_call_s_history(first):
+    """Under overlapped launches: a chunk of any kind, ss_kv8_read into a buffer, that buffer as the next chunk, another
+    read, its rows as the local segment."""
+    ssb = _ssb()
+    B, H_q, H_kv, d, T, n, T_loc = 8, 16, 8, 128, 4, 4096, 512
+    small, big = (make_cache(ssb, B, H_kv, d, page, room, seed) for page, room, seed in ((16, 256, 1), (64, n, 2)))
+    g = _gen(7)
+    Q = torch.randn(B, H_q, T, d, generator=g).bfloat16().to(DEV)
+    K0, V0 = (torch.randn(B, H_kv, 256, d, generator=g).bfloat16().to(DEV) for _ in range(2))
+    K, V = (torch.empty(B, H_kv, n, d, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    Kl, Vl = (torch.empty(B, H_kv, T_loc, d, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    off = torch.full((B,), n - T_loc, dtype=torch.int32, device=DEV)
+    O, LSE = torch.empty_like(Q), torch.empty(B, H_q, T, device=DEV)
+    ctx = ssb.Context(B, H_q, H_kv, d, T, T_loc, n, flags=ssb.SS_FLAG_OVERLAP_CHUNKS)
+    results = []
+    for _ in range(20):
+        for t in (K, V, Kl, Vl):
+            t.zero_()
+        ctx.ss_verify_begin(Q, d ** -0.5)
+        if first == "chunk8":
+            ctx.ss_verify_chunk8(small)
+        else:
+            ctx.ss_verify_chunk(K0, V0)
+        ctx.ss_kv8_read(big, K, V)
+        ctx.ss_verify_chunk(K, V)
+        ctx.ss_kv8_read(big, Kl, Vl, src_off=off)
+        ctx.ss_verify_local(Kl, Vl)
+        ctx.ss_verify_finalize(O, LSE)
+        results.append((O.clone(), LSE.clone()))
+    assert ctx.ss_poll_status() == (0, 0)
+    f = lambda t, b: t[b].double().cpu().numpy()
+
+    def kv(b, i):
+        k, v = history(big, b, n)
+        a = history(small, b, 256) if first == "chunk8" else [f(K0, b), f(V0, b)]
+        seen = slice(n - T_loc, n - T + i + 1)
+        return np.concatenate([a[0], k, k[:, seen]], 1), np.concatenate([a[1], v, v[:, seen]], 1)
+    for i in range(0, T, 3):
+        check_attention(Q[:1, :, i:i + 1], results[0][0][:1, :, i:i + 1], results[0][1][:1, :, i:i + 1], lambda b: kv(b, i),
+                        d ** -0.5)
+    for o, l in results[1:]:
+        assert torch.equal(o, results[0][0]) and torch.equal(l, results[0][1])
+    ctx.close()
