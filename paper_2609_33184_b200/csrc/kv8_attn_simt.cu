@@ -52,6 +52,8 @@ __global__ void __launch_bounds__(128) attn8_simt_kernel(const __grid_constant__
       if (r < g.nrows) {
         const int rg = g.row0 + r, h = g.kvh * p.G + rg / p.T_q, t = rg % p.T_q;
         v = __bfloat162float(p.Q[g.b * p.q_sb + h * p.q_sh + t * p.q_st + c]);
+        // (an infinite query too makes its scores NaN, whatever the signs of its products)
+        if (!(fabsf(v) < INFINITY)) v = __int_as_float(0x7fffffff);
       }
       q_s[r][c] = v;
     }
@@ -76,11 +78,12 @@ __global__ void __launch_bounds__(128) attn8_simt_kernel(const __grid_constant__
       float s[kRT], vs = 0.f;
 #pragma unroll
       for (int r = 0; r < kRT; ++r) s[r] = 0.f;
-      if (outer >= 0) {
+      if (ok) {  // (a page outside the pool is zeros: 0 * q, NaN where the query is)
         const uint8_t* k = p.kv.K + outer * p.kv.k_sb + g.kvh * p.kv.k_sh + inner * p.kv.k_st;
 #pragma unroll 2
         for (int c16 = 0; c16 < D; c16 += 16) {
-          const uint4 raw = *reinterpret_cast<const uint4*>(k + c16);
+          uint4 raw = make_uint4(0, 0, 0, 0);
+          if (outer >= 0) raw = *reinterpret_cast<const uint4*>(k + c16);
           const uint32_t w4[4] = {raw.x, raw.y, raw.z, raw.w};
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
@@ -92,8 +95,11 @@ __global__ void __launch_bounds__(128) attn8_simt_kernel(const __grid_constant__
             }
           }
         }
-        const uint8_t ek = p.kv.Ks[outer * p.kv.ks_sb + g.kvh * p.kv.ks_sh + inner * p.kv.ks_st];
-        const uint8_t ev = p.kv.Vs[outer * p.kv.vs_sb + g.kvh * p.kv.vs_sh + inner * p.kv.vs_st];
+        uint32_t ek = 127, ev = 127;
+        if (outer >= 0) {
+          ek = p.kv.Ks[outer * p.kv.ks_sb + g.kvh * p.kv.ks_sh + inner * p.kv.ks_st];
+          ev = p.kv.Vs[outer * p.kv.vs_sb + g.kvh * p.kv.vs_sh + inner * p.kv.vs_st];
+        }
         const float ks = scale8(byte8(ek)) * p.scale_log2;
         vs = scale8(byte8(ev));
 #pragma unroll

@@ -147,3 +147,35 @@ def test_rows_read_back_inside_a_round_are_the_next_call_s_history(first):
     for o, l in results[1:]:
         assert torch.equal(o, results[0][0]) and torch.equal(l, results[0][1])
     ctx.close()
+
+
+@pytest.mark.parametrize("page,kernel", [(24, "kv8-simt"), (16, "kv8-tcgen05")])
+@pytest.mark.parametrize("value", ["inf", "-inf", "nan"])
+def test_a_query_that_is_not_finite_makes_its_row_nan_on_both_kernels(page, kernel, value):
+    """Also where every product with it has the same sign, so that all scores would be -inf or all inf."""
+    ssb = _ssb()
+    B, H_q, H_kv, d, T, n = 1, 4, 2, 64, 2, 500
+    cache = make_cache(ssb, B, H_kv, d, page, n, 3)
+    K = cache.tensors[0]
+    K[..., 7] = (K[..., 7] & 0x7F) | 0x08       # positive, not zero (and no NaN: make_cache has none)
+    K[..., 7] = torch.where(K[..., 7] == 0x7F, torch.full_like(K[..., 7], 0x30), K[..., 7])
+    Q = torch.randn(B, H_q, T, d, generator=_gen(1)).bfloat16().to(DEV)
+    bad = Q.clone()
+    bad[0, 1, 0, 7], bad[0, 2, 1, 7] = float(value), float(value)
+    hit = torch.zeros(B, H_q, T, dtype=torch.bool, device=DEV)
+    hit[0, 1, 0] = hit[0, 2, 1] = True
+    ctx = ssb.Context(B, H_q, H_kv, d, T, T, 1024)
+    good, gl = decode(ssb, cache, Q, [n], ctx=ctx)
+    O, LSE = decode(ssb, cache, bad, [n], ctx=ctx)
+    assert ctx.last_chunk_kernel() == kernel
+    assert torch.isnan(O[hit]).all() and torch.isnan(LSE[hit]).all()
+    assert torch.equal(O[~hit], good[~hit]) and torch.equal(LSE[~hit], gl[~hit])
+    if page == 24:                              # with every page outside the pool the row is NaN all the same
+        table = cache.tensors[4].clone()
+        cache.tensors[4].fill_(-1)
+        vl = torch.tensor([n], dtype=torch.int32, device=DEV)
+        ctx.ss_decode8(bad, d ** -0.5, cache, vl, O, LSE)
+        assert ctx.ss_poll_status() == (ssb.SS_ERR_DEVICE_FLAG, ssb.SS_DEV_BAD_PAGE)
+        assert torch.isnan(O[hit]).all() and torch.isnan(LSE[hit]).all() and (O[~hit] == 0).all()
+        cache.tensors[4].copy_(table)
+    ctx.close()
