@@ -253,7 +253,8 @@ __device__ __forceinline__ bool seg_next8(const Attn8Params& p, const Share8& s,
   return true;
 }
 
-// Where a finished row goes: O and LSE, or a partial state.  `m` in the base-2 domain.
+// Where a finished row goes: O and LSE, or a partial state.  `m` in the base-2 domain.  The state of a row that is
+// NaN keeps a finite reference, 0: merges take the maximum of the references and drop states at -inf.
 __device__ __forceinline__ void put_ml8(const Attn8Params& p, const Seg8& g, int r, float m, float l) {
   const bool some = l > 0.f || l != l;
   if (p.O) {
@@ -261,7 +262,7 @@ __device__ __forceinline__ void put_ml8(const Attn8Params& p, const Seg8& g, int
       p.LSE[((int64_t)g.b * p.H_kv + g.kvh) * p.R + g.row0 + r] =
           some ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
   } else {
-    p.part_ml[((int64_t)g.b * p.H_kv + g.kvh) * p.R_stride + g.row0 + r] = make_float2(some ? m : -INFINITY, l);
+    p.part_ml[((int64_t)g.b * p.H_kv + g.kvh) * p.R_stride + g.row0 + r] = make_float2(l != l ? 0.f : some ? m : -INFINITY, l);
   }
 }
 __device__ __forceinline__ void put_a8(const Attn8Params& p, const Seg8& g, int r, int c, float l, float a) {

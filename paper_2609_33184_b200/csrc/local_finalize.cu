@@ -288,8 +288,9 @@ __global__ void __launch_bounds__(kWarpsPerCta * 32) merge_kernel(const MergePar
     }
     L = warp_sum(L);
   }
+  const bool some = L > 0.f || L != L;  // (a NaN in a visible key or in the query has to show)
   if (MODE == 2) {
-    if (lane == 0) p.fold_ml[row_id] = make_float2(L > 0.f ? M : -INFINITY, L);
+    if (lane == 0) p.fold_ml[row_id] = make_float2(some ? M : -INFINITY, L);
     float* out = p.fold_a + row_id * D + lane * CPL;
     if (CPL == 4)
       *reinterpret_cast<float4*>(out) = make_float4(acc[0], acc[1], acc[CPL - 2], acc[CPL - 1]);
@@ -297,14 +298,14 @@ __global__ void __launch_bounds__(kWarpsPerCta * 32) merge_kernel(const MergePar
       *reinterpret_cast<float2*>(out) = make_float2(acc[0], acc[1]);
   } else if (FOLD) {
     const size_t idx = slot0 * p.R_stride + r;
-    if (lane == 0) p.fold_ml[idx] = make_float2(L > 0.f ? M : -INFINITY, L);
+    if (lane == 0) p.fold_ml[idx] = make_float2(some ? M : -INFINITY, L);
     float* out = p.fold_a + idx * D + lane * CPL;
     if (CPL == 4)
       *reinterpret_cast<float4*>(out) = make_float4(acc[0], acc[1], acc[CPL - 2], acc[CPL - 1]);
     else
       *reinterpret_cast<float2*>(out) = make_float2(acc[0], acc[1]);
   } else {
-    const float inv = (L > 0.f) ? 1.f / L : 0.f;
+    const float inv = some ? 1.f / L : 0.f;
     __nv_bfloat16* o = p.O + row_id * D + lane * CPL;
     if (CPL == 4) {
       __nv_bfloat162 lo = __floats2bfloat162_rn(acc[0] * inv, acc[1] * inv);
@@ -317,7 +318,7 @@ __global__ void __launch_bounds__(kWarpsPerCta * 32) merge_kernel(const MergePar
       *reinterpret_cast<__nv_bfloat162*>(o) = __floats2bfloat162_rn(acc[0] * inv, acc[1] * inv);
     }
     if (p.LSE && lane == 0)
-      p.LSE[row_id] = (L > 0.f) ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
+      p.LSE[row_id] = some ? (M + log2f(L)) * 0.6931471805599453f : -INFINITY;
   }
 }
 

@@ -179,3 +179,57 @@ def test_a_query_that_is_not_finite_makes_its_row_nan_on_both_kernels(page, kern
         assert torch.isnan(O[hit]).all() and torch.isnan(LSE[hit]).all() and (O[~hit] == 0).all()
         cache.tensors[4].copy_(table)
     ctx.close()
+
+
+@pytest.mark.parametrize("what", ["two", "bf16", "fold", "export", "one"])
+@pytest.mark.parametrize("page", [16, 24])
+def test_nan_rows_pass_through_every_merge(what, page):
+    """A row made NaN by its query or by a NaN in a visible key stays NaN, O and LSE, whatever its states are
+    merged with and on whichever path; the other rows come out as without it."""
+    ssb = _ssb()
+    B, H_q, H_kv, d, T, lens = 2, 8, 2, 128, 3, [900, 140]
+    caches = [make_cache(ssb, B, H_kv, d, page, 912, 4 + k) for k in range(2)]
+    g = _gen(2)
+    rnd = lambda *s: torch.randn(s, generator=g).bfloat16().to(DEV)
+    Q, K, V, K_loc, V_loc = rnd(B, H_q, T, d), rnd(B, H_kv, 128, d), rnd(B, H_kv, 128, d), rnd(B, H_kv, T, d), rnd(B, H_kv, T, d)
+    vl = torch.tensor(lens, dtype=torch.int32, device=DEV)
+    ctx = ssb.Context(B, H_q, H_kv, d, T, T, 1024, max_chunks=2 if what == "fold" else 8)
+
+    def run(Q):
+        O, LSE = torch.empty_like(Q), torch.empty(B, H_q, T, device=DEV)
+        ctx.ss_verify_begin(Q, d ** -0.5)
+        ctx.ss_verify_chunk8(caches[0], vl)
+        if what in ("two", "fold"):
+            for k in (1, 0, 1):
+                ctx.ss_verify_chunk8(caches[k], vl)
+        elif what == "bf16":
+            ctx.ss_verify_chunk(K, V)
+        elif what == "export":
+            ml, a = torch.empty(B * H_q * T, 2, device=DEV), torch.empty(B * H_q * T, d, device=DEV)
+            ctx.ss_verify_export_state(ml, a)
+            ctx.ss_verify_abort()
+            ctx.ss_verify_begin(Q, d ** -0.5)
+            ctx.ss_verify_import_state(ml, a)
+        ctx.ss_verify_local(K_loc, V_loc)
+        ctx.ss_verify_finalize(O, LSE)
+        assert ctx.ss_poll_status() == (0, 0)
+        return O, LSE
+    good, gl = run(Q)
+    assert torch.isfinite(good).all() and torch.isfinite(gl).all()
+    bad = Q.clone()
+    hit = torch.zeros(B, H_q, T, dtype=torch.bool, device=DEV)
+    for i, (b, h, t) in enumerate([(0, 1, 0), (0, 6, 2), (1, 7, 1), (1, 0, 0)]):
+        bad[b, h, t, 5 * i] = [float("nan"), float("inf"), float("-inf"), float("nan")][i]
+        hit[b, h, t] = True
+    O, LSE = run(bad)
+    assert torch.isnan(O[hit]).all() and torch.isnan(LSE[hit]).all()
+    assert torch.equal(O[~hit], good[~hit]) and torch.equal(LSE[~hit], gl[~hit])
+    # one NaN code in a key of the second request's second head: all rows of that head
+    o, i = slots(caches[0], 1, [77])
+    caches[0].tensors[0][int(o[0]), 1, int(i[0]), 9] = 0x7F
+    O, LSE = run(Q)
+    hit.zero_()
+    hit[1, 4:] = True
+    assert torch.isnan(O[hit]).all() and torch.isnan(LSE[hit]).all()
+    assert torch.equal(O[~hit], good[~hit]) and torch.equal(LSE[~hit], gl[~hit])
+    ctx.close()
