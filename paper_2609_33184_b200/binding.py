@@ -298,7 +298,7 @@ class Cache8:
     def __init__(self, K: torch.Tensor, V: torch.Tensor, K_scale: torch.Tensor, V_scale: torch.Tensor,
                  page_table: Optional[torch.Tensor] = None):
         for t in (K, V):
-            assert t.dim() == 4 and t.element_size() == 1 and t.stride(3) == 1, (t.shape, t.dtype, t.stride())
+            assert t.dtype in (torch.uint8, torch.float8_e4m3fn) and t.dim() == 4 and t.stride(3) == 1, (t.shape, t.dtype, t.stride())
         for t in (K_scale, V_scale):
             assert t.dtype == torch.uint8 and t.shape == K.shape[:3], (t.shape, t.dtype)
         assert V.shape == K.shape

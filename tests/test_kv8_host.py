@@ -1,4 +1,5 @@
 """Host-only checks of the 8-bit cache's description."""
+import pytest
 import torch
 
 from oracle import kv8
@@ -18,3 +19,15 @@ def test_an_empty_cache_holds_rows_of_zeros_in_the_format():
 def test_scale_bytes_outside_the_format_count_as_its_ends():
     for byte, e in ((0, -32), (94, -32), (95, -32), (127, 0), (207, 80), (208, 80), (255, 80)):
         assert kv8.decode([0x38], byte)[0] == 2.0 ** e   # code 1.0
+
+
+@pytest.mark.parametrize("dtype", [torch.float8_e5m2, torch.int8, torch.bool])
+def test_codes_of_another_type_are_refused(dtype):
+    """Buffers of one byte per element that do not hold e4m3 codes."""
+    good = ssb.Cache8.empty(2, 1, 8, 64, device="cpu").tensors
+    for bad in (0, 1):
+        t = list(good[:4])
+        t[bad] = t[bad].to(torch.bool) if dtype is torch.bool else t[bad].view(dtype)
+        with pytest.raises(AssertionError):
+            ssb.Cache8(*t)
+    ssb.Cache8(good[0].view(torch.float8_e4m3fn), good[1], good[2], good[3])
