@@ -159,10 +159,11 @@ Layout layout_for(const ss_config* c) {
   L.off_ml = L.off_hist + kHistSlots * 2 * ss::kMaxHistChunks * sizeof(CUtensorMap);  // lists of tensor maps
   L.off_a = align_up(L.off_ml + (size_t)sets * rows * sizeof(float2), 256);
   L.off_scratch8 = align_up(L.off_a + (size_t)sets * rows * c->d * sizeof(float), 256);
-  const size_t rows8 = L.R_stride < ss::kRows8 ? L.R_stride : ss::kRows8;
-  const size_t few8 = L.R_stride < ss::kFew8 ? L.R_stride : ss::kFew8;
-  const size_t slots8 = 2 * (ss::kCtas8 * rows8 > ss::kCtasFew8 * few8 ? ss::kCtas8 * rows8 : ss::kCtasFew8 * few8);
-  L.off_plan8 = align_up(L.off_scratch8 + slots8 * (c->d + 4) * sizeof(float), 256);
+  // 8-bit states: two per CTA of the largest launch (attn8), of as many rows as a row tile can have
+  size_t rows8 = ss::kCtas8 * (size_t)(L.R_stride < ss::kRows8 ? L.R_stride : ss::kRows8);
+  const size_t few8 = c->d == 64 ? ss::kCtasFew8 * (size_t)(L.R_stride < ss::kFew8 ? L.R_stride : ss::kFew8) : 0;
+  if (rows8 < few8) rows8 = few8;
+  L.off_plan8 = align_up(L.off_scratch8 + 2 * rows8 * (c->d + 4) * sizeof(float), 256);
   L.total = align_up(L.off_plan8 + ((size_t)c->max_B + 1) * sizeof(uint32_t), 256);
   return L;
 }
