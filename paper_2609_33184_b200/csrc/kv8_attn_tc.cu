@@ -8,13 +8,14 @@
 // Q and P are split into terms of 8 bits whose products add up in the accumulators (tensor work is not
 // what bounds this kernel):
 //  * Q row * 2^-eq (maximum in (224, 448]) = hi + lo, both e4m3.  bf16 has 8 significant bits and a term
-//    holds 4, so the split is exact down to 2^-13 of the row's maximum, off by at most 2^-17 of it below.
+//    holds 4, so the split is exact as long as lo's last bit is on e4m3's smallest step, 2^-9: for values from 1/4
+//    on, 2^-9.8 of the row's maximum; below it is off by at most 2^-10, 2^-17.8 of the maximum.
 //    The score is S * 2^eq * 2^ek * scale: all factors powers of two but the caller's, the sums in fp32.
 //  * weights.  x = s2 + ev - M + 7 with s2 the score in base 2, ev the key's value exponent, M the row's
 //    reference; P = 2^x multiplies the codes of V directly.  P as f16 is cut into hi + mid / 8 + lo / 64 of
 //    e5m2, three bits each (the upper byte of an f16 IS an e5m2: the cut is a byte permutation, the rest
-//    an exact f16 subtraction), relative error <= 2^-9.  e5m2 and not e4m3 for its range: a weight keeps
-//    its 9 bits down to 2^-21 of the row's reference and is off by at most 2^-30 of it below, so a sink
+//    an exact f16 subtraction), relative error <= 1.1 * 2^-9, f16's own rounding in it.  e5m2 and not e4m3 for its range: a weight keeps
+//    its 9 bits down to 2^-20 of the row's reference and is off by at most 1.25 * 2^-30 of it below, so a sink
 //    token of large weight does not swallow the 10^5 small ones whose weights add up.
 //  * the row sum adds P * 2^-ev, unrounded, in fp32 (ev in [-32, 80], see kv8.cuh).
 // The terms of P stand side by side on the N axis (one pass of the MMA over V), and so do those of Q: as
