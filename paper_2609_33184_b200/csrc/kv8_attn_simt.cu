@@ -7,7 +7,8 @@
 // the finished sum, exactly); running maximum and sum per warp and row, in fp32; weights times the
 // value scale go through shared memory and every lane accumulates d / 32 head dims over the 32
 // keys.  The warps' states meet when a segment ends.  Bound by conversions and shared-memory
-// reads, not by memory: it is the general form, not the fast one.
+// reads, not by memory: it is the general form, not the fast one (decoding, 16 x 32768 tokens, 8 heads of 128, 4 rows:
+// 2600 us for pages of 4, 24 or 192 tokens, the tensor cores take 166 for pages of 64; 32 rows 10500 against 184).
 #include <cuda_fp8.h>
 
 #include "kv8.cuh"
