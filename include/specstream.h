@@ -349,6 +349,67 @@ ss_status ss_verify_chunk8(ss_ctx* ctx, const ss_cache8* cache, const int32_t* v
 ss_status ss_decode8(ss_ctx* ctx, ss_tensor Q, int32_t B, int32_t T_q, float scale, const ss_cache8* cache,
                      const int32_t* valid_len, void* O, float* LSE, void* stream);
 
+/* ---- rotary positions, and rows that join a cache ---------------------------------------------
+ * (The paper's models rotate queries and keys by their positions before attention; the calls above take
+ * them rotated.)  Pair i of a row at position p turns by the angle p * f_i: (x, y) becomes
+ * magnitude * (x cos - y sin, x sin + y cos).  The first rot_dim elements of a row form rot_dim / 2 pairs -
+ * elements i and i + rot_dim / 2, or 2 i and 2 i + 1 where `interleaved` - the others stay as they are.
+ * With several axes (time, height and width of images and video) each pair has one axis and a token a
+ * position on each.  The angle is off by less than 2^-23 at any int32 position; values are turned in
+ * fp32 and rounded once, to bf16. */
+typedef struct {
+  int32_t rot_dim;     /* a multiple of 16                                              */
+  int32_t n_axes;      /* 1..4                                                          */
+  int32_t interleaved;
+  float magnitude;
+  uint64_t turn[64];   /* revolutions of a pair per position, in units of 2^-64 (whole ones dropped) */
+  uint8_t axis[64];    /* axis of a pair                                                */
+} ss_rope;
+
+/* Fills *out (host only): inv_freq [rot_dim / 2] are the pairs' angles per position in radians, axis
+ * [rot_dim / 2] their axes (NULL: all 0).  SS_ERR_ARG for a null pointer, a frequency or magnitude that is not
+ * finite or an axis outside [0, n_axes); SS_ERR_SHAPE for a rot_dim that is not a multiple of 16 in 16..128 or
+ * n_axes outside 1..4. */
+ss_status ss_rope_init(ss_rope* out, int32_t rot_dim, int32_t interleaved, int32_t n_axes, const double* inv_freq,
+                       const int32_t* axis, float magnitude);
+
+/* Rotates row i < row_cnt[b] of Q [B, H_q, T, d] and K [B, H_kv, T, d] into Q_out and K_out (which may be Q and
+ * K themselves, but not overlap them otherwise): the queries and candidate keys of a round.  A null Q.ptr or
+ * K.ptr leaves that one out.  pos (device int32 [n_axes, B, T]) gives the positions; NULL: pos_off[b] + i on all
+ * axes (device int32 [B], NULL = 0).  row_cnt (device [B]) NULL = T; rows from row_cnt[b] on are left as they
+ * are; a count outside [0, T] is clamped (SS_DEV_BAD_ACCEPT).  rot_dim <= d (SS_ERR_SHAPE).  Independent of the
+ * round state; inside an open round the rows may be those of the very next call, also under
+ * SS_FLAG_OVERLAP_CHUNKS.  B * T * (H_q + 2 H_kv) < 2^31 (SS_ERR_SHAPE); T is not bound by max_Tloc. */
+ss_status ss_rope_rotate(ss_ctx* ctx, const ss_rope* rope, ss_tensor Q, ss_tensor K, int32_t B, int32_t T,
+                         const int32_t* pos, const int32_t* pos_off, const int32_t* row_cnt, ss_tensor Q_out,
+                         ss_tensor K_out, void* stream);
+
+/* A cache in bf16, as ss_verify_chunk_paged and the windowed calls read it.  Paged (page_table not NULL): K, V
+ * are pools [n_pages, H_kv, page_size, d] (stride_b = page stride), page_table (device int32 [B, pages_per_req])
+ * lists a request's pages.  Dense (page_table NULL): [B, H_kv, page_size, d], n_pages = requests in the buffer
+ * (>= the call's B), pages_per_req ignored.  Table entries of pages that a call does not touch may hold
+ * anything. */
+typedef struct {
+  ss_tensor K, V;               /* bf16, device                                              */
+  int32_t n_pages, page_size, pages_per_req;
+  const int32_t* page_table;    /* device [B, pages_per_req], or NULL                        */
+} ss_cache16;
+
+/* Rows join a cache, K rotated on the way: for each request b and k < row_cnt[b], row row_idx[b][k] of K, V
+ * [B, H_kv, T, d] becomes token dst_off[b] + k (lists and their defaults, checks and device flags as in
+ * ss_kv8_write; the tokens of one call must be distinct slots).  rope NULL: rows as they are, bit for bit.  pos
+ * (device int32 [n_axes, B, T], by input row) NULL: row k's position is its token, dst_off[b] + k, on all axes.
+ * Q (may be null; needs rope and no row_idx): rows k < row_cnt[b] of [B, H_q, T, d] are rotated by the same
+ * positions into Q_out, also where the token finds no room; Q_out may be Q.  ss_kv8_append writes the same bits
+ * as ss_rope_rotate and ss_kv8_write one after the other.  Independent of the round state.
+ * B * T * (H_q + 2 H_kv) < 2^31 (SS_ERR_SHAPE); T is not bound by max_Tloc. */
+ss_status ss_kv_append(ss_ctx* ctx, const ss_cache16* cache, ss_tensor K, ss_tensor V, int32_t B, int32_t T,
+                       const ss_rope* rope, const int32_t* pos, const int32_t* row_idx, const int32_t* row_cnt,
+                       const int32_t* dst_off, ss_tensor Q, ss_tensor Q_out, void* stream);
+ss_status ss_kv8_append(ss_ctx* ctx, const ss_cache8* cache, ss_tensor K, ss_tensor V, int32_t B, int32_t T,
+                        const ss_rope* rope, const int32_t* pos, const int32_t* row_idx, const int32_t* row_cnt,
+                        const int32_t* dst_off, ss_tensor Q, ss_tensor Q_out, void* stream);
+
 /* Read (and clear) the device status word after synchronising `stream`, waiting at most
  * timeout_ms (<= 0: wait without limit).  SS_OK, SS_ERR_DEVICE_FLAG (bits in *dev_bits if
  * non-NULL) or SS_ERR_TIMEOUT. */

@@ -34,7 +34,8 @@ EXPORTS = ["ss_workspace_bytes", "ss_create", "ss_destroy", "ss_verify_begin", "
            "ss_tier_d2h_bytes", "ss_verify_chunk_paged", "ss_width_create", "ss_width_destroy",
            "ss_width_observe", "ss_width_next", "ss_width_estimate", "ss_cohort_build", "ss_probe_read",
            "ss_selftest_wait_expiry", "ss_verify_abort", "ss_cta_log_set", "ss_get_stats", "ss_verify_round", "ss_verify_chunks",
-           "ss_time_rounds", "ss_kv8_write", "ss_kv8_read", "ss_verify_chunk8", "ss_decode8"]
+           "ss_time_rounds", "ss_kv8_write", "ss_kv8_read", "ss_verify_chunk8", "ss_decode8",
+           "ss_rope_init", "ss_rope_rotate", "ss_kv_append", "ss_kv8_append"]
 
 
 class ss_stats(C.Structure):
@@ -112,6 +113,16 @@ class ss_cache8(C.Structure):
                 ("page_table", C.c_void_p)]
 
 
+class ss_cache16(C.Structure):
+    _fields_ = [("K", ss_tensor), ("V", ss_tensor), ("n_pages", C.c_int32), ("page_size", C.c_int32),
+                ("pages_per_req", C.c_int32), ("page_table", C.c_void_p)]
+
+
+class ss_rope(C.Structure):
+    _fields_ = [("rot_dim", C.c_int32), ("n_axes", C.c_int32), ("interleaved", C.c_int32), ("magnitude", C.c_float),
+                ("turn", C.c_uint64 * 64), ("axis", C.c_uint8 * 64)]
+
+
 class ss_static_round(C.Structure):
     _fields_ = [("B", C.c_int32), ("H_q", C.c_int32), ("H_kv", C.c_int32), ("d", C.c_int32),
                 ("T_q", C.c_int32), ("T_loc", C.c_int32), ("L_c", C.c_int32), ("scale", C.c_float),
@@ -178,6 +189,14 @@ def load() -> C.CDLL:
     lib.ss_verify_chunk8.argtypes = [vp, c8, vp, vp]
     lib.ss_decode8.restype = C.c_int
     lib.ss_decode8.argtypes = [vp, ss_tensor, i32, i32, C.c_float, c8, vp, vp, vp, vp]
+    c16, rp = C.POINTER(ss_cache16), C.POINTER(ss_rope)
+    lib.ss_rope_init.restype = C.c_int
+    lib.ss_rope_init.argtypes = [rp, i32, i32, i32, C.POINTER(C.c_double), C.POINTER(C.c_int32), C.c_float]
+    lib.ss_rope_rotate.restype = C.c_int
+    lib.ss_rope_rotate.argtypes = [vp, rp, ss_tensor, ss_tensor, i32, i32, vp, vp, vp, ss_tensor, ss_tensor, vp]
+    for f, cache in ((lib.ss_kv_append, c16), (lib.ss_kv8_append, c8)):
+        f.restype = C.c_int
+        f.argtypes = [vp, cache, ss_tensor, ss_tensor, i32, i32, rp, vp, vp, vp, vp, ss_tensor, ss_tensor, vp]
     lib.ss_poll_status.restype = C.c_int
     lib.ss_poll_status.argtypes = [vp, vp, i32, u32p]
     lib.ss_stream_round.restype = C.c_int
@@ -323,6 +342,47 @@ class Cache8:
         fill = lambda value, *shape: torch.full(shape, value, dtype=torch.uint8, device=device)
         s = (outer, H_kv, tokens)
         return cls(fill(0, *s, d), fill(0, *s, d), fill(95, *s), fill(95, *s), page_table)   # 95: e = -32
+
+
+class Cache16:
+    """A bf16 KV cache: K, V [n_pages, H_kv, page_size, d] with page_table int32 [B, pages_per_req], or
+    [B, H_kv, tokens, d] without one, d contiguous.  Holds the tensors; the description is built once."""
+
+    def __init__(self, K: torch.Tensor, V: torch.Tensor, page_table: Optional[torch.Tensor] = None):
+        for t in (K, V):
+            assert t.dtype is torch.bfloat16 and t.dim() == 4 and t.stride(3) == 1, (t.shape, t.dtype, t.stride())
+        assert V.shape == K.shape
+        if page_table is not None:
+            assert page_table.dtype == torch.int32 and page_table.dim() == 2 and page_table.is_contiguous()
+        self.device = K.get_device()   # -1: the CPU
+        for t in (V, page_table):
+            assert t is None or t.get_device() == self.device, (t.device, K.device)
+        self.tensors = (K, V, page_table)
+        self.H_kv, self.d = K.shape[1], K.shape[3]
+        self.requests = K.shape[0] if page_table is None else page_table.shape[0]
+        self.desc = ss_cache16(as_ss_tensor(K), as_ss_tensor(V), K.shape[0], K.shape[2],
+                               1 if page_table is None else page_table.shape[1], _ptr(page_table))
+        self.ref = C.byref(self.desc)
+
+
+class Rope:
+    """A rotation (ss_rope): inv_freq, the angle per position of each of the rot_dim / 2 pairs; axis, the position
+    axis of each pair (None: the first); magnitude multiplies what is rotated."""
+
+    def __init__(self, inv_freq, axis=None, n_axes: int = 1, interleaved: bool = False, magnitude: float = 1.0):
+        f = [float(x) for x in inv_freq]
+        n = len(f)
+        assert axis is None or len(axis) == n, (len(axis), n)
+        self.desc = ss_rope()
+        st = load().ss_rope_init(C.byref(self.desc), 2 * n, 1 if interleaved else 0, n_axes, (C.c_double * max(1, n))(*f),
+                                 None if axis is None else (C.c_int32 * max(1, n))(*[int(a) for a in axis]), magnitude)
+        if st != SS_OK:
+            raise SpecStreamError(st, "ss_rope_init")
+        self.n_axes = n_axes
+        self.ref = C.byref(self.desc)
+
+
+_NO_ROWS = ss_tensor(None, 0, 0, 0)
 
 
 class Context:
@@ -510,6 +570,53 @@ class Context:
                                  None if LSE is None else LSE.data_ptr(), self._sp(stream))
         if st:
             self._check(st, "ss_decode8")
+
+    def _pair(self, x, out, heads, B, T, what):
+        """Rows in and rows out of the same shape (or neither)."""
+        if x is None:
+            if out is not None:
+                raise AssertionError(what + "_out without " + what)
+            return _NO_ROWS, _NO_ROWS
+        shape = (B, heads, T, self.d)
+        return self._rows(x, shape), self._rows(out, shape)
+
+    def ss_rope_rotate(self, rope: Rope, Q, K, Q_out, K_out, pos=None, pos_off=None, row_cnt=None, stream=None):
+        """Q [B, H_q, T, d] -> Q_out, K [B, H_kv, T, d] -> K_out (bf16; either pair may be None); pos int32
+        [n_axes, B, T], or positions pos_off[b] + row; row_cnt, pos_off int32 [B]."""
+        B, _, T, _ = (Q if K is None else K).shape
+        i32 = self._i32
+        q, qo = self._pair(Q, Q_out, self.H_q, B, T, "Q")
+        k, ko = self._pair(K, K_out, self.H_kv, B, T, "K")
+        st = self.lib.ss_rope_rotate(self.handle, rope.ref, q, k, B, T, i32(pos, rope.n_axes * B * T), i32(pos_off, B),
+                                     i32(row_cnt, B), qo, ko, self._sp(stream))
+        if st:
+            self._check(st, "ss_rope_rotate")
+
+    def _append(self, name, kind, cache, K, V, rope, pos, Q, Q_out, dst_off, row_cnt, row_idx, stream):
+        B, _, T, _ = K.shape
+        if type(cache) is not kind:
+            raise AssertionError("cache of another kind")
+        shape = (B, self.H_kv, T, self.d)
+        i32, rows = self._i32, self._rows
+        q, qo = self._pair(Q, Q_out, self.H_q, B, T, "Q")
+        st = getattr(self.lib, name)(self.handle, self._cache8(cache, B), rows(K, shape), rows(V, shape), B, T,
+                                     None if rope is None else rope.ref,
+                                     None if pos is None else i32(pos, (1 if rope is None else rope.n_axes) * B * T),
+                                     i32(row_idx, B * T), i32(row_cnt, B), i32(dst_off, B), q, qo, self._sp(stream))
+        if st:
+            self._check(st, name)
+
+    def ss_kv_append(self, cache: Cache16, K, V, rope: Optional[Rope] = None, pos=None, Q=None, Q_out=None, dst_off=None,
+                     row_cnt=None, row_idx=None, stream=None):
+        """Rows of K, V [B, H_kv, T, d] bf16 become tokens dst_off[b] + k of the cache, K rotated by rope; Q
+        [B, H_q, T, d] is rotated into Q_out.  pos int32 [n_axes, B, T] (None: the tokens), dst_off, row_cnt int32 [B],
+        row_idx int32 [B, T] on the device or None."""
+        self._append("ss_kv_append", Cache16, cache, K, V, rope, pos, Q, Q_out, dst_off, row_cnt, row_idx, stream)
+
+    def ss_kv8_append(self, cache: Cache8, K, V, rope: Optional[Rope] = None, pos=None, Q=None, Q_out=None, dst_off=None,
+                      row_cnt=None, row_idx=None, stream=None):
+        """The same into an 8-bit cache."""
+        self._append("ss_kv8_append", Cache8, cache, K, V, rope, pos, Q, Q_out, dst_off, row_cnt, row_idx, stream)
 
     def ss_poll_status(self, stream=None, timeout_ms: int = 0):
         """Returns (status, device_bits)."""

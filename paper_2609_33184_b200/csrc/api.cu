@@ -1,11 +1,13 @@
 // Host side of libspecstream: argument validation, round state machine, workspace layout,
 // tensor-map cache and kernel launches.  Allocates no device memory.
 #include <chrono>
+#include <cmath>
 #include <cstdlib>
 #include <cstring>
 #include <new>
 
 #include "kv8.cuh"
+#include "rope.cuh"
 #include "ss_internal.h"
 
 struct ss_ctx {
@@ -1254,9 +1256,23 @@ ss_status ss_commit_gather(ss_ctx* c, ss_tensor K_loc, ss_tensor V_loc, int32_t 
 }
 
 // ---- 8-bit KV cache ---------------------------------------------------------------------------
+// A bf16 cache described like an 8-bit one: strides in bytes, no scales.
+static ss_cache8 bytes_of(const ss_cache16& k) {
+  ss_cache8 b;
+  memset(&b, 0, sizeof(b));
+  b.K = {k.K.ptr, 2 * k.K.stride_b, 2 * k.K.stride_h, 2 * k.K.stride_t};
+  b.V = {k.V.ptr, 2 * k.V.stride_b, 2 * k.V.stride_h, 2 * k.V.stride_t};
+  b.n_pages = k.n_pages;
+  b.page_size = k.page_size;
+  b.pages_per_req = k.pages_per_req;
+  b.page_table = k.page_table;
+  return b;
+}
+
 // Checks a cache for B requests and fills the kernels' view of it.
-static ss_status view8(const ss_ctx* c, const ss_cache8* k, int32_t B, ss::View8* v) {
-  if (!k || !k->K.ptr || !k->V.ptr || !k->K_scale.ptr || !k->V_scale.ptr) return SS_ERR_ARG;
+static ss_status view_cache(const ss_cache8* k, int bits, int32_t B, ss::View8* v) {
+  if (!k || !k->K.ptr || !k->V.ptr) return SS_ERR_ARG;
+  if (bits == 8 && (!k->K_scale.ptr || !k->V_scale.ptr)) return SS_ERR_ARG;
   if (k->n_pages <= 0 || k->page_size <= 0) return SS_ERR_ARG;
   if (k->page_table && k->pages_per_req <= 0) return SS_ERR_ARG;
   if (!k->page_table && B > k->n_pages) return SS_ERR_SHAPE;
@@ -1286,6 +1302,7 @@ static ss_status view8(const ss_ctx* c, const ss_cache8* k, int32_t B, ss::View8
   v->page_tiles = k->page_table && k->page_size > ss::kTok8 ? k->page_size / ss::kTok8 : 1;
   return SS_OK;
 }
+static ss_status view8(const ss_cache8* k, int32_t B, ss::View8* v) { return view_cache(k, 8, B, v); }
 
 static ss_status copy8(ss_ctx* c, bool write, const ss_cache8* cache, ss_tensor K, ss_tensor V, int32_t B, int32_t T,
                        const int32_t* idx, const int32_t* cnt, const int32_t* off, void* stream) {
@@ -1293,7 +1310,7 @@ static ss_status copy8(ss_ctx* c, bool write, const ss_cache8* cache, ss_tensor 
   if (B > c->cfg.max_B || (int64_t)B * T * c->cfg.H_kv * 2 >= (1ll << 31)) return SS_ERR_SHAPE;
   ss::Copy8Params p;
   memset(&p, 0, sizeof(p));
-  const ss_status st = view8(c, cache, B, &p.kv);
+  const ss_status st = view8(cache, B, &p.kv);
   if (st != SS_OK) return st;
   if (!tensor_ok(K) || !tensor_ok(V)) return SS_ERR_ALIGN;
   if (((uintptr_t)idx | (uintptr_t)cnt | (uintptr_t)off) & 3) return SS_ERR_ALIGN;
@@ -1334,7 +1351,7 @@ ss_status ss_kv8_read(ss_ctx* c, const ss_cache8* cache, ss_tensor K, ss_tensor 
 // The attention launch that both entry points share; the caller has set where its result goes.
 static ss_status attn8(ss_ctx* c, const ss_tensor& Q, int32_t B, int32_t T_q, float scale, const ss_cache8* cache,
                        const int32_t* valid_len, ss::Attn8Params* p, cudaStream_t s) {
-  const ss_status st = view8(c, cache, B, &p->kv);
+  const ss_status st = view8(cache, B, &p->kv);
   if (st != SS_OK) return st;
   if (p->kv.room > c->cfg.max_Lc) return SS_ERR_SHAPE;
   if ((uintptr_t)valid_len & 3) return SS_ERR_ALIGN;
@@ -1396,7 +1413,7 @@ ss_status ss_verify_chunk8(ss_ctx* c, const ss_cache8* cache, const int32_t* val
   if (c->state != ss_ctx::OPEN || (cudaStream_t)stream != c->stream) return SS_ERR_STATE;
   ss::Attn8Params p;
   memset(&p, 0, sizeof(p));
-  ss_status st = view8(c, cache, c->B, &p.kv);  // (before a fold is enqueued)
+  ss_status st = view8(cache, c->B, &p.kv);  // (before a fold is enqueued)
   if (st != SS_OK) return st;
   if (p.kv.room > c->cfg.max_Lc) return SS_ERR_SHAPE;
   if ((uintptr_t)valid_len & 3) return SS_ERR_ALIGN;
@@ -1437,6 +1454,110 @@ ss_status ss_decode8(ss_ctx* c, ss_tensor Q, int32_t B, int32_t T_q, float scale
   ++c->stats.rounds;
   c->stats.rows += (int64_t)B * c->cfg.H_q * T_q;
   return SS_OK;
+}
+
+// ---- rotary positions, rows that join a cache ----------------------------------------------------
+ss_status ss_rope_init(ss_rope* out, int32_t rot_dim, int32_t interleaved, int32_t n_axes, const double* inv_freq,
+                       const int32_t* axis, float magnitude) {
+  if (!out || !inv_freq || !std::isfinite(magnitude)) return SS_ERR_ARG;
+  if (rot_dim < 16 || rot_dim > 2 * ss::kRopePairs || rot_dim % 16 || n_axes < 1 || n_axes > ss::kRopeAxes)
+    return SS_ERR_SHAPE;
+  for (int i = 0; i < rot_dim / 2; ++i)
+    if (!std::isfinite(inv_freq[i]) || (axis && (axis[i] < 0 || axis[i] >= n_axes))) return SS_ERR_ARG;
+  memset(out, 0, sizeof(*out));
+  out->rot_dim = rot_dim;
+  out->n_axes = n_axes;
+  out->interleaved = interleaved != 0;
+  out->magnitude = magnitude;
+  for (int i = 0; i < rot_dim / 2; ++i) {
+    // (long double: 64 bits of significand)
+    const long double turns = (long double)inv_freq[i] / 6.283185307179586476925286766559005768L;
+    const long double part = turns - floorl(turns);  // [0, 1]: a tiny negative one rounds to a whole revolution
+    const long double units = roundl(part * 18446744073709551616.0L);
+    out->turn[i] = units >= 18446744073709551616.0L ? 0 : (uint64_t)units;
+    out->axis[i] = axis ? (uint8_t)axis[i] : 0;
+  }
+  return SS_OK;
+}
+
+// What ss_rope_rotate and the appends share; the caller has filled in where rows go.
+static ss_status rope_rows(ss_ctx* c, ss::RopeParams* p, const ss_rope* rope, const ss_tensor& Q, const ss_tensor& K,
+                           int32_t B, int32_t T, const int32_t* pos, const int32_t* idx, const int32_t* cnt,
+                           const int32_t* off, const ss_tensor& Q_out, void* stream) {
+  if (B <= 0 || T <= 0 || (Q.ptr && !Q_out.ptr)) return SS_ERR_ARG;
+  if (B > c->cfg.max_B || (int64_t)B * T * (c->cfg.H_q + 2 * (int64_t)c->cfg.H_kv) >= (1ll << 31)) return SS_ERR_SHAPE;
+  if (rope && (rope->rot_dim < 16 || rope->rot_dim > c->cfg.d || rope->rot_dim % 16 || rope->n_axes < 1 ||
+               rope->n_axes > ss::kRopeAxes))
+    return SS_ERR_SHAPE;
+  if ((Q.ptr && (!tensor_ok(Q) || !tensor_ok(Q_out))) || (K.ptr && !tensor_ok(K))) return SS_ERR_ALIGN;
+  if (((uintptr_t)pos | (uintptr_t)idx | (uintptr_t)cnt | (uintptr_t)off) & 3) return SS_ERR_ALIGN;
+  if (rope) p->rope = *rope;
+  p->Q = (uint16_t*)Q.ptr;
+  p->Qo = (uint16_t*)Q_out.ptr;
+  p->K = (uint16_t*)K.ptr;
+  p->q_sb = Q.stride_b, p->q_sh = Q.stride_h, p->q_st = Q.stride_t;
+  p->qo_sb = Q_out.stride_b, p->qo_sh = Q_out.stride_h, p->qo_st = Q_out.stride_t;
+  p->k_sb = K.stride_b, p->k_sh = K.stride_h, p->k_st = K.stride_t;
+  p->pos = pos;
+  p->idx = idx;
+  p->cnt = cnt;
+  p->off = off;
+  p->B = B;
+  p->H_q = Q.ptr ? c->cfg.H_q : 0;
+  p->H_kv = K.ptr ? c->cfg.H_kv : 0;
+  p->T = T;
+  p->d = c->cfg.d;
+  p->status = c->status;
+  DeviceGuard on(c->cfg.device);
+  cudaError_t e = on.err;
+  if (e == cudaSuccess) e = ss::launch_rope(*p, (cudaStream_t)stream, true);
+  if (e != cudaSuccess) return cuda_fail(c, e);
+  ++c->launches;
+  // Its successor may start before its rows are stored, and a chunk or local kernel in the middle of a round
+  // loads without waiting: the next one has to, it may take these rows.
+  if (c->state == ss_ctx::OPEN) c->first_launch = true;
+  return SS_OK;
+}
+
+ss_status ss_rope_rotate(ss_ctx* c, const ss_rope* rope, ss_tensor Q, ss_tensor K, int32_t B, int32_t T,
+                         const int32_t* pos, const int32_t* pos_off, const int32_t* row_cnt, ss_tensor Q_out,
+                         ss_tensor K_out, void* stream) {
+  if (!c || !rope || (!Q.ptr && !K.ptr) || (K.ptr && !K_out.ptr)) return SS_ERR_ARG;
+  if (K.ptr && !tensor_ok(K_out)) return SS_ERR_ALIGN;
+  ss::RopeParams p;
+  memset(&p, 0, sizeof(p));
+  p.Ko = (uint16_t*)K_out.ptr;
+  p.ko_sb = K_out.stride_b, p.ko_sh = K_out.stride_h, p.ko_st = K_out.stride_t;
+  return rope_rows(c, &p, rope, Q, K, B, T, pos, nullptr, row_cnt, pos_off, Q_out, stream);
+}
+
+static ss_status append(ss_ctx* c, int bits, const ss_cache8* cache, ss_tensor K, ss_tensor V, int32_t B, int32_t T,
+                        const ss_rope* rope, const int32_t* pos, const int32_t* idx, const int32_t* cnt,
+                        const int32_t* off, ss_tensor Q, ss_tensor Q_out, void* stream) {
+  if (!c || !K.ptr || !V.ptr || (Q.ptr && (!rope || idx)) || (pos && !rope)) return SS_ERR_ARG;
+  if (!tensor_ok(V)) return SS_ERR_ALIGN;
+  ss::RopeParams p;
+  memset(&p, 0, sizeof(p));
+  const ss_status st = view_cache(cache, bits, B, &p.kv);
+  if (st != SS_OK) return st;
+  p.bits = bits;
+  p.V = (uint16_t*)V.ptr;
+  p.v_sb = V.stride_b, p.v_sh = V.stride_h, p.v_st = V.stride_t;
+  return rope_rows(c, &p, rope, Q, K, B, T, pos, idx, cnt, off, Q_out, stream);
+}
+
+ss_status ss_kv_append(ss_ctx* c, const ss_cache16* cache, ss_tensor K, ss_tensor V, int32_t B, int32_t T,
+                       const ss_rope* rope, const int32_t* pos, const int32_t* row_idx, const int32_t* row_cnt,
+                       const int32_t* dst_off, ss_tensor Q, ss_tensor Q_out, void* stream) {
+  if (!cache) return SS_ERR_ARG;
+  const ss_cache8 bytes = bytes_of(*cache);
+  return append(c, 16, &bytes, K, V, B, T, rope, pos, row_idx, row_cnt, dst_off, Q, Q_out, stream);
+}
+
+ss_status ss_kv8_append(ss_ctx* c, const ss_cache8* cache, ss_tensor K, ss_tensor V, int32_t B, int32_t T,
+                        const ss_rope* rope, const int32_t* pos, const int32_t* row_idx, const int32_t* row_cnt,
+                        const int32_t* dst_off, ss_tensor Q, ss_tensor Q_out, void* stream) {
+  return append(c, 8, cache, K, V, B, T, rope, pos, row_idx, row_cnt, dst_off, Q, Q_out, stream);
 }
 
 ss_status ss_poll_status(ss_ctx* c, void* stream, int32_t timeout_ms, uint32_t* dev_bits) {

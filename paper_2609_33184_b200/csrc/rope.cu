@@ -1,0 +1,258 @@
+// Rotary positions on Q and K rows, and rows that join a cache (bf16 or 8 bits), K rotated on the way.
+//
+// Pair i of a row at position p turns by p * f_i, which for far positions is thousands of revolutions: as an
+// fp32 product (24 bits) the angle of the fastest pair is off by 2^-7 at p = 2^17.  f_i is held as revolutions
+// in units of 2^-64 instead (ss_rope_init), so p * f_i is one integer product whose overflow drops the whole
+// revolutions, off by at most 2^-65 * |p| <= 2^-34 revolutions; the upper 32 bits go to sincospi.  Values are
+// turned in fp32 and rounded once, to bf16.  8 bits: the codes are those of the rounded bf16 rows, so a row is
+// the same bits as rotated and then written with ss_kv8_write.
+//
+// A row of d values is handled by d / 16 neighbouring lanes, each 8 values from two places half of the turning
+// part apart: that makes 8 pairs in either layout, and 16-byte accesses contiguous over the lanes.  A thread
+// keeps the sines of its 8 pairs for the rows of one token that it handles, one after the other over the heads
+// (Q, K, V).  Memory bound: 4 d bytes per row.
+#include <cuda_fp8.h>
+
+#include "rope.cuh"
+
+namespace ss {
+namespace {
+
+constexpr int kThreads = 128;
+
+// A block takes 2^shift consecutive tokens of a request and `heads` of its rows (of Q, K and V laid end to
+// end): `lanes` rows side by side, one after the other beyond.
+struct Plan {
+  int shift, lanes, heads;
+  int token_blocks, head_blocks;
+};
+
+__device__ __forceinline__ float lo_f(uint32_t two) { return __uint_as_float(two << 16); }
+__device__ __forceinline__ float hi_f(uint32_t two) { return __uint_as_float(two & 0xffff0000u); }
+__device__ __forceinline__ uint32_t pack(float lo, float hi) {
+  const __nv_bfloat162 o = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&o);
+}
+
+// The sines of a thread's 8 pairs.
+struct Turn {
+  float c[8], s[8];
+};
+// (cos x - sin y, sin x + cos y)
+__device__ __forceinline__ void turn2(float& x, float& y, float c, float s) {
+  const float u = fmaf(x, c, -(y * s));
+  y = fmaf(x, s, y * c);
+  x = u;
+}
+// Half-split layout: value k of the first place pairs with value k of the second.  Interleaved: neighbours.
+template <bool INTER>
+__device__ __forceinline__ void turn_row(uint4 (&raw)[2], const Turn& t) {
+  uint32_t a[4] = {raw[0].x, raw[0].y, raw[0].z, raw[0].w}, b[4] = {raw[1].x, raw[1].y, raw[1].z, raw[1].w};
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    float a0 = lo_f(a[k]), a1 = hi_f(a[k]), b0 = lo_f(b[k]), b1 = hi_f(b[k]);
+    if (INTER) {
+      turn2(a0, a1, t.c[k], t.s[k]);
+      turn2(b0, b1, t.c[4 + k], t.s[4 + k]);
+    } else {
+      turn2(a0, b0, t.c[2 * k], t.s[2 * k]);
+      turn2(a1, b1, t.c[2 * k + 1], t.s[2 * k + 1]);
+    }
+    a[k] = pack(a0, a1);
+    b[k] = pack(b0, b1);
+  }
+  raw[0] = make_uint4(a[0], a[1], a[2], a[3]);
+  raw[1] = make_uint4(b[0], b[1], b[2], b[3]);
+}
+
+// Largest finite magnitude (bf16 bits) of a thread's 16 values.
+__device__ __forceinline__ uint32_t top_of(const uint4 (&raw)[2]) {
+  const uint32_t x[8] = {raw[0].x, raw[0].y, raw[0].z, raw[0].w, raw[1].x, raw[1].y, raw[1].z, raw[1].w};
+  uint32_t top = 0;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const uint32_t lo = x[j] & 0x7fffu, hi = (x[j] >> 16) & 0x7fffu;
+    if (lo < 0x7f80u) top = max(top, lo);
+    if (hi < 0x7f80u) top = max(top, hi);
+  }
+  return top;
+}
+__device__ __forceinline__ uint2 codes_of(const uint4& raw, float inv) {
+  const uint32_t x[4] = {raw.x, raw.y, raw.z, raw.w};
+  uint32_t c[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    c[j] = __nv_cvt_float2_to_fp8x2(make_float2(lo_f(x[j]) * inv, hi_f(x[j]) * inv), __NV_SATFINITE, __NV_E4M3);
+  return make_uint2(c[0] | (c[1] << 16), c[2] | (c[3] << 16));
+}
+
+// BITS of the cache (0: rows go to Qo, Ko); U rows in flight per thread.
+template <int D, int BITS, bool INTER, int U>
+__global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ RopeParams p, const Plan plan) {
+  constexpr int LPR = D / 16;
+  __shared__ uint64_t freq_s[kRopePairs];
+  __shared__ uint8_t axis_s[kRopePairs];
+  const int tid = threadIdx.x, rot = p.rope.rot_dim;
+  if (tid < rot / 2) {
+    freq_s[tid] = p.rope.turn[tid];
+    axis_s[tid] = p.rope.axis[tid];
+  }
+  __syncthreads();
+  pdl_wait_prior();
+  pdl_launch_dependents();
+  int x = blockIdx.x;
+  const int tb = x % plan.token_blocks;
+  x /= plan.token_blocks;
+  const int hb = x % plan.head_blocks, b = x / plan.head_blocks;
+  int n = p.cnt ? p.cnt[b] : p.T;
+  const bool report = tb == 0 && hb == 0;
+  if (n < 0 || n > p.T) {
+    if (tid == 0 && report) atomicOr(p.status, SS_DEV_BAD_ACCEPT);
+    n = max(0, min(n, p.T));
+  }
+  const int slot = tid / LPR, part = tid % LPR;
+  const int k = (tb << plan.shift) + (slot & ((1 << plan.shift) - 1));   // row of the call
+  if ((tb << plan.shift) >= n) return;
+  const int base0 = hb * plan.heads, head0 = base0 + (slot >> plan.shift);
+  const int head1 = min(base0 + plan.heads, p.H_q + p.H_kv + (BITS ? p.H_kv : 0));
+  const int64_t off = p.off ? (int64_t)p.off[b] : 0, tok = off + k;
+
+  // the input row, and (cache) the token's place
+  bool live = k < n, store = live;
+  int src = k;
+  uint64_t outer = (uint64_t)b, inner = (uint64_t)tok;
+  if (BITS && live) {
+    const bool one = part == 0 && head0 == 0;   // who reports a row
+    if (p.idx) {
+      src = p.idx[(int64_t)b * p.T + k];
+      if (src < 0 || src >= p.T) {
+        if (one) atomicOr(p.status, SS_DEV_BAD_ACCEPT);
+        live = store = false;
+        src = 0;
+      }
+    }
+    if (live && (tok < 0 || tok >= p.kv.room)) {
+      if (one) atomicOr(p.status, SS_DEV_DST_OVERFLOW);
+      store = false;
+    }
+    if (store && p.kv.page_table) {
+      const uint32_t t = (uint32_t)tok, pg = p.kv.page_log2 >= 0 ? t >> p.kv.page_log2 : t / (uint32_t)p.kv.page_size;
+      inner = t - pg * p.kv.page_size;
+      const uint32_t id = (uint32_t)p.kv.page_table[(int64_t)b * p.kv.pages_per_req + pg];
+      if (id >= (uint32_t)p.kv.n_outer) {
+        if (one) atomicOr(p.status, SS_DEV_BAD_PAGE);
+        store = false;
+      }
+      outer = id;
+    }
+  }
+
+  // this thread's two places in a row, and its pairs' sines
+  const bool turning = part * 16 < rot;
+  const int at0 = turning ? part * 8 : rot + (part - rot / 16) * 8;
+  const int at1 = turning ? rot / 2 + part * 8 : rot + (D - rot) / 2 + (part - rot / 16) * 8;
+  Turn t;
+  if (turning && live && head0 < p.H_q + p.H_kv) {
+    int64_t pos[kRopeAxes];
+#pragma unroll
+    for (int a = 0; a < kRopeAxes; ++a)
+      pos[a] = p.pos && a < p.rope.n_axes ? (int64_t)p.pos[((int64_t)a * p.B + b) * p.T + src] : tok;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int pair = INTER ? (j < 4 ? part * 4 + j : rot / 4 + part * 4 + j - 4) : part * 8 + j;
+      const int a = axis_s[pair];
+      const int64_t at = a == 0 ? pos[0] : a == 1 ? pos[1] : a == 2 ? pos[2] : pos[3];
+      const uint64_t turns = freq_s[pair] * (uint64_t)at;                // whole revolutions overflow
+      sincospif((float)(int32_t)(turns >> 32) * 0x1p-31f, &t.s[j], &t.c[j]);
+      t.s[j] *= p.rope.magnitude;
+      t.c[j] *= p.rope.magnitude;
+    }
+  }
+
+#pragma unroll 1
+  for (int base = base0; base < head1; base += U * plan.lanes) {  // (as often for every lane of a warp)
+    const int g0 = base + (slot >> plan.shift);
+    uint4 raw[U][2];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int g = g0 + u * plan.lanes;
+      raw[u][0] = raw[u][1] = make_uint4(0, 0, 0, 0);
+      if (!live || g >= head1) continue;
+      const uint16_t* row = g < p.H_q ? p.Q + b * p.q_sb + g * p.q_sh + src * p.q_st
+                            : g < p.H_q + p.H_kv ? p.K + b * p.k_sb + (g - p.H_q) * p.k_sh + src * p.k_st
+                                                 : p.V + b * p.v_sb + (g - p.H_q - p.H_kv) * p.v_sh + src * p.v_st;
+      raw[u][0] = __ldcs(reinterpret_cast<const uint4*>(row + at0));
+      raw[u][1] = __ldcs(reinterpret_cast<const uint4*>(row + at1));
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int g = g0 + u * plan.lanes;
+      const bool is_q = g < p.H_q, is_v = g >= p.H_q + p.H_kv;
+      if (turning && !is_v && live && g < head1) turn_row<INTER>(raw[u], t);
+      uint32_t top = 0;
+      if (BITS == 8) {  // (by all lanes: a row's are neighbours)
+        top = top_of(raw[u]);
+#pragma unroll
+        for (int o = LPR / 2; o; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+      }
+      if (!live || g >= head1) continue;
+      if (is_q || BITS == 0) {
+        uint16_t* row = is_q ? p.Qo + b * p.qo_sb + g * p.qo_sh + src * p.qo_st
+                             : p.Ko + b * p.ko_sb + (g - p.H_q) * p.ko_sh + src * p.ko_st;
+        *reinterpret_cast<uint4*>(row + at0) = raw[u][0];
+        *reinterpret_cast<uint4*>(row + at1) = raw[u][1];
+      } else if (store) {
+        const int h = is_v ? g - p.H_q - p.H_kv : g - p.H_q;
+        uint8_t* row = is_v ? p.kv.V + outer * p.kv.v_sb + h * p.kv.v_sh + inner * p.kv.v_st
+                            : p.kv.K + outer * p.kv.k_sb + h * p.kv.k_sh + inner * p.kv.k_st;
+        if (BITS == 16) {
+          __stcs(reinterpret_cast<uint4*>(row + 2 * at0), raw[u][0]);
+          __stcs(reinterpret_cast<uint4*>(row + 2 * at1), raw[u][1]);
+        } else {
+          // top = (1 + f / 128) 2^(E - 127) against 448 = (1 + 96 / 128) 2^8
+          const int e = max(kMinExp8, min(kMaxExp8, (int)((top + 31u) >> 7) - 127 - 8));
+          const float inv = pow2_8(-e);
+          __stcs(reinterpret_cast<uint2*>(row + at0), codes_of(raw[u][0], inv));
+          __stcs(reinterpret_cast<uint2*>(row + at1), codes_of(raw[u][1], inv));
+          uint8_t* scale = is_v ? p.kv.Vs + outer * p.kv.vs_sb + h * p.kv.vs_sh + inner * p.kv.vs_st
+                                : p.kv.Ks + outer * p.kv.ks_sb + h * p.kv.ks_sh + inner * p.kv.ks_st;
+          if (part == 0) *scale = (uint8_t)(e + 127);
+        }
+      }
+    }
+  }
+}
+
+template <int D, int BITS, bool INTER, int U>
+cudaError_t launch_rows(const RopeParams& p, int heads, cudaStream_t s, bool pdl) {
+  constexpr int kSlots = kThreads * 16 / D;
+  const int all = p.H_q + p.H_kv + (BITS ? p.H_kv : 0);
+  Plan plan = {};
+  while (1 << plan.shift < p.T && 1 << plan.shift < kSlots) ++plan.shift;
+  plan.lanes = kSlots >> plan.shift;
+  plan.heads = heads * plan.lanes;
+  plan.token_blocks = (p.T + (1 << plan.shift) - 1) >> plan.shift;
+  plan.head_blocks = (all + plan.heads - 1) / plan.heads;
+  const dim3 grid((unsigned)plan.token_blocks * plan.head_blocks * p.B);  // below 2^31: see the caller
+  return launch_kernel(rope_kernel<D, BITS, INTER, U>, grid, dim3(kThreads), 0, s, pdl, p, plan);
+}
+template <int D, int BITS>
+cudaError_t launch_bits(const RopeParams& p, cudaStream_t s, bool pdl) {
+  const int all = p.H_q + p.H_kv + (BITS ? p.H_kv : 0);
+  const bool large = (int64_t)p.B * p.T * all > (int64_t)8 * kNumSM * kThreads * 16 / D;
+  if (p.rope.interleaved)
+    return large ? launch_rows<D, BITS, true, 4>(p, 8, s, pdl) : launch_rows<D, BITS, true, 1>(p, 1, s, pdl);
+  return large ? launch_rows<D, BITS, false, 4>(p, 8, s, pdl) : launch_rows<D, BITS, false, 1>(p, 1, s, pdl);
+}
+template <int D>
+cudaError_t launch_dim(const RopeParams& p, cudaStream_t s, bool pdl) {
+  return p.bits == 16 ? launch_bits<D, 16>(p, s, pdl) : p.bits == 8 ? launch_bits<D, 8>(p, s, pdl) : launch_bits<D, 0>(p, s, pdl);
+}
+
+}  // namespace
+
+cudaError_t launch_rope(const RopeParams& p, cudaStream_t s, bool pdl) {
+  return p.d == 128 ? launch_dim<128>(p, s, pdl) : launch_dim<64>(p, s, pdl);
+}
+
+}  // namespace ss
