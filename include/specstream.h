@@ -68,6 +68,7 @@ typedef enum {
 #define SS_DEV_DST_OVERFLOW 4u  /* dst_off + k outside [0, cap): row skipped           */
 #define SS_DEV_WAIT_EXPIRED 8u  /* a bounded in-kernel wait gave up: round is invalid  */
 #define SS_DEV_BAD_PAGE 16u     /* page id outside the pool: its tokens read as zeros  */
+#define SS_DEV_BAD_DEPTH 32u    /* depth[b][t] outside [0, T_q): clamped               */
 
 typedef struct {
   int32_t max_B;      /* requests per call                                          */
@@ -409,6 +410,37 @@ ss_status ss_kv_append(ss_ctx* ctx, const ss_cache16* cache, ss_tensor K, ss_ten
 ss_status ss_kv8_append(ss_ctx* ctx, const ss_cache8* cache, ss_tensor K, ss_tensor V, int32_t B, int32_t T,
                         const ss_rope* rope, const int32_t* pos, const int32_t* row_idx, const int32_t* row_cnt,
                         const int32_t* dst_off, ss_tensor Q, ss_tensor Q_out, void* stream);
+
+/* ---- attention over a window -------------------------------------------------------------------
+ * Layers whose queries see the last `window` tokens (their own among them) and, where they stay visible, the
+ * first `sinks` ones: a query at position p sees token j of its request, j < valid_len[b], when j <= p and
+ * (j < sinks or p - j < window).  window >= 1, sinks >= 0 (SS_ERR_ARG); a window of the whole history leaves
+ * plain causal attention.  Only the tokens that some query sees are read, and only their pages looked up, so
+ * table entries of pages between the sinks and the window may hold anything (a page given back).  The caches,
+ * valid_len and its default, device flags, the limits on scores and the workspace's rule are those of the 8-bit
+ * cache above (its room must not exceed max_Lc); the tensor cores take dense caches and pages of any multiple of
+ * 8 tokens, the CUDA cores other pages.  The split over the GPU follows the lengths on the device, so a captured
+ * call follows lengths that change between replays.  Tokens that no query of the request sees may hold anything, NaN
+ * included; a value that is not finite in a token that only some of them see may make the others' rows NaN.
+ *
+ * ss_decode_window, ss_decode8_window: the T_q queries of a request are the newest tokens of its cache, query t
+ * at position valid_len[b] - T_q + t - a decoding step (T_q = 1), or a piece of a prompt, after ss_kv_append or
+ * ss_kv8_append of the same tokens.  A query whose position is negative sees nothing.  O and LSE as
+ * ss_verify_finalize writes them.  SS_ERR_STATE while a round is open. */
+ss_status ss_decode_window(ss_ctx* ctx, ss_tensor Q, int32_t B, int32_t T_q, float scale, const ss_cache16* cache,
+                           int32_t window, int32_t sinks, const int32_t* valid_len, void* O, float* LSE, void* stream);
+ss_status ss_decode8_window(ss_ctx* ctx, ss_tensor Q, int32_t B, int32_t T_q, float scale, const ss_cache8* cache,
+                            int32_t window, int32_t sinks, const int32_t* valid_len, void* O, float* LSE, void* stream);
+
+/* The same as a chunk of the open round: its queries are candidates behind the cache, query t at position
+ * valid_len[b] + depth[b][t] (device int32 [B, T_q], the depth of a tree's nodes, 0 for the first; outside
+ * [0, T_q): clamped, SS_DEV_BAD_DEPTH; NULL = t, a chain).  The candidates' own keys go through ss_verify_local,
+ * whose mask is the caller's: with a window below T_q it has to leave out what is further back than that.  May be
+ * mixed with other chunks (their tokens are visible to every query). */
+ss_status ss_verify_chunk_window(ss_ctx* ctx, const ss_cache16* cache, int32_t window, int32_t sinks,
+                                 const int32_t* valid_len, const int32_t* depth, void* stream);
+ss_status ss_verify_chunk8_window(ss_ctx* ctx, const ss_cache8* cache, int32_t window, int32_t sinks,
+                                  const int32_t* valid_len, const int32_t* depth, void* stream);
 
 /* Read (and clear) the device status word after synchronising `stream`, waiting at most
  * timeout_ms (<= 0: wait without limit).  SS_OK, SS_ERR_DEVICE_FLAG (bits in *dev_bits if

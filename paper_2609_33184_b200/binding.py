@@ -22,6 +22,7 @@ STATUS_NAMES = ["SS_OK", "SS_ERR_ARG", "SS_ERR_SHAPE", "SS_ERR_ALIGN", "SS_ERR_S
 (SS_ERR_ARG, SS_ERR_SHAPE, SS_ERR_ALIGN, SS_ERR_STATE, SS_ERR_CAPACITY, SS_ERR_UNSUPPORTED,
  SS_ERR_CUDA, SS_ERR_DEVICE_FLAG, SS_ERR_TIMEOUT) = range(1, 10)
 SS_DEV_BAD_VALID_LEN, SS_DEV_BAD_ACCEPT, SS_DEV_DST_OVERFLOW, SS_DEV_WAIT_EXPIRED, SS_DEV_BAD_PAGE = 1, 2, 4, 8, 16
+SS_DEV_BAD_DEPTH = 32
 SS_FLAG_FORCE_SIMT, SS_FLAG_OVERLAP_CHUNKS, SS_FLAG_ROWS_ON_M, SS_FLAG_KEYS_ON_M, SS_FLAG_STREAM_TIMING = 1, 2, 4, 8, 16
 SS_MASK_CHAIN, SS_MASK_TREE_BITS = 0, 1
 
@@ -35,7 +36,8 @@ EXPORTS = ["ss_workspace_bytes", "ss_create", "ss_destroy", "ss_verify_begin", "
            "ss_width_observe", "ss_width_next", "ss_width_estimate", "ss_cohort_build", "ss_probe_read",
            "ss_selftest_wait_expiry", "ss_verify_abort", "ss_cta_log_set", "ss_get_stats", "ss_verify_round", "ss_verify_chunks",
            "ss_time_rounds", "ss_kv8_write", "ss_kv8_read", "ss_verify_chunk8", "ss_decode8",
-           "ss_rope_init", "ss_rope_rotate", "ss_kv_append", "ss_kv8_append"]
+           "ss_rope_init", "ss_rope_rotate", "ss_kv_append", "ss_kv8_append",
+           "ss_decode_window", "ss_decode8_window", "ss_verify_chunk_window", "ss_verify_chunk8_window"]
 
 
 class ss_stats(C.Structure):
@@ -194,6 +196,12 @@ def load() -> C.CDLL:
     lib.ss_rope_init.argtypes = [rp, i32, i32, i32, C.POINTER(C.c_double), C.POINTER(C.c_int32), C.c_float]
     lib.ss_rope_rotate.restype = C.c_int
     lib.ss_rope_rotate.argtypes = [vp, rp, ss_tensor, ss_tensor, i32, i32, vp, vp, vp, ss_tensor, ss_tensor, vp]
+    for f, cache in ((lib.ss_decode_window, c16), (lib.ss_decode8_window, c8)):
+        f.restype = C.c_int
+        f.argtypes = [vp, ss_tensor, i32, i32, C.c_float, cache, i32, i32, vp, vp, vp, vp]
+    for f, cache in ((lib.ss_verify_chunk_window, c16), (lib.ss_verify_chunk8_window, c8)):
+        f.restype = C.c_int
+        f.argtypes = [vp, cache, i32, i32, vp, vp, vp]
     for f, cache in ((lib.ss_kv_append, c16), (lib.ss_kv8_append, c8)):
         f.restype = C.c_int
         f.argtypes = [vp, cache, ss_tensor, ss_tensor, i32, i32, rp, vp, vp, vp, vp, ss_tensor, ss_tensor, vp]
@@ -402,7 +410,7 @@ class Context:
             raise SpecStreamError(st, "ss_create")
         self.H_q, self.H_kv, self.d = H_q, H_kv, d
         self._dev = device
-        self._B = 0   # requests of the open round
+        self._B = self._T = 0   # requests and queries of the open round
 
     def _sp(self, stream) -> int:
         """cudaStream_t of `stream`, else torch's current stream on this context's device."""
@@ -433,7 +441,7 @@ class Context:
         assert H_q == self.H_q and d == self.d
         self._check(self.lib.ss_verify_begin(self.handle, as_ss_tensor(Q), B, T_q, scale,
                                              self._sp(stream)), "ss_verify_begin")
-        self._B = B
+        self._B, self._T = B, T_q
 
     def ss_verify_chunk(self, K: torch.Tensor, V: torch.Tensor, valid_len: Optional[torch.Tensor] = None,
                         stream=None):
@@ -506,7 +514,7 @@ class Context:
 
     # The calls on the 8-bit cache are made once per step and layer, on small batches with more host
     # than device time: their checks are few and flat.
-    def _cache8(self, cache: Cache8, B: int):
+    def _cache8(self, cache, B: int):
         if cache.H_kv != self.cfg.H_kv or cache.d != self.d or cache.requests < B or cache.device != self._dev:
             raise AssertionError("cache of another shape or device")
         return cache.ref
@@ -555,9 +563,8 @@ class Context:
         if st:
             self._check(st, "ss_verify_chunk8")
 
-    def ss_decode8(self, Q: torch.Tensor, scale: float, cache: Cache8, valid_len: Optional[torch.Tensor],
-                   O: torch.Tensor, LSE: Optional[torch.Tensor] = None, stream=None):
-        """Q [B, H_q, T_q, d] over the first valid_len[b] tokens of the cache -> O (bf16), LSE (fp32 [B, H_q, T_q])."""
+    def _step(self, Q, O, LSE):
+        """B, T_q, Q and the pointers of a decoding call's outputs."""
         shape = Q.shape
         B, H, T, d = shape
         if O.dtype is not torch.bfloat16 or O.shape != shape or O.get_device() != self._dev or not O.is_contiguous():
@@ -565,11 +572,55 @@ class Context:
         if LSE is not None and (LSE.dtype is not torch.float32 or LSE.shape != shape[:3] or
                                 LSE.get_device() != self._dev or not LSE.is_contiguous()):
             raise AssertionError("LSE: contiguous fp32 [B, H_q, T_q] expected", LSE.shape, LSE.dtype)
-        st = self.lib.ss_decode8(self.handle, self._rows(Q, (B, self.H_q, T, self.d)), B, T, scale,
-                                 self._cache8(cache, B), self._i32(valid_len, B), O.data_ptr(),
-                                 None if LSE is None else LSE.data_ptr(), self._sp(stream))
+        return (B, T, self._rows(Q, (B, self.H_q, T, self.d)), O.data_ptr(), None if LSE is None else LSE.data_ptr())
+
+    def ss_decode8(self, Q: torch.Tensor, scale: float, cache: Cache8, valid_len: Optional[torch.Tensor],
+                   O: torch.Tensor, LSE: Optional[torch.Tensor] = None, stream=None):
+        """Q [B, H_q, T_q, d] over the first valid_len[b] tokens of the cache -> O (bf16), LSE (fp32 [B, H_q, T_q])."""
+        B, T, q, o, lse = self._step(Q, O, LSE)
+        st = self.lib.ss_decode8(self.handle, q, B, T, scale, self._cache8(cache, B), self._i32(valid_len, B), o, lse,
+                                 self._sp(stream))
         if st:
             self._check(st, "ss_decode8")
+
+    def _decode_window(self, name, kind, Q, scale, cache, window, sinks, valid_len, O, LSE, stream):
+        if type(cache) is not kind:
+            raise AssertionError("cache of another kind")
+        B, T, q, o, lse = self._step(Q, O, LSE)
+        st = getattr(self.lib, name)(self.handle, q, B, T, scale, self._cache8(cache, B), window, sinks,
+                                     self._i32(valid_len, B), o, lse, self._sp(stream))
+        if st:
+            self._check(st, name)
+
+    def ss_decode_window(self, Q: torch.Tensor, scale: float, cache: Cache16, window: int, sinks: int,
+                         valid_len: Optional[torch.Tensor], O: torch.Tensor, LSE: Optional[torch.Tensor] = None, stream=None):
+        """Q [B, H_q, T_q, d], the newest T_q of the cache's valid_len[b] tokens, over the last `window` tokens of each and
+        the first `sinks` ones -> O (bf16), LSE (fp32 [B, H_q, T_q])."""
+        self._decode_window("ss_decode_window", Cache16, Q, scale, cache, window, sinks, valid_len, O, LSE, stream)
+
+    def ss_decode8_window(self, Q: torch.Tensor, scale: float, cache: Cache8, window: int, sinks: int,
+                          valid_len: Optional[torch.Tensor], O: torch.Tensor, LSE: Optional[torch.Tensor] = None, stream=None):
+        """The same over an 8-bit cache."""
+        self._decode_window("ss_decode8_window", Cache8, Q, scale, cache, window, sinks, valid_len, O, LSE, stream)
+
+    def _chunk_window(self, name, kind, cache, window, sinks, valid_len, depth, stream):
+        if type(cache) is not kind:
+            raise AssertionError("cache of another kind")
+        B = self._B
+        st = getattr(self.lib, name)(self.handle, self._cache8(cache, B), window, sinks, self._i32(valid_len, B),
+                                     self._i32(depth, B * self._T), self._sp(stream))
+        if st:
+            self._check(st, name)
+
+    def ss_verify_chunk_window(self, cache: Cache16, window: int, sinks: int, valid_len: Optional[torch.Tensor] = None,
+                               depth: Optional[torch.Tensor] = None, stream=None):
+        """The window of the cache's tokens that the open round's candidates see; depth int32 [B, T_q]."""
+        self._chunk_window("ss_verify_chunk_window", Cache16, cache, window, sinks, valid_len, depth, stream)
+
+    def ss_verify_chunk8_window(self, cache: Cache8, window: int, sinks: int, valid_len: Optional[torch.Tensor] = None,
+                                depth: Optional[torch.Tensor] = None, stream=None):
+        """The same over an 8-bit cache."""
+        self._chunk_window("ss_verify_chunk8_window", Cache8, cache, window, sinks, valid_len, depth, stream)
 
     def _pair(self, x, out, heads, B, T, what):
         """Rows in and rows out of the same shape (or neither)."""

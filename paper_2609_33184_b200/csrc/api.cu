@@ -1302,7 +1302,6 @@ static ss_status view_cache(const ss_cache8* k, int bits, int32_t B, ss::View8* 
   v->page_tiles = k->page_table && k->page_size > ss::kTok8 ? k->page_size / ss::kTok8 : 1;
   return SS_OK;
 }
-static ss_status view8(const ss_cache8* k, int32_t B, ss::View8* v) { return view_cache(k, 8, B, v); }
 
 static ss_status copy8(ss_ctx* c, bool write, const ss_cache8* cache, ss_tensor K, ss_tensor V, int32_t B, int32_t T,
                        const int32_t* idx, const int32_t* cnt, const int32_t* off, void* stream) {
@@ -1310,7 +1309,7 @@ static ss_status copy8(ss_ctx* c, bool write, const ss_cache8* cache, ss_tensor 
   if (B > c->cfg.max_B || (int64_t)B * T * c->cfg.H_kv * 2 >= (1ll << 31)) return SS_ERR_SHAPE;
   ss::Copy8Params p;
   memset(&p, 0, sizeof(p));
-  const ss_status st = view8(cache, B, &p.kv);
+  const ss_status st = view_cache(cache, 8, B, &p.kv);
   if (st != SS_OK) return st;
   if (!tensor_ok(K) || !tensor_ok(V)) return SS_ERR_ALIGN;
   if (((uintptr_t)idx | (uintptr_t)cnt | (uintptr_t)off) & 3) return SS_ERR_ALIGN;
@@ -1348,10 +1347,29 @@ ss_status ss_kv8_read(ss_ctx* c, const ss_cache8* cache, ss_tensor K, ss_tensor 
   return copy8(c, false, cache, K, V, B, T, nullptr, row_cnt, src_off, stream);
 }
 
-// The attention launch that both entry points share; the caller has set where its result goes.
-static ss_status attn8(ss_ctx* c, const ss_tensor& Q, int32_t B, int32_t T_q, float scale, const ss_cache8* cache,
-                       const int32_t* valid_len, ss::Attn8Params* p, cudaStream_t s) {
-  const ss_status st = view8(cache, B, &p->kv);
+// A window, as the caller gave it (window = 0: none).
+struct Window8 {
+  int32_t window, sinks;
+  const int32_t* depth;
+};
+static ss_status window_ok(const Window8& w) {
+  if (w.window <= 0 || w.sinks < 0) return SS_ERR_ARG;
+  return ((uintptr_t)w.depth & 3) ? SS_ERR_ALIGN : SS_OK;
+}
+// log2 of a window's granules (kv8.cuh): the largest power of two, of 8 to 32 tokens, that a page is a multiple of;
+// 0 for other pages.  Larger ones would leave less out (a layer that sees 4 sinks and 128 tokens reads 160 with
+// granules of 32).
+static int granule_log2(const ss::View8& kv) {
+  if (!kv.page_table) return 5;
+  int g = 0;
+  while (g < 5 && kv.page_size % (2 << g) == 0) ++g;
+  return g >= 3 ? g : 0;
+}
+
+// The attention launch that the entry points share; the caller has set where its result goes.
+static ss_status attn8(ss_ctx* c, int bits, const ss_tensor& Q, int32_t B, int32_t T_q, float scale, const ss_cache8* cache,
+                       const int32_t* valid_len, const Window8& win, ss::Attn8Params* p, cudaStream_t s) {
+  const ss_status st = view_cache(cache, bits, B, &p->kv);
   if (st != SS_OK) return st;
   if (p->kv.room > c->cfg.max_Lc) return SS_ERR_SHAPE;
   if ((uintptr_t)valid_len & 3) return SS_ERR_ALIGN;
@@ -1371,11 +1389,24 @@ static ss_status attn8(ss_ctx* c, const ss_tensor& Q, int32_t B, int32_t T_q, fl
   // hold, take the CUDA cores.
   const int ps = cache->page_size;
   bool tc = c->tc_ok && (!cache->page_table || ps % ss::kTok8 == 0 || (ps >= 8 && ss::kTok8 % ps == 0));
+  int box = cache->page_table && ps < ss::kTok8 ? ps : ss::kTok8;
+  if (win.window) {
+    if (p->kv.room > 0x7fffffff - 16384) return SS_ERR_SHAPE;  // (positions and granules in 32 bits)
+    p->gran_log2 = granule_log2(p->kv);
+    tc = false;
+    box = 1 << p->gran_log2;
+  }
   CUtensorMap tmK, tmV;
   if (tc) {
-    const int box = cache->page_table && ps < ss::kTok8 ? ps : ss::kTok8;
     tc = encode_map(c, cache->K, cache->n_pages, ps, box, 1, &tmK) &&
          encode_map(c, cache->V, cache->n_pages, ps, box, 1, &tmV);
+  }
+  if (win.window) {
+    if (!tc) p->gran_log2 = 0;
+    p->window = (int32_t)(win.window < p->kv.room + T_q ? win.window : p->kv.room + T_q);
+    p->sinks = win.sinks;
+    p->before = p->O ? T_q : 0;
+    p->depth = win.depth;
   }
   const int most = tc ? ss::kRows8 : ss::kMinRows8;  // rows per unit, evenly spread
   p->row_tiles = (p->R + most - 1) / most;
@@ -1394,26 +1425,29 @@ static ss_status attn8(ss_ctx* c, const ss_tensor& Q, int32_t B, int32_t T_q, fl
   // Both kernels wait for the one in front of them before they touch anything, so they can always be
   // launched under programmatic stream serialization (only launch and set-up overlap).
   const bool pdl = !c->no_overlap;
-  cudaError_t e = tc ? ss::launch_attn8_tc(*p, tmK, tmV, s, pdl) : ss::launch_attn8_simt(*p, s, pdl);
+  cudaError_t e = tc ? ss::launch_attn8_tc(*p, tmK, tmV, s, pdl) : ss::launch_attn8_simt(*p, bits, s, pdl);
   if (e != cudaSuccess) return cuda_fail(c, e);
-  c->last_kernel = tc ? "kv8-tcgen05" : "kv8-simt";
+  c->last_kernel = win.window ? (bits == 8 ? "window8-simt" : "window-simt") : tc ? "kv8-tcgen05" : "kv8-simt";
   ++c->launches;
-  if (p->O && p->kv.room > ss::kTok8) {  // (a unit of one tile is never cut; a round joins later)
+  const int64_t most_seen = (int64_t)win.window + win.sinks + T_q;
+  const int64_t tokens = win.window && most_seen < p->kv.room ? most_seen : p->kv.room;  // most of a request that are read
+  if (p->O && tokens + 2 * 32 > ss::kTok8) {  // (a unit of one tile is never cut; a round joins later)
     e = ss::launch_attn8_join(*p, false, s, pdl);
     if (e != cudaSuccess) return cuda_fail(c, e);
     ++c->launches;
   }
   ++c->stats.chunk_calls;
-  c->stats.kv_bytes += (int64_t)B * p->kv.room * c->cfg.H_kv * (c->cfg.d + 1) * 2;
+  c->stats.kv_bytes += B * tokens * c->cfg.H_kv * (bits == 8 ? c->cfg.d + 1 : 2 * c->cfg.d) * 2;
   return SS_OK;
 }
 
-ss_status ss_verify_chunk8(ss_ctx* c, const ss_cache8* cache, const int32_t* valid_len, void* stream) {
-  if (!c || !cache) return SS_ERR_ARG;
+// A chunk of the open round from a cache.
+static ss_status chunk8(ss_ctx* c, int bits, const ss_cache8* cache, const int32_t* valid_len, const Window8& win,
+                        void* stream) {
   if (c->state != ss_ctx::OPEN || (cudaStream_t)stream != c->stream) return SS_ERR_STATE;
   ss::Attn8Params p;
   memset(&p, 0, sizeof(p));
-  ss_status st = view8(cache, c->B, &p.kv);  // (before a fold is enqueued)
+  ss_status st = view_cache(cache, bits, c->B, &p.kv);  // (before a fold is enqueued)
   if (st != SS_OK) return st;
   if (p.kv.room > c->cfg.max_Lc) return SS_ERR_SHAPE;
   if ((uintptr_t)valid_len & 3) return SS_ERR_ALIGN;
@@ -1426,7 +1460,7 @@ ss_status ss_verify_chunk8(ss_ctx* c, const ss_cache8* cache, const int32_t* val
   p.part_ml = c->part_ml + (int64_t)c->n_sets * c->set_stride_ml;
   p.part_a = c->part_a + (int64_t)c->n_sets * c->set_stride_a;
   p.R_stride = c->R_stride;
-  st = attn8(c, c->Q, c->B, c->T_q, c->scale, cache, valid_len, &p, c->stream);
+  st = attn8(c, bits, c->Q, c->B, c->T_q, c->scale, cache, valid_len, win, &p, c->stream);
   if (st != SS_OK) return st;
   c->splits[c->n_sets] = 1;
   memset(c->absent[c->n_sets], 0, sizeof(c->absent[0]));
@@ -1437,9 +1471,11 @@ ss_status ss_verify_chunk8(ss_ctx* c, const ss_cache8* cache, const int32_t* val
   return SS_OK;
 }
 
-ss_status ss_decode8(ss_ctx* c, ss_tensor Q, int32_t B, int32_t T_q, float scale, const ss_cache8* cache,
-                     const int32_t* valid_len, void* O, float* LSE, void* stream) {
-  if (!c || !Q.ptr || !cache || !O) return SS_ERR_ARG;
+// Attention over a cache alone.
+static ss_status decode8(ss_ctx* c, int bits, const ss_tensor& Q, int32_t B, int32_t T_q, float scale,
+                         const ss_cache8* cache, const int32_t* valid_len, const Window8& win, void* O, float* LSE,
+                         void* stream) {
+  if (!Q.ptr || !O) return SS_ERR_ARG;
   if (B <= 0 || T_q <= 0) return SS_ERR_ARG;
   if (!(scale > 0.f) || !(scale < 3.0e38f)) return SS_ERR_ARG;
   if (B > c->cfg.max_B || T_q > c->cfg.max_Tq) return SS_ERR_SHAPE;
@@ -1449,11 +1485,58 @@ ss_status ss_decode8(ss_ctx* c, ss_tensor Q, int32_t B, int32_t T_q, float scale
   memset(&p, 0, sizeof(p));
   p.O = (__nv_bfloat16*)O;
   p.LSE = LSE;
-  const ss_status st = attn8(c, Q, B, T_q, scale, cache, valid_len, &p, (cudaStream_t)stream);
+  const ss_status st = attn8(c, bits, Q, B, T_q, scale, cache, valid_len, win, &p, (cudaStream_t)stream);
   if (st != SS_OK) return st;
   ++c->stats.rounds;
   c->stats.rows += (int64_t)B * c->cfg.H_q * T_q;
   return SS_OK;
+}
+
+ss_status ss_verify_chunk8(ss_ctx* c, const ss_cache8* cache, const int32_t* valid_len, void* stream) {
+  if (!c || !cache) return SS_ERR_ARG;
+  return chunk8(c, 8, cache, valid_len, Window8{}, stream);
+}
+
+ss_status ss_decode8(ss_ctx* c, ss_tensor Q, int32_t B, int32_t T_q, float scale, const ss_cache8* cache,
+                     const int32_t* valid_len, void* O, float* LSE, void* stream) {
+  if (!c || !cache) return SS_ERR_ARG;
+  return decode8(c, 8, Q, B, T_q, scale, cache, valid_len, Window8{}, O, LSE, stream);
+}
+
+ss_status ss_verify_chunk_window(ss_ctx* c, const ss_cache16* cache, int32_t window, int32_t sinks,
+                                 const int32_t* valid_len, const int32_t* depth, void* stream) {
+  if (!c || !cache) return SS_ERR_ARG;
+  const Window8 w = {window, sinks, depth};
+  const ss_status st = window_ok(w);
+  if (st != SS_OK) return st;
+  const ss_cache8 bytes = bytes_of(*cache);
+  return chunk8(c, 16, &bytes, valid_len, w, stream);
+}
+
+ss_status ss_verify_chunk8_window(ss_ctx* c, const ss_cache8* cache, int32_t window, int32_t sinks,
+                                  const int32_t* valid_len, const int32_t* depth, void* stream) {
+  if (!c || !cache) return SS_ERR_ARG;
+  const Window8 w = {window, sinks, depth};
+  const ss_status st = window_ok(w);
+  return st != SS_OK ? st : chunk8(c, 8, cache, valid_len, w, stream);
+}
+
+ss_status ss_decode_window(ss_ctx* c, ss_tensor Q, int32_t B, int32_t T_q, float scale, const ss_cache16* cache,
+                           int32_t window, int32_t sinks, const int32_t* valid_len, void* O, float* LSE, void* stream) {
+  if (!c || !cache) return SS_ERR_ARG;
+  const Window8 w = {window, sinks, nullptr};
+  const ss_status st = window_ok(w);
+  if (st != SS_OK) return st;
+  const ss_cache8 bytes = bytes_of(*cache);
+  return decode8(c, 16, Q, B, T_q, scale, &bytes, valid_len, w, O, LSE, stream);
+}
+
+ss_status ss_decode8_window(ss_ctx* c, ss_tensor Q, int32_t B, int32_t T_q, float scale, const ss_cache8* cache,
+                            int32_t window, int32_t sinks, const int32_t* valid_len, void* O, float* LSE, void* stream) {
+  if (!c || !cache) return SS_ERR_ARG;
+  const Window8 w = {window, sinks, nullptr};
+  const ss_status st = window_ok(w);
+  return st != SS_OK ? st : decode8(c, 8, Q, B, T_q, scale, cache, valid_len, w, O, LSE, stream);
 }
 
 // ---- rotary positions, rows that join a cache ----------------------------------------------------

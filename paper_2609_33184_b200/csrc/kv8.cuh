@@ -66,6 +66,11 @@ struct Attn8Params {
   float* part_a;
   int R_stride;
   uint32_t* status;
+  // attention over a window (window = 0: over all tokens), see Span8
+  int window, sinks;
+  int before;                 // the first query stands at position len - before
+  int gran_log2;              // tokens are left out in granules of 2^gran_log2
+  const int32_t* depth;       // [B, T_q] positions behind the first query's, or null: query t at t
 };
 
 struct Final8 {               // end of a round
@@ -86,7 +91,7 @@ struct Copy8Params {          // write (bf16 -> cache) and read (cache -> bf16)
 
 cudaError_t launch_kv8_write(const Copy8Params& p, cudaStream_t s, bool pdl);
 cudaError_t launch_kv8_read(const Copy8Params& p, cudaStream_t s, bool pdl);
-cudaError_t launch_attn8_simt(const Attn8Params& p, cudaStream_t s, bool pdl);
+cudaError_t launch_attn8_simt(const Attn8Params& p, int bits, cudaStream_t s, bool pdl);  // bits: of the cache, 8 or 16
 cudaError_t launch_attn8_tc(const Attn8Params& p, const CUtensorMap& tmK, const CUtensorMap& tmV, cudaStream_t s, bool pdl);
 cudaError_t launch_attn8_join(const Attn8Params& p, bool from_plan, cudaStream_t s, bool pdl);
 cudaError_t launch_attn8_finalize(const Attn8Params& p, const Final8& out, cudaStream_t s, bool pdl);
@@ -98,10 +103,43 @@ __device__ __forceinline__ float scale8(uint32_t byte) { return __int_as_float((
 __device__ __forceinline__ uint32_t byte8(uint32_t byte) { return min(max(byte, (uint32_t)(kMinExp8 + 127)), (uint32_t)(kMaxExp8 + 127)); }
 
 // Length of a request in tokens, clamped to [0, room] (find_share8 reports one outside).
-__device__ __forceinline__ int len8(const Attn8Params& p, int b) {
+__device__ __forceinline__ int room_len8(const Attn8Params& p, int b) {
   if (!p.valid_len) return p.kv.room;
   const int v = p.valid_len[b];
   return max(0, min(v, p.kv.room));
+}
+
+// Window.  The queries of a request of n tokens stand at positions first .. first + T_q - 1, first = n - before (the
+// newest tokens: before = T_q; candidates behind the cache: 0); a query at position p sees token j when j <= p and
+// (j < sinks or p - j < window).  No query sees a token between the sinks and first + 1 - window, so these are
+// left out, in whole granules (a granule lies in one page, is a whole number of swizzle atoms and what one copy
+// brings), and what remains is numbered through: kernels walk `len` tokens as they walk a request of that
+// length, token v being token v of the request below `cut` and v + skip from there on.  Every granule left has a
+// token that some query sees, so no page without one is looked up.
+struct Span8 {
+  int len, cut, skip;
+};
+__device__ __forceinline__ Span8 span8(const Attn8Params& p, int n) {
+  const int up = (1 << p.gran_log2) - 1;
+  const int lo = max(0, n - p.before + 1 - p.window);
+  const int head = (min(p.sinks, n) + up) & ~up, from = lo & ~up;
+  if (lo >= n) return {min(head, n), 0, 0};   // the window begins behind the cache
+  if (from <= head) return {n, 0, 0};
+  return {n - (from - head), head, from - head};
+}
+// How far behind the first query query t stands (outside [0, T_q): reported and clamped).
+__device__ __forceinline__ int depth8(const Attn8Params& p, int b, int t) {
+  if (!p.depth) return t;
+  const int d = p.depth[(int64_t)b * p.T_q + t];
+  if (d >= 0 && d < p.T_q) return d;
+  atomicOr(p.status, SS_DEV_BAD_DEPTH);
+  return max(0, min(d, p.T_q - 1));
+}
+// Tokens of a request as the kernels walk them.
+template <bool WIN = false>
+__device__ __forceinline__ int len8(const Attn8Params& p, int b) {
+  const int n = room_len8(p, b);
+  return WIN ? span8(p, n).len : n;
 }
 __device__ __forceinline__ int tiles8(int len) { return (len + kTok8 - 1) / kTok8; }
 
@@ -142,6 +180,7 @@ __device__ __forceinline__ void set_shares8(uint32_t most, Share8* s) {
 
 // Tiles (all kv-heads) of requests b0 + 4 * lane .. + 3: 128 requests per step of a warp, whose loads go
 // out together.
+template <bool WIN = false>
 __device__ __forceinline__ uint32_t tiles_of_four8(const Attn8Params& p, int b0, uint32_t (&n)[4], bool* bad) {
   const uint32_t units = (uint32_t)p.H_kv;
   const int b = b0 + 4 * (threadIdx.x & 31);
@@ -152,7 +191,9 @@ __device__ __forceinline__ uint32_t tiles_of_four8(const Attn8Params& p, int b0,
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     *bad |= len[j] < 0 || len[j] > p.kv.room;
-    n[j] = units * tiles8(max(0, min(len[j], p.kv.room)));
+    len[j] = max(0, min(len[j], p.kv.room));
+    if (WIN) len[j] = span8(p, len[j]).len;
+    n[j] = units * tiles8(len[j]);
     sum += n[j];
   }
   return sum;
@@ -167,13 +208,14 @@ __device__ __forceinline__ uint32_t warp_scan8(uint32_t v) {  // inclusive
 }
 
 // By one whole warp.  CTA 0 also reports lengths that had to be clamped.
+template <bool WIN = false>
 __device__ __forceinline__ Share8 find_share8(const Attn8Params& p) {
   const int lane = threadIdx.x & 31;
   Share8 s = {};
   uint32_t n[4], sum = 0, mine = 0;
   bool bad = false;
 #pragma unroll 1
-  for (int b = 0; b < p.B; b += 128) sum += mine = tiles_of_four8(p, b, n, &bad);
+  for (int b = 0; b < p.B; b += 128) sum += mine = tiles_of_four8<WIN>(p, b, n, &bad);
   if (blockIdx.x == 0 && __any_sync(0xffffffffu, bad) && lane == 0) atomicOr(p.status, SS_DEV_BAD_VALID_LEN);
   s.total = __reduce_add_sync(0xffffffffu, sum);
   s.idx = blockIdx.x;
@@ -188,7 +230,7 @@ __device__ __forceinline__ Share8 find_share8(const Attn8Params& p) {
   uint32_t base = 0;
 #pragma unroll 1
   for (int b = 0; b < p.B; b += 128) {
-    if (p.B > 128) mine = tiles_of_four8(p, b, n, &bad);  // (else still there)
+    if (p.B > 128) mine = tiles_of_four8<WIN>(p, b, n, &bad);  // (else still there)
     const uint32_t incl = warp_scan8(mine);
     const unsigned past = __ballot_sync(0xffffffffu, base + incl > s.lo);
     if (past) {
@@ -215,7 +257,7 @@ __device__ __forceinline__ Share8 find_share8(const Attn8Params& p) {
 struct Seg8 {
   int b, kvh;
   int t0, t1, n;            // tiles [t0, t1) of the unit's n
-  int len;                  // tokens of the request
+  int len;                  // tokens of the request (window: those that remain)
   uint32_t base, start, pos;  // tiles before the request, before the unit, before the segment's end
   int row0, nrows;
 };
@@ -229,16 +271,18 @@ __device__ __forceinline__ void seg_set8(const Attn8Params& p, const Share8& s, 
   g->row0 = (int)s.rt * p.rows_per_tile;
   g->nrows = min(p.rows_per_tile, p.R - g->row0);
 }
+template <bool WIN = false>
 __device__ __forceinline__ bool seg_first8(const Attn8Params& p, const Share8& s, Seg8* g) {
   if (s.lo >= s.hi) return false;
   g->b = s.b0;
-  g->len = len8(p, g->b);
+  g->len = len8<WIN>(p, g->b);
   g->n = tiles8(g->len);
   g->pos = s.lo;
   g->base = s.base0;
   seg_set8(p, s, g);
   return true;
 }
+template <bool WIN = false>
 __device__ __forceinline__ bool seg_next8(const Attn8Params& p, const Share8& s, Seg8* g) {
   if (g->pos >= s.hi) return false;
   const uint32_t units = (uint32_t)p.H_kv;
@@ -246,7 +290,7 @@ __device__ __forceinline__ bool seg_next8(const Attn8Params& p, const Share8& s,
   while (g->pos >= g->base + units * g->n) {  // the next request with tokens (there is one: pos < hi <= total)
     g->base += units * g->n;
     ++g->b;
-    g->len = len8(p, g->b);
+    g->len = len8<WIN>(p, g->b);
     g->n = tiles8(g->len);
   }
   seg_set8(p, s, g);
@@ -275,10 +319,11 @@ __device__ __forceinline__ void put_a8(const Attn8Params& p, const Seg8& g, int 
 }
 // Requests without a visible token, by `n` threads of every CTA.  (Out of line, not unrolled: what a
 // kernel seldom runs should not stand between the parts that it always runs.)
+template <bool WIN = false>
 static __device__ __noinline__ void put_empty8(const Attn8Params& p, int tid, int n) {
 #pragma unroll 1
   for (int b = blockIdx.x; b < p.B; b += gridDim.x) {
-    if (len8(p, b) > 0) continue;
+    if (len8<WIN>(p, b) > 0) continue;
     const int rows = p.H_kv * p.R;
 #pragma unroll 1
     for (int i = tid; i < rows; i += n) {
@@ -295,13 +340,14 @@ static __device__ __noinline__ void put_empty8(const Attn8Params& p, int tid, in
 
 // The record of the lengths that this launch went by, for a join that runs later: by one warp of the
 // last CTA, which has the least to do.
+template <bool WIN = false>
 static __device__ __noinline__ void put_plan8(const Attn8Params& p) {
   const int lane = threadIdx.x & 31;
   uint32_t base = 0, n[4];
   bool bad = false;
 #pragma unroll 1
   for (int b = 0; b < p.B; b += 128) {
-    const uint32_t mine = tiles_of_four8(p, b, n, &bad), incl = warp_scan8(mine);
+    const uint32_t mine = tiles_of_four8<WIN>(p, b, n, &bad), incl = warp_scan8(mine);
     uint32_t before = base + incl - mine;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {

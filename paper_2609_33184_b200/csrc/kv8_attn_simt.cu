@@ -1,5 +1,5 @@
-// Attention over the 8-bit KV cache on the CUDA cores: any page size, any strides the tensor maps
-// cannot express, and head dims 64 and 128.
+// Attention over the 8-bit KV cache, and over a window of it or of a bf16 one, on the CUDA cores: any page
+// size, any strides the tensor maps cannot express, and head dims 64 and 128.
 //
 // A CTA walks its share of the tiles (kv8.cuh) for tiles of 8 query rows.  Each of its four warps
 // takes 32 keys of a 128-token tile, one per lane: the lane reads its key's codes 16 bytes at a
@@ -33,20 +33,57 @@ __device__ __forceinline__ float warp_sum8(float v) {
   return v;
 }
 
-template <int D>
+// 16 values of a row of the cache, from value c on (zeros where there is no row).
+template <int BITS>
+__device__ __forceinline__ void load16(const uint8_t* row, int c, bool there, float2 (&x)[8]) {
+  if (BITS == 8) {
+    uint4 raw = make_uint4(0, 0, 0, 0);
+    if (there) raw = *reinterpret_cast<const uint4*>(row + c);
+    const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = f2_of_e4m3x2((w[j / 2] >> (16 * (j & 1))) & 0xffffu);
+  } else {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      uint4 raw = make_uint4(0, 0, 0, 0);
+      if (there) raw = *reinterpret_cast<const uint4*>(row + 2 * c + 16 * h);
+      const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        x[4 * h + j] = make_float2(__uint_as_float(w[j] << 16), __uint_as_float(w[j] & 0xffff0000u));
+    }
+  }
+}
+template <int BITS>
+__device__ __forceinline__ float2 load2(const uint8_t* row, int c) {
+  if (BITS == 8) return f2_of_e4m3x2(*reinterpret_cast<const uint16_t*>(row + c));
+  const uint32_t w = *reinterpret_cast<const uint32_t*>(row + 2 * c);
+  return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+}
+
+template <int D, int BITS, bool WIN>
 __global__ void __launch_bounds__(128) attn8_simt_kernel(const __grid_constant__ Attn8Params p) {
   constexpr int CPL = D / 32;  // head dims per lane in the output
   __shared__ __align__(16) float q_s[kRT][D];
   __shared__ __align__(16) float w_s[4][32][kRT];
   __shared__ float2 ml_s[4][kRT];
   __shared__ float a_s[4][kRT][D];
+  __shared__ int pos_s[kRT];   // (window) the rows' positions
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   pdl_wait_prior();
   pdl_launch_dependents();
-  const Share8 share = find_share8(p);
+  const Share8 share = find_share8<WIN>(p);
   Seg8 g;
-  for (bool more = seg_first8(p, share, &g); more; more = seg_next8(p, share, &g)) {
+  for (bool more = seg_first8<WIN>(p, share, &g); more; more = seg_next8<WIN>(p, share, &g)) {
     __syncthreads();  // the previous segment's shared memory has been read
+    Span8 span = {};
+    int sinks = 0;
+    if (WIN) {
+      const int n = room_len8(p, g.b);
+      span = span8(p, n);
+      sinks = min(p.sinks, n);
+      if (tid < g.nrows) pos_s[tid] = n - p.before + depth8(p, g.b, (g.row0 + tid) % p.T_q);
+    }
     for (int i = tid; i < kRT * D; i += 128) {
       const int r = i / D, c = i % D;
       float v = 0.f;
@@ -68,9 +105,10 @@ __global__ void __launch_bounds__(128) attn8_simt_kernel(const __grid_constant__
       for (int c = 0; c < CPL; ++c) acc[r][c] = 0.f;
     }
     for (int t = g.t0; t < g.t1; ++t) {
-      const int tok0 = t * kTok8 + warp * 32, tok = tok0 + lane;
+      const int tok0 = t * kTok8 + warp * 32, v_tok = tok0 + lane;
       if (tok0 >= g.len) continue;
-      const bool ok = tok < g.len;
+      const bool ok = v_tok < g.len;
+      const int tok = WIN && v_tok >= span.cut ? v_tok + span.skip : v_tok;
       int inner = 0, outer = -1;
       if (ok) {
         outer = outer8(p.kv, g.b, tok, &inner);
@@ -83,12 +121,11 @@ __global__ void __launch_bounds__(128) attn8_simt_kernel(const __grid_constant__
         const uint8_t* k = p.kv.K + outer * p.kv.k_sb + g.kvh * p.kv.k_sh + inner * p.kv.k_st;
 #pragma unroll 2
         for (int c16 = 0; c16 < D; c16 += 16) {
-          uint4 raw = make_uint4(0, 0, 0, 0);
-          if (outer >= 0) raw = *reinterpret_cast<const uint4*>(k + c16);
-          const uint32_t w4[4] = {raw.x, raw.y, raw.z, raw.w};
+          float2 x[8];
+          load16<BITS>(k, c16, outer >= 0, x);
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const float2 k01 = f2_of_e4m3x2(w4[j] & 0xffffu), k23 = f2_of_e4m3x2(w4[j] >> 16);
+            const float2 k01 = x[2 * j], k23 = x[2 * j + 1];
 #pragma unroll
             for (int r = 0; r < kRT; ++r) {
               const float4 q = *reinterpret_cast<const float4*>(&q_s[r][c16 + j * 4]);
@@ -97,7 +134,7 @@ __global__ void __launch_bounds__(128) attn8_simt_kernel(const __grid_constant__
           }
         }
         uint32_t ek = 127, ev = 127;
-        if (outer >= 0) {
+        if (BITS == 8 && outer >= 0) {
           ek = p.kv.Ks[outer * p.kv.ks_sb + g.kvh * p.kv.ks_sh + inner * p.kv.ks_st];
           ev = p.kv.Vs[outer * p.kv.vs_sb + g.kvh * p.kv.vs_sh + inner * p.kv.vs_st];
         }
@@ -108,11 +145,12 @@ __global__ void __launch_bounds__(128) attn8_simt_kernel(const __grid_constant__
       }
 #pragma unroll
       for (int r = 0; r < kRT; ++r) {
-        const float x = ok ? s[r] : -INFINITY;
+        const bool seen = ok && (!WIN || (r < g.nrows && tok <= pos_s[r] && (tok < sinks || pos_s[r] - tok < p.window)));
+        const float x = seen ? s[r] : -INFINITY;
         const float top = fmaxf(m[r], warp_max8(x));
         const float f = (m[r] == top) ? 1.f : exp2f(m[r] - top);  // (equal also when both are -inf)
         // (no finite score so far: weight 0, except that a NaN score has to show)
-        const float w = !ok ? 0.f : (top == -INFINITY && x == x) ? 0.f : exp2f(x - top);
+        const float w = !seen ? 0.f : (top == -INFINITY && x == x) ? 0.f : exp2f(x - top);
         m[r] = top;
         l[r] = fmaf(l[r], f, w);
 #pragma unroll
@@ -125,19 +163,13 @@ __global__ void __launch_bounds__(128) attn8_simt_kernel(const __grid_constant__
       for (int j = 0; j < n; ++j) {
         const int o = __shfl_sync(0xffffffffu, outer, j), in = __shfl_sync(0xffffffffu, inner, j);
         if (o < 0) continue;
-        const uint8_t* v = p.kv.V + o * p.kv.v_sb + g.kvh * p.kv.v_sh + in * p.kv.v_st + lane * CPL;
+        const uint8_t* v = p.kv.V + o * p.kv.v_sb + g.kvh * p.kv.v_sh + in * p.kv.v_st + lane * CPL * (BITS / 8);
         float x[CPL];
-        if (CPL == 4) {
-          const uint32_t raw = *reinterpret_cast<const uint32_t*>(v);
-          const float2 a = f2_of_e4m3x2(raw & 0xffffu), b = f2_of_e4m3x2(raw >> 16);
-          x[0] = a.x;
-          x[1] = a.y;
-          x[CPL - 2] = b.x;
-          x[CPL - 1] = b.y;
-        } else {
-          const float2 a = f2_of_e4m3x2(*reinterpret_cast<const uint16_t*>(v));
-          x[0] = a.x;
-          x[1] = a.y;
+#pragma unroll
+        for (int c = 0; c < CPL; c += 2) {
+          const float2 a = load2<BITS>(v, c);
+          x[c] = a.x;
+          x[c + 1] = a.y;
         }
         float wr[kRT];
         *reinterpret_cast<float4*>(wr) = *reinterpret_cast<const float4*>(&w_s[warp][j][0]);
@@ -182,16 +214,18 @@ __global__ void __launch_bounds__(128) attn8_simt_kernel(const __grid_constant__
       }
     }
   }
-  if ((int)blockIdx.x < p.B) put_empty8(p, tid, 128);
-  if (p.plan && warp == 0 && blockIdx.x == gridDim.x - 1) put_plan8(p);
+  if ((int)blockIdx.x < p.B) put_empty8<WIN>(p, tid, 128);
+  if (p.plan && warp == 0 && blockIdx.x == gridDim.x - 1) put_plan8<WIN>(p);
 }
 
 }  // namespace
 
-cudaError_t launch_attn8_simt(const Attn8Params& p, cudaStream_t s, bool pdl) {
+cudaError_t launch_attn8_simt(const Attn8Params& p, int bits, cudaStream_t s, bool pdl) {
   const dim3 grid(p.shares * p.row_tiles), block(128);
-  return p.d == 128 ? launch_kernel(attn8_simt_kernel<128>, grid, block, 0, s, pdl, p)
-                    : launch_kernel(attn8_simt_kernel<64>, grid, block, 0, s, pdl, p);
+  auto kernel = !p.window   ? (p.d == 128 ? attn8_simt_kernel<128, 8, false> : attn8_simt_kernel<64, 8, false>)
+                : bits == 8 ? (p.d == 128 ? attn8_simt_kernel<128, 8, true> : attn8_simt_kernel<64, 8, true>)
+                            : (p.d == 128 ? attn8_simt_kernel<128, 16, true> : attn8_simt_kernel<64, 16, true>);
+  return launch_kernel(kernel, grid, block, 0, s, pdl, p);
 }
 
 }  // namespace ss

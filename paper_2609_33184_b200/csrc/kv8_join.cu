@@ -44,10 +44,11 @@ __device__ __forceinline__ Row8 row8(const Attn8Params& p, int64_t row, int lane
     g.n = (int)((__ldcg(&p.plan[g.b + 1]) - before) / units);
     s.total = __ldcg(&p.plan[p.B]);
   } else {
-    g.n = tiles8(len8(p, g.b));
+    const auto tiles = [&](int b) { return tiles8(p.window ? len8<true>(p, b) : len8(p, b)); };
+    g.n = tiles(g.b);
     uint32_t sum = 0;
     for (int b = lane; b < p.B; b += 32) {
-      const uint32_t n = units * tiles8(len8(p, b));
+      const uint32_t n = units * tiles(b);
       sum += n;
       if (b < g.b) before += n;
     }
