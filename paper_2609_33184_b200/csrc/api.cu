@@ -477,6 +477,7 @@ ss_status ss_create(ss_ctx** out, const ss_config* cfg, void* workspace, size_t 
     e = ss::chunk_tc_prepare();
     if (e == cudaSuccess) e = ss::chunk_tc_keys_prepare();
     if (e == cudaSuccess) e = ss::attn8_tc_prepare();
+    if (e == cudaSuccess) e = ss::window_tc_prepare();
     if (e != cudaSuccess) {
       delete c;
       return SS_ERR_CUDA;
@@ -1393,11 +1394,15 @@ static ss_status attn8(ss_ctx* c, int bits, const ss_tensor& Q, int32_t B, int32
   if (win.window) {
     if (p->kv.room > 0x7fffffff - 16384) return SS_ERR_SHAPE;  // (positions and granules in 32 bits)
     p->gran_log2 = granule_log2(p->kv);
-    tc = false;
+    tc = c->tc_ok && p->gran_log2 && bits == 16;
     box = 1 << p->gran_log2;
   }
   CUtensorMap tmK, tmV;
-  if (tc) {
+  if (tc && bits == 16) {
+    const auto elements = [](const ss_tensor& t) { return ss_tensor{t.ptr, t.stride_b / 2, t.stride_h / 2, t.stride_t / 2}; };
+    tc = get_tensor_map(c, elements(cache->K), cache->n_pages, ps, box, &tmK) &&
+         get_tensor_map(c, elements(cache->V), cache->n_pages, ps, box, &tmV);
+  } else if (tc) {
     tc = encode_map(c, cache->K, cache->n_pages, ps, box, 1, &tmK) &&
          encode_map(c, cache->V, cache->n_pages, ps, box, 1, &tmV);
   }
@@ -1414,7 +1419,7 @@ static ss_status attn8(ss_ctx* c, int bits, const ss_tensor& Q, int32_t B, int32
   // (the kernels number all tiles in 31 bits)
   if ((int64_t)B * ((p->kv.room + ss::kTok8 - 1) / ss::kTok8) * p->H_kv >= (1ll << 31)) return SS_ERR_SHAPE;
   // as many CTAs as are resident, and one for every row tile at least
-  p->shares = (tc && p->d == 64 && p->rows_per_tile <= ss::kFew8 ? ss::kCtasFew8 : ss::kCtas8) / p->row_tiles;
+  p->shares = (tc && bits == 8 && p->d == 64 && p->rows_per_tile <= ss::kFew8 ? ss::kCtasFew8 : ss::kCtas8) / p->row_tiles;
   if (p->shares < 1) p->shares = 1;
   p->scale_log2 = scale * 1.4426950408889634f;
   p->scratch = c->scratch8;
@@ -1425,9 +1430,13 @@ static ss_status attn8(ss_ctx* c, int bits, const ss_tensor& Q, int32_t B, int32
   // Both kernels wait for the one in front of them before they touch anything, so they can always be
   // launched under programmatic stream serialization (only launch and set-up overlap).
   const bool pdl = !c->no_overlap;
-  cudaError_t e = tc ? ss::launch_attn8_tc(*p, tmK, tmV, s, pdl) : ss::launch_attn8_simt(*p, bits, s, pdl);
+  cudaError_t e = !tc          ? ss::launch_attn8_simt(*p, bits, s, pdl)
+                  : bits == 16 ? ss::launch_window_tc(*p, tmK, tmV, s, pdl)
+                               : ss::launch_attn8_tc(*p, tmK, tmV, s, pdl);
   if (e != cudaSuccess) return cuda_fail(c, e);
-  c->last_kernel = win.window ? (bits == 8 ? "window8-simt" : "window-simt") : tc ? "kv8-tcgen05" : "kv8-simt";
+  c->last_kernel = !win.window ? (tc ? "kv8-tcgen05" : "kv8-simt")
+                   : bits == 8 ? (tc ? "window8-tcgen05" : "window8-simt")
+                               : (tc ? "window-tcgen05" : "window-simt");
   ++c->launches;
   const int64_t most_seen = (int64_t)win.window + win.sinks + T_q;
   const int64_t tokens = win.window && most_seen < p->kv.room ? most_seen : p->kv.room;  // most of a request that are read

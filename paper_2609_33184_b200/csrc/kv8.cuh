@@ -96,6 +96,8 @@ cudaError_t launch_attn8_tc(const Attn8Params& p, const CUtensorMap& tmK, const 
 cudaError_t launch_attn8_join(const Attn8Params& p, bool from_plan, cudaStream_t s, bool pdl);
 cudaError_t launch_attn8_finalize(const Attn8Params& p, const Final8& out, cudaStream_t s, bool pdl);
 cudaError_t attn8_tc_prepare();  // one-time function attributes
+cudaError_t launch_window_tc(const Attn8Params& p, const CUtensorMap& tmK, const CUtensorMap& tmV, cudaStream_t s, bool pdl);
+cudaError_t window_tc_prepare();
 
 // ---- device side ---------------------------------------------------------------------------
 __device__ __forceinline__ float pow2_8(int e) { return __int_as_float((e + 127) << 23); }  // |e| <= 126
@@ -317,6 +319,34 @@ __device__ __forceinline__ void put_a8(const Attn8Params& p, const Seg8& g, int 
     p.part_a[(((int64_t)g.b * p.H_kv + g.kvh) * p.R_stride + g.row0 + r) * p.d + c] = a;
   }
 }
+// A segment's window, for the kernels' masks.
+struct Win8 {
+  int cut, skip;              // see Span8
+  int n, sinks;               // tokens of the request, how many of them are sinks
+  int first;                  // position of the first query
+};
+__device__ __forceinline__ Win8 win8(const Attn8Params& p, int b) {
+  const int n = room_len8(p, b);
+  const Span8 s = span8(p, n);
+  return {s.cut, s.skip, n, min(p.sinks, n), n - p.before};
+}
+// Token of the request that the walk's token v is.
+__device__ __forceinline__ int win_token8(const Win8& w, int v) { return v < w.cut ? v : v + w.skip; }
+// Does every query see every token of tile t?
+__device__ __forceinline__ bool win_plain8(const Attn8Params& p, const Win8& w, int t) {
+  const int v0 = t * kTok8, v1 = v0 + kTok8 - 1;
+  const int j0 = win_token8(w, v0), j1 = win_token8(w, v1);
+  if (j1 >= w.n || j1 > w.first || (v0 < w.cut && v1 >= w.cut)) return false;
+  return j1 < w.sinks || j0 > w.first + p.T_q - 1 - p.window;
+}
+// Does some query see token j (one that is left)?
+__device__ __forceinline__ bool win_any8(const Attn8Params& p, const Win8& w, int j) {
+  return j < w.n && (j < w.sinks || j > w.first - p.window);
+}
+__device__ __forceinline__ bool win_sees8(const Attn8Params& p, const Win8& w, int pos, int j) {
+  return j <= pos && j < w.n && (j < w.sinks || pos - j < p.window);
+}
+
 // Requests without a visible token, by `n` threads of every CTA.  (Out of line, not unrolled: what a
 // kernel seldom runs should not stand between the parts that it always runs.)
 template <bool WIN = false>
