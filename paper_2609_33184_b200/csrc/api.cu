@@ -1394,7 +1394,7 @@ static ss_status attn8(ss_ctx* c, int bits, const ss_tensor& Q, int32_t B, int32
   if (win.window) {
     if (p->kv.room > 0x7fffffff - 16384) return SS_ERR_SHAPE;  // (positions and granules in 32 bits)
     p->gran_log2 = granule_log2(p->kv);
-    tc = c->tc_ok && p->gran_log2 && bits == 16;
+    tc = c->tc_ok && p->gran_log2;
     box = 1 << p->gran_log2;
   }
   CUtensorMap tmK, tmV;

@@ -157,6 +157,13 @@ __device__ __forceinline__ int outer8(const View8& kv, int b, int tok, int* inne
   return (id < 0 || id >= kv.n_outer) ? -1 : id;
 }
 
+// Page id of token *inner of request b, which becomes the token within its page (id not checked).
+__device__ __forceinline__ int page8(const View8& kv, int b, int* inner) {
+  const int pg = kv.page_log2 >= 0 ? *inner >> kv.page_log2 : *inner / kv.page_size;
+  *inner -= pg * kv.page_size;
+  return kv.page_table[(int64_t)b * kv.pages_per_req + pg];
+}
+
 // A CTA's share of all tiles, and the walk through its segments (a segment = the part of one unit
 // that lies in the share).  Tiles are numbered in 32 bits: the host sees to it that all rooms together
 // hold fewer than 2^31.  The first `more` shares have q + 1 tiles, the others q.

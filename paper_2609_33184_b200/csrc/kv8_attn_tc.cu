@@ -32,6 +32,8 @@
 // Every wait is bounded; on expiry the CTA raises SS_DEV_WAIT_EXPIRED and returns.
 #include <cuda_fp8.h>
 
+#include <type_traits>
+
 #include "kv8_tc.cuh"
 
 namespace ss {
@@ -56,8 +58,15 @@ struct alignas(16) Ctl8 {
   alignas(16) float smax[4][NQ];  // per warp: maxima of a tile; at a segment's end the row sums
 };
 
-// NR = rows, D = head dim.
-template <int NR, int D>
+// What attention over a window (span8 in kv8.cuh) keeps besides.
+template <int NQ>
+struct CtlWin8 : Ctl8<NQ> {
+  int unset;                      // rows without a reference
+  int pos[NQ];                    // the rows' positions
+};
+
+// NR = rows, D = head dim, WIN = over a window.
+template <int NR, int D, bool WIN>
 struct Cfg8 {
   static constexpr int kSoft = 128, kThreads = kSoft + 64; // softmax threads, all threads
   static constexpr int NQ = NR == 24 ? 32 : NR;            // rows of the Q operand (N has to be a multiple of 16)
@@ -66,7 +75,8 @@ struct Cfg8 {
   static constexpr int NP = (3 * NR + 15) / 16 * 16;       // weight columns
   static constexpr int kQBytes = 2 * NQ * D;
   static constexpr int kPBytes = kTok8 * NP;
-  static constexpr int kCtlBytes = (sizeof(Ctl8<NQ>) + 127) / 128 * 128;
+  using Ctl = std::conditional_t<WIN, CtlWin8<NQ>, Ctl8<NQ>>;
+  static constexpr int kCtlBytes = (sizeof(Ctl) + 127) / 128 * 128;
   static constexpr int kRest = (kQBytes + 1023) / 1024 * 1024 + kPBytes + kCtlBytes;
   // head dim 64: the output MMA's upper 64 rows read one unit further on (results never used), the
   // last unit's inside this window too
@@ -117,14 +127,14 @@ __device__ __forceinline__ __half2 bits_h2(uint32_t u) { return *reinterpret_cas
 __device__ __forceinline__ uint32_t residue(uint32_t w) {
   return h2_bits(__hmul2(__hsub2(bits_h2(w), bits_h2(w & 0xff00ff00u)), __float2half2_rn(8.f)));
 }
-template <int NR, int D>
-__global__ void __launch_bounds__(Cfg8<NR, D>::kThreads, Cfg8<NR, D>::kPerSM)
+template <int NR, int D, bool WIN>
+__global__ void __launch_bounds__(Cfg8<NR, D, WIN>::kThreads, Cfg8<NR, D, WIN>::kPerSM)
 attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ CUtensorMap tmK,
                 const __grid_constant__ CUtensorMap tmV) {
-  using C = Cfg8<NR, D>;
+  using C = Cfg8<NR, D, WIN>;
   constexpr int UNITS = C::kUnits, NQ = C::NQ, NS = C::NS, NP = C::NP, SOFT = C::kSoft;
   extern __shared__ __align__(1024) uint8_t smem[];
-  Ctl8<C::NQ>* ctl = reinterpret_cast<Ctl8<C::NQ>*>(smem + C::kOffCtl);
+  typename C::Ctl* ctl = reinterpret_cast<typename C::Ctl*>(smem + C::kOffCtl);
   uint8_t* q_s = smem + C::kOffQ;
   uint8_t* p_s = smem + C::kOffP;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -144,6 +154,7 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
       mbar_init(&ctl->pfree, 1);
       mbar_init(&ctl->qfull, SOFT);
       ctl->abort = 0;
+      if constexpr (WIN) ctl->unset = 0;
       fence_barrier_init();
     }
   }
@@ -158,10 +169,10 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   if (warp == 0) {
-    const Share8 share = find_share8(p);
+    const Share8 share = find_share8<WIN>(p);
     if (lane == 0) {
       ctl->share = share;
-      ctl->has[0] = seg_first8(p, share, &ctl->seg[0]);
+      ctl->has[0] = seg_first8<WIN>(p, share, &ctl->seg[0]);
     }
   }
   tc_fence_before();
@@ -180,14 +191,17 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
     // side by side have the layout of one.  The swizzle atom (8 rows) is also why other page sizes
     // take the CUDA-core kernel.  Pages past the request's last token are not looked up.
     const uint64_t pol = p.row_tiles > 1 ? l2_evict_normal_policy() : l2_evict_first_policy();
+    // Over a window lane i copies granule i.
     const bool small = p.kv.page_shift >= 0;
-    const int ps = small ? p.kv.page_size : kTok8;
+    const int ps = WIN ? 1 << p.gran_log2 : small ? p.kv.page_size : kTok8;
     const bool mine = lane * ps < kTok8;
     int j = 0, u = 0;      // units filled so far, the next one's place in the ring
     uint32_t ph = 1;       // parity of its release
     bool ok = true;
     Seg8 g;
-    for (bool more = seg_first8(p, share, &g); more && ok; more = seg_next8(p, share, &g)) {
+    for (bool more = seg_first8<WIN>(p, share, &g); more && ok; more = seg_next8<WIN>(p, share, &g)) {
+      Win8 w = {};
+      if (WIN) w = win8(p, g.b);
       int inner = 0, outer = 0;
       auto look = [&](int t) {  // this lane's page of tile t
         const int tok = t * kTok8 + lane * ps;
@@ -195,7 +209,10 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
         inner = 0;
         if (!mine || t >= g.t1 || tok >= g.len) return;
         int id = g.b;
-        if (!p.kv.page_table) {
+        if (WIN) {
+          inner = win_token8(w, tok);
+          if (p.kv.page_table) id = page8(p.kv, g.b, &inner);
+        } else if (!p.kv.page_table) {
           inner = tok;
         } else {
           const int pg = small ? tok >> p.kv.page_shift : p.kv.page_tiles == 1 ? t : t / p.kv.page_tiles;
@@ -256,7 +273,7 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
     int it0 = 0, seg = 0;  // tiles and segments before this one
     bool ok = true;
     Seg8 g;
-    for (bool more = seg_first8(p, share, &g); more && ok; more = seg_next8(p, share, &g), ++seg) {
+    for (bool more = seg_first8<WIN>(p, share, &g); more && ok; more = seg_next8<WIN>(p, share, &g), ++seg) {
       const int n = g.t1 - g.t0;
       int qi = 0, pi = 0;
       bool q_there = false;
@@ -336,6 +353,7 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
     constexpr int TPR = SOFT / NQ, kE = D / TPR, kQL = kE / 4;
     const int q_row = tid / TPR, q_part = tid % TPR;
     uint2 q_raw[kQL];
+    int q_pos = 0;  // (window) position of row tid
     auto q_load = [&](const Seg8& s) {
       const int rg = s.row0 + q_row, h = s.kvh * p.G + rg / p.T_q, t = rg % p.T_q;
       const __nv_bfloat16* src = p.Q + s.b * p.q_sb + h * p.q_sh + t * p.q_st + q_part * kE;
@@ -384,6 +402,9 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
         ctl->qf[q_row] = pow2_8(eq) * p.scale_log2;
         ctl->nm[q_row] = 0.f;
       }
+      if constexpr (WIN) {
+        if (tid < NQ) ctl->pos[tid] = q_pos;
+      }
       fence_proxy_async();
       mbar_arrive(&ctl->qfull);
     };
@@ -397,8 +418,17 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
     uint32_t ah_ek = 127, ah_ev = 127;  // bytes of the next tile's key
     const int32_t* ah_table = nullptr;  // the request's row of the page table
     const uint8_t *ah_ks = nullptr, *ah_vs = nullptr;  // the kv-head's scale bytes
+    Win8 w = {};                        // (window) the segment's
     auto ah_look = [&](int t, int t1, int len, uint32_t b) {
       ah_id = ~0u;
+      if (WIN) {
+        if (t < t1 && t * kTok8 + key < len) {
+          int inner = win_token8(w, t * kTok8 + key);
+          ah_id = paged ? (uint32_t)page8(p.kv, (int)b, &inner) : b;
+          ah_inner = inner;
+        }
+        return;
+      }
       if (t < t1 && t * kTok8 + key < len) {
         if (!paged) {
           ah_id = b;
@@ -427,6 +457,10 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
       ah_ks = p.kv.Ks + s.kvh * p.kv.ks_sh;
       ah_vs = p.kv.Vs + s.kvh * p.kv.vs_sh;
       if (paged) ah_table = p.kv.page_table + (int64_t)s.b * p.kv.pages_per_req;
+      if (WIN) {  // (rows that do not exist see what the first query sees)
+        w = win8(p, s.b);
+        if (tid < NQ) q_pos = w.first + (tid < s.nrows ? depth8(p, s.b, (s.row0 + tid) % p.T_q) : 0);
+      }
       ah_look(s.t0, s.t1, s.len, s.b);
       q_load(s);
     };
@@ -437,13 +471,14 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
       const int t0 = g.t0, t1 = g.t1, len = g.len, b = g.b;
       if (tid == 0) {  // the next segment, read by everybody after this one's tiles
         Seg8 s = g;
-        ctl->has[(k_seg + 1) & 1] = seg_next8(p, share, &s);
+        ctl->has[(k_seg + 1) & 1] = seg_next8<WIN>(p, share, &s);
         ctl->seg[(k_seg + 1) & 1] = s;
       }
       q_store();
       ah_fetch();    // (its page id has arrived by now)
       ah_look(t0 + 1, t1, len, b);
       bar8<SOFT>();  // (factors and references)
+      bool unset = false;  // (window; thread r < NR) row r has no reference yet
       float2 lsum[NR / 2];
 #pragma unroll
       for (int r = 0; r < NR / 2; ++r) lsum[r] = make_float2(0.f, 0.f);
@@ -455,9 +490,22 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
         ah_look(t + 2, t1, len, b);
         const int n_valid = min(kTok8, len - t * kTok8);
         const bool key_ok = key < n_valid, first = t == t0;
+        const bool masked = WIN && !win_plain8(p, w, t);
+        const int tok = WIN ? win_token8(w, t * kTok8 + key) : 0;
         wait(&ctl->sfull[it & 1], (it >> 1) & 1);
         tc_fence_after();
-        if (n_valid < kTok8) {
+        if (WIN) {
+          const unsigned dead = masked ? __ballot_sync(0xffffffffu, !win_any8(p, w, tok)) : 0u;
+          if (dead) {  // tokens that no query sees, as those past the length
+            const int jv = 2 * it + 1;
+            wait(&ctl->ufull[jv % UNITS], (jv / UNITS) & 1);
+            constexpr int kPieces = D / 16;  // 16-byte pieces of a row
+            uint8_t* v = smem + (jv % UNITS) * C::kUnitBytes + warp * 32 * D + (lane % kPieces) * 16;
+#pragma unroll 1
+            for (int r = lane / kPieces; r < 32; r += 32 / kPieces)
+              if (dead >> r & 1) *reinterpret_cast<uint4*>(v + r * D) = make_uint4(0, 0, 0, 0);
+          }
+        } else if (n_valid < kTok8) {
           // tokens past the length may hold anything; their weights are 0, so V must be finite there
           const int jv = 2 * it + 1;
           wait(&ctl->ufull[jv % UNITS], (jv / UNITS) & 1);
@@ -503,7 +551,23 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
             if (r0 + 8 < NR) load(r0 + 8);
           }
         }
-        if (n_valid < kTok8) {
+        if (WIN) {
+          if (masked) {
+            __syncwarp();
+            if (p.T_q == 1) {
+              const bool ok = win_sees8(p, w, w.first, tok);
+#pragma unroll
+              for (int r = 0; r < NR / 2; ++r)
+                if (!ok) x[r] = make_float2(-INFINITY, -INFINITY);
+            } else if constexpr (WIN) {
+#pragma unroll
+              for (int r = 0; r < NR / 2; ++r) {
+                if (!win_sees8(p, w, ctl->pos[2 * r], tok)) x[r].x = -INFINITY;
+                if (!win_sees8(p, w, ctl->pos[2 * r + 1], tok)) x[r].y = -INFINITY;
+              }
+            }
+          }
+        } else if (n_valid < kTok8) {
           __syncwarp();  // (kept a branch: as selects it costs every tile an instruction per score)
 #pragma unroll
           for (int r = 0; r < NR / 2; ++r)
@@ -512,7 +576,9 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
         float mx = -INFINITY;
 #pragma unroll
         for (int r = 0; r < NR / 2; ++r) mx = max3_f(mx, x[r].x, x[r].y);
-        if (bar_or8<SOFT>(first || mx > kOver)) {
+        bool missing = false;  // some row has no reference: it has seen nothing so far
+        if constexpr (WIN) missing = ctl->unset;
+        if (bar_or8<SOFT>(first || mx > kOver || missing)) {
           // ---- set the references to the exact maxima; later in a segment (rare) raise them, which
           // rescales O^T and the row sums ----
           float mine = -INFINITY;
@@ -525,9 +591,20 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
           bar8<SOFT>();
           if (tid < NR) {  // M rises by this much (in the first tile, from 0 to the maximum - bias)
             const float top = fmaxf(fmaxf(ctl->smax[0][tid], ctl->smax[1][tid]), fmaxf(ctl->smax[2][tid], ctl->smax[3][tid]));
-            const float up = first ? top - kBias : fmaxf(0.f, top - kBias);
+            float up = first ? top - kBias : fmaxf(0.f, top - kBias);
+            if (WIN) {
+              const bool none = top == -INFINITY;
+              if (first || unset) up = none ? 0.f : top - kBias;
+              unset = (first || unset) && none && tid < g.nrows;
+            }
             ctl->up[tid] = up;
             ctl->nm[tid] -= up;
+          }
+          if constexpr (WIN) {
+            if (warp == 0) {
+              const bool any = __any_sync(0xffffffffu, unset);
+              if (lane == 0) ctl->unset = any;
+            }
           }
           bar8<SOFT>();
           if (!first) {
@@ -542,7 +619,11 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
                 tmem_ld<8>(at, o);
                 tc_wait_ld();
 #pragma unroll
-                for (int c = 0; c < 8; ++c) o[c] = __float_as_uint(__uint_as_float(o[c]) * ex2_ftz(-ctl->up[r + c]));
+                for (int c = 0; c < 8; ++c) {
+                  const float a = __uint_as_float(o[c]);
+                  // (window: 0 stays 0, a first reference far below 0 makes the factor infinite)
+                  o[c] = WIN && a == 0.f ? 0u : __float_as_uint(a * ex2_ftz(-ctl->up[r + c]));
+                }
                 tmem_st8(at, o);
               }
             }
@@ -552,7 +633,12 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
           for (int r = 0; r < NR / 2; ++r) {
             const float2 up = *reinterpret_cast<const float2*>(&ctl->up[2 * r]);
             x[r] = __fadd2_rn(x[r], make_float2(-up.x, -up.y));
-            if (!first) lsum[r] = __fmul2_rn(lsum[r], make_float2(ex2_ftz(-up.x), ex2_ftz(-up.y)));
+            if (!first) {
+              float2 f = make_float2(ex2_ftz(-up.x), ex2_ftz(-up.y));
+              if (WIN && lsum[r].x == 0.f) f.x = 0.f;
+              if (WIN && lsum[r].y == 0.f) f.y = 0.f;
+              lsum[r] = __fmul2_rn(lsum[r], f);
+            }
           }
         }
         {
@@ -630,6 +716,9 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
         else reinterpret_cast<float2*>(slot)[tid] = make_float2(m, l);
         ctl->up[tid] = l > 0.f || l != l ? 1.f / l : 0.f;
       }
+      if constexpr (WIN) {
+        if (tid == 0) ctl->unset = 0;
+      }
       bar8<SOFT>();
       const int64_t pair = (int64_t)done.b * p.H_kv + done.kvh;
       const bool to_o = whole && p.O;
@@ -658,8 +747,8 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
       tc_fence_before();
       bar8<SOFT>();  // sums, references and Q may be written anew
     }
-    if ((int)blockIdx.x < p.B) put_empty8(p, tid, SOFT);
-    if (p.plan && warp == 0 && blockIdx.x == gridDim.x - 1) put_plan8(p);
+    if ((int)blockIdx.x < p.B) put_empty8<WIN>(p, tid, SOFT);
+    if (p.plan && warp == 0 && blockIdx.x == gridDim.x - 1) put_plan8<WIN>(p);
   }
 
   tc_fence_before();
@@ -668,41 +757,47 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(C::kTmemCols) : "memory");
 }
 
-template <int NR, int D>
+template <int NR, int D, bool WIN>
 cudaError_t prepare8() {
-  return cudaFuncSetAttribute(attn8_tc_kernel<NR, D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                              Cfg8<NR, D>::kSmem);
+  return cudaFuncSetAttribute(attn8_tc_kernel<NR, D, WIN>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                              Cfg8<NR, D, WIN>::kSmem);
 }
-template <int NR, int D>
+template <int NR, int D, bool WIN>
 cudaError_t launch8(const Attn8Params& p, const CUtensorMap& tmK, const CUtensorMap& tmV, cudaStream_t s, bool pdl) {
-  using C = Cfg8<NR, D>;
-  return launch_kernel(attn8_tc_kernel<NR, D>, dim3(p.shares * p.row_tiles), dim3(C::kThreads), C::kSmem, s, pdl, p, tmK, tmV);
+  using C = Cfg8<NR, D, WIN>;
+  return launch_kernel(attn8_tc_kernel<NR, D, WIN>, dim3(p.shares * p.row_tiles), dim3(C::kThreads), C::kSmem, s, pdl, p, tmK,
+                       tmV);
 }
-template <int D>
+template <int D, bool WIN>
+cudaError_t prepare_rows() {
+  cudaError_t e = prepare8<8, D, WIN>();
+  if (e == cudaSuccess) e = prepare8<16, D, WIN>();
+  if (e == cudaSuccess) e = prepare8<24, D, WIN>();
+  if (e == cudaSuccess) e = prepare8<32, D, WIN>();
+  return e;
+}
+template <int D, bool WIN>
 cudaError_t launch_rows(const Attn8Params& p, const CUtensorMap& tmK, const CUtensorMap& tmV, cudaStream_t s, bool pdl) {
   // (24 rows as 32: 247 us against 242 for 8 x 98304 tokens; 40 rows as 2 x 32 against 2 x 24: 172 and 155)
-  if (p.rows_per_tile <= 8) return launch8<8, D>(p, tmK, tmV, s, pdl);
-  if (p.rows_per_tile <= 16) return launch8<16, D>(p, tmK, tmV, s, pdl);
-  if (p.rows_per_tile <= 24) return launch8<24, D>(p, tmK, tmV, s, pdl);
-  return launch8<32, D>(p, tmK, tmV, s, pdl);
+  if (p.rows_per_tile <= 8) return launch8<8, D, WIN>(p, tmK, tmV, s, pdl);
+  if (p.rows_per_tile <= 16) return launch8<16, D, WIN>(p, tmK, tmV, s, pdl);
+  if (p.rows_per_tile <= 24) return launch8<24, D, WIN>(p, tmK, tmV, s, pdl);
+  return launch8<32, D, WIN>(p, tmK, tmV, s, pdl);
 }
 
 }  // namespace
 
 cudaError_t attn8_tc_prepare() {
-  cudaError_t e = prepare8<8, 128>();
-  if (e == cudaSuccess) e = prepare8<16, 128>();
-  if (e == cudaSuccess) e = prepare8<24, 128>();
-  if (e == cudaSuccess) e = prepare8<32, 128>();
-  if (e == cudaSuccess) e = prepare8<8, 64>();
-  if (e == cudaSuccess) e = prepare8<16, 64>();
-  if (e == cudaSuccess) e = prepare8<24, 64>();
-  if (e == cudaSuccess) e = prepare8<32, 64>();
+  cudaError_t e = prepare_rows<128, false>();
+  if (e == cudaSuccess) e = prepare_rows<64, false>();
+  if (e == cudaSuccess) e = prepare_rows<128, true>();
+  if (e == cudaSuccess) e = prepare_rows<64, true>();
   return e;
 }
 
 cudaError_t launch_attn8_tc(const Attn8Params& p, const CUtensorMap& tmK, const CUtensorMap& tmV, cudaStream_t s, bool pdl) {
-  return p.d == 128 ? launch_rows<128>(p, tmK, tmV, s, pdl) : launch_rows<64>(p, tmK, tmV, s, pdl);
+  if (p.window) return p.d == 128 ? launch_rows<128, true>(p, tmK, tmV, s, pdl) : launch_rows<64, true>(p, tmK, tmV, s, pdl);
+  return p.d == 128 ? launch_rows<128, false>(p, tmK, tmV, s, pdl) : launch_rows<64, false>(p, tmK, tmV, s, pdl);
 }
 
 }  // namespace ss

@@ -151,11 +151,7 @@ window_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ 
         if (!mine || t >= g.t1 || v >= g.len) return;
         inner = win_token8(w, v);
         int id = g.b;
-        if (p.kv.page_table) {
-          const int pg = p.kv.page_log2 >= 0 ? inner >> p.kv.page_log2 : inner / p.kv.page_size;
-          inner -= pg * p.kv.page_size;
-          id = p.kv.page_table[(int64_t)g.b * p.kv.pages_per_req + pg];
-        }
+        if (p.kv.page_table) id = page8(p.kv, g.b, &inner);
         if (id >= 0 && id < p.kv.n_outer) outer = id;
         else atomicOr(p.status, SS_DEV_BAD_PAGE);
       };

@@ -178,7 +178,7 @@ def test_one_token(bits, page, d, G, order, window, sinks):
     Q = queries(g, B, H_kv * G, 1, d, "bthd")
     hide(cache, LENS, 1, window, sinks, room)
     for flags in ((0, ssb.SS_FLAG_FORCE_SIMT) if bits == 16 and page in (16, 24) else (0,)):
-        kernel = "simt" if flags or page in (1, 3, 5) else "tcgen05" if bits == 16 else None
+        kernel = "simt" if flags or page in (1, 3, 5) else "tcgen05"
         O, LSE = step(ssb, bits, cache, Q, LENS, window, sinks, flags=flags, kernel=kernel)
         check(Q, O, LSE, keys_of(cache, H_kv, LENS, 1, window, sinks), d ** -0.5, bits)
 
