@@ -7,6 +7,7 @@ the shared library is missing or the device is not sm_100, calls raise.
 from __future__ import annotations
 
 import ctypes as C
+import importlib.util
 import os
 from typing import Optional, Sequence
 
@@ -143,6 +144,22 @@ class ss_stream_stats(C.Structure):
 
 
 _lib = None
+_marshal = None
+
+
+def marshal():
+    """The extension module that checks the tensors of a call and makes it (raises if it has not been built)."""
+    global _marshal
+    if _marshal is None:
+        load()
+        path = os.path.join(_PKG, "_marshal.so")
+        if not os.path.exists(path):
+            raise RuntimeError(f"{path} not found: build it with `python -m paper_2609_33184_b200.build`")
+        spec = importlib.util.spec_from_file_location("_marshal", path)
+        module = importlib.util.module_from_spec(spec)
+        spec.loader.exec_module(module)
+        _marshal = module
+    return _marshal
 
 
 def load() -> C.CDLL:
@@ -341,6 +358,7 @@ class Cache8:
         self.desc = ss_cache8(t8(K), t8(V), t8(K_scale), t8(V_scale), K.shape[0], K.shape[2],
                               1 if page_table is None else page_table.shape[1], _ptr(page_table))
         self.ref = C.byref(self.desc)
+        self.known = marshal().cache(C.addressof(self.desc), 8, self.H_kv, self.d, self.requests, self.device)
 
     @classmethod
     def empty(cls, outer: int, H_kv: int, tokens: int, d: int, page_table: Optional[torch.Tensor] = None,
@@ -371,6 +389,7 @@ class Cache16:
         self.desc = ss_cache16(as_ss_tensor(K), as_ss_tensor(V), K.shape[0], K.shape[2],
                                1 if page_table is None else page_table.shape[1], _ptr(page_table))
         self.ref = C.byref(self.desc)
+        self.known = marshal().cache(C.addressof(self.desc), 16, self.H_kv, self.d, self.requests, self.device)
 
 
 class Rope:
@@ -388,9 +407,7 @@ class Rope:
             raise SpecStreamError(st, "ss_rope_init")
         self.n_axes = n_axes
         self.ref = C.byref(self.desc)
-
-
-_NO_ROWS = ss_tensor(None, 0, 0, 0)
+        self.at = C.addressof(self.desc)
 
 
 class Context:
@@ -411,6 +428,8 @@ class Context:
         self.H_q, self.H_kv, self.d = H_q, H_kv, d
         self._dev = device
         self._B = self._T = 0   # requests and queries of the open round
+        self._m = marshal()
+        self._me = self._m.context(self.handle.value, device, H_q, H_kv, d)   # None once closed
 
     def _sp(self, stream) -> int:
         """cudaStream_t of `stream`, else torch's current stream on this context's device."""
@@ -428,6 +447,7 @@ class Context:
         if self.handle:
             self.lib.ss_destroy(self.handle)
             self.handle = C.c_void_p()
+            self._me = None
 
     def __del__(self):
         try:
@@ -563,8 +583,9 @@ class Context:
         if st:
             self._check(st, "ss_verify_chunk8")
 
-    def _step(self, Q, O, LSE):
-        """B, T_q, Q and the pointers of a decoding call's outputs."""
+    def ss_decode8(self, Q: torch.Tensor, scale: float, cache: Cache8, valid_len: Optional[torch.Tensor],
+                   O: torch.Tensor, LSE: Optional[torch.Tensor] = None, stream=None):
+        """Q [B, H_q, T_q, d] over the first valid_len[b] tokens of the cache -> O (bf16), LSE (fp32 [B, H_q, T_q])."""
         shape = Q.shape
         B, H, T, d = shape
         if O.dtype is not torch.bfloat16 or O.shape != shape or O.get_device() != self._dev or not O.is_contiguous():
@@ -572,102 +593,68 @@ class Context:
         if LSE is not None and (LSE.dtype is not torch.float32 or LSE.shape != shape[:3] or
                                 LSE.get_device() != self._dev or not LSE.is_contiguous()):
             raise AssertionError("LSE: contiguous fp32 [B, H_q, T_q] expected", LSE.shape, LSE.dtype)
-        return (B, T, self._rows(Q, (B, self.H_q, T, self.d)), O.data_ptr(), None if LSE is None else LSE.data_ptr())
-
-    def ss_decode8(self, Q: torch.Tensor, scale: float, cache: Cache8, valid_len: Optional[torch.Tensor],
-                   O: torch.Tensor, LSE: Optional[torch.Tensor] = None, stream=None):
-        """Q [B, H_q, T_q, d] over the first valid_len[b] tokens of the cache -> O (bf16), LSE (fp32 [B, H_q, T_q])."""
-        B, T, q, o, lse = self._step(Q, O, LSE)
-        st = self.lib.ss_decode8(self.handle, q, B, T, scale, self._cache8(cache, B), self._i32(valid_len, B), o, lse,
-                                 self._sp(stream))
+        st = self.lib.ss_decode8(self.handle, self._rows(Q, (B, self.H_q, T, self.d)), B, T, scale,
+                                 self._cache8(cache, B), self._i32(valid_len, B), O.data_ptr(),
+                                 None if LSE is None else LSE.data_ptr(), self._sp(stream))
         if st:
             self._check(st, "ss_decode8")
 
-    def _decode_window(self, name, kind, Q, scale, cache, window, sinks, valid_len, O, LSE, stream):
-        if type(cache) is not kind:
-            raise AssertionError("cache of another kind")
-        B, T, q, o, lse = self._step(Q, O, LSE)
-        st = getattr(self.lib, name)(self.handle, q, B, T, scale, self._cache8(cache, B), window, sinks,
-                                     self._i32(valid_len, B), o, lse, self._sp(stream))
-        if st:
-            self._check(st, name)
-
+    # The calls from here to ss_verify_chunk8_window check their tensors in the extension module (csrc/marshal.cpp).
     def ss_decode_window(self, Q: torch.Tensor, scale: float, cache: Cache16, window: int, sinks: int,
                          valid_len: Optional[torch.Tensor], O: torch.Tensor, LSE: Optional[torch.Tensor] = None, stream=None):
         """Q [B, H_q, T_q, d], the newest T_q of the cache's valid_len[b] tokens, over the last `window` tokens of each and
         the first `sinks` ones -> O (bf16), LSE (fp32 [B, H_q, T_q])."""
-        self._decode_window("ss_decode_window", Cache16, Q, scale, cache, window, sinks, valid_len, O, LSE, stream)
+        st = self._m.decode_window(self._me, Q, scale, cache.known, window, sinks, valid_len, O, LSE, self._sp(stream))
+        if st:
+            self._check(st, "ss_decode_window")
 
     def ss_decode8_window(self, Q: torch.Tensor, scale: float, cache: Cache8, window: int, sinks: int,
                           valid_len: Optional[torch.Tensor], O: torch.Tensor, LSE: Optional[torch.Tensor] = None, stream=None):
         """The same over an 8-bit cache."""
-        self._decode_window("ss_decode8_window", Cache8, Q, scale, cache, window, sinks, valid_len, O, LSE, stream)
-
-    def _chunk_window(self, name, kind, cache, window, sinks, valid_len, depth, stream):
-        if type(cache) is not kind:
-            raise AssertionError("cache of another kind")
-        B = self._B
-        st = getattr(self.lib, name)(self.handle, self._cache8(cache, B), window, sinks, self._i32(valid_len, B),
-                                     self._i32(depth, B * self._T), self._sp(stream))
+        st = self._m.decode8_window(self._me, Q, scale, cache.known, window, sinks, valid_len, O, LSE, self._sp(stream))
         if st:
-            self._check(st, name)
+            self._check(st, "ss_decode8_window")
 
     def ss_verify_chunk_window(self, cache: Cache16, window: int, sinks: int, valid_len: Optional[torch.Tensor] = None,
                                depth: Optional[torch.Tensor] = None, stream=None):
         """The window of the cache's tokens that the open round's candidates see; depth int32 [B, T_q]."""
-        self._chunk_window("ss_verify_chunk_window", Cache16, cache, window, sinks, valid_len, depth, stream)
+        st = self._m.verify_chunk_window(self._me, cache.known, window, sinks, valid_len, depth, self._B, self._T,
+                                         self._sp(stream))
+        if st:
+            self._check(st, "ss_verify_chunk_window")
 
     def ss_verify_chunk8_window(self, cache: Cache8, window: int, sinks: int, valid_len: Optional[torch.Tensor] = None,
                                 depth: Optional[torch.Tensor] = None, stream=None):
         """The same over an 8-bit cache."""
-        self._chunk_window("ss_verify_chunk8_window", Cache8, cache, window, sinks, valid_len, depth, stream)
-
-    def _pair(self, x, out, heads, B, T, what):
-        """Rows in and rows out of the same shape (or neither)."""
-        if x is None:
-            if out is not None:
-                raise AssertionError(what + "_out without " + what)
-            return _NO_ROWS, _NO_ROWS
-        shape = (B, heads, T, self.d)
-        return self._rows(x, shape), self._rows(out, shape)
+        st = self._m.verify_chunk8_window(self._me, cache.known, window, sinks, valid_len, depth, self._B, self._T,
+                                          self._sp(stream))
+        if st:
+            self._check(st, "ss_verify_chunk8_window")
 
     def ss_rope_rotate(self, rope: Rope, Q, K, Q_out, K_out, pos=None, pos_off=None, row_cnt=None, stream=None):
         """Q [B, H_q, T, d] -> Q_out, K [B, H_kv, T, d] -> K_out (bf16; either pair may be None); pos int32
         [n_axes, B, T], or positions pos_off[b] + row; row_cnt, pos_off int32 [B]."""
-        B, _, T, _ = (Q if K is None else K).shape
-        i32 = self._i32
-        q, qo = self._pair(Q, Q_out, self.H_q, B, T, "Q")
-        k, ko = self._pair(K, K_out, self.H_kv, B, T, "K")
-        st = self.lib.ss_rope_rotate(self.handle, rope.ref, q, k, B, T, i32(pos, rope.n_axes * B * T), i32(pos_off, B),
-                                     i32(row_cnt, B), qo, ko, self._sp(stream))
+        st = self._m.rope_rotate(self._me, rope.at, Q, K, Q_out, K_out, pos, pos_off, row_cnt, self._sp(stream))
         if st:
             self._check(st, "ss_rope_rotate")
-
-    def _append(self, name, kind, cache, K, V, rope, pos, Q, Q_out, dst_off, row_cnt, row_idx, stream):
-        B, _, T, _ = K.shape
-        if type(cache) is not kind:
-            raise AssertionError("cache of another kind")
-        shape = (B, self.H_kv, T, self.d)
-        i32, rows = self._i32, self._rows
-        q, qo = self._pair(Q, Q_out, self.H_q, B, T, "Q")
-        st = getattr(self.lib, name)(self.handle, self._cache8(cache, B), rows(K, shape), rows(V, shape), B, T,
-                                     None if rope is None else rope.ref,
-                                     None if pos is None else i32(pos, (1 if rope is None else rope.n_axes) * B * T),
-                                     i32(row_idx, B * T), i32(row_cnt, B), i32(dst_off, B), q, qo, self._sp(stream))
-        if st:
-            self._check(st, name)
 
     def ss_kv_append(self, cache: Cache16, K, V, rope: Optional[Rope] = None, pos=None, Q=None, Q_out=None, dst_off=None,
                      row_cnt=None, row_idx=None, stream=None):
         """Rows of K, V [B, H_kv, T, d] bf16 become tokens dst_off[b] + k of the cache, K rotated by rope; Q
         [B, H_q, T, d] is rotated into Q_out.  pos int32 [n_axes, B, T] (None: the tokens), dst_off, row_cnt int32 [B],
         row_idx int32 [B, T] on the device or None."""
-        self._append("ss_kv_append", Cache16, cache, K, V, rope, pos, Q, Q_out, dst_off, row_cnt, row_idx, stream)
+        st = self._m.kv_append(self._me, cache.known, K, V, None if rope is None else rope.at, pos, Q, Q_out, dst_off,
+                               row_cnt, row_idx, self._sp(stream))
+        if st:
+            self._check(st, "ss_kv_append")
 
     def ss_kv8_append(self, cache: Cache8, K, V, rope: Optional[Rope] = None, pos=None, Q=None, Q_out=None, dst_off=None,
                       row_cnt=None, row_idx=None, stream=None):
         """The same into an 8-bit cache."""
-        self._append("ss_kv8_append", Cache8, cache, K, V, rope, pos, Q, Q_out, dst_off, row_cnt, row_idx, stream)
+        st = self._m.kv8_append(self._me, cache.known, K, V, None if rope is None else rope.at, pos, Q, Q_out, dst_off,
+                                row_cnt, row_idx, self._sp(stream))
+        if st:
+            self._check(st, "ss_kv8_append")
 
     def ss_poll_status(self, stream=None, timeout_ms: int = 0):
         """Returns (status, device_bits)."""
