@@ -288,6 +288,10 @@ struct DeviceGuard {
 // reads its set, and before the scratch area is used again.
 cudaError_t settle8(ss_ctx* c) {
   if (!c->pend8) return cudaSuccess;
+  if (c->last8.mode != ss::kCut8) {  // (its states are whole)
+    c->pend8 = false;
+    return cudaSuccess;
+  }
   DeviceGuard on(c->cfg.device);
   if (on.err != cudaSuccess) return on.err;
   const cudaError_t e = ss::launch_attn8_join(c->last8, true, c->stream, !c->no_overlap);
@@ -1367,6 +1371,31 @@ static int granule_log2(const ss::View8& kv) {
   return g >= 3 ? g : 0;
 }
 
+// How a window's units meet CTAs (kv8.cuh): the form whose estimated time is least.  `tiles`: most tiles of a unit.  A
+// tile takes a CTA `one` us when little else runs (the latency of its copies and steps; small granules mean more
+// copies), and all CTAs together what memory gives; joining in a cluster takes 0.3 us, walking from unit to unit 1 us,
+// joining by another kernel 2.6 us and more for many states or rows.  Clusters of other sizes than 1, 2, 4 or 8 leave places of a GPC empty (96 clusters of 3
+// ran as two rounds: 19.3 us against 12.2 with 96 of 2), so those are taken up to half the CTAs only.
+// Measured, head dim 128, 4 rows, pages of 16, 128 units of 33 tiles: clusters of one 65 us, of two 45.6, cut 47.9; one unit
+// of 33 tiles: 60, clusters of eight 12.4, cut 11.0; 384 units of 32 rows, head dim 64, two tiles: whole 18.6, cut 22.4.
+static void window_mode(ss::Attn8Params* p, int64_t tiles) {
+  const int64_t N = (int64_t)p->shares * p->row_tiles, U = (int64_t)p->B * p->H_kv * p->row_tiles;
+  const double one = (p->d == 128 ? 1.2 : 0.8) * (p->gran_log2 >= 5 ? 1.0 : p->gran_log2 == 4 ? 1.3 : 2.1);
+  const double share = p->d / 128.0 * 0.0094 / p->row_tiles;  // of memory's time, per CTA that is at work
+  const auto tile_us = [&](int64_t ctas) { return pow(pow(one, 4) + pow(share * ctas, 4), 0.25); };
+  const int64_t full = U / N, rest = U % N, steps = (U * tiles + N - 1) / N;
+  const double whole = tiles * (full * tile_us(N) + (rest ? tile_us(rest) : 0.0)) + 1.0;
+  const double cut = steps * tile_us(N < U * tiles ? N : U * tiles) + 2.6 + 0.08 * tiles / steps + (double)U * p->rows_per_tile / 3500;
+  int64_t c = N * 9 / 10 / U;
+  if (c > tiles) c = tiles;
+  if (c > ss::kMostCluster8) c = ss::kMostCluster8;
+  if (U * c > N / 2) c = c >= 8 ? 8 : c >= 4 ? 4 : c >= 2 ? 2 : 1;
+  if (c < 1 && U <= N) c = 1;
+  const double cluster = c < 1 ? 1e30 : (tiles + c - 1) / c * tile_us(U * c) + (c > 1 ? 0.3 : 0.0);
+  p->mode = cluster <= whole && cluster <= cut ? ss::kCluster8 : whole <= cut ? ss::kWhole8 : ss::kCut8;
+  p->cluster = (int)c;
+}
+
 // The attention launch that the entry points share; the caller has set where its result goes.
 static ss_status attn8(ss_ctx* c, int bits, const ss_tensor& Q, int32_t B, int32_t T_q, float scale, const ss_cache8* cache,
                        const int32_t* valid_len, const Window8& win, ss::Attn8Params* p, cudaStream_t s) {
@@ -1421,9 +1450,15 @@ static ss_status attn8(ss_ctx* c, int bits, const ss_tensor& Q, int32_t B, int32
   // as many CTAs as are resident, and one for every row tile at least
   p->shares = (tc && bits == 8 && p->d == 64 && p->rows_per_tile <= ss::kFew8 ? ss::kCtasFew8 : ss::kCtas8) / p->row_tiles;
   if (p->shares < 1) p->shares = 1;
+  // the most tokens and tiles that are walked of a request (a window: granules at its ends)
+  const int64_t seen = (int64_t)win.window + win.sinks + T_q, room = p->kv.room;
+  const int64_t tokens = win.window && seen < room ? seen : room;
+  const int64_t walked = win.window && seen + 2 * 32 < room ? seen + 2 * 32 : room;
+  const int64_t most_tiles = (walked + ss::kTok8 - 1) / ss::kTok8;
+  if (win.window && tc && bits == 16) window_mode(p, most_tiles);
   p->scale_log2 = scale * 1.4426950408889634f;
   p->scratch = c->scratch8;
-  p->plan = p->O ? nullptr : c->plan8;
+  p->plan = p->O || p->mode != ss::kCut8 ? nullptr : c->plan8;
   p->status = c->status;
   DeviceGuard on(c->cfg.device);
   if (on.err != cudaSuccess) return cuda_fail(c, on.err);
@@ -1438,9 +1473,7 @@ static ss_status attn8(ss_ctx* c, int bits, const ss_tensor& Q, int32_t B, int32
                    : bits == 8 ? (tc ? "window8-tcgen05" : "window8-simt")
                                : (tc ? "window-tcgen05" : "window-simt");
   ++c->launches;
-  const int64_t most_seen = (int64_t)win.window + win.sinks + T_q;
-  const int64_t tokens = win.window && most_seen < p->kv.room ? most_seen : p->kv.room;  // most of a request that are read
-  if (p->O && tokens + 2 * 32 > ss::kTok8) {  // (a unit of one tile is never cut; a round joins later)
+  if (p->O && most_tiles > 1 && p->mode == ss::kCut8) {  // (a unit of one tile is never cut; a round joins later)
     e = ss::launch_attn8_join(*p, false, s, pdl);
     if (e != cudaSuccess) return cuda_fail(c, e);
     ++c->launches;

@@ -71,7 +71,15 @@ struct Attn8Params {
   int before;                 // the first query stands at position len - before
   int gran_log2;              // tokens are left out in granules of 2^gran_log2
   const int32_t* depth;       // [B, T_q] positions behind the first query's, or null: query t at t
+  int mode;                   // kCut8, kWhole8 or kCluster8
+  int cluster;                // CTAs of a cluster (kCluster8)
 };
+// How units meet CTAs.  kCut8: equal shares, units cut at their ends, joined by another kernel.  The other two need no
+// join, as a window bounds the units: kWhole8: a CTA takes the units that begin in its share; kCluster8: a unit (and
+// row tile) is one thread-block cluster's (of one CTA or more), each CTA takes an equal part of its tiles and the parts
+// are joined through distributed shared memory.
+constexpr int kCut8 = 0, kWhole8 = 1, kCluster8 = 2;
+constexpr int kMostCluster8 = 8;
 
 struct Final8 {               // end of a round
   const float2* loc_ml;       // the local segment's states, null without one
@@ -263,6 +271,14 @@ __device__ __forceinline__ Share8 find_share8(const Attn8Params& p) {
   return s;
 }
 
+// (kCluster8) Which unit and row tile this CTA's cluster has, and which part of it is the CTA's.
+struct Place8 {
+  uint32_t rank, rt, b, kvh;
+};
+__device__ __forceinline__ Place8 cluster_place8(const Attn8Params& p) {
+  const uint32_t w = blockIdx.x / (uint32_t)p.cluster, unit = w / (uint32_t)p.row_tiles, b = unit / (uint32_t)p.H_kv;
+  return {blockIdx.x - w * p.cluster, w - unit * p.row_tiles, b, unit - b * p.H_kv};
+}
 struct Seg8 {
   int b, kvh;
   int t0, t1, n;            // tiles [t0, t1) of the unit's n
@@ -270,15 +286,29 @@ struct Seg8 {
   uint32_t base, start, pos;  // tiles before the request, before the unit, before the segment's end
   int row0, nrows;
 };
+template <bool WIN = false>
 __device__ __forceinline__ void seg_set8(const Attn8Params& p, const Share8& s, Seg8* g) {
   const uint32_t u = (g->pos - g->base) / (uint32_t)g->n;
   g->kvh = (int)u;
   g->start = g->base + u * g->n;
   g->t0 = (int)(g->pos - g->start);
-  g->pos = min(g->start + g->n, s.hi);
+  g->pos = g->start + g->n;
+  if (!WIN || p.mode != kWhole8) g->pos = min(g->pos, s.hi);
   g->t1 = (int)(g->pos - g->start);
   g->row0 = (int)s.rt * p.rows_per_tile;
   g->nrows = min(p.rows_per_tile, p.R - g->row0);
+}
+// Moves on to the request that holds tile pos (there is one: pos < hi <= total).
+template <bool WIN = false>
+__device__ __forceinline__ void seg_skip8(const Attn8Params& p, Seg8* g) {
+  const uint32_t units = (uint32_t)p.H_kv;
+#pragma unroll 1
+  while (g->pos >= g->base + units * g->n) {  // the next request with tokens
+    g->base += units * g->n;
+    ++g->b;
+    g->len = len8<WIN>(p, g->b);
+    g->n = tiles8(g->len);
+  }
 }
 template <bool WIN = false>
 __device__ __forceinline__ bool seg_first8(const Attn8Params& p, const Share8& s, Seg8* g) {
@@ -288,22 +318,40 @@ __device__ __forceinline__ bool seg_first8(const Attn8Params& p, const Share8& s
   g->n = tiles8(g->len);
   g->pos = s.lo;
   g->base = s.base0;
-  seg_set8(p, s, g);
+  if (WIN && p.mode == kWhole8) {  // the first unit that begins in the share
+    g->pos = g->base + (g->pos - g->base + g->n - 1) / (uint32_t)g->n * g->n;
+    if (g->pos >= s.hi) return false;
+    seg_skip8<WIN>(p, g);
+  }
+  seg_set8<WIN>(p, s, g);
   return true;
 }
 template <bool WIN = false>
 __device__ __forceinline__ bool seg_next8(const Attn8Params& p, const Share8& s, Seg8* g) {
   if (g->pos >= s.hi) return false;
-  const uint32_t units = (uint32_t)p.H_kv;
-#pragma unroll 1
-  while (g->pos >= g->base + units * g->n) {  // the next request with tokens (there is one: pos < hi <= total)
-    g->base += units * g->n;
-    ++g->b;
-    g->len = len8<WIN>(p, g->b);
-    g->n = tiles8(g->len);
-  }
-  seg_set8(p, s, g);
+  seg_skip8<WIN>(p, g);
+  seg_set8<WIN>(p, s, g);
   return true;
+}
+
+// (kCluster8) The CTA's part of its unit; false: it has no tile.
+__device__ __forceinline__ bool cluster_seg8(const Attn8Params& p, const Place8& at, Seg8* g) {
+  int n = p.kv.room;
+  if (p.valid_len) {
+    const int v = p.valid_len[at.b];
+    n = max(0, min(v, n));
+    if (v != n && at.rank == 0 && at.kvh == 0 && at.rt == 0 && (threadIdx.x & 31) == 0) atomicOr(p.status, SS_DEV_BAD_VALID_LEN);
+  }
+  g->b = (int)at.b;
+  g->kvh = (int)at.kvh;
+  g->len = span8(p, n).len;
+  g->n = tiles8(g->len);
+  g->t0 = (int)(g->n * at.rank / (uint32_t)p.cluster);
+  g->t1 = (int)(g->n * (at.rank + 1) / (uint32_t)p.cluster);
+  g->base = g->start = g->pos = 0;
+  g->row0 = (int)at.rt * p.rows_per_tile;
+  g->nrows = min(p.rows_per_tile, p.R - g->row0);
+  return g->t0 < g->t1;
 }
 
 // Where a finished row goes: O and LSE, or a partial state.  `m` in the base-2 domain.  The state of a row that is

@@ -13,7 +13,11 @@ namespace ss {
 namespace {
 
 constexpr int kWarps = 4;
-constexpr int kFlight = 16;  // states in flight
+// States in flight: 16, and 4 where the registers of 16 (three blocks per SM) would keep a window's rows from
+// running side by side: many rows mean many units, so few states of each (a round of 16 x 8 candidates over 8192
+// tokens 104 us against 106; with few rows 16 are better, 3 x 24 queries over 1000 tokens 10.7 us against 12.0).
+constexpr int kFlight = 16, kFlightMany = 4;
+bool many_rows(const Attn8Params& p) { return p.window && (int64_t)p.B * p.H_kv * p.R > 3 * kWarps * kNumSM; }
 
 // A query row and where its unit's states are: n of them, the first at `first`, the others `step` floats
 // apart from `rest`; n = 0: empty request, n = 1: finished by one CTA, not in the scratch area.
@@ -36,6 +40,10 @@ __device__ __forceinline__ Row8 row8(const Attn8Params& p, int64_t row, int lane
   w.r = w.rr - rt * p.rows_per_tile;
   g.row0 = rt * p.rows_per_tile;
   g.nrows = min(p.rows_per_tile, p.R - g.row0);
+  if (p.mode != kCut8) {  // (in a round's end) every state is whole
+    w.n = 1;
+    return w;
+  }
   const uint32_t units = (uint32_t)p.H_kv;
   Share8 s = {};
   uint32_t before = 0;  // tiles of the requests before this one
@@ -86,7 +94,7 @@ __device__ __forceinline__ void load_a(const float* x, float (&v)[CPL]) {
 }
 
 // Adds the row's n states to (m, l, a); a lane holds D / 32 head dims.
-template <int D>
+template <int D, int kFlight>
 __device__ __forceinline__ void add_states(const Attn8Params& p, const Row8& w, int lane, float& m, float& l,
                                            float (&a)[D / 32]) {
   constexpr int CPL = D / 32;
@@ -99,9 +107,10 @@ __device__ __forceinline__ void add_states(const Attn8Params& p, const Row8& w, 
       st = __ldcg(reinterpret_cast<const float2*>(own == 0 ? w.first : w.rest + (own - 1) * w.step) + w.r);
     float v[kFlight][CPL];
 #pragma unroll
-    for (int j = 0; j < kFlight; ++j) {
-      const int i = min(j0 + j, w.n - 1);
-      load_a<CPL>((i == 0 ? w.first : w.rest + (i - 1) * w.step) + 4 * p.rows_per_tile + w.r * D + lane * CPL, v[j]);
+    for (int j = 0; j < kFlight; ++j) {  // (a row of a window has two or three: loads past the last would be most of them)
+      const int i = j0 + j;
+      if (i < w.n)
+        load_a<CPL>((i == 0 ? w.first : w.rest + (i - 1) * w.step) + 4 * p.rows_per_tile + w.r * D + lane * CPL, v[j]);
     }
     float top = st.y != 0.f ? st.x : -INFINITY;  // (l = 0: an empty state)
 #pragma unroll
@@ -127,7 +136,7 @@ __device__ __forceinline__ void add_states(const Attn8Params& p, const Row8& w, 
   }
 }
 
-template <int D, bool PLAN>
+template <int D, bool PLAN, int FLIGHT>
 __global__ void __launch_bounds__(kWarps * 32) attn8_join_kernel(const __grid_constant__ Attn8Params p) {
   constexpr int CPL = D / 32;
   pdl_launch_dependents();
@@ -142,7 +151,7 @@ __global__ void __launch_bounds__(kWarps * 32) attn8_join_kernel(const __grid_co
   float m = -INFINITY, l = 0.f, a[CPL];
 #pragma unroll
   for (int c = 0; c < CPL; ++c) a[c] = 0.f;
-  add_states<D>(p, w, lane, m, l, a);
+  add_states<D, FLIGHT>(p, w, lane, m, l, a);
   if (lane == 0) put_ml8(p, w.g, w.r, m, l);
 #pragma unroll
   for (int c = 0; c < CPL; ++c) put_a8(p, w.g, w.r, lane * CPL + c, l, a[c]);
@@ -150,7 +159,7 @@ __global__ void __launch_bounds__(kWarps * 32) attn8_join_kernel(const __grid_co
 
 // End of a round whose history is one 8-bit chunk: its states, joined or not, and the local segment's
 // straight to O and LSE.
-template <int D>
+template <int D, int FLIGHT>
 __global__ void __launch_bounds__(kWarps * 32) attn8_finalize_kernel(const __grid_constant__ Attn8Params p,
                                                                      const Final8 out) {
   constexpr int CPL = D / 32;
@@ -178,7 +187,7 @@ __global__ void __launch_bounds__(kWarps * 32) attn8_finalize_kernel(const __gri
     for (int c = 0; c < CPL; ++c) a[c] = v[c];
   }
   if (w.n >= 2) {
-    add_states<D>(p, w, lane, m, l, a);
+    add_states<D, FLIGHT>(p, w, lane, m, l, a);
   } else if (w.n == 1) {
     const float2 st = __ldcg(p.part_ml + at);
     if (st.y != 0.f) {
@@ -203,17 +212,26 @@ dim3 join_grid(const Attn8Params& p) {
   return dim3((unsigned)((rows + kWarps - 1) / kWarps));
 }
 
+template <int D, int FLIGHT>
+cudaError_t join(const Attn8Params& p, bool from_plan, cudaStream_t s, bool pdl) {
+  auto kernel = from_plan ? attn8_join_kernel<D, true, FLIGHT> : attn8_join_kernel<D, false, FLIGHT>;
+  return launch_kernel(kernel, join_grid(p), dim3(kWarps * 32), 0, s, pdl, p);
+}
+template <int D, int FLIGHT>
+cudaError_t finalize(const Attn8Params& p, const Final8& out, cudaStream_t s, bool pdl) {
+  return launch_kernel(attn8_finalize_kernel<D, FLIGHT>, join_grid(p), dim3(kWarps * 32), 0, s, pdl, p, out);
+}
+
 }  // namespace
 
 cudaError_t launch_attn8_join(const Attn8Params& p, bool from_plan, cudaStream_t s, bool pdl) {
-  auto kernel = p.d == 128 ? (from_plan ? attn8_join_kernel<128, true> : attn8_join_kernel<128, false>)
-                           : (from_plan ? attn8_join_kernel<64, true> : attn8_join_kernel<64, false>);
-  return launch_kernel(kernel, join_grid(p), dim3(kWarps * 32), 0, s, pdl, p);
+  if (many_rows(p)) return p.d == 128 ? join<128, kFlightMany>(p, from_plan, s, pdl) : join<64, kFlightMany>(p, from_plan, s, pdl);
+  return p.d == 128 ? join<128, kFlight>(p, from_plan, s, pdl) : join<64, kFlight>(p, from_plan, s, pdl);
 }
 
 cudaError_t launch_attn8_finalize(const Attn8Params& p, const Final8& out, cudaStream_t s, bool pdl) {
-  return launch_kernel(p.d == 128 ? attn8_finalize_kernel<128> : attn8_finalize_kernel<64>, join_grid(p), dim3(kWarps * 32),
-                       0, s, pdl, p, out);
+  if (many_rows(p)) return p.d == 128 ? finalize<128, kFlightMany>(p, out, s, pdl) : finalize<64, kFlightMany>(p, out, s, pdl);
+  return p.d == 128 ? finalize<128, kFlight>(p, out, s, pdl) : finalize<64, kFlight>(p, out, s, pdl);
 }
 
 }  // namespace ss

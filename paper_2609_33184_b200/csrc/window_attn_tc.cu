@@ -70,10 +70,36 @@ struct CfgW {
   static constexpr uint32_t kColO = 2 * NQ;                 // two score buffers, then O^T
   static constexpr int kCols = 2 * NQ + NP;
   static constexpr uint32_t kTmemCols = kCols <= 64 ? 64 : 128;
-  static_assert(kUnits >= 3 && kCols <= 128 && kPBytes >= 4 * NR * 4, "shape");
+  static_assert(kUnits >= 3 && kCols <= 128 && kPBytes >= 4 * NR * 4 && kUnits * kUnitBytes >= NR * (D + 5) * 4, "shape");
 };
 
-template <int NR, int D>
+// Barrier of all threads of the cluster; orders their shared memory.
+__device__ __forceinline__ void cluster_sync() {
+  __syncwarp();
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// The same place in the shared memory of the cluster's CTA number `rank`.
+__device__ __forceinline__ uint32_t peer_addr(const void* x, int rank) {
+  uint32_t at;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(x)), "r"(rank));
+  return at;
+}
+__device__ __forceinline__ float peer_f(const float* x, int rank) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(peer_addr(x, rank)) : "memory");
+  return v;
+}
+__device__ __forceinline__ float4 peer_f4(const float* x, int rank) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+               : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+               : "r"(peer_addr(x, rank))
+               : "memory");
+  return v;
+}
+
+// CL: a unit is one cluster's (kCluster8), each CTA has one segment.
+template <int NR, int D, bool CL>
 __global__ void __launch_bounds__(CfgW<NR, D>::kThreads, CfgW<NR, D>::kPerSM)
 window_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ CUtensorMap tmK,
                  const __grid_constant__ CUtensorMap tmV) {
@@ -83,7 +109,11 @@ window_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ 
   CtlW<NR>* ctl = reinterpret_cast<CtlW<NR>*>(smem + C::kOffCtl);
   uint8_t* q_s = smem + C::kOffQ;
   uint8_t* p_s = smem + C::kOffP;
-  float* smax = reinterpret_cast<float*>(p_s);  // [4][NR] maxima and sums of the warps, while P is not in use
+  float* smax = reinterpret_cast<float*>(p_s);    // [4][NR] maxima and sums of the warps, while P is not in use
+  // (CL) state of this CTA's part, where the ring was: m[NR], row sums of the four warps [NR][4], a[NR][D]
+  float* part_m = reinterpret_cast<float*>(smem);
+  float* part_l = part_m + NR;
+  float* part_a = part_l + 4 * NR;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   constexpr int kProducerWarp = 4, kMmaWarp = 5;
 
@@ -104,28 +134,43 @@ window_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ 
       ctl->unset = 0;
       fence_barrier_init();
     }
+    __syncwarp();
+    // The others wait for this below; the producer goes on: its first copies have a chain of dependent loads in
+    // front of them (length, page id, K) that all the rest waits for.
+    __threadfence_block();
+    asm volatile("barrier.cta.arrive 2, %0;" ::"n"(C::kThreads) : "memory");
   }
+  Place8 place = {};
+  if (CL) place = cluster_place8(p);
+  auto find = [&]() {
+    Share8 s = {};
+    if (!CL) s = find_share8<true>(p);
+    return s;
+  };
+  auto seg_first = [&](const Share8& s, Seg8* g) { return CL ? cluster_seg8(p, place, g) : seg_first8<true>(p, s, g); };
+  auto seg_next = [&](const Share8& s, Seg8* g) { return !CL && seg_next8<true>(p, s, g); };
   // (tensor memory is taken after the wait: the kernel in front may still be about to allocate its own)
   pdl_wait_prior();
   pdl_launch_dependents();
-  if (warp == kProducerWarp) {
-    __syncwarp();
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctl->tmem_base)),
-                 "r"(C::kTmemCols)
-                 : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-  }
-  if (warp == 0) {
-    const Share8 share = find_share8<true>(p);
-    if (lane == 0) {
-      ctl->share = share;
-      ctl->has[0] = seg_first8<true>(p, share, &ctl->seg[0]);
+  if (warp != kProducerWarp) {
+    if (warp == kMmaWarp) {
+      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctl->tmem_base)),
+                   "r"(C::kTmemCols)
+                   : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
+    if (warp == 0) {
+      const Share8 share = find();
+      if (lane == 0) {
+        ctl->share = share;
+        ctl->has[0] = seg_first(share, &ctl->seg[0]);
+      }
+    }
+    tc_fence_before();
+    asm volatile("barrier.cta.sync 2, %0;" ::"n"(C::kThreads) : "memory");
+    tc_fence_after();
   }
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
-  const uint32_t tmem = ctl->tmem_base;
+  const uint32_t tmem = ctl->tmem_base;  // (not for the producer, as the share)
   const Share8& share = ctl->share;
   auto mwait = [&](uint64_t* bar, uint32_t parity) {
     return mbar_try_wait(bar, parity) || wait_slow(bar, parity, &ctl->abort, p.status);
@@ -140,8 +185,9 @@ window_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ 
     int j = 0, u = 0;      // units filled so far, the next one's place in the ring
     uint32_t ph = 1;       // parity of its release
     bool ok = true;
+    const Share8 share = find();
     Seg8 g;
-    for (bool more = seg_first8<true>(p, share, &g); more && ok; more = seg_next8<true>(p, share, &g)) {
+    for (bool more = seg_first(share, &g); more && ok; more = seg_next(share, &g)) {
       const Win8 w = win8(p, g.b);
       int inner = 0, outer = 0;
       auto look = [&](int t) {  // this lane's granule of tile t
@@ -191,7 +237,7 @@ window_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ 
     int it0 = 0, seg = 0;  // tiles and segments before this one
     bool ok = true;
     Seg8 g;
-    for (bool more = seg_first8<true>(p, share, &g); more && ok; more = seg_next8<true>(p, share, &g), ++seg) {
+    for (bool more = seg_first(share, &g); more && ok; more = seg_next(share, &g), ++seg) {
       const int n = g.t1 - g.t0;
       int qi = 0, pi = 0;
       bool q_there = false;
@@ -307,7 +353,7 @@ window_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ 
       const Win8 w = win8(p, g.b);
       if (tid == 0) {  // the next segment, read by everybody after this one's tiles
         Seg8 s = g;
-        ctl->has[(k_seg + 1) & 1] = seg_next8<true>(p, share, &s);
+        ctl->has[(k_seg + 1) & 1] = seg_next(share, &s);
         ctl->seg[(k_seg + 1) & 1] = s;
       }
       q_store();
@@ -336,18 +382,9 @@ window_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ 
             x[r / 2 + 1] = fma2_f(make_float2(__uint_as_float(raw[r + 2]), __uint_as_float(raw[r + 3])), sc2, make_float2(nm.z, nm.w));
           }
         }
+        unsigned dead = 0;  // keys of this warp that no query sees
         if (!plain) {
-          const unsigned dead = __ballot_sync(0xffffffffu, !win_any8(p, w, tok));
-          if (dead) {  // tokens that no query sees may hold anything; their weights are 0, so V must be finite there
-            const int jv = 2 * it + 1;
-            wait(&ctl->ufull[jv % UNITS], (jv / UNITS) & 1);
-            constexpr int kPieces = 8 * C::kHalves;  // 16-byte pieces of a row
-            const int piece = lane % kPieces;
-            uint8_t* v = smem + (jv % UNITS) * C::kUnitBytes + (piece >> 3) * kBox + warp * 32 * 128 + (piece & 7) * 16;
-#pragma unroll 1
-            for (int r = lane / kPieces; r < 32; r += 32 / kPieces)
-              if (dead >> r & 1) *reinterpret_cast<uint4*>(v + r * 128) = make_uint4(0, 0, 0, 0);
-          }
+          dead = __ballot_sync(0xffffffffu, !win_any8(p, w, tok));
           if (p.T_q == 1) {
             const bool ok = win_sees8(p, w, w.first, tok);
 #pragma unroll
@@ -365,7 +402,7 @@ window_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ 
         float mx = -INFINITY;
 #pragma unroll
         for (int r = 0; r < NR / 2; ++r) mx = max3_f(mx, x[r].x, x[r].y);
-        if (bar_or8<SOFT>(first || mx > kOver || ctl->unset)) {
+        if (first || bar_or8<SOFT>(mx > kOver || ctl->unset)) {
           // ---- set the references to the exact maxima; later in a segment (rare) raise them, which
           // rescales O^T and the row sums ----
           if (!first) {
@@ -440,6 +477,16 @@ window_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ 
               *reinterpret_cast<uint4*>(p_s + (NR / 8 + c) * (kTok8 * 16) + key * 16) =
                   make_uint4(lo[4 * c], lo[4 * c + 1], lo[4 * c + 2], lo[4 * c + 3]);
           }
+          if (dead) {  // such tokens may hold anything; their weights are 0, so V must be finite there
+            const int jv = 2 * it + 1;
+            wait(&ctl->ufull[jv % UNITS], (jv / UNITS) & 1);
+            constexpr int kPieces = 8 * C::kHalves;  // 16-byte pieces of a row
+            const int piece = lane % kPieces;
+            uint8_t* v = smem + (jv % UNITS) * C::kUnitBytes + (piece >> 3) * kBox + warp * 32 * 128 + (piece & 7) * 16;
+#pragma unroll 1
+            for (int r = lane / kPieces; r < 32; r += 32 / kPieces)
+              if (dead >> r & 1) *reinterpret_cast<uint4*>(v + r * 128) = make_uint4(0, 0, 0, 0);
+          }
           fence_proxy_async();
           tc_fence_before();
         }
@@ -474,6 +521,24 @@ window_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ 
       }
       wait(&ctl->pfree, (it - 1) & 1);
       tc_fence_after();
+      if (CL) {
+        if (lane % (32 / NR) == 0) part_l[lane / (32 / NR) * 4 + warp] = v[0];
+        if (tid < NR) part_m[tid] = -ctl->nm[tid];
+#pragma unroll 1
+        for (int q = 0; q < NR && q < done.nrows; q += 8) {
+          uint32_t o[C::kTerms][8];
+#pragma unroll
+          for (int k = 0; k < C::kTerms; ++k) tmem_ld<8>(tmem + lane_off + C::kColO + k * NR + q, o[k]);
+          tc_wait_ld();
+#pragma unroll
+          for (int c = 0; c < 8; ++c) {
+            float a = __uint_as_float(o[0][c]);
+            if (C::kTerms == 2) a += __uint_as_float(o[C::kTerms - 1][c]);
+            if (key < D) part_a[(q + c) * D + key] = a;
+          }
+        }
+        break;
+      }
       bar8<SOFT>();  // (nobody's P is in use)
       if (lane % (32 / NR) == 0) smax[warp * NR + lane / (32 / NR)] = v[0];
       bar8<SOFT>();
@@ -515,24 +580,85 @@ window_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ 
       tc_fence_before();
       bar8<SOFT>();  // sums, references and Q may be written anew
     }
-    if ((int)blockIdx.x < p.B) put_empty8<true>(p, tid, SOFT);
-    if (p.plan && warp == 0 && blockIdx.x == gridDim.x - 1) put_plan8<true>(p);
+    if (CL) {
+      if (!ctl->has[0] && tid < 4 * NR) part_l[tid] = 0.f;
+    } else if ((int)blockIdx.x < p.B) {
+      put_empty8<true>(p, tid, SOFT);
+    }
+    if (!CL && p.plan && warp == 0 && blockIdx.x == gridDim.x - 1) put_plan8<true>(p);
   }
 
   tc_fence_before();
-  __syncthreads();
-  if (warp == kProducerWarp)
+  if (!CL) {
+    __syncthreads();
+  } else {
+    // ---- the cluster's parts: a CTA joins every cluster-th row, in the order of the parts; a thread four head
+    // dims, so that a pass takes 4 or 8 rows (one row a pass: a round's 16 rows a CTA took 8 us) ----
+    cluster_sync();
+    if (tid < SOFT) {
+      Seg8 g = {};
+      g.b = place.b;
+      g.kvh = place.kvh;
+      g.row0 = place.rt * p.rows_per_tile;
+      g.nrows = min(p.rows_per_tile, p.R - g.row0);
+      const int c = tid % (D / 4) * 4;
+#pragma unroll 1
+      for (int r = place.rank + tid / (D / 4) * p.cluster; r < g.nrows; r += SOFT / (D / 4) * p.cluster) {
+        float m[kMostCluster8], M = -INFINITY, L = 0.f;
+        float4 l[kMostCluster8], a[kMostCluster8], A = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int i = 0; i < kMostCluster8; ++i) {
+          l[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+          if (i < p.cluster) {
+            m[i] = peer_f(part_m + r, i);
+            l[i] = peer_f4(part_l + 4 * r, i);
+            a[i] = peer_f4(part_a + r * D + c, i);
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < kMostCluster8; ++i) {
+          l[i].x = (l[i].x + l[i].y) + (l[i].z + l[i].w);
+          if (l[i].x != 0.f) M = fmaxf(M, m[i]);  // (l = 0: an empty state, whose m and a[] may be anything)
+        }
+#pragma unroll
+        for (int i = 0; i < kMostCluster8; ++i) {
+          if (l[i].x == 0.f) continue;
+          const float f = m[i] == M ? 1.f : exp2f(m[i] - M);
+          L = fmaf(f, l[i].x, L);
+          A.x = fmaf(f, a[i].x, A.x);
+          A.y = fmaf(f, a[i].y, A.y);
+          A.z = fmaf(f, a[i].z, A.z);
+          A.w = fmaf(f, a[i].w, A.w);
+        }
+        if (c == 0) put_ml8(p, g, r, M, L);
+        if (p.O) {
+          const float inv = (L > 0.f || L != L) ? 1.f / L : 0.f;
+          const __nv_bfloat162 lo = __floats2bfloat162_rn(A.x * inv, A.y * inv), hi = __floats2bfloat162_rn(A.z * inv, A.w * inv);
+          *reinterpret_cast<uint2*>(p.O + (((int64_t)g.b * p.H_kv + g.kvh) * p.R + g.row0 + r) * D + c) =
+              make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+        } else {
+          *reinterpret_cast<float4*>(p.part_a + (((int64_t)g.b * p.H_kv + g.kvh) * p.R_stride + g.row0 + r) * D + c) = A;
+        }
+      }
+    }
+    cluster_sync();  // (nobody leaves while its state may be read)
+  }
+  if (warp == kMmaWarp)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(C::kTmemCols) : "memory");
 }
 
 template <int NR, int D>
 cudaError_t prepare() {
-  return cudaFuncSetAttribute(window_tc_kernel<NR, D>, cudaFuncAttributeMaxDynamicSharedMemorySize, CfgW<NR, D>::kSmem);
+  const cudaError_t e = cudaFuncSetAttribute(window_tc_kernel<NR, D, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, CfgW<NR, D>::kSmem);
+  return e != cudaSuccess ? e : cudaFuncSetAttribute(window_tc_kernel<NR, D, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, CfgW<NR, D>::kSmem);
 }
 template <int NR, int D>
 cudaError_t launch(const Attn8Params& p, const CUtensorMap& tmK, const CUtensorMap& tmV, cudaStream_t s, bool pdl) {
   using C = CfgW<NR, D>;
-  return launch_kernel(window_tc_kernel<NR, D>, dim3(p.shares * p.row_tiles), dim3(C::kThreads), C::kSmem, s, pdl, p, tmK, tmV);
+  if (p.mode == kCluster8)
+    return launch_kernel_cluster(window_tc_kernel<NR, D, true>, dim3((unsigned)p.B * p.H_kv * p.row_tiles * p.cluster),
+                                 dim3(C::kThreads), C::kSmem, s, pdl, (unsigned)p.cluster, p, tmK, tmV);
+  return launch_kernel(window_tc_kernel<NR, D, false>, dim3(p.shares * p.row_tiles), dim3(C::kThreads), C::kSmem, s, pdl, p, tmK, tmV);
 }
 template <int D>
 cudaError_t launch_rows(const Attn8Params& p, const CUtensorMap& tmK, const CUtensorMap& tmV, cudaStream_t s, bool pdl) {
