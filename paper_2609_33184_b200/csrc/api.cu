@@ -1378,10 +1378,10 @@ static int granule_log2(const ss::View8& kv) {
 // ran as two rounds: 19.3 us against 12.2 with 96 of 2), so those are taken up to half the CTAs only.
 // Measured, head dim 128, 4 rows, pages of 16, 128 units of 33 tiles: clusters of one 65 us, of two 45.6, cut 47.9; one unit
 // of 33 tiles: 60, clusters of eight 12.4, cut 11.0; 384 units of 32 rows, head dim 64, two tiles: whole 18.6, cut 22.4.
-static void window_mode(ss::Attn8Params* p, int64_t tiles) {
+static void window_mode(ss::Attn8Params* p, int bits, int64_t tiles) {
   const int64_t N = (int64_t)p->shares * p->row_tiles, U = (int64_t)p->B * p->H_kv * p->row_tiles;
   const double one = (p->d == 128 ? 1.2 : 0.8) * (p->gran_log2 >= 5 ? 1.0 : p->gran_log2 == 4 ? 1.3 : 2.1);
-  const double share = p->d / 128.0 * 0.0094 / p->row_tiles;  // of memory's time, per CTA that is at work
+  const double share = p->d * bits / 2048.0 * 0.0094 / p->row_tiles;  // of memory's time, per CTA that is at work
   const auto tile_us = [&](int64_t ctas) { return pow(pow(one, 4) + pow(share * ctas, 4), 0.25); };
   const int64_t full = U / N, rest = U % N, steps = (U * tiles + N - 1) / N;
   const double whole = tiles * (full * tile_us(N) + (rest ? tile_us(rest) : 0.0)) + 1.0;
@@ -1455,7 +1455,7 @@ static ss_status attn8(ss_ctx* c, int bits, const ss_tensor& Q, int32_t B, int32
   const int64_t tokens = win.window && seen < room ? seen : room;
   const int64_t walked = win.window && seen + 2 * 32 < room ? seen + 2 * 32 : room;
   const int64_t most_tiles = (walked + ss::kTok8 - 1) / ss::kTok8;
-  if (win.window && tc && bits == 16) window_mode(p, most_tiles);
+  if (win.window && tc) window_mode(p, bits, most_tiles);
   p->scale_log2 = scale * 1.4426950408889634f;
   p->scratch = c->scratch8;
   p->plan = p->O || p->mode != ss::kCut8 ? nullptr : c->plan8;

@@ -94,7 +94,7 @@ struct Cfg8 {
   static constexpr int kCols = 2 * NS + NP;
   static constexpr uint32_t kTmemCols = kCols <= 64 ? 64 : kCols <= 128 ? 128 : 256;
   static constexpr uint32_t kColO = 2 * NS;
-  static_assert(kUnits >= 4 && kCols <= 256 && NR % 8 == 0, "shape");
+  static_assert(kUnits >= 4 && kCols <= 256 && NR % 8 == 0 && kUnits * kUnitBytes >= NQ * (D + 5) * 4, "shape");
 };
 
 // A descriptor's low word holds the address / 16 (and the LBO above it), so the operands of the steps of
@@ -127,7 +127,8 @@ __device__ __forceinline__ __half2 bits_h2(uint32_t u) { return *reinterpret_cas
 __device__ __forceinline__ uint32_t residue(uint32_t w) {
   return h2_bits(__hmul2(__hsub2(bits_h2(w), bits_h2(w & 0xff00ff00u)), __float2half2_rn(8.f)));
 }
-template <int NR, int D, bool WIN>
+// WIN: over a window; CL: a unit is one cluster's (kCluster8), each CTA has one segment.
+template <int NR, int D, bool WIN, bool CL>
 __global__ void __launch_bounds__(Cfg8<NR, D, WIN>::kThreads, Cfg8<NR, D, WIN>::kPerSM)
 attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ CUtensorMap tmK,
                 const __grid_constant__ CUtensorMap tmV) {
@@ -139,6 +140,14 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
   uint8_t* p_s = smem + C::kOffP;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   constexpr int kProducerWarp = 4, kMmaWarp = 5;
+
+  // (CL) state of this CTA's part, where the ring was: m[NQ], row sums of the four warps [NQ][4], a[NQ][D]
+  float* part_m = reinterpret_cast<float*>(smem);
+  float* part_l = part_m + NQ;
+  float* part_a = part_l + 4 * NQ;
+  // The warp that takes the tensor memory.  Over a window the producer is free of it and of the barrier in front of
+  // the roles: its first copies have a chain of dependent loads in front of them that all the rest waits for.
+  constexpr int kTmemWarp = WIN ? kMmaWarp : kProducerWarp;
 
   if (warp == kProducerWarp) {
     if (lane == 0) {
@@ -157,11 +166,25 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
       if constexpr (WIN) ctl->unset = 0;
       fence_barrier_init();
     }
+    if (WIN) {
+      __syncwarp();
+      __threadfence_block();
+      asm volatile("barrier.cta.arrive 2, %0;" ::"n"(C::kThreads) : "memory");
+    }
   }
+  Place8 place = {};
+  if (CL) place = cluster_place8(p);
+  auto find = [&]() {
+    Share8 s = {};
+    if (!CL) s = find_share8<WIN>(p);
+    return s;
+  };
+  auto seg_first = [&](const Share8& s, Seg8* g) { return CL ? cluster_seg8(p, place, g) : seg_first8<WIN>(p, s, g); };
+  auto seg_next = [&](const Share8& s, Seg8* g) { return !CL && seg_next8<WIN>(p, s, g); };
   // (tensor memory is taken after the wait: the kernel in front may still be about to allocate its own)
   pdl_wait_prior();
   pdl_launch_dependents();
-  if (warp == kProducerWarp) {
+  if (warp == kTmemWarp) {
     __syncwarp();
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctl->tmem_base)),
                  "r"(C::kTmemCols)
@@ -169,15 +192,21 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   if (warp == 0) {
-    const Share8 share = find_share8<WIN>(p);
+    const Share8 share = find();
     if (lane == 0) {
       ctl->share = share;
-      ctl->has[0] = seg_first8<WIN>(p, share, &ctl->seg[0]);
+      ctl->has[0] = seg_first(share, &ctl->seg[0]);
     }
   }
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
+  if (!WIN) {
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+  } else if (warp != kProducerWarp) {
+    tc_fence_before();
+    asm volatile("barrier.cta.sync 2, %0;" ::"n"(C::kThreads) : "memory");
+    tc_fence_after();
+  }
   const uint32_t tmem = ctl->tmem_base;
   const Share8& share = ctl->share;
   auto mwait = [&](uint64_t* bar, uint32_t parity) {
@@ -199,7 +228,8 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
     uint32_t ph = 1;       // parity of its release
     bool ok = true;
     Seg8 g;
-    for (bool more = seg_first8<WIN>(p, share, &g); more && ok; more = seg_next8<WIN>(p, share, &g)) {
+    const Share8 mine_share = WIN ? find() : share;
+    for (bool more = seg_first(mine_share, &g); more && ok; more = seg_next(mine_share, &g)) {
       Win8 w = {};
       if (WIN) w = win8(p, g.b);
       int inner = 0, outer = 0;
@@ -273,7 +303,7 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
     int it0 = 0, seg = 0;  // tiles and segments before this one
     bool ok = true;
     Seg8 g;
-    for (bool more = seg_first8<WIN>(p, share, &g); more && ok; more = seg_next8<WIN>(p, share, &g), ++seg) {
+    for (bool more = seg_first(share, &g); more && ok; more = seg_next(share, &g), ++seg) {
       const int n = g.t1 - g.t0;
       int qi = 0, pi = 0;
       bool q_there = false;
@@ -471,7 +501,7 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
       const int t0 = g.t0, t1 = g.t1, len = g.len, b = g.b;
       if (tid == 0) {  // the next segment, read by everybody after this one's tiles
         Seg8 s = g;
-        ctl->has[(k_seg + 1) & 1] = seg_next8<WIN>(p, share, &s);
+        ctl->has[(k_seg + 1) & 1] = seg_next(share, &s);
         ctl->seg[(k_seg + 1) & 1] = s;
       }
       q_store();
@@ -494,17 +524,9 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
         const int tok = WIN ? win_token8(w, t * kTok8 + key) : 0;
         wait(&ctl->sfull[it & 1], (it >> 1) & 1);
         tc_fence_after();
+        unsigned dead = 0;  // (window) keys of this warp that no query sees
         if (WIN) {
-          const unsigned dead = masked ? __ballot_sync(0xffffffffu, !win_any8(p, w, tok)) : 0u;
-          if (dead) {  // tokens that no query sees, as those past the length
-            const int jv = 2 * it + 1;
-            wait(&ctl->ufull[jv % UNITS], (jv / UNITS) & 1);
-            constexpr int kPieces = D / 16;  // 16-byte pieces of a row
-            uint8_t* v = smem + (jv % UNITS) * C::kUnitBytes + warp * 32 * D + (lane % kPieces) * 16;
-#pragma unroll 1
-            for (int r = lane / kPieces; r < 32; r += 32 / kPieces)
-              if (dead >> r & 1) *reinterpret_cast<uint4*>(v + r * D) = make_uint4(0, 0, 0, 0);
-          }
+          if (masked) dead = __ballot_sync(0xffffffffu, !win_any8(p, w, tok));
         } else if (n_valid < kTok8) {
           // tokens past the length may hold anything; their weights are 0, so V must be finite there
           const int jv = 2 * it + 1;
@@ -578,7 +600,7 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
         for (int r = 0; r < NR / 2; ++r) mx = max3_f(mx, x[r].x, x[r].y);
         bool missing = false;  // some row has no reference: it has seen nothing so far
         if constexpr (WIN) missing = ctl->unset;
-        if (bar_or8<SOFT>(first || mx > kOver || missing)) {
+        if ((WIN && first) || bar_or8<SOFT>(first || mx > kOver || missing)) {
           // ---- set the references to the exact maxima; later in a segment (rare) raise them, which
           // rescales O^T and the row sums ----
           float mine = -INFINITY;
@@ -669,6 +691,15 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
           for (int k = 0; k < NP / 16; ++k)
             *reinterpret_cast<uint4*>(p_s + k * (kTok8 * 16) + key * 16) =
                 make_uint4(word[4 * k], word[4 * k + 1], word[4 * k + 2], word[4 * k + 3]);
+          if (WIN && dead) {  // such tokens may hold anything; their weights are 0, so V must be finite there
+            const int jv = 2 * it + 1;
+            wait(&ctl->ufull[jv % UNITS], (jv / UNITS) & 1);
+            constexpr int kPieces = D / 16;  // 16-byte pieces of a row
+            uint8_t* v = smem + (jv % UNITS) * C::kUnitBytes + warp * 32 * D + (lane % kPieces) * 16;
+#pragma unroll 1
+            for (int r = lane / kPieces; r < 32; r += 32 / kPieces)
+              if (dead >> r & 1) *reinterpret_cast<uint4*>(v + r * D) = make_uint4(0, 0, 0, 0);
+          }
           fence_proxy_async();
           tc_fence_before();
         }
@@ -699,6 +730,25 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
           } else {
             v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
           }
+        }
+        if (CL) {
+          wait(&ctl->pfree, (it - 1) & 1);
+          tc_fence_after();
+          if (lane % (32 / NQ) == 0) part_l[lane / (32 / NQ) * 4 + warp] = v[0];
+          if (tid < NQ) part_m[tid] = -ctl->nm[tid];
+#pragma unroll 1
+          for (int q = 0; q < NR && q < done.nrows; q += 8) {
+            uint32_t o[3][8];
+#pragma unroll
+            for (int k = 0; k < 3; ++k) tmem_ld<8>(tmem + lane_off + C::kColO + k * NR + q, o[k]);
+            tc_wait_ld();
+#pragma unroll
+            for (int c = 0; c < 8; ++c)
+              if (key < D)
+                part_a[(q + c) * D + key] = fmaf(__uint_as_float(o[2][c]), 1.f / 64.f,
+                                                 fmaf(__uint_as_float(o[1][c]), 0.125f, __uint_as_float(o[0][c])));
+          }
+          break;
         }
         bar8<SOFT>();  // (every thread is done with smax as maxima)
         if (lane % (32 / NQ) == 0) ctl->smax[warp][lane / (32 / NQ)] = v[0];
@@ -747,33 +797,47 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
       tc_fence_before();
       bar8<SOFT>();  // sums, references and Q may be written anew
     }
-    if ((int)blockIdx.x < p.B) put_empty8<WIN>(p, tid, SOFT);
-    if (p.plan && warp == 0 && blockIdx.x == gridDim.x - 1) put_plan8<WIN>(p);
+    if (CL) {
+      if (!ctl->has[0] && tid < 4 * NQ) part_l[tid] = 0.f;
+    } else if ((int)blockIdx.x < p.B) {
+      put_empty8<WIN>(p, tid, SOFT);
+    }
+    if (!CL && p.plan && warp == 0 && blockIdx.x == gridDim.x - 1) put_plan8<WIN>(p);
   }
 
   tc_fence_before();
-  __syncthreads();
-  if (warp == kProducerWarp)
+  if (!CL) {
+    __syncthreads();
+  } else {
+    cluster_end8<NQ, D>(p, place, part_m, part_l, part_a);
+  }
+  if (warp == kTmemWarp)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(C::kTmemCols) : "memory");
 }
 
-template <int NR, int D, bool WIN>
+template <int NR, int D, bool WIN, bool CL>
 cudaError_t prepare8() {
-  return cudaFuncSetAttribute(attn8_tc_kernel<NR, D, WIN>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+  return cudaFuncSetAttribute(attn8_tc_kernel<NR, D, WIN, CL>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                               Cfg8<NR, D, WIN>::kSmem);
 }
 template <int NR, int D, bool WIN>
 cudaError_t launch8(const Attn8Params& p, const CUtensorMap& tmK, const CUtensorMap& tmV, cudaStream_t s, bool pdl) {
   using C = Cfg8<NR, D, WIN>;
-  return launch_kernel(attn8_tc_kernel<NR, D, WIN>, dim3(p.shares * p.row_tiles), dim3(C::kThreads), C::kSmem, s, pdl, p, tmK,
-                       tmV);
+  if constexpr (WIN) {
+    if (p.mode == kCluster8)
+      return launch_kernel_cluster(attn8_tc_kernel<NR, D, true, true>,
+                                   dim3((unsigned)p.B * p.H_kv * p.row_tiles * p.cluster), dim3(C::kThreads), C::kSmem, s,
+                                   pdl, (unsigned)p.cluster, p, tmK, tmV);
+  }
+  return launch_kernel(attn8_tc_kernel<NR, D, WIN, false>, dim3(p.shares * p.row_tiles), dim3(C::kThreads), C::kSmem, s, pdl,
+                       p, tmK, tmV);
 }
-template <int D, bool WIN>
+template <int D, bool WIN, bool CL>
 cudaError_t prepare_rows() {
-  cudaError_t e = prepare8<8, D, WIN>();
-  if (e == cudaSuccess) e = prepare8<16, D, WIN>();
-  if (e == cudaSuccess) e = prepare8<24, D, WIN>();
-  if (e == cudaSuccess) e = prepare8<32, D, WIN>();
+  cudaError_t e = prepare8<8, D, WIN, CL>();
+  if (e == cudaSuccess) e = prepare8<16, D, WIN, CL>();
+  if (e == cudaSuccess) e = prepare8<24, D, WIN, CL>();
+  if (e == cudaSuccess) e = prepare8<32, D, WIN, CL>();
   return e;
 }
 template <int D, bool WIN>
@@ -788,10 +852,12 @@ cudaError_t launch_rows(const Attn8Params& p, const CUtensorMap& tmK, const CUte
 }  // namespace
 
 cudaError_t attn8_tc_prepare() {
-  cudaError_t e = prepare_rows<128, false>();
-  if (e == cudaSuccess) e = prepare_rows<64, false>();
-  if (e == cudaSuccess) e = prepare_rows<128, true>();
-  if (e == cudaSuccess) e = prepare_rows<64, true>();
+  cudaError_t e = prepare_rows<128, false, false>();
+  if (e == cudaSuccess) e = prepare_rows<64, false, false>();
+  if (e == cudaSuccess) e = prepare_rows<128, true, false>();
+  if (e == cudaSuccess) e = prepare_rows<64, true, false>();
+  if (e == cudaSuccess) e = prepare_rows<128, true, true>();
+  if (e == cudaSuccess) e = prepare_rows<64, true, true>();
   return e;
 }
 

@@ -52,5 +52,105 @@ __device__ __forceinline__ void tmem_ld(uint32_t taddr, uint32_t* r) {
   }
 }
 
+// Barrier of all threads of the cluster; orders their shared memory.
+__device__ __forceinline__ void cluster_sync() {
+  __syncwarp();
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// The same place in the shared memory of the cluster's CTA number `rank`.  (The loads stay between the barriers, as
+// all volatile ones do, but may pass stores to other memory.)
+__device__ __forceinline__ uint32_t peer_addr(const void* x, int rank) {
+  uint32_t at;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(x)), "r"(rank));
+  return at;
+}
+__device__ __forceinline__ float peer_f(const float* x, int rank) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(peer_addr(x, rank)));
+  return v;
+}
+__device__ __forceinline__ float4 peer_f4(const float* x, int rank) {
+  float4 v;
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+               : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
+               : "r"(peer_addr(x, rank)));
+  return v;
+}
+
+// The parts of a unit and row tile that a cluster's CTAs (kCluster8) have left in their shared memory - m[N], the
+// row sums of four warps [N][4], a[N][D] - to the output: each CTA joins every cluster-th row, in the order of the
+// parts.  By 128 threads, four head dims each, so 4 or 8 rows side by side, and ROWS of those in flight (PARTS: most
+// CTAs of the cluster): with one row a pass the 16 rows a CTA of a round's cluster took 8 us.
+template <int N, int D, int PARTS, int ROWS>
+__device__ __forceinline__ void cluster_join8(const Attn8Params& p, const Place8& place, const float* part_m,
+                                              const float* part_l, const float* part_a) {
+  Seg8 g = {};
+  g.b = place.b;
+  g.kvh = place.kvh;
+  g.row0 = place.rt * p.rows_per_tile;
+  g.nrows = min(p.rows_per_tile, p.R - g.row0);
+  const int c = threadIdx.x % (D / 4) * 4, step = 128 / (D / 4) * p.cluster;
+#pragma unroll 1
+  for (int r0 = place.rank + threadIdx.x / (D / 4) * p.cluster; r0 < g.nrows; r0 += ROWS * step) {
+    float m[ROWS][PARTS];
+    float4 l[ROWS][PARTS], a[ROWS][PARTS];
+#pragma unroll
+    for (int k = 0; k < ROWS; ++k) {
+      const int r = r0 + k * step;
+#pragma unroll
+      for (int i = 0; i < PARTS; ++i) {
+        l[k][i] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (i < p.cluster && r < g.nrows) {
+          m[k][i] = peer_f(part_m + r, i);
+          l[k][i] = peer_f4(part_l + 4 * r, i);
+          a[k][i] = peer_f4(part_a + r * D + c, i);
+        }
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < ROWS; ++k) {
+      const int r = r0 + k * step;
+      if (r >= g.nrows) break;
+      float M = -INFINITY, L = 0.f;
+      float4 A = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int i = 0; i < PARTS; ++i) {
+        l[k][i].x = (l[k][i].x + l[k][i].y) + (l[k][i].z + l[k][i].w);
+        if (l[k][i].x != 0.f) M = fmaxf(M, m[k][i]);  // (l = 0: an empty state, whose m and a[] may be anything)
+      }
+#pragma unroll
+      for (int i = 0; i < PARTS; ++i) {
+        if (l[k][i].x == 0.f) continue;
+        const float f = m[k][i] == M ? 1.f : exp2f(m[k][i] - M);
+        L = fmaf(f, l[k][i].x, L);
+        A.x = fmaf(f, a[k][i].x, A.x);
+        A.y = fmaf(f, a[k][i].y, A.y);
+        A.z = fmaf(f, a[k][i].z, A.z);
+        A.w = fmaf(f, a[k][i].w, A.w);
+      }
+      if (c == 0) put_ml8(p, g, r, M, L);
+      if (p.O) {
+        const float inv = (L > 0.f || L != L) ? 1.f / L : 0.f;
+        const __nv_bfloat162 lo = __floats2bfloat162_rn(A.x * inv, A.y * inv), hi = __floats2bfloat162_rn(A.z * inv, A.w * inv);
+        *reinterpret_cast<uint2*>(p.O + (((int64_t)g.b * p.H_kv + g.kvh) * p.R + g.row0 + r) * D + c) =
+            make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+      } else {
+        *reinterpret_cast<float4*>(p.part_a + (((int64_t)g.b * p.H_kv + g.kvh) * p.R_stride + g.row0 + r) * D + c) = A;
+      }
+    }
+  }
+}
+// All of it, by the whole CTA.
+template <int N, int D>
+__device__ __forceinline__ void cluster_end8(const Attn8Params& p, const Place8& place, const float* part_m,
+                                             const float* part_l, const float* part_a) {
+  cluster_sync();
+  if (threadIdx.x < 128) {
+    if (p.cluster <= 2) cluster_join8<N, D, 2, N < 16 ? 1 : 4>(p, place, part_m, part_l, part_a);
+    else cluster_join8<N, D, kMostCluster8, 1>(p, place, part_m, part_l, part_a);
+  }
+  cluster_sync();  // (nobody leaves while its state may be read)
+}
+
 }  // namespace tc
 }  // namespace ss

@@ -73,31 +73,6 @@ struct CfgW {
   static_assert(kUnits >= 3 && kCols <= 128 && kPBytes >= 4 * NR * 4 && kUnits * kUnitBytes >= NR * (D + 5) * 4, "shape");
 };
 
-// Barrier of all threads of the cluster; orders their shared memory.
-__device__ __forceinline__ void cluster_sync() {
-  __syncwarp();
-  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-// The same place in the shared memory of the cluster's CTA number `rank`.
-__device__ __forceinline__ uint32_t peer_addr(const void* x, int rank) {
-  uint32_t at;
-  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(x)), "r"(rank));
-  return at;
-}
-__device__ __forceinline__ float peer_f(const float* x, int rank) {
-  float v;
-  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(peer_addr(x, rank)) : "memory");
-  return v;
-}
-__device__ __forceinline__ float4 peer_f4(const float* x, int rank) {
-  float4 v;
-  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
-               : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w)
-               : "r"(peer_addr(x, rank))
-               : "memory");
-  return v;
-}
-
 // CL: a unit is one cluster's (kCluster8), each CTA has one segment.
 template <int NR, int D, bool CL>
 __global__ void __launch_bounds__(CfgW<NR, D>::kThreads, CfgW<NR, D>::kPerSM)
@@ -592,56 +567,7 @@ window_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ 
   if (!CL) {
     __syncthreads();
   } else {
-    // ---- the cluster's parts: a CTA joins every cluster-th row, in the order of the parts; a thread four head
-    // dims, so that a pass takes 4 or 8 rows (one row a pass: a round's 16 rows a CTA took 8 us) ----
-    cluster_sync();
-    if (tid < SOFT) {
-      Seg8 g = {};
-      g.b = place.b;
-      g.kvh = place.kvh;
-      g.row0 = place.rt * p.rows_per_tile;
-      g.nrows = min(p.rows_per_tile, p.R - g.row0);
-      const int c = tid % (D / 4) * 4;
-#pragma unroll 1
-      for (int r = place.rank + tid / (D / 4) * p.cluster; r < g.nrows; r += SOFT / (D / 4) * p.cluster) {
-        float m[kMostCluster8], M = -INFINITY, L = 0.f;
-        float4 l[kMostCluster8], a[kMostCluster8], A = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-        for (int i = 0; i < kMostCluster8; ++i) {
-          l[i] = make_float4(0.f, 0.f, 0.f, 0.f);
-          if (i < p.cluster) {
-            m[i] = peer_f(part_m + r, i);
-            l[i] = peer_f4(part_l + 4 * r, i);
-            a[i] = peer_f4(part_a + r * D + c, i);
-          }
-        }
-#pragma unroll
-        for (int i = 0; i < kMostCluster8; ++i) {
-          l[i].x = (l[i].x + l[i].y) + (l[i].z + l[i].w);
-          if (l[i].x != 0.f) M = fmaxf(M, m[i]);  // (l = 0: an empty state, whose m and a[] may be anything)
-        }
-#pragma unroll
-        for (int i = 0; i < kMostCluster8; ++i) {
-          if (l[i].x == 0.f) continue;
-          const float f = m[i] == M ? 1.f : exp2f(m[i] - M);
-          L = fmaf(f, l[i].x, L);
-          A.x = fmaf(f, a[i].x, A.x);
-          A.y = fmaf(f, a[i].y, A.y);
-          A.z = fmaf(f, a[i].z, A.z);
-          A.w = fmaf(f, a[i].w, A.w);
-        }
-        if (c == 0) put_ml8(p, g, r, M, L);
-        if (p.O) {
-          const float inv = (L > 0.f || L != L) ? 1.f / L : 0.f;
-          const __nv_bfloat162 lo = __floats2bfloat162_rn(A.x * inv, A.y * inv), hi = __floats2bfloat162_rn(A.z * inv, A.w * inv);
-          *reinterpret_cast<uint2*>(p.O + (((int64_t)g.b * p.H_kv + g.kvh) * p.R + g.row0 + r) * D + c) =
-              make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
-        } else {
-          *reinterpret_cast<float4*>(p.part_a + (((int64_t)g.b * p.H_kv + g.kvh) * p.R_stride + g.row0 + r) * D + c) = A;
-        }
-      }
-    }
-    cluster_sync();  // (nobody leaves while its state may be read)
+    cluster_end8<NR, D>(p, place, part_m, part_l, part_a);
   }
   if (warp == kMmaWarp)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(C::kTmemCols) : "memory");
