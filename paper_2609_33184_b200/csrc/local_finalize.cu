@@ -162,6 +162,111 @@ __global__ void __launch_bounds__(kWarpsPerCta * 32) local_kernel(const LocalPar
   if (blockIdx.x == 0) pdl_wait_prior();  // one CTA keeps the completion order along the stream
 }
 
+// The same for up to 8 local keys (a chain of 2 to 8 candidates): a warp keeps the kv-head's K and V rows in
+// registers for its rows, and the 8 scores of a row are summed over the lanes together, halving the keys a lane holds
+// at every step (9 shuffles instead of 40).  The sums run in the order of the kernel above, so the states are the same
+// bits.  (16 requests, 8 kv-heads, 32 rows, 8 keys: 7.6 -> 5.2 us.)
+constexpr int kFewKeys = 8, kFewRows = 4;  // rows of a warp
+
+template <int D>
+__global__ void __launch_bounds__(kWarpsPerCta * 32) local_few_kernel(const LocalParams p) {
+  constexpr int CPL = D / 32;  // columns per lane
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int R = p.G * p.T_q, per_pair = (R + kWarpsPerCta * kFewRows - 1) / (kWarpsPerCta * kFewRows);
+  pdl_launch_dependents();
+  const int pair = blockIdx.x / per_pair, b = pair / p.H_kv, kvh = pair - b * p.H_kv;
+  const int r0 = (blockIdx.x - pair * per_pair) * (kWarpsPerCta * kFewRows) + warp * kFewRows;
+  auto load_row = [&](const __nv_bfloat16* ptr, float (&v)[CPL]) {  // this lane's elements as floats
+#pragma unroll
+    for (int c = 0; c < CPL; c += 4) {
+      if (CPL == 4) {
+        const uint2 raw = *reinterpret_cast<const uint2*>(ptr);
+        v[0] = __uint_as_float(raw.x << 16);
+        v[1] = __uint_as_float(raw.x & 0xffff0000u);
+        v[CPL - 2] = __uint_as_float(raw.y << 16);
+        v[CPL - 1] = __uint_as_float(raw.y & 0xffff0000u);
+      } else {
+        const uint32_t raw = *reinterpret_cast<const uint32_t*>(ptr);
+        v[0] = __uint_as_float(raw << 16);
+        v[1] = __uint_as_float(raw & 0xffff0000u);
+      }
+    }
+  };
+  if (r0 < R) {
+    float q[kFewRows][CPL], k[kFewKeys][CPL], v[kFewKeys][CPL];
+    unsigned vis[kFewRows];
+#pragma unroll
+    for (int n = 0; n < kFewRows; ++n) {
+      const int r = min(r0 + n, R - 1), i = r % p.T_q, h = kvh * p.G + r / p.T_q;
+      load_row(p.Q + b * p.q_sb + (int64_t)h * p.q_sh + i * p.q_st + lane * CPL, q[n]);
+      const uint64_t* bits = p.mask_bits ? p.mask_bits + ((int64_t)b * p.T_q + i) * p.mask_words : nullptr;
+      vis[n] = (unsigned)visible_word(bits, 0, i + (p.T_loc - p.T_q), p.T_loc);
+    }
+#pragma unroll
+    for (int u = 0; u < kFewKeys; ++u) {
+#pragma unroll
+      for (int c = 0; c < CPL; ++c) k[u][c] = v[u][c] = 0.f;
+      if (u < p.T_loc) {
+        load_row(p.K + b * p.k_sb + kvh * p.k_sh + u * p.k_st + lane * CPL, k[u]);
+        load_row(p.V + b * p.v_sb + kvh * p.v_sh + u * p.v_st + lane * CPL, v[u]);
+      }
+    }
+    const int key = (lane & 16 ? 4 : 0) + (lane & 8 ? 2 : 0) + (lane & 4 ? 1 : 0);  // the key whose score this lane gets
+#pragma unroll
+    for (int n = 0; n < kFewRows; ++n) {
+      if (r0 + n >= R) break;
+      float s[kFewKeys];
+#pragma unroll
+      for (int u = 0; u < kFewKeys; ++u) {
+        s[u] = 0.f;
+#pragma unroll
+        for (int c = 0; c < CPL; ++c) s[u] = fmaf(q[n][c], k[u][c], s[u]);
+      }
+#pragma unroll
+      for (int o = 16, m = kFewKeys / 2; o >= 4; o >>= 1, m >>= 1) {
+        const bool up = lane & o;
+#pragma unroll
+        for (int u = 0; u < kFewKeys / 2; ++u) {
+          if (u < m) {
+            const float send = up ? s[u] : s[u + m], keep = up ? s[u + m] : s[u];
+            s[u] = keep + __shfl_xor_sync(0xffffffffu, send, o);
+          }
+        }
+      }
+#pragma unroll
+      for (int o = 2; o; o >>= 1) s[0] += __shfl_xor_sync(0xffffffffu, s[0], o);
+      const float sv = s[0] * p.scale_log2;
+      const bool seen = vis[n] >> key & 1;
+      float mx = seen ? sv : -INFINITY;
+#pragma unroll
+      for (int o = 16; o >= 4; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+      float l = 0.f, acc[CPL];
+#pragma unroll
+      for (int c = 0; c < CPL; ++c) acc[c] = 0.f;
+      if (mx > -INFINITY) {
+        const float w = seen ? exp2f(sv - mx) : 0.f;
+#pragma unroll
+        for (int u = 0; u < kFewKeys; ++u) {
+          const float wu = __shfl_sync(0xffffffffu, w, (u & 4 ? 16 : 0) + (u & 2 ? 8 : 0) + (u & 1 ? 4 : 0));
+          if (vis[n] >> u & 1) {  // (what is not visible may hold anything)
+            l += wu;
+#pragma unroll
+            for (int c = 0; c < CPL; ++c) acc[c] = fmaf(wu, v[u][c], acc[c]);
+          }
+        }
+      }
+      const size_t at = ((size_t)b * p.H_kv + kvh) * p.R_stride + r0 + n;
+      if (lane == 0) p.part_ml[at] = make_float2(mx, l);
+      float* out = p.part_a + at * D + lane * CPL;
+      if (CPL == 4)
+        *reinterpret_cast<float4*>(out) = make_float4(acc[0], acc[1], acc[CPL - 2], acc[CPL - 1]);
+      else
+        *reinterpret_cast<float2*>(out) = make_float2(acc[0], acc[1]);
+    }
+  }
+  if (blockIdx.x == 0) pdl_wait_prior();  // one CTA keeps the completion order along the stream
+}
+
 // ---------------------------------------------------------------------------------------
 // Merge of every partial state of a row (Eq. 14, as one max + one rescaled sum, which is
 // the same value as the serial recurrence up to rounding order), then either O = a / l
@@ -391,6 +496,11 @@ __global__ void __launch_bounds__(256) gather_kernel(const GatherParams p) {
 }  // namespace
 
 cudaError_t launch_local(const LocalParams& p, cudaStream_t s, bool pdl) {
+  if (p.T_loc <= kFewKeys) {
+    const int R = p.G * p.T_q, per_pair = (R + kWarpsPerCta * kFewRows - 1) / (kWarpsPerCta * kFewRows);
+    const dim3 grid((unsigned)p.B * p.H_kv * per_pair), block(kWarpsPerCta * 32);
+    return launch_kernel(p.d == 128 ? local_few_kernel<128> : local_few_kernel<64>, grid, block, 0, s, pdl, p);
+  }
   const int64_t rows = (int64_t)p.B * p.H_q * p.T_q;
   dim3 grid((unsigned)((rows + kWarpsPerCta - 1) / kWarpsPerCta)), block(kWarpsPerCta * 32);
   const size_t smem = (size_t)kWarpsPerCta * p.T_loc * sizeof(float);
