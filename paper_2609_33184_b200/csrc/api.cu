@@ -72,7 +72,6 @@ struct ss_ctx {
   uint64_t hist_age[4];
   bool hist_pinned[4];      // the list was used under a stream capture: a graph may replay the launch, never evicted
   float* scratch8;          // 8-bit cache: partial states of units cut by a share's end
-  uint32_t* plan8;          // and the tiles before each request that the launch went by
   bool pend8;               // the open round's 8-bit chunk is not joined yet: its launch is ...
   ss::Attn8Params last8;    // ... this one
   cudaEvent_t* ev_pool;     // timing events of the streamed round (SS_FLAG_STREAM_TIMING)
@@ -143,7 +142,7 @@ int slot_capacity_for(const ss_config* c) {
 
 constexpr int kHistSlots = 4;
 struct Layout {
-  size_t off_hist, off_ml, off_a, off_scratch8, off_plan8, total;
+  size_t off_hist, off_ml, off_a, off_scratch8, total;
   int64_t set_stride_ml, set_stride_a;
   int R_stride;
 };
@@ -165,8 +164,7 @@ Layout layout_for(const ss_config* c) {
   size_t rows8 = ss::kCtas8 * (size_t)(L.R_stride < ss::kRows8 ? L.R_stride : ss::kRows8);
   const size_t few8 = c->d == 64 ? ss::kCtasFew8 * (size_t)(L.R_stride < ss::kFew8 ? L.R_stride : ss::kFew8) : 0;
   if (rows8 < few8) rows8 = few8;
-  L.off_plan8 = align_up(L.off_scratch8 + 2 * rows8 * (c->d + 4) * sizeof(float), 256);
-  L.total = align_up(L.off_plan8 + ((size_t)c->max_B + 1) * sizeof(uint32_t), 256);
+  L.total = align_up(L.off_scratch8 + 2 * rows8 * (c->d + 4) * sizeof(float), 256);
   return L;
 }
 
@@ -294,7 +292,7 @@ cudaError_t settle8(ss_ctx* c) {
   }
   DeviceGuard on(c->cfg.device);
   if (on.err != cudaSuccess) return on.err;
-  const cudaError_t e = ss::launch_attn8_join(c->last8, true, c->stream, !c->no_overlap);
+  const cudaError_t e = ss::launch_attn8_join(c->last8, c->stream, !c->no_overlap);
   if (e != cudaSuccess) return e;
   c->pend8 = false;
   ++c->launches;
@@ -446,7 +444,6 @@ ss_status ss_create(ss_ctx** out, const ss_config* cfg, void* workspace, size_t 
   c->round_counters = (unsigned int*)(c->ws + 256 + align_up(ss::kTraceWords * sizeof(unsigned long long), 256));
   c->hist_maps = (CUtensorMap*)(c->ws + L.off_hist);
   c->scratch8 = (float*)(c->ws + L.off_scratch8);
-  c->plan8 = (uint32_t*)(c->ws + L.off_plan8);
   c->part_ml = (float2*)(c->ws + L.off_ml);
   c->part_a = (float*)(c->ws + L.off_a);
   c->set_stride_ml = L.set_stride_ml;
@@ -1458,7 +1455,6 @@ static ss_status attn8(ss_ctx* c, int bits, const ss_tensor& Q, int32_t B, int32
   if (win.window && tc) window_mode(p, bits, most_tiles);
   p->scale_log2 = scale * 1.4426950408889634f;
   p->scratch = c->scratch8;
-  p->plan = p->O || p->mode != ss::kCut8 ? nullptr : c->plan8;
   p->status = c->status;
   DeviceGuard on(c->cfg.device);
   if (on.err != cudaSuccess) return cuda_fail(c, on.err);
@@ -1474,7 +1470,7 @@ static ss_status attn8(ss_ctx* c, int bits, const ss_tensor& Q, int32_t B, int32
                                : (tc ? "window-tcgen05" : "window-simt");
   ++c->launches;
   if (p->O && most_tiles > 1 && p->mode == ss::kCut8) {  // (a unit of one tile is never cut; a round joins later)
-    e = ss::launch_attn8_join(*p, false, s, pdl);
+    e = ss::launch_attn8_join(*p, s, pdl);
     if (e != cudaSuccess) return cuda_fail(c, e);
     ++c->launches;
   }

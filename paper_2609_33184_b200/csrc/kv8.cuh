@@ -59,10 +59,9 @@ struct Attn8Params {
   float scale_log2;
   int shares;                 // most shares; the attention launch has shares * row_tiles CTAs
   float* scratch;             // 2 slots per CTA of rows_per_tile * (d + 4) floats: (m, l) pairs, room, a[]
-  uint32_t* plan;             // [B + 1] or null: receives the tiles before each request (all kv-heads), and their total
   __nv_bfloat16* O;           // either the finished output ...
   float* LSE;
-  float2* part_ml;            // ... or (O null) one partial state per row, as the chunk kernels leave them
+  float2* part_ml;            // ... or (O null) one partial state per row, as the chunk kernels leave them (put_cut8)
   float* part_a;
   int R_stride;
   uint32_t* status;
@@ -101,7 +100,7 @@ cudaError_t launch_kv8_write(const Copy8Params& p, cudaStream_t s, bool pdl);
 cudaError_t launch_kv8_read(const Copy8Params& p, cudaStream_t s, bool pdl);
 cudaError_t launch_attn8_simt(const Attn8Params& p, int bits, cudaStream_t s, bool pdl);  // bits: of the cache, 8 or 16
 cudaError_t launch_attn8_tc(const Attn8Params& p, const CUtensorMap& tmK, const CUtensorMap& tmV, cudaStream_t s, bool pdl);
-cudaError_t launch_attn8_join(const Attn8Params& p, bool from_plan, cudaStream_t s, bool pdl);
+cudaError_t launch_attn8_join(const Attn8Params& p, cudaStream_t s, bool pdl);
 cudaError_t launch_attn8_finalize(const Attn8Params& p, const Final8& out, cudaStream_t s, bool pdl);
 cudaError_t attn8_tc_prepare();  // one-time function attributes
 cudaError_t launch_window_tc(const Attn8Params& p, const CUtensorMap& tmK, const CUtensorMap& tmV, cudaStream_t s, bool pdl);
@@ -423,32 +422,25 @@ static __device__ __noinline__ void put_empty8(const Attn8Params& p, int tid, in
   }
 }
 
-// The record of the lengths that this launch went by, for a join that runs later: by one warp of the
-// last CTA, which has the least to do.
-template <bool WIN = false>
-static __device__ __noinline__ void put_plan8(const Attn8Params& p) {
-  const int lane = threadIdx.x & 31;
-  uint32_t base = 0, n[4];
-  bool bad = false;
-#pragma unroll 1
-  for (int b = 0; b < p.B; b += 128) {
-    const uint32_t mine = tiles_of_four8<WIN>(p, b, n, &bad), incl = warp_scan8(mine);
-    uint32_t before = base + incl - mine;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      if (b + 4 * lane + j < p.B) p.plan[b + 4 * lane + j] = before;
-      before += n[j];
-    }
-    base += __shfl_sync(0xffffffffu, incl, 31);
-  }
-  if (lane == 0) p.plan[p.B] = base;
-}
-
 // Slot of share i's state of the unit that begins at tile `start` (in row tile s.rt): the first segment
 // of a share uses the even slot of its CTA, a later one (always the last) the odd slot.
+__device__ __forceinline__ uint32_t slot_number8(const Attn8Params& p, const Share8& s, uint32_t start, uint32_t i) {
+  return 2 * (i * p.row_tiles + s.rt) + (share_lo8(s, i) < start ? 1 : 0);
+}
+__device__ __forceinline__ float* slot_at8(const Attn8Params& p, uint32_t number) {
+  return p.scratch + (int64_t)number * p.rows_per_tile * (p.d + 4);
+}
 __device__ __forceinline__ float* slot8(const Attn8Params& p, const Share8& s, uint32_t start, uint32_t i) {
-  const int odd = share_lo8(s, i) < start ? 1 : 0;
-  return p.scratch + (int64_t)(2 * (i * p.row_tiles + s.rt) + odd) * p.rows_per_tile * (p.d + 4);
+  return slot_at8(p, slot_number8(p, s, start, i));
+}
+// (In a round) a row of a unit that is cut: instead of its state, the slot of the first part and the number of parts,
+// negative as no row sum is; the other parts are in the even slots of the CTAs that follow.  By the CTA that
+// has the first part.  So whoever joins the round's states, later than the lengths may be there, needs neither
+// them nor the shares (worked out anew from a record of the lengths by every row: 7 us of a round instead of 3.4).
+__device__ __forceinline__ void put_cut8(const Attn8Params& p, const Share8& s, const Seg8& g, int r) {
+  const uint32_t last = min(share_of8(s, g.start + g.n - 1), (uint32_t)p.shares - 1);
+  p.part_ml[((int64_t)g.b * p.H_kv + g.kvh) * p.R_stride + g.row0 + r] =
+      make_float2((float)slot_number8(p, s, g.start, s.idx), -(float)(last - s.idx + 1));
 }
 
 }  // namespace ss

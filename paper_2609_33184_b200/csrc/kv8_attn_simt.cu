@@ -210,12 +210,12 @@ __global__ void __launch_bounds__(128) attn8_simt_kernel(const __grid_constant__
         put_a8(p, g, r, c, L, A);
       } else {
         if (c == 0) reinterpret_cast<float2*>(slot)[r] = make_float2(M, L);
+        if (c == 0 && g.t0 == 0 && !p.O) put_cut8(p, share, g, r);
         slot[4 * p.rows_per_tile + r * D + c] = A;
       }
     }
   }
   if ((int)blockIdx.x < p.B) put_empty8<WIN>(p, tid, 128);
-  if (p.plan && warp == 0 && blockIdx.x == gridDim.x - 1) put_plan8<WIN>(p);
 }
 
 }  // namespace

@@ -764,6 +764,7 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
         const float m = -ctl->nm[tid], l = (ctl->smax[0][tid] + ctl->smax[1][tid]) + (ctl->smax[2][tid] + ctl->smax[3][tid]);
         if (whole) put_ml8(p, done, tid, m, l);
         else reinterpret_cast<float2*>(slot)[tid] = make_float2(m, l);
+        if (!whole && done.t0 == 0 && !p.O) put_cut8(p, share, done, tid);
         ctl->up[tid] = l > 0.f || l != l ? 1.f / l : 0.f;
       }
       if constexpr (WIN) {
@@ -802,7 +803,6 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
     } else if ((int)blockIdx.x < p.B) {
       put_empty8<WIN>(p, tid, SOFT);
     }
-    if (!CL && p.plan && warp == 0 && blockIdx.x == gridDim.x - 1) put_plan8<WIN>(p);
   }
 
   tc_fence_before();

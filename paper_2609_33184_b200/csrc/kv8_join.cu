@@ -6,7 +6,7 @@
 // Directly behind the attention kernel (decoding) a warp works the shares out again from the lengths, and
 // does so before it waits: the attention kernel let this one start only after everything in front of it, the
 // lengths' producer too, was complete.  At a round's end, when the lengths' buffer may have been written
-// anew, it reads the attention kernel's own record of them.  Bound by dependent reads of L2.
+// anew, it finds a cut unit's parts where the attention kernel says (put_cut8).  Bound by dependent reads of L2.
 #include "kv8.cuh"
 
 namespace ss {
@@ -23,50 +23,46 @@ bool many_rows(const Attn8Params& p) { return p.window && (int64_t)p.B * p.H_kv 
 // apart from `rest`; n = 0: empty request, n = 1: finished by one CTA, not in the scratch area.
 struct Row8 {
   Seg8 g;
-  int r, rr;                // row in its unit, in its kv-head
+  int r, rr, rt;            // row in its unit, in its kv-head; row tile
   int n;
   const float *first, *rest;
   int64_t step;
 };
-template <bool PLAN>
-__device__ __forceinline__ Row8 row8(const Attn8Params& p, int64_t row, int lane) {
+// Which row it is (nothing that the kernel in front has to write), and where its states are.
+__device__ __forceinline__ Row8 row_at8(const Attn8Params& p, uint32_t row) {
   Row8 w;
   Seg8& g = w.g;
-  const int pair = (int)(row / p.R);
-  w.rr = (int)(row - (int64_t)pair * p.R);
-  g.b = pair / p.H_kv;
-  g.kvh = pair - g.b * p.H_kv;
-  const int rt = w.rr / p.rows_per_tile;
+  const uint32_t pair = row / (uint32_t)p.R;
+  w.rr = (int)(row - pair * p.R);
+  g.b = (int)(pair / (uint32_t)p.H_kv);
+  g.kvh = (int)pair - g.b * p.H_kv;
+  const int rt = (int)((uint32_t)w.rr / (uint32_t)p.rows_per_tile);
   w.r = w.rr - rt * p.rows_per_tile;
   g.row0 = rt * p.rows_per_tile;
   g.nrows = min(p.rows_per_tile, p.R - g.row0);
-  if (p.mode != kCut8) {  // (in a round's end) every state is whole
-    w.n = 1;
-    return w;
-  }
-  const uint32_t units = (uint32_t)p.H_kv;
-  Share8 s = {};
-  uint32_t before = 0;  // tiles of the requests before this one
-  if (PLAN) {
-    before = __ldcg(&p.plan[g.b]);
-    g.n = (int)((__ldcg(&p.plan[g.b + 1]) - before) / units);
-    s.total = __ldcg(&p.plan[p.B]);
-  } else {
-    const auto tiles = [&](int b) { return tiles8(p.window ? len8<true>(p, b) : len8(p, b)); };
-    g.n = tiles(g.b);
-    uint32_t sum = 0;
-    for (int b = lane; b < p.B; b += 32) {
-      const uint32_t n = units * tiles(b);
-      sum += n;
-      if (b < g.b) before += n;
-    }
-    s.total = __reduce_add_sync(0xffffffffu, sum);
-    before = __reduce_add_sync(0xffffffffu, before);
-  }
-  w.n = 0;
+  w.rt = rt;
+  w.n = 1;
   w.first = w.rest = nullptr;
   w.step = (int64_t)2 * p.row_tiles * p.rows_per_tile * (p.d + 4);
-  s.rt = (uint32_t)rt;
+  return w;
+}
+// Decoding: from the lengths.
+__device__ __forceinline__ void row_states8(const Attn8Params& p, Row8& w, int lane) {
+  Seg8& g = w.g;
+  const uint32_t units = (uint32_t)p.H_kv;
+  Share8 s = {};
+  const auto tiles = [&](int b) { return tiles8(p.window ? len8<true>(p, b) : len8(p, b)); };
+  g.n = tiles(g.b);
+  uint32_t sum = 0, before = 0;  // tiles of the requests before this one
+  for (int b = lane; b < p.B; b += 32) {
+    const uint32_t n = units * tiles(b);
+    sum += n;
+    if (b < g.b) before += n;
+  }
+  s.total = __reduce_add_sync(0xffffffffu, sum);
+  before = __reduce_add_sync(0xffffffffu, before);
+  w.n = 0;
+  s.rt = (uint32_t)w.rt;
   if (g.n > 0) {
     set_shares8(p.shares, &s);
     g.start = before + (uint32_t)g.kvh * g.n;
@@ -75,7 +71,14 @@ __device__ __forceinline__ Row8 row8(const Attn8Params& p, int64_t row, int lane
     w.first = slot8(p, s, g.start, i0);
     w.rest = slot8(p, s, g.start, i0 + 1);
   }
-  return w;
+}
+// In a round: from what the attention kernel has left in the row's state.
+__device__ __forceinline__ void row_states8(const Attn8Params& p, Row8& w, float2 st) {
+  if (!(st.y < 0.f)) return;
+  const uint32_t slot = (uint32_t)st.x;
+  w.n = (int)-st.y;
+  w.first = slot_at8(p, slot);
+  w.rest = slot_at8(p, 2 * (slot / 2 + p.row_tiles));
 }
 
 template <int CPL>
@@ -136,17 +139,18 @@ __device__ __forceinline__ void add_states(const Attn8Params& p, const Row8& w, 
   }
 }
 
-template <int D, bool PLAN, int FLIGHT>
+template <int D, bool ROUND, int FLIGHT>
 __global__ void __launch_bounds__(kWarps * 32) attn8_join_kernel(const __grid_constant__ Attn8Params p) {
   constexpr int CPL = D / 32;
   pdl_launch_dependents();
   const int lane = threadIdx.x & 31;
-  const int64_t row = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);  // (request, kv-head, row)
-  if (row >= (int64_t)p.B * p.H_kv * p.R) return;  // (the block's first warp has a row)
-  if (PLAN) pdl_wait_prior();
-  const Row8 w = row8<PLAN>(p, row, lane);
+  const uint32_t row = blockIdx.x * kWarps + (threadIdx.x >> 5);  // (request, kv-head, row)
+  if (row >= (uint32_t)p.B * p.H_kv * p.R) return;  // (the block's first warp has a row)
+  Row8 w = row_at8(p, row);
+  if (!ROUND) row_states8(p, w, lane);
   // Every warp waits, those with nothing to join too: this grid must not be complete before the other is.
-  if (!PLAN) pdl_wait_prior();
+  pdl_wait_prior();
+  if (ROUND) row_states8(p, w, __ldcg(p.part_ml + ((int64_t)w.g.b * p.H_kv + w.g.kvh) * p.R_stride + w.rr));
   if (w.n < 2) return;  // written by the attention kernel
   float m = -INFINITY, l = 0.f, a[CPL];
 #pragma unroll
@@ -165,21 +169,24 @@ __global__ void __launch_bounds__(kWarps * 32) attn8_finalize_kernel(const __gri
   constexpr int CPL = D / 32;
   pdl_launch_dependents();
   const int lane = threadIdx.x & 31;
-  const int64_t row = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
-  if (row >= (int64_t)p.B * p.H_kv * p.R) return;
+  const uint32_t row = blockIdx.x * kWarps + (threadIdx.x >> 5);
+  if (row >= (uint32_t)p.B * p.H_kv * p.R) return;
+  Row8 w = row_at8(p, row);
+  const int64_t at = ((int64_t)w.g.b * p.H_kv + w.g.kvh) * p.R_stride + w.rr;
   pdl_wait_prior();
-  const int64_t pair = row / p.R, at = pair * p.R_stride + (row - pair * p.R);
   float m = -INFINITY, l = 0.f, a[CPL];
 #pragma unroll
   for (int c = 0; c < CPL; ++c) a[c] = 0.f;
-  // the local segment's state (fetched while the unit's place is worked out)
+  // the local segment's state and the row's, if it was finished by one CTA (fetched while that is worked out)
   float2 ml = make_float2(-INFINITY, 0.f);
-  float v[CPL];
+  float v[CPL], whole[CPL];
   if (out.loc_ml) {
     ml = __ldcg(out.loc_ml + at);
     load_a<CPL>(out.loc_a + at * D + lane * CPL, v);
   }
-  const Row8 w = row8<true>(p, row, lane);
+  const float2 st = __ldcg(p.part_ml + at);
+  load_a<CPL>(p.part_a + at * D + lane * CPL, whole);
+  row_states8(p, w, st);
   if (ml.y != 0.f && ml.x != -INFINITY) {  // (an identity state's a[] is undefined)
     m = ml.x;
     l = ml.y;
@@ -188,20 +195,16 @@ __global__ void __launch_bounds__(kWarps * 32) attn8_finalize_kernel(const __gri
   }
   if (w.n >= 2) {
     add_states<D, FLIGHT>(p, w, lane, m, l, a);
-  } else if (w.n == 1) {
-    const float2 st = __ldcg(p.part_ml + at);
-    if (st.y != 0.f) {
-      load_a<CPL>(p.part_a + at * D + lane * CPL, v);
-      const float top = fmaxf(m, st.x), f = m == top ? 1.f : exp2f(m - top), wt = st.x == top ? 1.f : exp2f(st.x - top);
-      m = top;
-      l = fmaf(l, f, wt * st.y);
+  } else if (w.n == 1 && st.y != 0.f) {
+    const float top = fmaxf(m, st.x), f = m == top ? 1.f : exp2f(m - top), wt = st.x == top ? 1.f : exp2f(st.x - top);
+    m = top;
+    l = fmaf(l, f, wt * st.y);
 #pragma unroll
-      for (int c = 0; c < CPL; ++c) a[c] = fmaf(wt, v[c], a[c] * f);
-    }
+    for (int c = 0; c < CPL; ++c) a[c] = fmaf(wt, whole[c], a[c] * f);
   }
   const bool some = l > 0.f || l != l;
   const float inv = some ? 1.f / l : 0.f;
-  __nv_bfloat162* o = reinterpret_cast<__nv_bfloat162*>(out.O + row * D + lane * CPL);
+  __nv_bfloat162* o = reinterpret_cast<__nv_bfloat162*>(out.O + (int64_t)row * D + lane * CPL);
 #pragma unroll
   for (int c = 0; c < CPL / 2; ++c) o[c] = __floats2bfloat162_rn(a[2 * c] * inv, a[2 * c + 1] * inv);
   if (out.LSE && lane == 0) out.LSE[row] = some ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
@@ -213,8 +216,8 @@ dim3 join_grid(const Attn8Params& p) {
 }
 
 template <int D, int FLIGHT>
-cudaError_t join(const Attn8Params& p, bool from_plan, cudaStream_t s, bool pdl) {
-  auto kernel = from_plan ? attn8_join_kernel<D, true, FLIGHT> : attn8_join_kernel<D, false, FLIGHT>;
+cudaError_t join(const Attn8Params& p, cudaStream_t s, bool pdl) {
+  auto kernel = p.O ? attn8_join_kernel<D, false, FLIGHT> : attn8_join_kernel<D, true, FLIGHT>;
   return launch_kernel(kernel, join_grid(p), dim3(kWarps * 32), 0, s, pdl, p);
 }
 template <int D, int FLIGHT>
@@ -224,9 +227,9 @@ cudaError_t finalize(const Attn8Params& p, const Final8& out, cudaStream_t s, bo
 
 }  // namespace
 
-cudaError_t launch_attn8_join(const Attn8Params& p, bool from_plan, cudaStream_t s, bool pdl) {
-  if (many_rows(p)) return p.d == 128 ? join<128, kFlightMany>(p, from_plan, s, pdl) : join<64, kFlightMany>(p, from_plan, s, pdl);
-  return p.d == 128 ? join<128, kFlight>(p, from_plan, s, pdl) : join<64, kFlight>(p, from_plan, s, pdl);
+cudaError_t launch_attn8_join(const Attn8Params& p, cudaStream_t s, bool pdl) {
+  if (many_rows(p)) return p.d == 128 ? join<128, kFlightMany>(p, s, pdl) : join<64, kFlightMany>(p, s, pdl);
+  return p.d == 128 ? join<128, kFlight>(p, s, pdl) : join<64, kFlight>(p, s, pdl);
 }
 
 cudaError_t launch_attn8_finalize(const Attn8Params& p, const Final8& out, cudaStream_t s, bool pdl) {

@@ -524,6 +524,7 @@ window_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ 
         const float m = -ctl->nm[tid], l = (smax[tid] + smax[NR + tid]) + (smax[2 * NR + tid] + smax[3 * NR + tid]);
         if (whole) put_ml8(p, done, tid, m, l);
         else reinterpret_cast<float2*>(slot)[tid] = make_float2(m, l);
+        if (!whole && done.t0 == 0 && !p.O) put_cut8(p, share, done, tid);
         ctl->up[tid] = l > 0.f || l != l ? 1.f / l : 0.f;
       }
       if (tid == 0) ctl->unset = 0;
@@ -560,7 +561,6 @@ window_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ 
     } else if ((int)blockIdx.x < p.B) {
       put_empty8<true>(p, tid, SOFT);
     }
-    if (!CL && p.plan && warp == 0 && blockIdx.x == gridDim.x - 1) put_plan8<true>(p);
   }
 
   tc_fence_before();
