@@ -20,11 +20,11 @@ namespace {
 
 constexpr int kThreads = 128;
 
-// A block takes 2^shift consecutive tokens of a request and `heads` of its rows (of Q, K and V laid end to
-// end): `lanes` rows side by side, one after the other beyond.
+// A block takes 2^shift consecutive tokens of a request and `heads` rows of Q, of K or of V (q_blocks and twice
+// kv_blocks of them): `lanes` rows side by side, one after the other beyond.
 struct Plan {
   int shift, lanes, heads;
-  int token_blocks, head_blocks;
+  int token_blocks, q_blocks, kv_blocks, head_blocks;
 };
 
 __device__ __forceinline__ float lo_f(uint32_t two) { return __uint_as_float(two << 16); }
@@ -68,12 +68,18 @@ __device__ __forceinline__ void turn_row(uint4 (&raw)[2], const Turn& t) {
 // Largest finite magnitude (bf16 bits) of a thread's 16 values.
 __device__ __forceinline__ uint32_t top_of(const uint4 (&raw)[2]) {
   const uint32_t x[8] = {raw[0].x, raw[0].y, raw[0].z, raw[0].w, raw[1].x, raw[1].y, raw[1].z, raw[1].w};
-  uint32_t top = 0;
+  uint32_t two = 0;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const uint32_t lo = x[j] & 0x7fffu, hi = (x[j] >> 16) & 0x7fffu;
-    if (lo < 0x7f80u) top = max(top, lo);
-    if (hi < 0x7f80u) top = max(top, hi);
+  for (int j = 0; j < 8; ++j) two = __vmaxu2(two, x[j] & 0x7fff7fffu);
+  uint32_t top = max(two & 0xffffu, two >> 16);
+  if (__any_sync(0xffffffffu, top >= 0x7f80u)) {  // infinities and NaN do not count
+    top = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint32_t lo = x[j] & 0x7fffu, hi = (x[j] >> 16) & 0x7fffu;
+      if (lo < 0x7f80u) top = max(top, lo);
+      if (hi < 0x7f80u) top = max(top, hi);
+    }
   }
   return top;
 }
@@ -110,11 +116,12 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ 
     if (tid == 0 && report) atomicOr(p.status, SS_DEV_BAD_ACCEPT);
     n = max(0, min(n, p.T));
   }
-  const int slot = tid / LPR, part = tid % LPR;
-  const int k = (tb << plan.shift) + (slot & ((1 << plan.shift) - 1));   // row of the call
+  const int slot = tid / LPR, part = tid % LPR, head = slot >> plan.shift;  // (of the heads side by side)
+  const int k = (tb << plan.shift) + (slot & ((1 << plan.shift) - 1));       // row of the call
   if ((tb << plan.shift) >= n) return;
-  const int base0 = hb * plan.heads, head0 = base0 + (slot >> plan.shift);
-  const int head1 = min(base0 + plan.heads, p.H_q + p.H_kv + (BITS ? p.H_kv : 0));
+  const bool is_q = hb < plan.q_blocks, is_v = hb >= plan.q_blocks + plan.kv_blocks;
+  const int from = (is_q ? hb : is_v ? hb - plan.q_blocks - plan.kv_blocks : hb - plan.q_blocks) * plan.heads;
+  const int to = min(from + plan.heads, is_q ? p.H_q : p.H_kv);               // the block's heads
   const int64_t off = p.off ? (int64_t)p.off[b] : 0, tok = off + k;
 
   // the input row, and (cache) the token's place
@@ -122,7 +129,7 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ 
   int src = k;
   uint64_t outer = (uint64_t)b, inner = (uint64_t)tok;
   if (BITS && live) {
-    const bool one = part == 0 && head0 == 0;   // who reports a row
+    const bool one = part == 0 && head == 0 && hb == 0;   // who reports a row
     if (p.idx) {
       src = p.idx[(int64_t)b * p.T + k];
       if (src < 0 || src >= p.T) {
@@ -152,7 +159,7 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ 
   const int at0 = turning ? part * 8 : rot + (part - rot / 16) * 8;
   const int at1 = turning ? rot / 2 + part * 8 : rot + (D - rot) / 2 + (part - rot / 16) * 8;
   Turn t;
-  if (turning && live && head0 < p.H_q + p.H_kv) {
+  if (turning && live && !is_v) {
     int64_t pos[kRopeAxes];
 #pragma unroll
     for (int a = 0; a < kRopeAxes; ++a)
@@ -169,80 +176,99 @@ __global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ 
     }
   }
 
+  // The block's rows, head 0 of this token being at `in`; put(head, row) stores one.  As often for every lane of a warp.
+  auto rows = [&](const uint16_t* in, int64_t in_sh, bool turn, bool ok, auto put) {
+    const uint16_t* at = in + (from + head) * in_sh;
+    const int64_t step = plan.lanes * in_sh;
 #pragma unroll 1
-  for (int base = base0; base < head1; base += U * plan.lanes) {  // (as often for every lane of a warp)
-    const int g0 = base + (slot >> plan.shift);
-    uint4 raw[U][2];
+    for (int h0 = from + head; h0 - head < to; h0 += U * plan.lanes) {
+      uint4 raw[U][2];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int g = g0 + u * plan.lanes;
-      raw[u][0] = raw[u][1] = make_uint4(0, 0, 0, 0);
-      if (!live || g >= head1) continue;
-      const uint16_t* row = g < p.H_q ? p.Q + b * p.q_sb + g * p.q_sh + src * p.q_st
-                            : g < p.H_q + p.H_kv ? p.K + b * p.k_sb + (g - p.H_q) * p.k_sh + src * p.k_st
-                                                 : p.V + b * p.v_sb + (g - p.H_q - p.H_kv) * p.v_sh + src * p.v_st;
-      raw[u][0] = __ldcs(reinterpret_cast<const uint4*>(row + at0));
-      raw[u][1] = __ldcs(reinterpret_cast<const uint4*>(row + at1));
+      for (int u = 0; u < U; ++u) {
+        raw[u][0] = raw[u][1] = make_uint4(0, 0, 0, 0);
+        if (ok && h0 + u * plan.lanes < to) {
+          raw[u][0] = __ldcs(reinterpret_cast<const uint4*>(at + at0));
+          raw[u][1] = __ldcs(reinterpret_cast<const uint4*>(at + at1));
+        }
+        at += step;
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (turn) turn_row<INTER>(raw[u], t);
+        put(h0 + u * plan.lanes, ok && h0 + u * plan.lanes < to, raw[u]);
+      }
     }
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int g = g0 + u * plan.lanes;
-      const bool is_q = g < p.H_q, is_v = g >= p.H_q + p.H_kv;
-      if (turning && !is_v && live && g < head1) turn_row<INTER>(raw[u], t);
-      uint32_t top = 0;
-      if (BITS == 8) {  // (by all lanes: a row's are neighbours)
-        top = top_of(raw[u]);
+  };
+  auto to_rows = [&](uint16_t* out, int64_t out_sh) {
+    return [=](int h, bool ok, const uint4 (&raw)[2]) {
+      if (!ok) return;
+      uint16_t* row = out + h * out_sh;
+      *reinterpret_cast<uint4*>(row + at0) = raw[0];
+      *reinterpret_cast<uint4*>(row + at1) = raw[1];
+    };
+  };
+  auto to_cache = [&](uint8_t* out, int64_t out_sh, uint8_t* scale, int64_t scale_sh) {
+    return [=](int h, bool ok, const uint4 (&raw)[2]) {
+      uint8_t* row = out + h * out_sh;
+      if (BITS == 16) {
+        if (!ok) return;
+        __stcs(reinterpret_cast<uint4*>(row + 2 * at0), raw[0]);
+        __stcs(reinterpret_cast<uint4*>(row + 2 * at1), raw[1]);
+      } else {
+        uint32_t top = top_of(raw);  // (by all lanes: a row's are neighbours)
 #pragma unroll
         for (int o = LPR / 2; o; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+        if (!ok) return;
+        // top = (1 + f / 128) 2^(E - 127) against 448 = (1 + 96 / 128) 2^8
+        const int e = max(kMinExp8, min(kMaxExp8, (int)((top + 31u) >> 7) - 127 - 8));
+        const float inv = pow2_8(-e);
+        __stcs(reinterpret_cast<uint2*>(row + at0), codes_of(raw[0], inv));
+        __stcs(reinterpret_cast<uint2*>(row + at1), codes_of(raw[1], inv));
+        if (part == 0) scale[h * scale_sh] = (uint8_t)(e + 127);
       }
-      if (!live || g >= head1) continue;
-      if (is_q || BITS == 0) {
-        uint16_t* row = is_q ? p.Qo + b * p.qo_sb + g * p.qo_sh + src * p.qo_st
-                             : p.Ko + b * p.ko_sb + (g - p.H_q) * p.ko_sh + src * p.ko_st;
-        *reinterpret_cast<uint4*>(row + at0) = raw[u][0];
-        *reinterpret_cast<uint4*>(row + at1) = raw[u][1];
-      } else if (store) {
-        const int h = is_v ? g - p.H_q - p.H_kv : g - p.H_q;
-        uint8_t* row = is_v ? p.kv.V + outer * p.kv.v_sb + h * p.kv.v_sh + inner * p.kv.v_st
-                            : p.kv.K + outer * p.kv.k_sb + h * p.kv.k_sh + inner * p.kv.k_st;
-        if (BITS == 16) {
-          __stcs(reinterpret_cast<uint4*>(row + 2 * at0), raw[u][0]);
-          __stcs(reinterpret_cast<uint4*>(row + 2 * at1), raw[u][1]);
-        } else {
-          // top = (1 + f / 128) 2^(E - 127) against 448 = (1 + 96 / 128) 2^8
-          const int e = max(kMinExp8, min(kMaxExp8, (int)((top + 31u) >> 7) - 127 - 8));
-          const float inv = pow2_8(-e);
-          __stcs(reinterpret_cast<uint2*>(row + at0), codes_of(raw[u][0], inv));
-          __stcs(reinterpret_cast<uint2*>(row + at1), codes_of(raw[u][1], inv));
-          uint8_t* scale = is_v ? p.kv.Vs + outer * p.kv.vs_sb + h * p.kv.vs_sh + inner * p.kv.vs_st
-                                : p.kv.Ks + outer * p.kv.ks_sb + h * p.kv.ks_sh + inner * p.kv.ks_st;
-          if (part == 0) *scale = (uint8_t)(e + 127);
-        }
-      }
-    }
+    };
+  };
+  if (is_q) {
+    rows(p.Q + b * p.q_sb + src * p.q_st, p.q_sh, turning, live, to_rows(p.Qo + b * p.qo_sb + src * p.qo_st, p.qo_sh));
+  } else if (BITS == 0) {
+    rows(p.K + b * p.k_sb + src * p.k_st, p.k_sh, turning, live, to_rows(p.Ko + b * p.ko_sb + src * p.ko_st, p.ko_sh));
+  } else if (!is_v) {
+    rows(p.K + b * p.k_sb + src * p.k_st, p.k_sh, turning, store,
+         to_cache(p.kv.K + outer * p.kv.k_sb + inner * p.kv.k_st, p.kv.k_sh,
+                  p.kv.Ks + outer * p.kv.ks_sb + inner * p.kv.ks_st, p.kv.ks_sh));
+  } else {
+    rows(p.V + b * p.v_sb + src * p.v_st, p.v_sh, false, store,
+         to_cache(p.kv.V + outer * p.kv.v_sb + inner * p.kv.v_st, p.kv.v_sh,
+                  p.kv.Vs + outer * p.kv.vs_sb + inner * p.kv.vs_st, p.kv.vs_sh));
   }
 }
 
 template <int D, int BITS, bool INTER, int U>
 cudaError_t launch_rows(const RopeParams& p, int heads, cudaStream_t s, bool pdl) {
   constexpr int kSlots = kThreads * 16 / D;
-  const int all = p.H_q + p.H_kv + (BITS ? p.H_kv : 0);
   Plan plan = {};
   while (1 << plan.shift < p.T && 1 << plan.shift < kSlots) ++plan.shift;
   plan.lanes = kSlots >> plan.shift;
   plan.heads = heads * plan.lanes;
   plan.token_blocks = (p.T + (1 << plan.shift) - 1) >> plan.shift;
-  plan.head_blocks = (all + plan.heads - 1) / plan.heads;
+  plan.q_blocks = (p.H_q + plan.heads - 1) / plan.heads;
+  plan.kv_blocks = (p.H_kv + plan.heads - 1) / plan.heads;
+  plan.head_blocks = plan.q_blocks + (BITS ? 2 : 1) * plan.kv_blocks;
   const dim3 grid((unsigned)plan.token_blocks * plan.head_blocks * p.B);  // below 2^31: see the caller
   return launch_kernel(rope_kernel<D, BITS, INTER, U>, grid, dim3(kThreads), 0, s, pdl, p, plan);
 }
 template <int D, int BITS>
 cudaError_t launch_bits(const RopeParams& p, cudaStream_t s, bool pdl) {
   const int all = p.H_q + p.H_kv + (BITS ? p.H_kv : 0);
+  // large: more rows than 8 blocks per SM would take, a row a thread.  There a thread turns 8 rows with its sines, 4 in
+  // flight (2 into 8 bits, whose conversions want the registers: 66 -> 59 us for 49,000 tokens of 8 heads); 4 rows
+  // instead of 8: 207 us against 187 for a batch of prompts, 16: 188, and 6.2 against 4.7 for 1024 tokens.  Small
+  // calls take two rows a thread (one: 4.9 us against 2.9 for 256 tokens of 48 rows, as much for less).
   const bool large = (int64_t)p.B * p.T * all > (int64_t)8 * kNumSM * kThreads * 16 / D;
+  constexpr int kU = BITS == 8 ? 2 : 4;
   if (p.rope.interleaved)
-    return large ? launch_rows<D, BITS, true, 4>(p, 8, s, pdl) : launch_rows<D, BITS, true, 1>(p, 1, s, pdl);
-  return large ? launch_rows<D, BITS, false, 4>(p, 8, s, pdl) : launch_rows<D, BITS, false, 1>(p, 1, s, pdl);
+    return large ? launch_rows<D, BITS, true, kU>(p, 8, s, pdl) : launch_rows<D, BITS, true, 2>(p, 2, s, pdl);
+  return large ? launch_rows<D, BITS, false, kU>(p, 8, s, pdl) : launch_rows<D, BITS, false, 2>(p, 2, s, pdl);
 }
 template <int D>
 cudaError_t launch_dim(const RopeParams& p, cudaStream_t s, bool pdl) {
