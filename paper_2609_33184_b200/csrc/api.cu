@@ -1370,19 +1370,23 @@ static int granule_log2(const ss::View8& kv) {
 
 // How a window's units meet CTAs (kv8.cuh): the form whose estimated time is least.  `tiles`: most tiles of a unit.  A
 // tile takes a CTA `one` us when little else runs (the latency of its copies and steps; small granules mean more
-// copies), and all CTAs together what memory gives; joining in a cluster takes 0.3 us, walking from unit to unit 1 us,
-// joining by another kernel 2.6 us and more for many states or rows.  Clusters of other sizes than 1, 2, 4 or 8 leave places of a GPC empty (96 clusters of 3
-// ran as two rounds: 19.3 us against 12.2 with 96 of 2), so those are taken up to half the CTAs only.
-// Measured, head dim 128, 4 rows, pages of 16, 128 units of 33 tiles: clusters of one 65 us, of two 45.6, cut 47.9; one unit
-// of 33 tiles: 60, clusters of eight 12.4, cut 11.0; 384 units of 32 rows, head dim 64, two tiles: whole 18.6, cut 22.4.
+// copies, rows more steps), and all CTAs together what memory gives; joining in a cluster takes 0.3 us, walking from unit to unit 1 us,
+// joining by another kernel 3.1 us and more for many states or rows.  Clusters of other sizes than 1, 2, 4 or 8 leave
+// places of a GPC empty (96 clusters of 3 ran as two rounds: 19.3 us against 12.2 with 96 of 2), so those are taken up
+// to half the CTAs only.
+// Measured, head dim 128, 4 rows: 128 units of 33 tiles in pages of 16 clusters of one 65 us, of two 45.6, cut 47.9; one
+// unit of 33 tiles clusters of eight 11.0, cut 9.4, of 17 tiles 8.5 and 9.3; 384 units of 32 rows, head dim 64, two
+// tiles: whole 18.6, cut 22.4.
 static void window_mode(ss::Attn8Params* p, int bits, int64_t tiles) {
   const int64_t N = (int64_t)p->shares * p->row_tiles, U = (int64_t)p->B * p->H_kv * p->row_tiles;
-  const double one = (p->d == 128 ? 1.2 : 0.8) * (p->gran_log2 >= 5 ? 1.0 : p->gran_log2 == 4 ? 1.3 : 2.1);
+  const double one = (p->d * bits == 2048 ? 1.2 : 0.8) * (p->gran_log2 >= 5 ? 1.0 : p->gran_log2 == 4 ? 1.3 : 2.1) *
+                     (1.0 + p->rows_per_tile * (bits == 8 ? 0.015 : 0.004));
   const double share = p->d * bits / 2048.0 * 0.0094 / p->row_tiles;  // of memory's time, per CTA that is at work
   const auto tile_us = [&](int64_t ctas) { return pow(pow(one, 4) + pow(share * ctas, 4), 0.25); };
   const int64_t full = U / N, rest = U % N, steps = (U * tiles + N - 1) / N;
+  const double rows = (double)p->B * p->H_kv * p->R;
   const double whole = tiles * (full * tile_us(N) + (rest ? tile_us(rest) : 0.0)) + 1.0;
-  const double cut = steps * tile_us(N < U * tiles ? N : U * tiles) + 2.6 + 0.08 * tiles / steps + (double)U * p->rows_per_tile / 3500;
+  const double cut = steps * tile_us(N < U * tiles ? N : U * tiles) + 3.1 + (rows <= 3 * ss::kNumSM ? 0.02 : 0.08) * tiles / steps + rows / 3500;
   int64_t c = N * 9 / 10 / U;
   if (c > tiles) c = tiles;
   if (c > ss::kMostCluster8) c = ss::kMostCluster8;
@@ -1465,9 +1469,10 @@ static ss_status attn8(ss_ctx* c, int bits, const ss_tensor& Q, int32_t B, int32
                   : bits == 16 ? ss::launch_window_tc(*p, tmK, tmV, s, pdl)
                                : ss::launch_attn8_tc(*p, tmK, tmV, s, pdl);
   if (e != cudaSuccess) return cuda_fail(c, e);
-  c->last_kernel = !win.window ? (tc ? "kv8-tcgen05" : "kv8-simt")
-                   : bits == 8 ? (tc ? "window8-tcgen05" : "window8-simt")
-                               : (tc ? "window-tcgen05" : "window-simt");
+  static const char* const names[2][4] = {
+      {"window-tcgen05", "window-tcgen05-whole", "window-tcgen05-cluster", "window-simt"},
+      {"window8-tcgen05", "window8-tcgen05-whole", "window8-tcgen05-cluster", "window8-simt"}};
+  c->last_kernel = win.window ? names[bits == 8][tc ? p->mode : 3] : tc ? "kv8-tcgen05" : "kv8-simt";
   ++c->launches;
   if (p->O && most_tiles > 1 && p->mode == ss::kCut8) {  // (a unit of one tile is never cut; a round joins later)
     e = ss::launch_attn8_join(*p, s, pdl);

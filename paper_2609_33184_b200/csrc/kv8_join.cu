@@ -18,6 +18,7 @@ constexpr int kWarps = 4;
 // tokens 104 us against 106; with few rows 16 are better, 3 x 24 queries over 1000 tokens 10.7 us against 12.0).
 constexpr int kFlight = 16, kFlightMany = 4;
 bool many_rows(const Attn8Params& p) { return p.window && (int64_t)p.B * p.H_kv * p.R > 3 * kWarps * kNumSM; }
+bool few_rows(const Attn8Params& p) { return p.window && p.mode == kCut8 && (int64_t)p.B * p.H_kv * p.R <= 3 * kNumSM; }
 
 // A query row and where its unit's states are: n of them, the first at `first`, the others `step` floats
 // apart from `rest`; n = 0: empty request, n = 1: finished by one CTA, not in the scratch area.
@@ -96,23 +97,23 @@ __device__ __forceinline__ void load_a(const float* x, float (&v)[CPL]) {
   }
 }
 
-// Adds the row's n states to (m, l, a); a lane holds D / 32 head dims.
+// Adds states j0 .. n - 1 of the row to (m, l, a); a lane holds D / 32 head dims.
 template <int D, int kFlight>
-__device__ __forceinline__ void add_states(const Attn8Params& p, const Row8& w, int lane, float& m, float& l,
+__device__ __forceinline__ void add_states(const Attn8Params& p, const Row8& w, int j0, int n, int lane, float& m, float& l,
                                            float (&a)[D / 32]) {
   constexpr int CPL = D / 32;
 #pragma unroll 1
-  for (int j0 = 0; j0 < w.n; j0 += kFlight) {
+  for (; j0 < n; j0 += kFlight) {
     // (m, l) one state per lane, a[] all lanes of one state after the other
     const int own = j0 + (lane & (kFlight - 1));
     float2 st = make_float2(-INFINITY, 0.f);
-    if (own < w.n)
+    if (own < n)
       st = __ldcg(reinterpret_cast<const float2*>(own == 0 ? w.first : w.rest + (own - 1) * w.step) + w.r);
     float v[kFlight][CPL];
 #pragma unroll
     for (int j = 0; j < kFlight; ++j) {  // (a row of a window has two or three: loads past the last would be most of them)
       const int i = j0 + j;
-      if (i < w.n)
+      if (i < n)
         load_a<CPL>((i == 0 ? w.first : w.rest + (i - 1) * w.step) + 4 * p.rows_per_tile + w.r * D + lane * CPL, v[j]);
     }
     float top = st.y != 0.f ? st.x : -INFINITY;  // (l = 0: an empty state)
@@ -131,7 +132,7 @@ __device__ __forceinline__ void add_states(const Attn8Params& p, const Row8& w, 
 #pragma unroll
     for (int j = 0; j < kFlight; ++j) {
       const float wj = __shfl_sync(0xffffffffu, wt, j);
-      if (j0 + j < w.n) {
+      if (j0 + j < n) {
 #pragma unroll
         for (int c = 0; c < CPL; ++c) a[c] = fmaf(wj, v[j][c], a[c]);
       }
@@ -139,12 +140,52 @@ __device__ __forceinline__ void add_states(const Attn8Params& p, const Row8& w, 
   }
 }
 
-template <int D, bool ROUND, int FLIGHT>
+// All of them.  SPLIT: the block's warps take a quarter each and the first adds what the others have found: one row a
+// block, where rows are few and their states many (129 states one after the other took 10 us).  True in the warp that
+// has the result.
+template <int D, int FLIGHT, bool SPLIT>
+__device__ __forceinline__ bool add_all(const Attn8Params& p, const Row8& w, int lane, float& m, float& l,
+                                        float (&a)[D / 32]) {
+  constexpr int CPL = D / 32;
+  if (!SPLIT) {
+    add_states<D, FLIGHT>(p, w, 0, w.n, lane, m, l, a);
+    return true;
+  }
+  __shared__ float2 ml_s[kWarps];
+  __shared__ float a_s[kWarps][D];
+  const int warp = threadIdx.x >> 5, j0 = w.n * warp / kWarps, j1 = w.n * (warp + 1) / kWarps;
+  if (warp == 0) {
+    add_states<D, FLIGHT>(p, w, j0, j1, lane, m, l, a);
+  } else {
+    float m1 = -INFINITY, l1 = 0.f, a1[CPL];
+#pragma unroll
+    for (int c = 0; c < CPL; ++c) a1[c] = 0.f;
+    add_states<D, FLIGHT>(p, w, j0, j1, lane, m1, l1, a1);
+    if (lane == 0) ml_s[warp] = make_float2(m1, l1);
+#pragma unroll
+    for (int c = 0; c < CPL; ++c) a_s[warp][lane * CPL + c] = a1[c];
+  }
+  __syncthreads();
+  if (warp) return false;
+#pragma unroll
+  for (int i = 1; i < kWarps; ++i) {
+    const float2 st = ml_s[i];
+    if (st.y == 0.f) continue;
+    const float top = fmaxf(m, st.x), f = m == top ? 1.f : exp2f(m - top), wt = st.x == top ? 1.f : exp2f(st.x - top);
+    m = top;
+    l = fmaf(l, f, wt * st.y);
+#pragma unroll
+    for (int c = 0; c < CPL; ++c) a[c] = fmaf(wt, a_s[i][lane * CPL + c], a[c] * f);
+  }
+  return true;
+}
+
+template <int D, bool ROUND, int FLIGHT, bool SPLIT>
 __global__ void __launch_bounds__(kWarps * 32) attn8_join_kernel(const __grid_constant__ Attn8Params p) {
   constexpr int CPL = D / 32;
   pdl_launch_dependents();
   const int lane = threadIdx.x & 31;
-  const uint32_t row = blockIdx.x * kWarps + (threadIdx.x >> 5);  // (request, kv-head, row)
+  const uint32_t row = SPLIT ? blockIdx.x : blockIdx.x * kWarps + (threadIdx.x >> 5);  // (request, kv-head, row)
   if (row >= (uint32_t)p.B * p.H_kv * p.R) return;  // (the block's first warp has a row)
   Row8 w = row_at8(p, row);
   if (!ROUND) row_states8(p, w, lane);
@@ -155,7 +196,7 @@ __global__ void __launch_bounds__(kWarps * 32) attn8_join_kernel(const __grid_co
   float m = -INFINITY, l = 0.f, a[CPL];
 #pragma unroll
   for (int c = 0; c < CPL; ++c) a[c] = 0.f;
-  add_states<D, FLIGHT>(p, w, lane, m, l, a);
+  if (!add_all<D, FLIGHT, SPLIT>(p, w, lane, m, l, a)) return;
   if (lane == 0) put_ml8(p, w.g, w.r, m, l);
 #pragma unroll
   for (int c = 0; c < CPL; ++c) put_a8(p, w.g, w.r, lane * CPL + c, l, a[c]);
@@ -163,13 +204,13 @@ __global__ void __launch_bounds__(kWarps * 32) attn8_join_kernel(const __grid_co
 
 // End of a round whose history is one 8-bit chunk: its states, joined or not, and the local segment's
 // straight to O and LSE.
-template <int D, int FLIGHT>
+template <int D, int FLIGHT, bool SPLIT>
 __global__ void __launch_bounds__(kWarps * 32) attn8_finalize_kernel(const __grid_constant__ Attn8Params p,
                                                                      const Final8 out) {
   constexpr int CPL = D / 32;
   pdl_launch_dependents();
   const int lane = threadIdx.x & 31;
-  const uint32_t row = blockIdx.x * kWarps + (threadIdx.x >> 5);
+  const uint32_t row = SPLIT ? blockIdx.x : blockIdx.x * kWarps + (threadIdx.x >> 5);
   if (row >= (uint32_t)p.B * p.H_kv * p.R) return;
   Row8 w = row_at8(p, row);
   const int64_t at = ((int64_t)w.g.b * p.H_kv + w.g.kvh) * p.R_stride + w.rr;
@@ -194,7 +235,9 @@ __global__ void __launch_bounds__(kWarps * 32) attn8_finalize_kernel(const __gri
     for (int c = 0; c < CPL; ++c) a[c] = v[c];
   }
   if (w.n >= 2) {
-    add_states<D, FLIGHT>(p, w, lane, m, l, a);
+    if (!add_all<D, FLIGHT, SPLIT>(p, w, lane, m, l, a)) return;
+  } else if (SPLIT && threadIdx.x >= 32) {
+    return;
   } else if (w.n == 1 && st.y != 0.f) {
     const float top = fmaxf(m, st.x), f = m == top ? 1.f : exp2f(m - top), wt = st.x == top ? 1.f : exp2f(st.x - top);
     m = top;
@@ -210,31 +253,27 @@ __global__ void __launch_bounds__(kWarps * 32) attn8_finalize_kernel(const __gri
   if (out.LSE && lane == 0) out.LSE[row] = some ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
 }
 
-dim3 join_grid(const Attn8Params& p) {
+template <int D, int FLIGHT, bool SPLIT>
+cudaError_t launch(const Attn8Params& p, const Final8* out, cudaStream_t s, bool pdl) {
   const int64_t rows = (int64_t)p.B * p.H_kv * p.R;  // below 2^31 (ss_create)
-  return dim3((unsigned)((rows + kWarps - 1) / kWarps));
+  const dim3 grid((unsigned)(SPLIT ? rows : (rows + kWarps - 1) / kWarps)), block(kWarps * 32);
+  if (out) return launch_kernel(attn8_finalize_kernel<D, FLIGHT, SPLIT>, grid, block, 0, s, pdl, p, *out);
+  auto kernel = p.O ? attn8_join_kernel<D, false, FLIGHT, SPLIT> : attn8_join_kernel<D, true, FLIGHT, SPLIT>;
+  return launch_kernel(kernel, grid, block, 0, s, pdl, p);
 }
-
-template <int D, int FLIGHT>
-cudaError_t join(const Attn8Params& p, cudaStream_t s, bool pdl) {
-  auto kernel = p.O ? attn8_join_kernel<D, false, FLIGHT> : attn8_join_kernel<D, true, FLIGHT>;
-  return launch_kernel(kernel, join_grid(p), dim3(kWarps * 32), 0, s, pdl, p);
-}
-template <int D, int FLIGHT>
-cudaError_t finalize(const Attn8Params& p, const Final8& out, cudaStream_t s, bool pdl) {
-  return launch_kernel(attn8_finalize_kernel<D, FLIGHT>, join_grid(p), dim3(kWarps * 32), 0, s, pdl, p, out);
+template <int D>
+cudaError_t launch_rows(const Attn8Params& p, const Final8* out, cudaStream_t s, bool pdl) {
+  if (many_rows(p)) return launch<D, kFlightMany, false>(p, out, s, pdl);
+  return few_rows(p) ? launch<D, kFlight, true>(p, out, s, pdl) : launch<D, kFlight, false>(p, out, s, pdl);
 }
 
 }  // namespace
 
 cudaError_t launch_attn8_join(const Attn8Params& p, cudaStream_t s, bool pdl) {
-  if (many_rows(p)) return p.d == 128 ? join<128, kFlightMany>(p, s, pdl) : join<64, kFlightMany>(p, s, pdl);
-  return p.d == 128 ? join<128, kFlight>(p, s, pdl) : join<64, kFlight>(p, s, pdl);
+  return p.d == 128 ? launch_rows<128>(p, nullptr, s, pdl) : launch_rows<64>(p, nullptr, s, pdl);
 }
-
 cudaError_t launch_attn8_finalize(const Attn8Params& p, const Final8& out, cudaStream_t s, bool pdl) {
-  if (many_rows(p)) return p.d == 128 ? finalize<128, kFlightMany>(p, out, s, pdl) : finalize<64, kFlightMany>(p, out, s, pdl);
-  return p.d == 128 ? finalize<128, kFlight>(p, out, s, pdl) : finalize<64, kFlight>(p, out, s, pdl);
+  return p.d == 128 ? launch_rows<128>(p, &out, s, pdl) : launch_rows<64>(p, &out, s, pdl);
 }
 
 }  // namespace ss

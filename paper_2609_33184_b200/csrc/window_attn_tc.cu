@@ -73,6 +73,13 @@ struct CfgW {
   static_assert(kUnits >= 3 && kCols <= 128 && kPBytes >= 4 * NR * 4 && kUnits * kUnitBytes >= NR * (D + 5) * 4, "shape");
 };
 
+// Two bf16 values, infinities made NaN: an infinite query's scores might all be -inf, and its row look empty.
+__device__ __forceinline__ uint32_t nan_of(uint32_t two) {
+  if ((two & 0x7f80u) == 0x7f80u) two |= 0x7fffu;
+  if ((two & 0x7f800000u) == 0x7f800000u) two |= 0x7fff0000u;
+  return two;
+}
+
 // CL: a unit is one cluster's (kCluster8), each CTA has one segment.
 template <int NR, int D, bool CL>
 __global__ void __launch_bounds__(CfgW<NR, D>::kThreads, CfgW<NR, D>::kPerSM)
@@ -310,6 +317,7 @@ window_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ 
 #pragma unroll
       for (int i = 0; i < kQP; ++i) {
         const int n = (tid + i * SOFT) / (D / 8), c8 = (tid + i * SOFT) % (D / 8);
+        q_raw[i] = make_uint4(nan_of(q_raw[i].x), nan_of(q_raw[i].y), nan_of(q_raw[i].z), nan_of(q_raw[i].w));
         *reinterpret_cast<uint4*>(q_s + (c8 >> 3) * C::kQHalf + n * 128 + (((c8 & 7) ^ (n & 7)) << 4)) = q_raw[i];
       }
       if (tid < NR) {

@@ -78,7 +78,7 @@ def hide(cache, lens, T, window, sinks, room, depth=None, decode=True):
                     table[b, pg] = (-7, 1 << 30)[pg % 2]
 
 
-def check(Q, O, LSE, keys, scale, bits):
+def check(Q, O, LSE, keys, scale, bits, only=None):
     """keys(b, h, t) -> K, V fp64 that query t of request b sees on kv-head h.  Tolerances: O is bf16 (half a step: 2^-8
     of the value); a weight is off by at most half a step of bf16, 2^-8 of itself, where it is held in 16 bits, or by
     2^-30 of the largest weight where three short terms underflow; scores and exponentials in fp32 add below 2^-13 (d
@@ -93,6 +93,8 @@ def check(Q, O, LSE, keys, scale, bits):
     for b in range(B):
         for h in range(H_kv):
             for t in range(T):
+                if only is not None and not only(b, h, t):
+                    continue
                 K, V = keys(b, h, t)
                 qr, og, lg = q[b, h * G:(h + 1) * G, t], Og[b, h * G:(h + 1) * G, t], Lg[b, h * G:(h + 1) * G, t]
                 o, lse, A = kv8.attention(qr, K, V, scale)
@@ -144,7 +146,7 @@ def step(ssb, bits, cache, Q, lens, window, sinks, scale=None, ctx=None, flags=0
     torch.cuda.synchronize()
     assert ctx.ss_poll_status() == (0, 0)
     if kernel:
-        assert ctx.last_chunk_kernel().endswith(kernel), ctx.last_chunk_kernel()
+        assert kernel in ctx.last_chunk_kernel(), ctx.last_chunk_kernel()
     if own:
         ctx.close()
     return O, LSE
@@ -248,3 +250,112 @@ def test_rounds(bits, page, d, G, T, window, sinks, tree):
     local = lambda b, h, t: (kl[b, h][seen[b, t]], vl[b, h][seen[b, t]])
     check(Q, O, LSE, keys_of(cache, H_kv, lens, T, window, sinks, depth, False, local), d ** -0.5, bits)
     ctx.close()
+
+
+# The three ways units meet CTAs: a few units long enough to be cut, clusters of several sizes, whole units.
+FORMS = [
+    ("tcgen05", 1, 1, 8500, 4, (9000,)), ("tcgen05", 3, 1, 8800, 130, (0, 9000, 4100)), ("tcgen05", 1, 2, 2 ** 31 - 1, 0, (8999,)),
+    ("tcgen05-cluster", 1, 1, 1000, 4, (9000,)), ("tcgen05-cluster", 1, 1, 250, 0, (9000,)), ("tcgen05-cluster", 4, 2, 300, 3, (0, 9, 400, 9000)),
+    ("tcgen05-cluster", 100, 2, 200, 4, None), ("tcgen05-whole", 250, 2, 300, 20, None), ("tcgen05-whole", 300, 3, 100, 0, None),
+]
+
+
+@pytest.mark.parametrize("form,B,H_kv,window,sinks,lens", FORMS)
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("d,G,T", [(128, 4, 1), (64, 2, 1), (64, 5, 5), (128, 8, 4)])
+def test_forms(form, B, H_kv, window, sinks, lens, bits, d, G, T):
+    ssb = _ssb()
+    g = _gen(B + window % 1000 + d)
+    room = 9024 if lens else 704
+    lens = list(lens) if lens else [int(x) for x in torch.randint(0, 700, (B,), generator=g)]
+    cache = make(ssb, bits, B, H_kv, d, 32, room, B)
+    Q = queries(g, B, H_kv * G, T, d)
+    if B < 10:
+        hide(cache, lens, T, window, sinks, room)
+    O, LSE = step(ssb, bits, cache, Q, lens, window, sinks, kernel="tcgen05")
+    ctx = ssb.Context(B, H_kv * G, H_kv, d, T, 1, room)
+    O2, LSE2 = step(ssb, bits, cache, Q, lens, window, sinks, ctx=ctx)
+    assert torch.equal(O, O2) and torch.equal(LSE, LSE2)       # the same bits again
+    if T == 1:                                                 # (with more rows the estimate may take another form)
+        assert ctx.last_chunk_kernel().endswith(form), ctx.last_chunk_kernel()
+    ctx.close()
+    only = None if B < 10 else (lambda b, h, t: b % 37 == 0 or lens[b] < 3)
+    check(Q, O, LSE, keys_of(cache, H_kv, lens, T, window, sinks), d ** -0.5, bits, only)
+
+
+@pytest.mark.parametrize("form,B,H_kv,window,sinks,lens", FORMS)
+@pytest.mark.parametrize("bits,d,G,T", [(16, 128, 4, 8), (16, 64, 2, 3), (8, 128, 4, 6), (8, 64, 8, 2)])
+def test_forms_in_rounds(form, B, H_kv, window, sinks, lens, bits, d, G, T):
+    """The forms as chunks: alone, and behind another chunk of the same round with the sets folded."""
+    ssb = _ssb()
+    g = _gen(B + window % 1000 + d + 1)
+    room = 9024 if lens else 704
+    lens = list(lens) if lens else [int(x) for x in torch.randint(0, 700, (B,), generator=g)]
+    cache = make(ssb, bits, B, H_kv, d, 16, room, B)
+    Q, K_loc, V_loc = queries(g, B, H_kv * G, T, d), queries(g, B, H_kv, T, d), queries(g, B, H_kv, T, d)
+    if B < 10:
+        hide(cache, lens, T, window, sinks, room, None, False)
+    more = queries(g, B, H_kv, 40, d), queries(g, B, H_kv, 40, d)
+    n = _i32(lens)
+    kl, vl, km, vm = (x.double().cpu().numpy() for x in (K_loc, V_loc) + more)
+    only = None if B < 10 else (lambda b, h, t: b % 53 == 0 or lens[b] < 3)
+    for flags in (0, ssb.SS_FLAG_OVERLAP_CHUNKS):
+        ctx = ssb.Context(B, H_kv * G, H_kv, d, T, T, room, max_chunks=2, flags=flags)
+        chunk = ctx.ss_verify_chunk8_window if bits == 8 else ctx.ss_verify_chunk_window
+        for behind in (0, 1, 2):                               # other chunks in front: 2 fill the sets, which are folded
+            O, LSE = torch.full_like(Q, float("nan")), torch.full(Q.shape[:3], float("nan"), device=DEV)
+            ctx.ss_verify_begin(Q, d ** -0.5)
+            for _ in range(behind):
+                ctx.ss_verify_chunk(*more)
+            chunk(cache, window, sinks, n)
+            ctx.ss_verify_local(K_loc, V_loc)
+            ctx.ss_verify_finalize(O, LSE)
+            assert ctx.ss_poll_status() == (0, 0)
+
+            def local(b, h, t):
+                k, v = [km[b, h]] * behind + [kl[b, h, : t + 1]], [vm[b, h]] * behind + [vl[b, h, : t + 1]]
+                return np.concatenate(k), np.concatenate(v)
+            check(Q, O, LSE, keys_of(cache, H_kv, lens, T, window, sinks, None, False, local), d ** -0.5, bits, only)
+        ctx.close()
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+@pytest.mark.parametrize("kernel", ["tcgen05", "simt"])
+def test_states_and_mixed_chunks(bits, kernel):
+    """Window chunks beside each other, beside plain and whole-history chunks, exported in between and imported elsewhere."""
+    ssb = _ssb()
+    B, H_kv, G, d, T, room, page = 3, 2, 4, 128, 4, 2048, 16 if kernel == "tcgen05" else 5
+    lens, lens8 = [900, 0, 2040], [100, 300, 0]
+    g = _gen(3)
+    c16, c8 = make(ssb, 16, B, H_kv, d, page, room, 1), make(ssb, 8, B, H_kv, d, page, room, 2)
+    Q, K_loc, V_loc = queries(g, B, H_kv * G, T, d), queries(g, B, H_kv, T, d), queries(g, B, H_kv, T, d)
+    K, V = queries(g, B, H_kv, 64, d), queries(g, B, H_kv, 64, d)
+    one, two = (ssb.Context(B, H_kv * G, H_kv, d, T, T, room + page, max_chunks=3) for _ in range(2))
+    rows = B * H_kv * G * T
+    ml, a = torch.empty(rows, 2, device=DEV), torch.empty(rows, d, device=DEV)
+    O, LSE = torch.empty_like(Q), torch.empty(Q.shape[:3], device=DEV)
+    one.ss_verify_begin(Q, d ** -0.5)
+    one.ss_verify_chunk_window(c16, 500, 4, _i32(lens))
+    one.ss_verify_chunk8(c8, _i32(lens8))
+    one.ss_verify_chunk8_window(c8, 70, 2, _i32(lens))
+    one.ss_verify_export_state(ml, a)
+    one.ss_verify_abort()
+    two.ss_verify_begin(Q, d ** -0.5)
+    two.ss_verify_chunk(K, V)
+    two.ss_verify_chunk_window(c16, 33, 0, _i32(lens8))
+    two.ss_verify_import_state(ml, a)
+    two.ss_verify_local(K_loc, V_loc)
+    two.ss_verify_finalize(O, LSE)
+    assert one.ss_poll_status() == (0, 0) and two.ss_poll_status() == (0, 0)
+    parts = [keys_of(c16, H_kv, lens, T, 500, 4, None, False), keys_of(c8, H_kv, lens8, T, 10 ** 6, 0, None, False),
+             keys_of(c8, H_kv, lens, T, 70, 2, None, False), keys_of(c16, H_kv, lens8, T, 33, 0, None, False)]
+    kl, vl, km, vm = (x.double().cpu().numpy() for x in (K_loc, V_loc, K, V))
+
+    def keys(b, h, t):
+        if h is None:
+            return H_kv
+        kv = [f(b, h, t) for f in parts] + [(km[b, h], vm[b, h]), (kl[b, h, : t + 1], vl[b, h, : t + 1])]
+        return np.concatenate([x[0] for x in kv]), np.concatenate([x[1] for x in kv])
+    check(Q, O, LSE, keys, d ** -0.5, 8)
+    one.close()
+    two.close()
