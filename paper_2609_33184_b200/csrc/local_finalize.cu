@@ -48,6 +48,7 @@ __global__ void __launch_bounds__(kWarpsPerCta * 32) local_kernel(const LocalPar
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t row_id = (int64_t)blockIdx.x * kWarpsPerCta + warp;
   const int64_t n_rows = (int64_t)p.B * p.H_q * p.T_q;
+  if (p.wait_first) pdl_wait_prior();
   pdl_launch_dependents();
   if (row_id < n_rows) {
     float* sc = sc_all + (size_t)warp * p.T_loc;
@@ -159,7 +160,7 @@ __global__ void __launch_bounds__(kWarpsPerCta * 32) local_kernel(const LocalPar
     else
       *reinterpret_cast<float2*>(out) = make_float2(acc[0], acc[1]);
   }
-  if (blockIdx.x == 0) pdl_wait_prior();  // one CTA keeps the completion order along the stream
+  if (!p.wait_first && blockIdx.x == 0) pdl_wait_prior();  // one CTA keeps the completion order along the stream
 }
 
 // The same for up to 8 local keys (a chain of 2 to 8 candidates): a warp keeps the kv-head's K and V rows in
@@ -173,6 +174,7 @@ __global__ void __launch_bounds__(kWarpsPerCta * 32) local_few_kernel(const Loca
   constexpr int CPL = D / 32;  // columns per lane
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int R = p.G * p.T_q, per_pair = (R + kWarpsPerCta * kFewRows - 1) / (kWarpsPerCta * kFewRows);
+  if (p.wait_first) pdl_wait_prior();
   pdl_launch_dependents();
   const int pair = blockIdx.x / per_pair, b = pair / p.H_kv, kvh = pair - b * p.H_kv;
   const int r0 = (blockIdx.x - pair * per_pair) * (kWarpsPerCta * kFewRows) + warp * kFewRows;
@@ -264,7 +266,7 @@ __global__ void __launch_bounds__(kWarpsPerCta * 32) local_few_kernel(const Loca
         *reinterpret_cast<float2*>(out) = make_float2(acc[0], acc[1]);
     }
   }
-  if (blockIdx.x == 0) pdl_wait_prior();  // one CTA keeps the completion order along the stream
+  if (!p.wait_first && blockIdx.x == 0) pdl_wait_prior();  // one CTA keeps the completion order along the stream
 }
 
 // ---------------------------------------------------------------------------------------

@@ -131,6 +131,7 @@ struct LocalParams {
   float2* part_ml;  // local set: slot = b * H_kv + kvh
   float* part_a;
   int R_stride;
+  int wait_first;   // 1: wait for the preceding kernel before reading inputs
 };
 
 struct MergeParams {
