@@ -397,9 +397,12 @@ __device__ __forceinline__ bool win_plain8(const Attn8Params& p, const Win8& w, 
 __device__ __forceinline__ bool win_any8(const Attn8Params& p, const Win8& w, int j) {
   return j < w.n && (j < w.sinks || j > w.first - p.window);
 }
-__device__ __forceinline__ bool win_sees8(const Attn8Params& p, const Win8& w, int pos, int j) {
-  return j <= pos && j < w.n && (j < w.sinks || pos - j < p.window);
+// Does a query at position pos see token j?  As one comparison per query: `reach` = how far in front of a query the token
+// may lie (0: token behind the last; 2^31: a sink, any distance).
+__device__ __forceinline__ uint32_t win_reach8(const Attn8Params& p, const Win8& w, int j) {
+  return j >= w.n ? 0u : j < w.sinks ? 0x80000000u : (uint32_t)p.window;
 }
+__device__ __forceinline__ bool win_sees8(int pos, int j, uint32_t reach) { return (uint32_t)(pos - j) < reach; }
 
 // Requests without a visible token, by `n` threads of every CTA.  (Out of line, not unrolled: what a
 // kernel seldom runs should not stand between the parts that it always runs.)

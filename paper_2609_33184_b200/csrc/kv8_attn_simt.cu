@@ -76,13 +76,10 @@ __global__ void __launch_bounds__(128) attn8_simt_kernel(const __grid_constant__
   Seg8 g;
   for (bool more = seg_first8<WIN>(p, share, &g); more; more = seg_next8<WIN>(p, share, &g)) {
     __syncthreads();  // the previous segment's shared memory has been read
-    Span8 span = {};
-    int sinks = 0;
+    Win8 w = {};
     if (WIN) {
-      const int n = room_len8(p, g.b);
-      span = span8(p, n);
-      sinks = min(p.sinks, n);
-      if (tid < g.nrows) pos_s[tid] = n - p.before + depth8(p, g.b, (g.row0 + tid) % p.T_q);
+      w = win8(p, g.b);
+      if (tid < g.nrows) pos_s[tid] = w.first + depth8(p, g.b, (g.row0 + tid) % p.T_q);
     }
     for (int i = tid; i < kRT * D; i += 128) {
       const int r = i / D, c = i % D;
@@ -108,7 +105,8 @@ __global__ void __launch_bounds__(128) attn8_simt_kernel(const __grid_constant__
       const int tok0 = t * kTok8 + warp * 32, v_tok = tok0 + lane;
       if (tok0 >= g.len) continue;
       const bool ok = v_tok < g.len;
-      const int tok = WIN && v_tok >= span.cut ? v_tok + span.skip : v_tok;
+      const int tok = WIN ? win_token8(w, v_tok) : v_tok;
+      const uint32_t reach = WIN ? win_reach8(p, w, tok) : 0u;
       int inner = 0, outer = -1;
       if (ok) {
         outer = outer8(p.kv, g.b, tok, &inner);
@@ -145,7 +143,7 @@ __global__ void __launch_bounds__(128) attn8_simt_kernel(const __grid_constant__
       }
 #pragma unroll
       for (int r = 0; r < kRT; ++r) {
-        const bool seen = ok && (!WIN || (r < g.nrows && tok <= pos_s[r] && (tok < sinks || pos_s[r] - tok < p.window)));
+        const bool seen = ok && (!WIN || (r < g.nrows && win_sees8(pos_s[r], tok, reach)));
         const float x = seen ? s[r] : -INFINITY;
         const float top = fmaxf(m[r], warp_max8(x));
         const float f = (m[r] == top) ? 1.f : exp2f(m[r] - top);  // (equal also when both are -inf)

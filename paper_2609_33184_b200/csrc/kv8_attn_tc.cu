@@ -62,7 +62,7 @@ struct alignas(16) Ctl8 {
 template <int NQ>
 struct CtlWin8 : Ctl8<NQ> {
   int unset;                      // rows without a reference
-  int pos[NQ];                    // the rows' positions
+  alignas(16) int pos[NQ];        // the rows' positions
 };
 
 // NR = rows, D = head dim, WIN = over a window.
@@ -77,7 +77,8 @@ struct Cfg8 {
   static constexpr int kPBytes = kTok8 * NP;
   using Ctl = std::conditional_t<WIN, CtlWin8<NQ>, Ctl8<NQ>>;
   static constexpr int kCtlBytes = (sizeof(Ctl) + 127) / 128 * 128;
-  static constexpr int kRest = (kQBytes + 1023) / 1024 * 1024 + kPBytes + kCtlBytes;
+  static constexpr int kPartsBytes = WIN ? Parts8<NQ, D, NR == 8>::kBytes : 0;   // (clusters)
+  static constexpr int kRest = (kQBytes + 1023) / 1024 * 1024 + kPBytes + kCtlBytes + kPartsBytes;
   // head dim 64: the output MMA's upper 64 rows read one unit further on (results never used), the
   // last unit's inside this window too
   static constexpr int kAfter = D == 64 && kRest < kUnitBytes ? kUnitBytes : kRest;
@@ -90,6 +91,7 @@ struct Cfg8 {
   static constexpr int kOffQ = kUnits * kUnitBytes;
   static constexpr int kOffP = kOffQ + (kQBytes + 1023) / 1024 * 1024;
   static constexpr int kOffCtl = kOffP + kPBytes;
+  static constexpr int kOffParts = kOffCtl + kCtlBytes;
   static constexpr int kSmem = kOffQ + kAfter;
   static constexpr int kCols = 2 * NS + NP;
   static constexpr uint32_t kTmemCols = kCols <= 64 ? 64 : kCols <= 128 ? 128 : 256;
@@ -141,10 +143,6 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   constexpr int kProducerWarp = 4, kMmaWarp = 5;
 
-  // (CL) state of this CTA's part, where the ring was: m[NQ], row sums of the four warps [NQ][4], a[NQ][D]
-  float* part_m = reinterpret_cast<float*>(smem);
-  float* part_l = part_m + NQ;
-  float* part_a = part_l + 4 * NQ;
   // The warp that takes the tensor memory.  Over a window the producer is free of it and of the barrier in front of
   // the roles: its first copies have a chain of dependent loads in front of them that all the rest waits for.
   constexpr int kTmemWarp = WIN ? kMmaWarp : kProducerWarp;
@@ -174,6 +172,8 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
   }
   Place8 place = {};
   if (CL) place = cluster_place8(p);
+  constexpr bool PUSH = CL && NR == 8;
+  const Parts8<NQ, D, PUSH> parts(reinterpret_cast<float*>(smem + (PUSH ? C::kOffParts : 0)), p, place);
   auto find = [&]() {
     Share8 s = {};
     if (!CL) s = find_share8<WIN>(p);
@@ -576,16 +576,20 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
         if (WIN) {
           if (masked) {
             __syncwarp();
+            const uint32_t reach = win_reach8(p, w, tok);
             if (p.T_q == 1) {
-              const bool ok = win_sees8(p, w, w.first, tok);
+              const bool ok = win_sees8(w.first, tok, reach);
 #pragma unroll
               for (int r = 0; r < NR / 2; ++r)
                 if (!ok) x[r] = make_float2(-INFINITY, -INFINITY);
             } else if constexpr (WIN) {
 #pragma unroll
-              for (int r = 0; r < NR / 2; ++r) {
-                if (!win_sees8(p, w, ctl->pos[2 * r], tok)) x[r].x = -INFINITY;
-                if (!win_sees8(p, w, ctl->pos[2 * r + 1], tok)) x[r].y = -INFINITY;
+              for (int r = 0; r < NR; r += 4) {
+                const int4 pos = *reinterpret_cast<const int4*>(&ctl->pos[r]);
+                if (!win_sees8(pos.x, tok, reach)) x[r / 2].x = -INFINITY;
+                if (!win_sees8(pos.y, tok, reach)) x[r / 2].y = -INFINITY;
+                if (!win_sees8(pos.z, tok, reach)) x[r / 2 + 1].x = -INFINITY;
+                if (!win_sees8(pos.w, tok, reach)) x[r / 2 + 1].y = -INFINITY;
               }
             }
           }
@@ -734,8 +738,9 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
         if (CL) {
           wait(&ctl->pfree, (it - 1) & 1);
           tc_fence_after();
-          if (lane % (32 / NQ) == 0) part_l[lane / (32 / NQ) * 4 + warp] = v[0];
-          if (tid < NQ) part_m[tid] = -ctl->nm[tid];
+          parts.ready();
+          if (lane % (32 / NQ) == 0) parts.put_l(lane / (32 / NQ), warp, v[0]);
+          if (tid < NQ) parts.put_m(tid, -ctl->nm[tid]);
 #pragma unroll 1
           for (int q = 0; q < NR && q < done.nrows; q += 8) {
             uint32_t o[3][8];
@@ -745,8 +750,8 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
 #pragma unroll
             for (int c = 0; c < 8; ++c)
               if (key < D)
-                part_a[(q + c) * D + key] = fmaf(__uint_as_float(o[2][c]), 1.f / 64.f,
-                                                 fmaf(__uint_as_float(o[1][c]), 0.125f, __uint_as_float(o[0][c])));
+                parts.put_a(q + c, key, fmaf(__uint_as_float(o[2][c]), 1.f / 64.f,
+                                             fmaf(__uint_as_float(o[1][c]), 0.125f, __uint_as_float(o[0][c]))));
           }
           break;
         }
@@ -799,7 +804,10 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
       bar8<SOFT>();  // sums, references and Q may be written anew
     }
     if (CL) {
-      if (!ctl->has[0] && tid < 4 * NQ) part_l[tid] = 0.f;
+      if (!ctl->has[0]) {
+        parts.ready();
+        parts.put_none(tid);
+      }
     } else if ((int)blockIdx.x < p.B) {
       put_empty8<WIN>(p, tid, SOFT);
     }
@@ -809,7 +817,8 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
   if (!CL) {
     __syncthreads();
   } else {
-    cluster_end8<NQ, D>(p, place, part_m, part_l, part_a);
+    if (warp >= 4) parts.ready();
+    parts.end(p, place);
   }
   if (warp == kTmemWarp)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(C::kTmemCols) : "memory");

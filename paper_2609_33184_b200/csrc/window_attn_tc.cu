@@ -40,7 +40,7 @@ struct alignas(16) CtlW {
   Share8 share;
   alignas(16) float nm[NR];       // -M
   alignas(16) float up[NR];       // rise of the references; at a segment's end 1 / row sum
-  int pos[NR];                    // the rows' positions
+  alignas(16) int pos[NR];        // the rows' positions
 };
 
 // NR = rows, D = head dim.
@@ -56,7 +56,8 @@ struct CfgW {
   static constexpr int kQBytes = kHalves * kQHalf;
   static constexpr int kPBytes = kTok8 * NP * 2;
   static constexpr int kCtlBytes = (sizeof(CtlW<NR>) + 127) / 128 * 128;
-  static constexpr int kRest = (kQBytes + 1023) / 1024 * 1024 + kPBytes + kCtlBytes;
+  static constexpr int kPartsBytes = Parts8<NR, D, NR == 8>::kBytes;   // (clusters)
+  static constexpr int kRest = (kQBytes + 1023) / 1024 * 1024 + kPBytes + kCtlBytes + kPartsBytes;
   // head dim 64: the output MMA's upper 64 rows read one box further on (results never used), the last
   // unit's inside this window too
   static constexpr int kAfter = D == 64 && kRest < kBox ? kBox : kRest;
@@ -66,6 +67,7 @@ struct CfgW {
   static constexpr int kOffQ = kUnits * kUnitBytes;
   static constexpr int kOffP = kOffQ + (kQBytes + 1023) / 1024 * 1024;
   static constexpr int kOffCtl = kOffP + kPBytes;
+  static constexpr int kOffParts = kOffCtl + kCtlBytes;
   static constexpr int kSmem = kOffQ + kAfter;
   static constexpr uint32_t kColO = 2 * NQ;                 // two score buffers, then O^T
   static constexpr int kCols = 2 * NQ + NP;
@@ -92,10 +94,6 @@ window_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ 
   uint8_t* q_s = smem + C::kOffQ;
   uint8_t* p_s = smem + C::kOffP;
   float* smax = reinterpret_cast<float*>(p_s);    // [4][NR] maxima and sums of the warps, while P is not in use
-  // (CL) state of this CTA's part, where the ring was: m[NR], row sums of the four warps [NR][4], a[NR][D]
-  float* part_m = reinterpret_cast<float*>(smem);
-  float* part_l = part_m + NR;
-  float* part_a = part_l + 4 * NR;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   constexpr int kProducerWarp = 4, kMmaWarp = 5;
 
@@ -124,6 +122,8 @@ window_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ 
   }
   Place8 place = {};
   if (CL) place = cluster_place8(p);
+  using P = Parts8<NR, D, CL && NR == 8>;
+  const P parts(reinterpret_cast<float*>(smem + (NR == 8 ? C::kOffParts : 0)), p, place);
   auto find = [&]() {
     Share8 s = {};
     if (!CL) s = find_share8<true>(p);
@@ -368,17 +368,20 @@ window_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ 
         unsigned dead = 0;  // keys of this warp that no query sees
         if (!plain) {
           dead = __ballot_sync(0xffffffffu, !win_any8(p, w, tok));
+          const uint32_t reach = win_reach8(p, w, tok);
           if (p.T_q == 1) {
-            const bool ok = win_sees8(p, w, w.first, tok);
+            const bool ok = win_sees8(w.first, tok, reach);
 #pragma unroll
             for (int r = 0; r < NR / 2; ++r)
               if (!ok) x[r] = make_float2(-INFINITY, -INFINITY);
           } else {
 #pragma unroll
-            for (int r = 0; r < NR / 2; ++r) {
-              const int2 pos = *reinterpret_cast<const int2*>(&ctl->pos[2 * r]);
-              if (!win_sees8(p, w, pos.x, tok)) x[r].x = -INFINITY;
-              if (!win_sees8(p, w, pos.y, tok)) x[r].y = -INFINITY;
+            for (int r = 0; r < NR; r += 4) {
+              const int4 pos = *reinterpret_cast<const int4*>(&ctl->pos[r]);
+              if (!win_sees8(pos.x, tok, reach)) x[r / 2].x = -INFINITY;
+              if (!win_sees8(pos.y, tok, reach)) x[r / 2].y = -INFINITY;
+              if (!win_sees8(pos.z, tok, reach)) x[r / 2 + 1].x = -INFINITY;
+              if (!win_sees8(pos.w, tok, reach)) x[r / 2 + 1].y = -INFINITY;
             }
           }
         }
@@ -505,8 +508,9 @@ window_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ 
       wait(&ctl->pfree, (it - 1) & 1);
       tc_fence_after();
       if (CL) {
-        if (lane % (32 / NR) == 0) part_l[lane / (32 / NR) * 4 + warp] = v[0];
-        if (tid < NR) part_m[tid] = -ctl->nm[tid];
+        parts.ready();
+        if (lane % (32 / NR) == 0) parts.put_l(lane / (32 / NR), warp, v[0]);
+        if (tid < NR) parts.put_m(tid, -ctl->nm[tid]);
 #pragma unroll 1
         for (int q = 0; q < NR && q < done.nrows; q += 8) {
           uint32_t o[C::kTerms][8];
@@ -517,7 +521,7 @@ window_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ 
           for (int c = 0; c < 8; ++c) {
             float a = __uint_as_float(o[0][c]);
             if (C::kTerms == 2) a += __uint_as_float(o[C::kTerms - 1][c]);
-            if (key < D) part_a[(q + c) * D + key] = a;
+            if (key < D) parts.put_a(q + c, key, a);
           }
         }
         break;
@@ -565,7 +569,10 @@ window_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ 
       bar8<SOFT>();  // sums, references and Q may be written anew
     }
     if (CL) {
-      if (!ctl->has[0] && tid < 4 * NR) part_l[tid] = 0.f;
+      if (!ctl->has[0]) {
+        parts.ready();
+        parts.put_none(tid);
+      }
     } else if ((int)blockIdx.x < p.B) {
       put_empty8<true>(p, tid, SOFT);
     }
@@ -575,7 +582,8 @@ window_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ 
   if (!CL) {
     __syncthreads();
   } else {
-    cluster_end8<NR, D>(p, place, part_m, part_l, part_a);
+    if (warp >= 4) parts.ready();
+    parts.end(p, place);
   }
   if (warp == kMmaWarp)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(C::kTmemCols) : "memory");
