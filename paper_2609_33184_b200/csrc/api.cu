@@ -1400,6 +1400,21 @@ static void window_mode(ss::Attn8Params* p, int bits, int64_t tiles) {
   p->cluster = (int)c;
 }
 
+// Most rows of a window's unit.  A tile takes a CTA less time with fewer rows (a latency of steps, not of memory), but all
+// of a unit's rows read K and V once, and every unit again (out of L2).  So units of 8 or 16 rows are formed while each
+// still has an SM to itself and what an SM reads stays short.
+// Measured, head dim 128, groups of 4, with 32 / 16 / 8 rows in us: 8 heads, 24 rows over a window of 128, bf16 8.6 / 7.5 /
+// 7.4; of 1000 11.4 / 10.9 / 12.8, 8 bits 11.7 / 10.0 / 10.0; of 4000 14.8 / 18.3 / 26.4 and 14.5 / 14.6 / 20.8; 1 head,
+// 8 positions over 128, bf16 8.5 / 6.9 / 5.8, 8 bits 8.7 / 6.9 / 5.4; 64 heads over 128 9.4 / 8.5 / 9.9 and 9.7 / 8.2 / 8.8.
+static int window_rows(int bits, int64_t heads, int R, int64_t walked) {
+  for (int most = ss::kMinRows8; most < ss::kRows8; most *= 2) {
+    const int64_t units = heads * ((R + most - 1) / most);
+    const int tokens = bits == 8 ? 900 : most == 8 ? 160 : 700;  // that an SM's unit reads, on average over the SMs
+    if (units <= ss::kNumSM && units * walked <= (int64_t)tokens * ss::kNumSM) return most;
+  }
+  return ss::kRows8;
+}
+
 // The attention launch that the entry points share; the caller has set where its result goes.
 static ss_status attn8(ss_ctx* c, int bits, const ss_tensor& Q, int32_t B, int32_t T_q, float scale, const ss_cache8* cache,
                        const int32_t* valid_len, const Window8& win, ss::Attn8Params* p, cudaStream_t s) {
@@ -1446,19 +1461,19 @@ static ss_status attn8(ss_ctx* c, int bits, const ss_tensor& Q, int32_t B, int32
     p->before = p->O ? T_q : 0;
     p->depth = win.depth;
   }
-  const int most = tc ? ss::kRows8 : ss::kMinRows8;  // rows per unit, evenly spread
-  p->row_tiles = (p->R + most - 1) / most;
+  // the most tokens and tiles that are walked of a request (a window: granules at its ends)
+  const int64_t seen = (int64_t)win.window + win.sinks + T_q, room = p->kv.room;
+  const int64_t tokens = win.window && seen < room ? seen : room;
+  const int64_t walked = win.window && seen + 2 * 32 < room ? seen + 2 * 32 : room;
+  const int64_t most_tiles = (walked + ss::kTok8 - 1) / ss::kTok8;
+  const int most = !tc ? ss::kMinRows8 : win.window ? window_rows(bits, (int64_t)B * p->H_kv, p->R, walked) : ss::kRows8;
+  p->row_tiles = (p->R + most - 1) / most;  // units of `most` rows at most, evenly spread
   p->rows_per_tile = (p->R + p->row_tiles - 1) / p->row_tiles;
   // (the kernels number all tiles in 31 bits)
   if ((int64_t)B * ((p->kv.room + ss::kTok8 - 1) / ss::kTok8) * p->H_kv >= (1ll << 31)) return SS_ERR_SHAPE;
   // as many CTAs as are resident, and one for every row tile at least
   p->shares = (tc && bits == 8 && p->d == 64 && p->rows_per_tile <= ss::kFew8 ? ss::kCtasFew8 : ss::kCtas8) / p->row_tiles;
   if (p->shares < 1) p->shares = 1;
-  // the most tokens and tiles that are walked of a request (a window: granules at its ends)
-  const int64_t seen = (int64_t)win.window + win.sinks + T_q, room = p->kv.room;
-  const int64_t tokens = win.window && seen < room ? seen : room;
-  const int64_t walked = win.window && seen + 2 * 32 < room ? seen + 2 * 32 : room;
-  const int64_t most_tiles = (walked + ss::kTok8 - 1) / ss::kTok8;
   if (win.window && tc) window_mode(p, bits, most_tiles);
   p->scale_log2 = scale * 1.4426950408889634f;
   p->scratch = c->scratch8;
