@@ -391,6 +391,13 @@ class Cache16:
         self.ref = C.byref(self.desc)
         self.known = marshal().cache(C.addressof(self.desc), 16, self.H_kv, self.d, self.requests, self.device)
 
+    @classmethod
+    def empty(cls, outer: int, H_kv: int, tokens: int, d: int, page_table: Optional[torch.Tensor] = None,
+              device="cuda:0") -> "Cache16":
+        """A cache of zeros: `outer` pages of `tokens` tokens, or `outer` requests with room for them."""
+        zeros = lambda: torch.zeros(outer, H_kv, tokens, d, dtype=torch.bfloat16, device=device)
+        return cls(zeros(), zeros(), page_table)
+
 
 class Rope:
     """A rotation (ss_rope): inv_freq, the angle per position of each of the rot_dim / 2 pairs; axis, the position

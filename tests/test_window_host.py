@@ -100,3 +100,12 @@ def test_a_cache_of_another_type_is_refused(dtype):
             ssb.Cache16(K, V)
     with pytest.raises(AssertionError):
         ssb.Cache16(good, good, torch.zeros(2, 1))
+
+
+def test_an_empty_cache():
+    table = torch.zeros(2, 3, dtype=torch.int32)
+    cache = ssb.Cache16.empty(6, 2, 16, 64, table, device="cpu")
+    assert [t.shape for t in cache.tensors] == [(6, 2, 16, 64), (6, 2, 16, 64), (2, 3)] and cache.requests == 2
+    assert all(t.dtype is torch.bfloat16 and not t.any() for t in cache.tensors[:2])
+    assert cache.tensors[0].data_ptr() != cache.tensors[1].data_ptr()
+    assert ssb.Cache16.empty(3, 2, 16, 64, device="cpu").requests == 3
