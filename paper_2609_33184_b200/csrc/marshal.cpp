@@ -6,6 +6,8 @@
 #include <Python.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <exception>
+
 #include "specstream.h"
 
 namespace {
@@ -79,7 +81,7 @@ bool sizes(PyObject* o, int64_t* B, int64_t* T) {
   if (t.dim() != 4) return fail("tensor [B, H, T, d] expected");
   *B = t.size(0);
   *T = t.size(2);
-  return true;
+  return (*B <= INT32_MAX && *T <= INT32_MAX) || fail("too many rows");
 }
 // Rows in and rows out, or neither.
 bool pair(const Ctx* c, PyObject* x, PyObject* out, int64_t B, int64_t H, int64_t T, ss_tensor* a, ss_tensor* b) {
@@ -221,7 +223,18 @@ PyObject* chunk_window(PyObject*, Args a, Py_ssize_t n) {
                                    : ss_verify_chunk_window(c->handle, static_cast<const ss_cache16*>(cache->desc), window, sinks, len, depth, stream));
 }
 
-#define SS_METHOD(name, f) {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
+// A tensor without strides or storage (sparse, nested) throws when it is asked for them: no exception leaves a call.
+template <PyObject* (*F)(PyObject*, Args, Py_ssize_t)>
+PyObject* guarded(PyObject* self, Args a, Py_ssize_t n) {
+  try {
+    return F(self, a, n);
+  } catch (const std::exception& e) {
+    PyErr_SetString(PyExc_AssertionError, e.what());
+    return nullptr;
+  }
+}
+#define SS_METHOD(name, ...) \
+  {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(guarded<__VA_ARGS__>)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {SS_METHOD("context", context),
                          SS_METHOD("cache", cache),
                          SS_METHOD("rope_rotate", rope_rotate),

@@ -109,3 +109,18 @@ def test_an_empty_cache():
     assert all(t.dtype is torch.bfloat16 and not t.any() for t in cache.tensors[:2])
     assert cache.tensors[0].data_ptr() != cache.tensors[1].data_ptr()
     assert ssb.Cache16.empty(3, 2, 16, 64, device="cpu").requests == 3
+
+
+def test_a_tensor_without_strides_is_refused(call):
+    m, me, z, c16, _ = call
+    Q, K, n = z(3, 4, 5, 64), z(3, 2, 5, 64), torch.zeros(3, dtype=torch.int32)
+    nested = torch.nested.nested_tensor([K[0], K[1], K[2]])
+    wide = z(64).as_strided((3, 2, 2 ** 32 + 1, 64), (0, 0, 0, 1))  # more rows than a call takes
+    for bad in (K.to_sparse(), nested, wide):
+        for f in (lambda: m.kv_append(me, c16.known, bad, K, None, None, None, None, None, None, None, 0),
+                  lambda: m.kv_append(me, c16.known, K, bad, None, None, None, None, None, None, None, 0),
+                  lambda: m.decode_window(me, bad, 1.0, c16.known, 1, 0, n, Q, None, 0),
+                  lambda: m.decode_window(me, Q, 1.0, c16.known, 1, 0, n.to_sparse(), Q, None, 0),
+                  lambda: m.decode_window(me, Q, 1.0, c16.known, 1, 0, n, Q.to_sparse(), None, 0)):
+            with pytest.raises(AssertionError):
+                f()
