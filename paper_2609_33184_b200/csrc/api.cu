@@ -1440,7 +1440,7 @@ static ss_status attn8(ss_ctx* c, int bits, const ss_tensor& Q, int32_t B, int32
   bool tc = c->tc_ok && (!cache->page_table || ps % ss::kTok8 == 0 || (ps >= 8 && ss::kTok8 % ps == 0));
   int box = cache->page_table && ps < ss::kTok8 ? ps : ss::kTok8;
   if (win.window) {
-    if (p->kv.room > 0x7fffffff - 16384) return SS_ERR_SHAPE;  // (positions and granules in 32 bits)
+    if (p->kv.room + 2ll * T_q > 0x7fffffff - 16384) return SS_ERR_SHAPE;  // (positions and granules in 32 bits)
     p->gran_log2 = granule_log2(p->kv);
     tc = c->tc_ok && p->gran_log2;
     box = 1 << p->gran_log2;

@@ -376,3 +376,76 @@ def test_a_request_from_prompt_to_rounds(bits, d, page, window, sinks):
         lens = [a + b for a, b in zip(lens, took)]
     assert ctx.ss_poll_status() == (0, 0)
     ctx.close()
+
+
+def test_room_and_queries_that_pass_31_bits_together_are_refused():
+    ssb = _ssb()
+    room = 2 ** 31 - 16384 - 64
+    table = torch.zeros(1, room // 64, dtype=torch.int32, device=DEV)
+    cache = ssb.Cache16.empty(1, 1, 64, 64, table)
+    for T, fits in ((4, True), (40, False)):
+        ctx = ssb.Context(1, 1, 1, 64, T, T, room)
+        Q, O = (torch.ones(1, 1, T, 64, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+        call = lambda: ctx.ss_decode_window(Q, 1.0, cache, 2 ** 31 - 1, 2 ** 31 - 1, _i32([7]), O)
+        if fits:
+            call()
+            assert ctx.ss_poll_status() == (0, 0) and not O.any()
+        else:
+            with pytest.raises(ssb.SpecStreamError) as e:
+                call()
+            assert e.value.status == ssb.SS_ERR_SHAPE
+        ctx.close()
+
+
+@pytest.mark.parametrize("bits", [16, 8])
+def test_captured_behind_copies_and_other_kernels(bits):
+    """A step and a round in one graph, each call right behind a copy or a kernel that writes what it reads."""
+    ssb = _ssb()
+    B, H_kv, G, d, T, room, window = 3, 2, 2, 64, 2, 320, 70
+    g = _gen(17)
+    cache, other = (make(ssb, bits, B, H_kv, d, 16, room, 3) for _ in range(2))
+    ctx = ssb.Context(B, H_kv * G, H_kv, d, T, T, room)
+    rope = ssb.Rope([1.0 / (i + 1) for i in range(d // 2)])
+    src = [queries(g, B, h, T, d) for h in (H_kv * G, H_kv, H_kv)]
+    buf = [torch.zeros_like(x) for x in src]
+    lens = [_i32([5, 200, 0]), _i32([71, 90, 300])]
+    here, n, after = (torch.zeros(B, dtype=torch.int32, device=DEV) for _ in range(3))
+    out = [(torch.empty_like(src[0]), torch.empty(src[0].shape[:3], device=DEV)) for _ in range(4)]
+    append = ctx.ss_kv8_append if bits == 8 else ctx.ss_kv_append
+    decode = ctx.ss_decode8_window if bits == 8 else ctx.ss_decode_window
+    chunk = ctx.ss_verify_chunk8_window if bits == 8 else ctx.ss_verify_chunk_window
+
+    def run(c, a, b):
+        n.copy_(here)
+        append(c, buf[1], buf[2], rope, None, buf[0], buf[0], n)
+        torch.add(n, T, out=after)
+        decode(buf[0], 0.125, c, window, 3, after, *a)
+        n.copy_(after)
+        ctx.ss_verify_begin(buf[0], 0.125)
+        chunk(c, window, 3, n)
+        buf[1].copy_(src[1])
+        ctx.ss_verify_local(buf[1], buf[2])
+        ctx.ss_verify_finalize(*b)
+
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            run(cache, *out[:2])
+        for k in (0, 1, 0):
+            for c, go in ((cache, graph.replay), (other, lambda: run(other, *out[2:]))):
+                here.copy_(lens[k])
+                for x, y in zip(buf, src):
+                    x.copy_(y)
+                go()
+            stream.synchronize()
+            for x, y in zip(out[:2], out[2:]):
+                assert torch.equal(x[0], y[0]) and torch.equal(x[1], y[1])
+            for x, y in zip(cache.tensors, other.tensors):
+                assert torch.equal(x, y)
+            now = (lens[k] + T).tolist()
+            local = lambda b, h, t: [x[b, h, :t + 1].double().cpu().numpy() for x in src[1:]]
+            check(buf[0], *out[0], keys_of(cache, H_kv, now, T, window, 3), 0.125, bits)
+            check(buf[0], *out[1], keys_of(cache, H_kv, now, T, window, 3, decode=False, local=local), 0.125, bits)
+    assert ctx.ss_poll_status(stream) == (0, 0)
+    ctx.close()
