@@ -174,10 +174,17 @@ __global__ void __launch_bounds__(kWarpsPerCta * 32) local_few_kernel(const Loca
   constexpr int CPL = D / 32;  // columns per lane
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int R = p.G * p.T_q, per_pair = (R + kWarpsPerCta * kFewRows - 1) / (kWarpsPerCta * kFewRows);
-  if (p.wait_first) pdl_wait_prior();
-  pdl_launch_dependents();
   const int pair = blockIdx.x / per_pair, b = pair / p.H_kv, kvh = pair - b * p.H_kv;
   const int r0 = (blockIdx.x - pair * per_pair) * (kWarpsPerCta * kFewRows) + warp * kFewRows;
+  if (p.wait_first) {
+    // Towards L2 while the kernel in front runs on (whatever is written there meanwhile, L2 has it): a lane half a row of
+    // K or V.  (16 requests, 8 candidates over a window of 8192 tokens: a round 95.4 -> 94.2 us.)
+    const int u = lane >> 1 & 7, c = (lane & 1) * (D / 2);
+    const __nv_bfloat16* at = lane < 16 ? p.K + b * p.k_sb + kvh * p.k_sh + u * p.k_st : p.V + b * p.v_sb + kvh * p.v_sh + u * p.v_st;
+    if (r0 < R && u < p.T_loc) asm volatile("prefetch.global.L2 [%0];" ::"l"(at + c));
+    pdl_wait_prior();
+  }
+  pdl_launch_dependents();
   auto load_row = [&](const __nv_bfloat16* ptr, float (&v)[CPL]) {  // this lane's elements as floats
 #pragma unroll
     for (int c = 0; c < CPL; c += 4) {
