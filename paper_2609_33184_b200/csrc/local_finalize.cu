@@ -176,11 +176,21 @@ __global__ void __launch_bounds__(kWarpsPerCta * 32) local_few_kernel(const Loca
   const int R = p.G * p.T_q, per_pair = (R + kWarpsPerCta * kFewRows - 1) / (kWarpsPerCta * kFewRows);
   const int pair = blockIdx.x / per_pair, b = pair / p.H_kv, kvh = pair - b * p.H_kv;
   const int r0 = (blockIdx.x - pair * per_pair) * (kWarpsPerCta * kFewRows) + warp * kFewRows;
+  const __nv_bfloat16 *q_at[kFewRows], *k_at = p.K + b * p.k_sb + kvh * p.k_sh, *v_at = p.V + b * p.v_sb + kvh * p.v_sh;
+  const uint64_t* bits_at[kFewRows];
+  int last[kFewRows];
+#pragma unroll
+  for (int n = 0; n < kFewRows; ++n) {
+    const int r = min(r0 + n, R - 1), g = (int)((unsigned)r / (unsigned)p.T_q), i = r - g * p.T_q;
+    q_at[n] = p.Q + b * p.q_sb + (int64_t)(kvh * p.G + g) * p.q_sh + i * p.q_st + lane * CPL;
+    bits_at[n] = p.mask_bits ? p.mask_bits + ((int64_t)b * p.T_q + i) * p.mask_words : nullptr;
+    last[n] = i + (p.T_loc - p.T_q);
+  }
   if (p.wait_first) {
     // Towards L2 while the kernel in front runs on (whatever is written there meanwhile, L2 has it): a lane half a row of
     // K or V.  (16 requests, 8 candidates over a window of 8192 tokens: a round 95.4 -> 94.2 us.)
     const int u = lane >> 1 & 7, c = (lane & 1) * (D / 2);
-    const __nv_bfloat16* at = lane < 16 ? p.K + b * p.k_sb + kvh * p.k_sh + u * p.k_st : p.V + b * p.v_sb + kvh * p.v_sh + u * p.v_st;
+    const __nv_bfloat16* at = lane < 16 ? k_at + u * p.k_st : v_at + u * p.v_st;
     if (r0 < R && u < p.T_loc) asm volatile("prefetch.global.L2 [%0];" ::"l"(at + c));
     pdl_wait_prior();
   }
@@ -206,18 +216,16 @@ __global__ void __launch_bounds__(kWarpsPerCta * 32) local_few_kernel(const Loca
     unsigned vis[kFewRows];
 #pragma unroll
     for (int n = 0; n < kFewRows; ++n) {
-      const int r = min(r0 + n, R - 1), i = r % p.T_q, h = kvh * p.G + r / p.T_q;
-      load_row(p.Q + b * p.q_sb + (int64_t)h * p.q_sh + i * p.q_st + lane * CPL, q[n]);
-      const uint64_t* bits = p.mask_bits ? p.mask_bits + ((int64_t)b * p.T_q + i) * p.mask_words : nullptr;
-      vis[n] = (unsigned)visible_word(bits, 0, i + (p.T_loc - p.T_q), p.T_loc);
+      load_row(q_at[n], q[n]);
+      vis[n] = (unsigned)visible_word(bits_at[n], 0, last[n], p.T_loc);
     }
 #pragma unroll
     for (int u = 0; u < kFewKeys; ++u) {
 #pragma unroll
       for (int c = 0; c < CPL; ++c) k[u][c] = v[u][c] = 0.f;
       if (u < p.T_loc) {
-        load_row(p.K + b * p.k_sb + kvh * p.k_sh + u * p.k_st + lane * CPL, k[u]);
-        load_row(p.V + b * p.v_sb + kvh * p.v_sh + u * p.v_st + lane * CPL, v[u]);
+        load_row(k_at + u * p.k_st + lane * CPL, k[u]);
+        load_row(v_at + u * p.v_st + lane * CPL, v[u]);
       }
     }
     const int key = (lane & 16 ? 4 : 0) + (lane & 8 ? 2 : 0) + (lane & 4 ? 1 : 0);  // the key whose score this lane gets
