@@ -1373,10 +1373,11 @@ static int granule_log2(const ss::View8& kv) {
 
 // How a window's units meet CTAs (kv8.cuh): the form whose estimated time is least.  `tiles`: most tiles of a unit.  A
 // tile takes a CTA `one` us when little else runs (the latency of its copies and steps; small granules mean more
-// copies, rows more steps), and all CTAs together what memory gives; joining in a cluster takes 0.3 us, walking from unit to unit 1 us,
-// joining by another kernel 3.1 us and more for many states or rows.  Clusters of other sizes than 1, 2, 4 or 8 leave
-// places of a GPC empty (96 clusters of 3 ran as two rounds: 19.3 us against 12.2 with 96 of 2), so those are taken up
-// to half the CTAs only.
+// copies, rows more steps), and all CTAs together what memory gives; joining in a cluster takes 0.3 us, for one CTA with more than 8 rows
+// (whose state goes through shared memory all the same) 2, walking from unit to unit 1 us and more where some CTAs have one unit more than
+// the others, joining by another kernel 3.1 us and more for many states or rows.  All clusters have to be resident at once (96 of
+// 3 ran as two rounds: 19.3 us against 12.2 with 96 of 2).  Those of 2 fill the GPU (144 of 2 48.9 us, of 1 54.1, cut 51.8), larger
+// ones leave places of a GPC empty (the device holds 93 of 3, 71 of 4, 45 of 6, 33 of 8), so they are taken up to 7/8 of the CTAs.
 // Measured, head dim 128, 4 rows: 128 units of 33 tiles in pages of 16 clusters of one 65 us, of two 45.6, cut 47.9; one
 // unit of 33 tiles clusters of eight 11.0, cut 9.4, of 17 tiles 8.5 and 9.3; 384 units of 32 rows, head dim 64, two
 // tiles: whole 18.6, cut 22.4.
@@ -1388,14 +1389,15 @@ static void window_mode(ss::Attn8Params* p, int bits, int64_t tiles) {
   const auto tile_us = [&](int64_t ctas) { return pow(pow(one, 4) + pow(share * ctas, 4), 0.25); };
   const int64_t full = U / N, rest = U % N, steps = (U * tiles + N - 1) / N;
   const double rows = (double)p->B * p->H_kv * p->R;
-  const double whole = tiles * (full * tile_us(N) + (rest ? tile_us(rest) : 0.0)) + 1.0;
+  const double whole = tiles * (full * tile_us(N) + (rest ? tile_us(rest) + (full ? 0.25 * (N - rest) / N : 0.0) : 0.0)) + 1.0;
   const double cut = steps * tile_us(N < U * tiles ? N : U * tiles) + 3.1 + (rows <= 3 * ss::kNumSM ? 0.02 : 0.08) * tiles / steps + rows / 3500;
-  int64_t c = N * 9 / 10 / U;
+  int64_t c = N * 7 / 8 / U;
+  if (c < 2 && U <= N) c = 2 * U <= N - 8 ? 2 : 1;
   if (c > tiles) c = tiles;
   if (c > ss::kMostCluster8) c = ss::kMostCluster8;
-  if (U * c > N / 2) c = c >= 8 ? 8 : c >= 4 ? 4 : c >= 2 ? 2 : 1;
-  if (c < 1 && U <= N) c = 1;
-  const double cluster = c < 1 ? 1e30 : (tiles + c - 1) / c * tile_us(U * c) + (c > 1 ? 0.3 : 0.0);
+  // (no more of them than the longest part needs: 9 tiles by 5 CTAs 7.2 us, by 8 8.2)
+  if (c > 1) c = (tiles + (tiles + c - 1) / c - 1) / ((tiles + c - 1) / c);
+  const double cluster = c < 1 ? 1e30 : (tiles + c - 1) / c * tile_us(U * c) + (c > 1 ? 0.3 : p->rows_per_tile > 8 ? 2.0 : 0.0);
   p->mode = cluster <= whole && cluster <= cut ? ss::kCluster8 : whole <= cut ? ss::kWhole8 : ss::kCut8;
   p->cluster = (int)c;
 }
@@ -1461,10 +1463,11 @@ static ss_status attn8(ss_ctx* c, int bits, const ss_tensor& Q, int32_t B, int32
     p->before = p->O ? T_q : 0;
     p->depth = win.depth;
   }
-  // the most tokens and tiles that are walked of a request (a window: granules at its ends)
+  // the most tokens and tiles that are walked of a request (a window: what all queries see, in granules)
   const int64_t seen = (int64_t)win.window + win.sinks + T_q, room = p->kv.room;
   const int64_t tokens = win.window && seen < room ? seen : room;
-  const int64_t walked = win.window && seen + 2 * 32 < room ? seen + 2 * 32 : room;
+  const int64_t up = (1 << p->gran_log2) - 1, wide = ((win.sinks + up) & ~up) + (int64_t)win.window + T_q - 1 + up;
+  const int64_t walked = win.window && wide < room ? wide : room;
   const int64_t most_tiles = (walked + ss::kTok8 - 1) / ss::kTok8;
   const int most = !tc ? ss::kMinRows8 : win.window ? window_rows(bits, (int64_t)B * p->H_kv, p->R, walked) : ss::kRows8;
   p->row_tiles = (p->R + most - 1) / most;  // units of `most` rows at most, evenly spread
