@@ -1405,13 +1405,14 @@ static void window_mode(ss::Attn8Params* p, int bits, int64_t tiles) {
 // Most rows of a window's unit.  A tile takes a CTA less time with fewer rows (a latency of steps, not of memory), but all
 // of a unit's rows read K and V once, and every unit again (out of L2).  So units of 8 or 16 rows are formed while each
 // still has an SM to itself and what an SM reads stays short.
-// Measured, head dim 128, groups of 4, with 32 / 16 / 8 rows in us: 8 heads, 24 rows over a window of 128, bf16 8.6 / 7.5 /
-// 7.4; of 1000 11.4 / 10.9 / 12.8, 8 bits 11.7 / 10.0 / 10.0; of 4000 14.8 / 18.3 / 26.4 and 14.5 / 14.6 / 20.8; 1 head,
-// 8 positions over 128, bf16 8.5 / 6.9 / 5.8, 8 bits 8.7 / 6.9 / 5.4; 64 heads over 128 9.4 / 8.5 / 9.9 and 9.7 / 8.2 / 8.8.
+// Measured, head dim 128, groups of 4, with 32 / 16 / 8 rows in us: 8 heads, 24 positions over a window of 128, bf16 8.5 /
+// 7.3 / 7.4; of 1000 10.6 / 9.3 / 12.8, 8 bits 10.9 / 9.4 / 9.9; of 4000 14.7 / 16.9 / 26.3 and 14.4 / 13.9 / 20.7; 1 head,
+// 8 positions over 128, bf16 8.0 / 6.7 / 5.8, 8 bits 8.1 / 6.7 / 5.2; 64 heads over 128 9.4 / 8.6 / 10.0 and 9.7 / 8.2 /
+// 8.8, over 1000 15.0 / 15.6 / 20.4 and 14.0 / 12.2 / 14.5.
 static int window_rows(int bits, int64_t heads, int R, int64_t walked) {
   for (int most = ss::kMinRows8; most < ss::kRows8; most *= 2) {
     const int64_t units = heads * ((R + most - 1) / most);
-    const int tokens = bits == 8 ? 900 : most == 8 ? 160 : 700;  // that an SM's unit reads, on average over the SMs
+    const int tokens = most == 8 ? (bits == 8 ? 900 : 160) : (bits == 8 ? 1000 : 700);  // that an SM's unit reads, on average over the SMs
     if (units <= ss::kNumSM && units * walked <= (int64_t)tokens * ss::kNumSM) return most;
   }
   return ss::kRows8;
