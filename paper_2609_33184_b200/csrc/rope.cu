@@ -3,7 +3,7 @@
 // Pair i of a row at position p turns by p * f_i, which for far positions is thousands of revolutions: as an
 // fp32 product (24 bits) the angle of the fastest pair is off by 2^-7 at p = 2^17.  f_i is held as revolutions
 // in units of 2^-64 instead (ss_rope_init), so p * f_i is one integer product whose overflow drops the whole
-// revolutions, off by at most 2^-65 * |p| <= 2^-34 revolutions; the upper 32 bits go to sincospi.  Values are
+// revolutions, off by at most 2^-65 * |p| <= 2^-34 revolutions; sine and cosine come from the upper 32 bits.  Values are
 // turned in fp32 and rounded once, to bf16.  8 bits: the codes are those of the rounded bf16 rows, so a row is
 // the same bits as rotated and then written with ss_kv8_write.
 //
@@ -21,7 +21,7 @@ namespace {
 constexpr int kThreads = 128;
 
 // A block takes 2^shift consecutive tokens of a request and `heads` rows of Q, of K or of V (q_blocks and twice
-// kv_blocks of them): `lanes` rows side by side, one after the other beyond.
+// kv_blocks of them): `lanes` rows side by side, one after the other beyond.  JOINT: all rows of its tokens.
 struct Plan {
   int shift, lanes, heads;
   int token_blocks, q_blocks, kv_blocks, head_blocks;
@@ -32,6 +32,20 @@ __device__ __forceinline__ float hi_f(uint32_t two) { return __uint_as_float(two
 __device__ __forceinline__ uint32_t pack(float lo, float hi) {
   const __nv_bfloat162 o = __floats2bfloat162_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&o);
+}
+
+// Sine and cosine of t / 2^32 revolutions.  The nearest quarter is taken off in the integer (exact) and |x| <= pi / 4 is
+// left, where the Taylor series to x^9 and x^8 are off by 2^-29 and 2^-25; x is rounded twice (2^-24 at most).  (sincospif
+// and the registers it asked for: 187 us against 186 for a batch of prompts, 124 against 107 for the same with 5 heads.)
+__device__ __forceinline__ void sincos_turn(int32_t t, float* s, float* c) {
+  const uint32_t quarter = ((uint32_t)t + 0x20000000u) >> 30;
+  const float x = (float)(int32_t)((uint32_t)t - (quarter << 30)) * 1.46291807926715968105e-9f;  // 2 pi / 2^32
+  const float y = x * x;
+  const float a = fmaf(x * y, fmaf(y, fmaf(y, fmaf(y, 1.f / 362880.f, -1.f / 5040.f), 1.f / 120.f), -1.f / 6.f), x);
+  const float b = fmaf(y, fmaf(y, fmaf(y, fmaf(y, 1.f / 40320.f, -1.f / 720.f), 1.f / 24.f), -0.5f), 1.f);
+  const float u = quarter & 1 ? b : a, v = quarter & 1 ? a : b;
+  *s = __uint_as_float(__float_as_uint(u) ^ ((quarter & 2) << 30));
+  *c = __uint_as_float(__float_as_uint(v) ^ ((quarter + 1 & 2) << 30));
 }
 
 // The sines of a thread's 8 pairs.
@@ -92,10 +106,10 @@ __device__ __forceinline__ uint2 codes_of(const uint4& raw, float inv) {
   return make_uint2(c[0] | (c[1] << 16), c[2] | (c[3] << 16));
 }
 
-// BITS of the cache (0: rows go to Qo, Ko); U rows in flight per thread.  Into 8 bits the compiler is held to 64
-// registers (72 otherwise: 178.6 us against 176.2 for 49,000 tokens of 48 rows).
-template <int D, int BITS, bool INTER, int U>
-__global__ void __launch_bounds__(kThreads, BITS == 8 ? 8 : 1) rope_kernel(const __grid_constant__ RopeParams p, const Plan plan) {
+// BITS of the cache (0: rows go to Qo, Ko); U rows in flight per thread.  The compiler is held to 64, 72 or 80 registers
+// (left alone it works out all sines side by side in 96 to 104: 194 us against 186 for a batch of prompts).
+template <int D, int BITS, bool INTER, int U, bool JOINT>
+__global__ void __launch_bounds__(kThreads, JOINT || BITS == 8 ? 8 : U == 4 ? 6 : 7) rope_kernel(const __grid_constant__ RopeParams p, const Plan plan) {
   constexpr int LPR = D / 16;
   __shared__ uint64_t freq_s[kRopePairs];
   __shared__ uint8_t axis_s[kRopePairs];
@@ -120,9 +134,9 @@ __global__ void __launch_bounds__(kThreads, BITS == 8 ? 8 : 1) rope_kernel(const
   const int slot = tid / LPR, part = tid % LPR, head = slot >> plan.shift;  // (of the heads side by side)
   const int k = (tb << plan.shift) + (slot & ((1 << plan.shift) - 1));       // row of the call
   if ((tb << plan.shift) >= n) return;
-  const bool is_q = hb < plan.q_blocks, is_v = hb >= plan.q_blocks + plan.kv_blocks;
+  const bool is_q = !JOINT && hb < plan.q_blocks, is_v = !JOINT && hb >= plan.q_blocks + plan.kv_blocks;
   const int from = (is_q ? hb : is_v ? hb - plan.q_blocks - plan.kv_blocks : hb - plan.q_blocks) * plan.heads;
-  const int to = min(from + plan.heads, is_q ? p.H_q : p.H_kv);               // the block's heads
+  const int to = JOINT ? p.H_q + (BITS ? 2 : 1) * p.H_kv : min(from + plan.heads, is_q ? p.H_q : p.H_kv);  // the block's heads
   const int64_t off = p.off ? (int64_t)p.off[b] : 0, tok = off + k;
 
   // the input row
@@ -153,14 +167,20 @@ __global__ void __launch_bounds__(kThreads, BITS == 8 ? 8 : 1) rope_kernel(const
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       raw[u][0] = raw[u][1] = make_uint4(0, 0, 0, 0);
+      if (JOINT) {
+        const int h = h0 + u, k = h - p.H_q, v = k - p.H_kv;
+        at = h < p.H_q ? p.Q + b * p.q_sb + src * p.q_st + h * p.q_sh
+             : v < 0   ? p.K + b * p.k_sb + src * p.k_st + k * p.k_sh
+                       : p.V + b * p.v_sb + src * p.v_st + v * p.v_sh;
+      }
       if (live && h0 + u * plan.lanes < to) {
         raw[u][0] = __ldcs(reinterpret_cast<const uint4*>(at + at0));
         raw[u][1] = __ldcs(reinterpret_cast<const uint4*>(at + at1));
       }
-      at += step;
+      if (!JOINT) at += step;
     }
   };
-  load(from + head);
+  load(JOINT ? 0 : from + head);
 
   // (cache) the token's place
   bool store = live;
@@ -195,7 +215,7 @@ __global__ void __launch_bounds__(kThreads, BITS == 8 ? 8 : 1) rope_kernel(const
       const int a = axis_s[pair];
       const int64_t at = a == 0 ? pos[0] : a == 1 ? pos[1] : a == 2 ? pos[2] : pos[3];
       const uint64_t turns = freq_s[pair] * (uint64_t)at;                // whole revolutions overflow
-      sincospif((float)(int32_t)(turns >> 32) * 0x1p-31f, &t.s[j], &t.c[j]);
+      sincos_turn((int32_t)(turns >> 32), &t.s[j], &t.c[j]);
       t.s[j] *= p.rope.magnitude;
       t.c[j] *= p.rope.magnitude;
     }
@@ -244,7 +264,30 @@ __global__ void __launch_bounds__(kThreads, BITS == 8 ? 8 : 1) rope_kernel(const
       }
     };
   };
-  if (is_q) {
+  if (JOINT) {
+    const auto put_q = to_rows(p.Qo + b * p.qo_sb + src * p.qo_st, p.qo_sh);
+    const auto put_k = to_rows(p.Ko + b * p.ko_sb + src * p.ko_st, p.ko_sh);
+    const auto put_k8 = to_cache(p.kv.K + outer * p.kv.k_sb + inner * p.kv.k_st, p.kv.k_sh,
+                                 p.kv.Ks + outer * p.kv.ks_sb + inner * p.kv.ks_st, p.kv.ks_sh);
+    const auto put_v8 = to_cache(p.kv.V + outer * p.kv.v_sb + inner * p.kv.v_st, p.kv.v_sh,
+                                 p.kv.Vs + outer * p.kv.vs_sb + inner * p.kv.vs_st, p.kv.vs_sh);
+#pragma unroll 1
+    for (int h0 = 0;;) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int h = h0 + u, k = h - p.H_q, v = k - p.H_kv;
+        if (h >= to) break;
+        if (v < 0 && turning) turn_row<INTER>(raw[u], t);
+        if (k < 0) put_q(h, live, raw[u]);
+        else if (BITS == 0) put_k(k, live, raw[u]);
+        else if (v < 0) put_k8(k, store, raw[u]);
+        else put_v8(v, store, raw[u]);
+      }
+      h0 += U;
+      if (h0 >= to) break;
+      load(h0);
+    }
+  } else if (is_q) {
     rows(turning, live, to_rows(p.Qo + b * p.qo_sb + src * p.qo_st, p.qo_sh));
   } else if (BITS == 0) {
     rows(turning, live, to_rows(p.Ko + b * p.ko_sb + src * p.ko_st, p.ko_sh));
@@ -257,7 +300,7 @@ __global__ void __launch_bounds__(kThreads, BITS == 8 ? 8 : 1) rope_kernel(const
   }
 }
 
-template <int D, int BITS, bool INTER, int U>
+template <int D, int BITS, bool INTER, int U, bool JOINT = false>
 cudaError_t launch_rows(const RopeParams& p, int heads, cudaStream_t s, bool pdl) {
   constexpr int kSlots = kThreads * 16 / D;
   Plan plan = {};
@@ -267,12 +310,12 @@ cudaError_t launch_rows(const RopeParams& p, int heads, cudaStream_t s, bool pdl
   plan.token_blocks = (p.T + (1 << plan.shift) - 1) >> plan.shift;
   plan.q_blocks = (p.H_q + plan.heads - 1) / plan.heads;
   plan.kv_blocks = (p.H_kv + plan.heads - 1) / plan.heads;
-  plan.head_blocks = plan.q_blocks + (BITS ? 2 : 1) * plan.kv_blocks;
+  plan.head_blocks = JOINT ? 1 : plan.q_blocks + (BITS ? 2 : 1) * plan.kv_blocks;
   const dim3 grid((unsigned)plan.token_blocks * plan.head_blocks * p.B);  // below 2^31: see the caller
-  return launch_kernel(rope_kernel<D, BITS, INTER, U>, grid, dim3(kThreads), 0, s, pdl, p, plan);
+  return launch_kernel(rope_kernel<D, BITS, INTER, U, JOINT>, grid, dim3(kThreads), 0, s, pdl, p, plan);
 }
-template <int D, int BITS>
-cudaError_t launch_bits(const RopeParams& p, cudaStream_t s, bool pdl) {
+template <int D, int BITS, bool INTER>
+cudaError_t launch_layout(const RopeParams& p, cudaStream_t s, bool pdl) {
   const int all = p.H_q + p.H_kv + (BITS ? p.H_kv : 0);
   // large: more rows than 8 blocks per SM would take, a row a thread.  There a thread turns 8 rows with its sines, 4 in
   // flight (2 into 8 bits, whose conversions want the registers: 66 -> 59 us for 49,000 tokens of 8 heads); 4 rows
@@ -280,9 +323,16 @@ cudaError_t launch_bits(const RopeParams& p, cudaStream_t s, bool pdl) {
   // calls take two rows a thread (one: 4.9 us against 2.9 for 256 tokens of 48 rows, as much for less).
   const bool large = (int64_t)p.B * p.T * all > (int64_t)8 * kNumSM * kThreads * 16 / D;
   constexpr int kU = BITS == 8 ? 2 : 4;
-  if (p.rope.interleaved)
-    return large ? launch_rows<D, BITS, true, kU>(p, 8, s, pdl) : launch_rows<D, BITS, true, 2>(p, 2, s, pdl);
-  return large ? launch_rows<D, BITS, false, kU>(p, 8, s, pdl) : launch_rows<D, BITS, false, 2>(p, 2, s, pdl);
+  // Few heads (a GPU's part of a model's): a token's rows in one block, or its sines and its start would be paid for two or
+  // three blocks (6 x 9000 tokens, 2 + 1 heads, rows into bf16 38.4 -> 22.2 us, 4 + 1 41.5 -> 30.1, 6 + 1 48.0 -> 38.3, K and V
+  // of 4 35.3 and 37.2; into 8 bits 2 + 1 33.9 -> 24.2, 4 + 1 37.7 -> 31.9, 8 + 1 47.1 and 49.6, K and V of 4 35.5 and 38.9).
+  const int few = BITS == 8 || !p.H_q ? 6 : 8;
+  if (large && all <= few && p.T >= kThreads * 16 / D) return launch_rows<D, BITS, INTER, 2, true>(p, all, s, pdl);
+  return large ? launch_rows<D, BITS, INTER, kU>(p, 8, s, pdl) : launch_rows<D, BITS, INTER, 2>(p, 2, s, pdl);
+}
+template <int D, int BITS>
+cudaError_t launch_bits(const RopeParams& p, cudaStream_t s, bool pdl) {
+  return p.rope.interleaved ? launch_layout<D, BITS, true>(p, s, pdl) : launch_layout<D, BITS, false>(p, s, pdl);
 }
 template <int D>
 cudaError_t launch_dim(const RopeParams& p, cudaStream_t s, bool pdl) {

@@ -374,3 +374,58 @@ def test_captured_on_another_stream():
                 assert torch.equal(x, y)
     assert ctx.ss_poll_status(stream) == (0, 0)
     ctx.close()
+
+
+@pytest.mark.parametrize("d,H_q,H_kv,rot,inter,axes", [(128, 4, 1, 128, False, 1), (64, 3, 1, 32, True, 3), (128, 8, 2, 64, False, 2), (64, 2, 2, 64, True, 1)])
+@pytest.mark.parametrize("bits,listed", [(0, False), (16, False), (16, True), (8, False), (8, True)])
+def test_a_large_call_is_many_small_ones(bits, listed, d, H_q, H_kv, rot, inter, axes):
+    """The same bits, whichever way rows are dealt to threads; ragged, with and without Q, rows in order and by a list."""
+    ssb = _ssb()
+    B, T, piece = 3, 4007, 200
+    g = _gen(d + H_q + bits)
+    Q, K, V = (_rows(g, (B, h, T, d), "bthd") for h in (H_q, H_kv, H_kv))
+    freq, axis = _freq(rot, axes)
+    rope = ssb.Rope(freq, axis, axes, inter, 1.25)
+    pos = _positions(g, axes, B, T, True)
+    cnt, off = torch.tensor([T, 1300, T - 7], dtype=torch.int32), torch.tensor([0, 100, 5], dtype=torch.int32)
+    idx = torch.stack([torch.randperm(T, generator=g) for _ in range(B)]) if listed else None
+    ctx = ssb.Context(B, H_q, H_kv, d, 1, 1, 8)
+    caches = [None, None]
+    if bits == 16:
+        caches = [_cache16(ssb, B, H_kv, d, 16, 4128, 3) for _ in range(2)]
+    elif bits == 8:
+        table = torch.arange(3 * 258, dtype=torch.int32, device=DEV).view(3, 258)
+        caches = [ssb.Cache8.empty(3 * 258, H_kv, 16, d, table) for _ in range(2)]
+
+    def call(cache, Q, K, V, Qo, Ko, pos, off, cnt, idx):
+        pos, off, cnt = (x.contiguous().to(DEV) for x in (pos, off, cnt))
+        if cache is None:
+            ctx.ss_rope_rotate(rope, Q, K, Qo, Ko, pos, row_cnt=cnt)
+        else:
+            idx = None if idx is None else idx.to(torch.int32).to(DEV)
+            (ctx.ss_kv8_append if bits == 8 else ctx.ss_kv_append)(cache, K, V, rope, pos, Q, Qo, off, cnt, idx)
+
+    outs = [(None if listed else torch.full_like(Q, 7.0), torch.full_like(K, 7.0)) for _ in range(2)]
+    call(caches[0], None if listed else Q, K, V, *outs[0], pos, off, cnt, idx)
+    if listed:   # the listed rows, in order
+        rows = idx.to(DEV)[:, None, :, None].expand(B, H_kv, T, d)
+        K, V = K.gather(2, rows), V.gather(2, rows)
+        pos = pos.gather(2, idx[None].expand(axes, B, T))
+    for s in range(0, T, piece):
+        e = min(s + piece, T)
+        cut = lambda x: None if x is None else x[:, :, s:e]
+        call(caches[1], None if listed else cut(Q), cut(K), cut(V), cut(outs[1][0]), cut(outs[1][1]), cut(pos), off + s,
+             (cnt - s).clamp(0, e - s), None)
+    assert ctx.ss_poll_status() == (0, 0)
+    for x, y in zip(outs[0], outs[1]):
+        assert x is None or torch.equal(x, y)
+    if bits:
+        for x, y in zip(caches[0].tensors, caches[1].tensors):
+            assert torch.equal(x, y)
+    if not listed:
+        for b in range(B):
+            n = int(cnt[b])
+            some = torch.randperm(n, generator=g)[:50].numpy()
+            want, size = _want(Q[b].cpu()[:, some], b, _at(pos, None, axis, b, some), freq, inter, 1.25)
+            _close(outs[0][0][b].cpu()[:, some], want, size)
+    ctx.close()
