@@ -76,8 +76,9 @@ __device__ __forceinline__ void row_states8(const Attn8Params& p, Row8& w, int l
 // In a round: from what the attention kernel has left in the row's state.
 __device__ __forceinline__ void row_states8(const Attn8Params& p, Row8& w, float2 st) {
   if (!(st.y < 0.f)) return;
-  const uint32_t slot = (uint32_t)st.x;
-  w.n = (int)-st.y;
+  // (what an aborted launch leaves may be an older call's: inside the scratch area all the same)
+  const uint32_t slot = min((uint32_t)st.x, 2 * (uint32_t)p.shares * p.row_tiles - 1);
+  w.n = min((int)-st.y, p.shares - (int)(slot / (2 * (uint32_t)p.row_tiles)));
   w.first = slot_at8(p, slot);
   w.rest = slot_at8(p, 2 * (slot / 2 + p.row_tiles));
 }
