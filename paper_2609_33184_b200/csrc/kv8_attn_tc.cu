@@ -302,8 +302,8 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
     };
     int it0 = 0, seg = 0;  // tiles and segments before this one
     bool ok = true;
-    Seg8 g;
-    for (bool more = seg_first(share, &g); more && ok; more = seg_next(share, &g), ++seg) {
+    Seg8 g = ctl->seg[0];
+    for (bool more = ctl->has[0]; more && ok; more = seg_next(share, &g), ++seg) {
       const int n = g.t1 - g.t0;
       int qi = 0, pi = 0;
       bool q_there = false;
@@ -607,13 +607,18 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
         if ((WIN && first) || bar_or8<SOFT>(first || mx > kOver || missing)) {
           // ---- set the references to the exact maxima; later in a segment (rare) raise them, which
           // rescales O^T and the row sums ----
-          float mine = -INFINITY;
+          if constexpr (WIN) {
+            const float mine = rows_max<NQ, NR>(x);  // of row lane / (32 / NQ)
+            if (lane % (32 / NQ) == 0) ctl->smax[warp][lane / (32 / NQ)] = mine;
+          } else {
+            float mine = -INFINITY;
 #pragma unroll
-          for (int r = 0; r < NR; ++r) {
-            const float m = redux_max(r & 1 ? x[r / 2].y : x[r / 2].x);
-            if (lane == r) mine = m;
+            for (int r = 0; r < NR; ++r) {
+              const float m = redux_max(r & 1 ? x[r / 2].y : x[r / 2].x);
+              if (lane == r) mine = m;
+            }
+            if (lane < NR) ctl->smax[warp][lane] = mine;
           }
-          if (lane < NR) ctl->smax[warp][lane] = mine;
           bar8<SOFT>();
           if (tid < NR) {  // M rises by this much (in the first tile, from 0 to the maximum - bias)
             const float top = fmaxf(fmaxf(ctl->smax[0][tid], ctl->smax[1][tid]), fmaxf(ctl->smax[2][tid], ctl->smax[3][tid]));

@@ -38,22 +38,23 @@ __device__ __forceinline__ void wait8(uint64_t* bar, uint32_t parity, volatile u
   __syncwarp();
 }
 
-// Maxima over a warp's lanes of NR values each, halving the rows a lane holds at every step: lane's result is row
-// lane / (32 / NR)'s.  (With a redux for each of 32 rows a first tile's references took 2,000 cycles instead of 1,750.)
-template <int NR>
-__device__ __forceinline__ float rows_max(const float2 (&x)[NR / 2]) {
+// Maxima over a warp's lanes of ROWS values each, halving the rows a lane holds (of N, a power of two) at every step:
+// lane's result is row lane / (32 / N)'s.  (With a redux for each of 32 rows a first tile's references took 2,000 cycles
+// instead of 1,750.)
+template <int N, int ROWS>
+__device__ __forceinline__ float rows_max(const float2 (&x)[ROWS / 2]) {
   const int lane = threadIdx.x & 31;
-  float v[NR];
+  float v[N];
 #pragma unroll
-  for (int r = 0; r < NR; ++r) v[r] = r & 1 ? x[r / 2].y : x[r / 2].x;
-  int n = NR;
+  for (int r = 0; r < N; ++r) v[r] = r >= ROWS ? -INFINITY : r & 1 ? x[r / 2 % (ROWS / 2)].y : x[r / 2 % (ROWS / 2)].x;
+  int n = N;
 #pragma unroll
   for (int o = 16; o; o >>= 1) {
     if (n > 1) {
       n /= 2;
       const bool up = lane & o;
 #pragma unroll
-      for (int i = 0; i < NR / 2; ++i) {
+      for (int i = 0; i < N / 2; ++i) {
         if (i < n) {
           const float send = up ? v[i] : v[i + n], keep = up ? v[i + n] : v[i];
           v[i] = fmaxf(keep, __shfl_xor_sync(0xffffffffu, send, o));

@@ -409,7 +409,7 @@ window_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ 
             wait(&ctl->pfree, (it - 1) & 1);  // the output MMAs of the tile before have retired
             tc_fence_after();
           }
-          const float mine = rows_max<NR>(x);  // of row lane / (32 / NR)
+          const float mine = rows_max<NR, NR>(x);  // of row lane / (32 / NR)
           if (lane % (32 / NR) == 0) smax[warp * NR + lane / (32 / NR)] = mine;
           bar8<SOFT>();
           if (warp == 0) {  // M rises by this much (from 0 to the maximum where there was none)
