@@ -8,7 +8,7 @@
 // by granule and runs ahead across segment ends, an MMA issuer warp, 4 softmax warps whose thread is a key of the
 // tile in the scores and a head dim in the output; references M raised lazily (exact maximum of the first tile,
 // later when a score exceeds M by 16 in base 2), row sums in fp32 from unrounded weights.  Weights go to the output
-// MMA as two bf16 terms side by side on the N axis (off by 2^-17), where shared memory has room for them: with up
+// MMA as two bf16 terms side by side on the N axis (off by 2^-16), where shared memory has room for them: with up
 // to 8 rows the second term takes the columns that N = 16 leaves idle; 17 to 32 rows at head dim 128 take one term
 // (off by 2^-8 at most, as in the chunk kernels), or the ring would lose one of its three units.
 //
