@@ -429,3 +429,45 @@ def test_a_large_call_is_many_small_ones(bits, listed, d, H_q, H_kv, rot, inter,
             want, size = _want(Q[b].cpu()[:, some], b, _at(pos, None, axis, b, some), freq, inter, 1.25)
             _close(outs[0][0][b].cpu()[:, some], want, size)
     ctx.close()
+
+
+@pytest.mark.parametrize("T", [1, 3, 11])
+@pytest.mark.parametrize("d,H_q,H_kv,bits", [(128, 16, 4, 16), (128, 16, 4, 8), (64, 40, 8, 0), (64, 4, 1, 8), (128, 3, 1, 16)])
+def test_many_requests_of_few_tokens(d, H_q, H_kv, bits, T):
+    """Enough requests for a large call, rows of several heads side by side in a block: the bits of calls of a few requests."""
+    ssb = _ssb()
+    B, room = 60 + 80000 * d // 64 // (H_q + 2 * H_kv) // T, 16
+    g = _gen(T + d)
+    Q, K, V = (_rows(g, (B, h, T, d)) for h in (H_q, H_kv, H_kv))
+    rope = ssb.Rope(*_freq(d, 2), 2, False)
+    pos = _positions(g, 2, B, T, True).to(DEV)
+    cnt, off = (torch.randint(0, top, (B,), generator=g, dtype=torch.int32).to(DEV) for top in (T + 1, room + 1 - T))
+    ctx = ssb.Context(B, H_q, H_kv, d, 1, 1, room)
+    kind = {16: ssb.Cache16, 8: ssb.Cache8}.get(bits)
+    caches = [kind.empty(B, H_kv, room, d) for _ in range(2)] if bits else [None, None]
+    outs = [(torch.full_like(Q, 7.0), torch.full_like(K, 7.0)) for _ in range(2)]
+
+    def call(cache, out, at):
+        Qs, Ks, Vs, Qo, Ko, ps = Q[at], K[at], V[at], out[0][at], out[1][at], pos[:, at].contiguous()
+        if not bits:
+            ctx.ss_rope_rotate(rope, Qs, Ks, Qo, Ko, ps, row_cnt=cnt[at])
+        else:
+            part = kind(*(x[at] for x in cache.tensors[:-1]))
+            (ctx.ss_kv8_append if bits == 8 else ctx.ss_kv_append)(part, Ks, Vs, rope, ps, Qs, Qo, off[at], cnt[at])
+
+    call(caches[0], outs[0], slice(0, B))
+    for s in range(0, B, B // 9):
+        call(caches[1], outs[1], slice(s, min(s + B // 9, B)))
+    assert ctx.ss_poll_status() == (0, 0)
+    for x, y in zip(outs[0], outs[1]):
+        assert torch.equal(x, y)
+    if bits:
+        for x, y in zip(caches[0].tensors[:-1], caches[1].tensors[:-1]):
+            assert torch.equal(x, y)
+    live = (torch.arange(T, device=DEV)[None] < cnt[:, None])[:, None, :, None].expand_as(Q)
+    assert (outs[0][0][~live] == 7.0).all()
+    b = int(cnt.argmax())
+    n = int(cnt[b])
+    if n:
+        _close(outs[0][0][b, :, :n].cpu(), *_want(Q[b].cpu()[:, :n], b, _at(pos.cpu(), None, _freq(d, 2)[1], b, np.arange(n)), _freq(d, 2)[0], False, 1.0))
+    ctx.close()
