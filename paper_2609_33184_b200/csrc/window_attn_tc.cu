@@ -34,7 +34,10 @@ struct alignas(16) CtlW {
   uint64_t sfull[2], pready, pfree, qfull, segfull;
   uint32_t tmem_base;
   volatile uint32_t abort;
-  int has[2];                     // the current and the next segment (in use by turns; the MMA warp finds the next)
+  // The current and the next segment, in use by turns.  The MMA warp writes the next one's slot behind a segment's first
+  // scores, that is once all softmax threads have arrived on qfull for that segment: from their arrival for segment k + 1
+  // on they read nothing of segment k's slot.
+  int has[2];
   int unset;                      // rows without a reference
   int go;                         // a segment follows
   Seg8 seg[2];
@@ -489,7 +492,7 @@ window_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ 
       }
 
       // ---- the segment's end: what the next one needs is fetched first ----
-      const Seg8& done = g;
+      const Seg8 done = g;  // (by value: its slot is the MMA warp's from q_store on)
       const int next = (k_seg + 1) & 1;
       if (!CL) {
         wait(&ctl->segfull, k_seg & 1);
