@@ -356,7 +356,7 @@ ss_status ss_decode8(ss_ctx* ctx, ss_tensor Q, int32_t B, int32_t T_q, float sca
  * magnitude * (x cos - y sin, x sin + y cos).  The first rot_dim elements of a row form rot_dim / 2 pairs -
  * elements i and i + rot_dim / 2, or 2 i and 2 i + 1 where `interleaved` - the others stay as they are.
  * With several axes (time, height and width of images and video) each pair has one axis and a token a
- * position on each.  The angle is off by less than 2^-23 at any int32 position; values are turned in
+ * position on each.  The angle is off by less than 2^-23 at any int32 position and frequency; values are turned in
  * fp32 and rounded once, to bf16. */
 typedef struct {
   int32_t rot_dim;     /* a multiple of 16                                              */
@@ -368,9 +368,9 @@ typedef struct {
 } ss_rope;
 
 /* Fills *out (host only): inv_freq [rot_dim / 2] are the pairs' angles per position in radians, axis
- * [rot_dim / 2] their axes (NULL: all 0).  SS_ERR_ARG for a null pointer, a frequency or magnitude that is not
- * finite or an axis outside [0, n_axes); SS_ERR_SHAPE for a rot_dim that is not a multiple of 16 in 16..128 or
- * n_axes outside 1..4. */
+ * [rot_dim / 2] their axes (NULL: all 0).  SS_ERR_ARG for a null pointer, a frequency of 2^64 or more (of either
+ * sign) or not finite, a magnitude that is not finite or an axis outside [0, n_axes); SS_ERR_SHAPE for a rot_dim
+ * that is not a multiple of 16 in 16..128 or n_axes outside 1..4. */
 ss_status ss_rope_init(ss_rope* out, int32_t rot_dim, int32_t interleaved, int32_t n_axes, const double* inv_freq,
                        const int32_t* axis, float magnitude);
 

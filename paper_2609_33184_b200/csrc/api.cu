@@ -1605,24 +1605,47 @@ ss_status ss_decode8_window(ss_ctx* c, ss_tensor Q, int32_t B, int32_t T_q, floa
 }
 
 // ---- rotary positions, rows that join a cache ----------------------------------------------------
+// Revolutions of f radians (|f| < 2^64), whole ones dropped, in units of 2^-64: the nearest unit.  The product of f's 53
+// bits and 1 / (2 pi) is formed in integers, so the whole revolutions of a high frequency cost no bits of the rest.
+static uint64_t turn_of(double f) {
+  static const uint64_t kTurns[3] = {0x36d8a5664f10e410, 0x7f09d5f47d4d3770, 0x28be60db9391054a};  // 2^192 / (2 pi), low word first
+  int e;
+  const uint64_t m = (uint64_t)ldexp(frexp(fabs(f), &e), 53);  // |f| = m 2^(e - 53)
+  uint64_t w[5] = {};                                          // m * kTurns, in units of 2^(e - 245) revolutions
+  unsigned __int128 carry = 0;
+  for (int i = 0; i < 3; ++i) {
+    carry += (unsigned __int128)m * kTurns[i];
+    w[i] = (uint64_t)carry;
+    carry >>= 64;
+  }
+  w[3] = (uint64_t)carry;
+  const int s = 181 - e;  // units of 2^-64 begin at bit s (117 and up: kTurns' last place is off by 2^(53 - s) units)
+  if (s > 245) return 0;  // the product has 243 bits: less than half a unit
+  const int half = s - 1;  // half a unit
+  uint64_t add = 1ull << (half & 63);
+  for (int i = half >> 6; i < 4 && add; ++i) {
+    w[i] += add;
+    add = w[i] < add ? 1 : 0;
+  }
+  const int i = s >> 6, b = s & 63;
+  const uint64_t units = b ? (w[i] >> b) | (w[i + 1] << (64 - b)) : w[i];
+  return f < 0 ? 0 - units : units;
+}
+
 ss_status ss_rope_init(ss_rope* out, int32_t rot_dim, int32_t interleaved, int32_t n_axes, const double* inv_freq,
                        const int32_t* axis, float magnitude) {
   if (!out || !inv_freq || !std::isfinite(magnitude)) return SS_ERR_ARG;
   if (rot_dim < 16 || rot_dim > 2 * ss::kRopePairs || rot_dim % 16 || n_axes < 1 || n_axes > ss::kRopeAxes)
     return SS_ERR_SHAPE;
   for (int i = 0; i < rot_dim / 2; ++i)
-    if (!std::isfinite(inv_freq[i]) || (axis && (axis[i] < 0 || axis[i] >= n_axes))) return SS_ERR_ARG;
+    if (!(fabs(inv_freq[i]) < 0x1p64) || (axis && (axis[i] < 0 || axis[i] >= n_axes))) return SS_ERR_ARG;
   memset(out, 0, sizeof(*out));
   out->rot_dim = rot_dim;
   out->n_axes = n_axes;
   out->interleaved = interleaved != 0;
   out->magnitude = magnitude;
   for (int i = 0; i < rot_dim / 2; ++i) {
-    // (long double: 64 bits of significand)
-    const long double turns = (long double)inv_freq[i] / 6.283185307179586476925286766559005768L;
-    const long double part = turns - floorl(turns);  // [0, 1]: a tiny negative one rounds to a whole revolution
-    const long double units = roundl(part * 18446744073709551616.0L);
-    out->turn[i] = units >= 18446744073709551616.0L ? 0 : (uint64_t)units;
+    out->turn[i] = turn_of(inv_freq[i]);
     out->axis[i] = axis ? (uint8_t)axis[i] : 0;
   }
   return SS_OK;
