@@ -68,7 +68,7 @@ typedef enum {
 #define SS_DEV_DST_OVERFLOW 4u  /* dst_off + k outside [0, cap): row skipped           */
 #define SS_DEV_WAIT_EXPIRED 8u  /* a bounded in-kernel wait gave up: round is invalid  */
 #define SS_DEV_BAD_PAGE 16u     /* page id outside the pool: its tokens read as zeros  */
-#define SS_DEV_BAD_DEPTH 32u    /* depth[b][t] outside [0, T_q): clamped               */
+#define SS_DEV_BAD_DEPTH 32u    /* depth[b][t] outside [0, T_q): clamped; no depth of 0 */
 
 typedef struct {
   int32_t max_B;      /* requests per call                                          */
@@ -433,8 +433,10 @@ ss_status ss_decode8_window(ss_ctx* ctx, ss_tensor Q, int32_t B, int32_t T_q, fl
                             int32_t window, int32_t sinks, const int32_t* valid_len, void* O, float* LSE, void* stream);
 
 /* The same as a chunk of the open round: its queries are candidates behind the cache, query t at position
- * valid_len[b] + depth[b][t] (device int32 [B, T_q], the depth of a tree's nodes, 0 for the first; outside
- * [0, T_q): clamped, SS_DEV_BAD_DEPTH; NULL = t, a chain).  The candidates' own keys go through ss_verify_local,
+ * valid_len[b] + depth[b][t] (device int32 [B, T_q], the depth of a tree's nodes; outside [0, T_q): clamped,
+ * SS_DEV_BAD_DEPTH; NULL = t, a chain).  Each request has a query of depth 0, wherever in its row: what the call leaves
+ * unread goes by position valid_len[b], and where no query stands there (SS_DEV_BAD_DEPTH too) tokens and pages that only
+ * it would see are read all the same, so what they hold matters.  The candidates' own keys go through ss_verify_local,
  * whose mask is the caller's: with a window below T_q it has to leave out what is further back than that.  May be
  * mixed with other chunks (their tokens are visible to every query). */
 ss_status ss_verify_chunk_window(ss_ctx* ctx, const ss_cache16* cache, int32_t window, int32_t sinks,

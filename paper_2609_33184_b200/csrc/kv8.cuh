@@ -144,6 +144,17 @@ __device__ __forceinline__ int depth8(const Attn8Params& p, int b, int t) {
   atomicOr(p.status, SS_DEV_BAD_DEPTH);
   return max(0, min(d, p.T_q - 1));
 }
+// Reports requests without a query at depth 0: what the walk leaves out goes by the first position.  By one whole warp of
+// every CTA, one that is done with its part.
+static __device__ __noinline__ void check_depths8(const Attn8Params& p) {
+#pragma unroll 1
+  for (int b = blockIdx.x; b < p.B; b += gridDim.x) {
+    bool some = false;
+#pragma unroll 1
+    for (int t = threadIdx.x & 31; t < p.T_q; t += 32) some |= p.depth[(int64_t)b * p.T_q + t] == 0;
+    if (!__any_sync(0xffffffffu, some) && (threadIdx.x & 31) == 0) atomicOr(p.status, SS_DEV_BAD_DEPTH);
+  }
+}
 // Tokens of a request as the kernels walk them.
 template <bool WIN = false>
 __device__ __forceinline__ int len8(const Attn8Params& p, int b) {

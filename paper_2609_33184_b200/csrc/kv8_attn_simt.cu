@@ -214,6 +214,7 @@ __global__ void __launch_bounds__(128) attn8_simt_kernel(const __grid_constant__
     }
   }
   if ((int)blockIdx.x < p.B) put_empty8<WIN>(p, tid, 128);
+  if (WIN && p.depth && warp == 0) check_depths8(p);
 }
 
 }  // namespace

@@ -281,6 +281,10 @@ attn8_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ C
         while (!mbar_try_wait(&ctl->ufull[i % UNITS], (i / UNITS) & 1) && gtime_ns() - t0 < kWaitNs) {
         }
     }
+    if constexpr (WIN) {
+      __syncwarp();
+      if (p.depth) check_depths8(p);
+    }
   } else if (warp == kMmaWarp) {
     // ===== MMA issuer: polls for whichever of its two next operations can go =====
     constexpr uint32_t idesc_qk = idesc8(NS, 0, false), idesc_pv = idesc8(NP, 1, true);

@@ -219,6 +219,8 @@ window_tc_kernel(const __grid_constant__ Attn8Params p, const __grid_constant__ 
         while (!mbar_try_wait(&ctl->ufull[i % UNITS], (i / UNITS) & 1) && gtime_ns() - t0 < kWaitNs) {
         }
     }
+    __syncwarp();
+    if (p.depth) check_depths8(p);
   } else if (warp == kMmaWarp) {
     // ===== MMA issuer: polls for whichever of its two next operations can go =====
     constexpr uint32_t idesc_qk = make_idesc_major(128, NQ, false, false), idesc_pv = make_idesc_major(128, C::NP, true, true);
