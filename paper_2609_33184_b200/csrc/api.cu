@@ -1418,13 +1418,24 @@ static int window_rows(int bits, int64_t heads, int R, int64_t walked) {
   return ss::kRows8;
 }
 
+// What attention refuses of a cache and its lengths, before anything is enqueued; fills the kernels' view of the cache.
+static ss_status cache_ok(const ss_ctx* c, int bits, int32_t B, int32_t T_q, const ss_cache8* cache,
+                          const int32_t* valid_len, const Window8& win, ss::View8* kv) {
+  const ss_status st = view_cache(cache, bits, B, kv);
+  if (st != SS_OK) return st;
+  if (kv->room > c->cfg.max_Lc) return SS_ERR_SHAPE;
+  if ((uintptr_t)valid_len & 3) return SS_ERR_ALIGN;
+  if (win.window && kv->room + 2ll * T_q > 0x7fffffff - 16384) return SS_ERR_SHAPE;  // (positions and granules in 32 bits)
+  // (the kernels number all tiles in 31 bits)
+  if ((int64_t)B * ((kv->room + ss::kTok8 - 1) / ss::kTok8) * c->cfg.H_kv >= (1ll << 31)) return SS_ERR_SHAPE;
+  return SS_OK;
+}
+
 // The attention launch that the entry points share; the caller has set where its result goes.
 static ss_status attn8(ss_ctx* c, int bits, const ss_tensor& Q, int32_t B, int32_t T_q, float scale, const ss_cache8* cache,
                        const int32_t* valid_len, const Window8& win, ss::Attn8Params* p, cudaStream_t s) {
-  const ss_status st = view_cache(cache, bits, B, &p->kv);
+  const ss_status st = cache_ok(c, bits, B, T_q, cache, valid_len, win, &p->kv);
   if (st != SS_OK) return st;
-  if (p->kv.room > c->cfg.max_Lc) return SS_ERR_SHAPE;
-  if ((uintptr_t)valid_len & 3) return SS_ERR_ALIGN;
   p->Q = (const __nv_bfloat16*)Q.ptr;
   p->q_sb = Q.stride_b;
   p->q_sh = Q.stride_h;
@@ -1443,7 +1454,6 @@ static ss_status attn8(ss_ctx* c, int bits, const ss_tensor& Q, int32_t B, int32
   bool tc = c->tc_ok && (!cache->page_table || ps % ss::kTok8 == 0 || (ps >= 8 && ss::kTok8 % ps == 0));
   int box = cache->page_table && ps < ss::kTok8 ? ps : ss::kTok8;
   if (win.window) {
-    if (p->kv.room + 2ll * T_q > 0x7fffffff - 16384) return SS_ERR_SHAPE;  // (positions and granules in 32 bits)
     p->gran_log2 = granule_log2(p->kv);
     tc = c->tc_ok && p->gran_log2;
     box = 1 << p->gran_log2;
@@ -1473,8 +1483,6 @@ static ss_status attn8(ss_ctx* c, int bits, const ss_tensor& Q, int32_t B, int32
   const int most = !tc ? ss::kMinRows8 : win.window ? window_rows(bits, (int64_t)B * p->H_kv, p->R, walked) : ss::kRows8;
   p->row_tiles = (p->R + most - 1) / most;  // units of `most` rows at most, evenly spread
   p->rows_per_tile = (p->R + p->row_tiles - 1) / p->row_tiles;
-  // (the kernels number all tiles in 31 bits)
-  if ((int64_t)B * ((p->kv.room + ss::kTok8 - 1) / ss::kTok8) * p->H_kv >= (1ll << 31)) return SS_ERR_SHAPE;
   // as many CTAs as are resident, and one for every row tile at least
   p->shares = (tc && bits == 8 && p->d == 64 && p->rows_per_tile <= ss::kFew8 ? ss::kCtasFew8 : ss::kCtas8) / p->row_tiles;
   if (p->shares < 1) p->shares = 1;
@@ -1512,10 +1520,8 @@ static ss_status chunk8(ss_ctx* c, int bits, const ss_cache8* cache, const int32
   if (c->state != ss_ctx::OPEN || (cudaStream_t)stream != c->stream) return SS_ERR_STATE;
   ss::Attn8Params p;
   memset(&p, 0, sizeof(p));
-  ss_status st = view_cache(cache, bits, c->B, &p.kv);  // (before a fold is enqueued)
+  ss_status st = cache_ok(c, bits, c->B, c->T_q, cache, valid_len, win, &p.kv);  // (before a fold is enqueued)
   if (st != SS_OK) return st;
-  if (p.kv.room > c->cfg.max_Lc) return SS_ERR_SHAPE;
-  if ((uintptr_t)valid_len & 3) return SS_ERR_ALIGN;
   DeviceGuard on(c->cfg.device);
   if (on.err != cudaSuccess) return cuda_fail(c, on.err);
   cudaError_t e = settle8(c);
