@@ -129,6 +129,17 @@ bool count(Py_ssize_t n, Py_ssize_t want) {
 }
 using Args = PyObject* const*;
 
+// The entry point's status.  It runs without the interpreter's lock, as a launch may wait for room in the device's queue
+// (the caller keeps tensors, context and cache alive).
+template <typename F>
+PyObject* status_of(F call) {
+  ss_status st;
+  Py_BEGIN_ALLOW_THREADS;
+  st = call();
+  Py_END_ALLOW_THREADS;
+  return PyLong_FromLong(st);
+}
+
 // context(handle, dev, H_q, H_kv, d)
 PyObject* context(PyObject*, Args a, Py_ssize_t n) {
   Ctx c;
@@ -159,7 +170,7 @@ PyObject* rope_rotate(PyObject*, Args a, Py_ssize_t n) {
       !pair(c, a[3], a[5], B, c->H_kv, T, &k, &ko) || !ints(c, a[6], (rope ? rope->n_axes : 1) * B * T, &pos) ||
       !ints(c, a[7], B, &off) || !ints(c, a[8], B, &cnt) || !address_of(a[9], &stream))
     return nullptr;
-  return PyLong_FromLong(ss_rope_rotate(c->handle, rope, q, k, (int32_t)B, (int32_t)T, pos, off, cnt, qo, ko, stream));
+  return status_of([&] { return ss_rope_rotate(c->handle, rope, q, k, (int32_t)B, (int32_t)T, pos, off, cnt, qo, ko, stream); });
 }
 
 // kv_append / kv8_append(context, cache, K, V, rope, pos, Q, Q_out, dst_off, row_cnt, row_idx, stream)
@@ -178,9 +189,10 @@ PyObject* append(PyObject*, Args a, Py_ssize_t n) {
       !ints(c, a[8], B, &off) || !ints(c, a[9], B, &cnt) || !ints(c, a[10], B * T, &idx) || !address_of(a[11], &stream))
     return nullptr;
   const int32_t b = (int32_t)B, t = (int32_t)T;
-  return PyLong_FromLong(
-      BITS == 8 ? ss_kv8_append(c->handle, static_cast<const ss_cache8*>(cache->desc), k, v, b, t, rope, pos, idx, cnt, off, q, qo, stream)
-                : ss_kv_append(c->handle, static_cast<const ss_cache16*>(cache->desc), k, v, b, t, rope, pos, idx, cnt, off, q, qo, stream));
+  return status_of([&] {
+    return BITS == 8 ? ss_kv8_append(c->handle, static_cast<const ss_cache8*>(cache->desc), k, v, b, t, rope, pos, idx, cnt, off, q, qo, stream)
+                     : ss_kv_append(c->handle, static_cast<const ss_cache16*>(cache->desc), k, v, b, t, rope, pos, idx, cnt, off, q, qo, stream);
+  });
 }
 
 // decode_window / decode8_window(context, Q, scale, cache, window, sinks, valid_len, O, LSE, stream)
@@ -200,10 +212,12 @@ PyObject* decode_window(PyObject*, Args a, Py_ssize_t n) {
       (a[8] != Py_None && !output(c, a[8], at::kFloat, B, T, false, &lse)) || !address_of(a[9], &stream))
     return nullptr;
   const int32_t b = (int32_t)B, t = (int32_t)T;
-  return PyLong_FromLong(BITS == 8 ? ss_decode8_window(c->handle, q, b, t, scale, static_cast<const ss_cache8*>(cache->desc), window,
-                                                       sinks, len, o, static_cast<float*>(lse), stream)
-                                   : ss_decode_window(c->handle, q, b, t, scale, static_cast<const ss_cache16*>(cache->desc), window,
-                                                      sinks, len, o, static_cast<float*>(lse), stream));
+  return status_of([&] {
+    return BITS == 8 ? ss_decode8_window(c->handle, q, b, t, scale, static_cast<const ss_cache8*>(cache->desc), window, sinks, len, o,
+                                         static_cast<float*>(lse), stream)
+                     : ss_decode_window(c->handle, q, b, t, scale, static_cast<const ss_cache16*>(cache->desc), window, sinks, len, o,
+                                        static_cast<float*>(lse), stream);
+  });
 }
 
 // verify_chunk_window / verify_chunk8_window(context, cache, window, sinks, valid_len, depth, B, T_q, stream)
@@ -219,8 +233,10 @@ PyObject* chunk_window(PyObject*, Args a, Py_ssize_t n) {
       !int32_of(a[2], &window) || !int32_of(a[3], &sinks) || !ints(c, a[4], B, &len) || !ints(c, a[5], B * T, &depth) ||
       !address_of(a[8], &stream))
     return nullptr;
-  return PyLong_FromLong(BITS == 8 ? ss_verify_chunk8_window(c->handle, static_cast<const ss_cache8*>(cache->desc), window, sinks, len, depth, stream)
-                                   : ss_verify_chunk_window(c->handle, static_cast<const ss_cache16*>(cache->desc), window, sinks, len, depth, stream));
+  return status_of([&] {
+    return BITS == 8 ? ss_verify_chunk8_window(c->handle, static_cast<const ss_cache8*>(cache->desc), window, sinks, len, depth, stream)
+                     : ss_verify_chunk_window(c->handle, static_cast<const ss_cache16*>(cache->desc), window, sinks, len, depth, stream);
+  });
 }
 
 // A tensor without strides or storage (sparse, nested) throws when it is asked for them: no exception leaves a call.
