@@ -7,6 +7,7 @@ the shared library is missing or the device is not sm_100, calls raise.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import importlib.util
 import os
 from typing import Optional, Sequence
@@ -358,7 +359,11 @@ class Cache8:
         self.desc = ss_cache8(t8(K), t8(V), t8(K_scale), t8(V_scale), K.shape[0], K.shape[2],
                               1 if page_table is None else page_table.shape[1], _ptr(page_table))
         self.ref = C.byref(self.desc)
-        self.known = marshal().cache(C.addressof(self.desc), 8, self.H_kv, self.d, self.requests, self.device)
+
+    @functools.cached_property
+    def known(self):
+        """What the extension module's calls take for this cache (the older calls go without the module)."""
+        return marshal().cache(C.addressof(self.desc), 8, self.H_kv, self.d, self.requests, self.device)
 
     @classmethod
     def empty(cls, outer: int, H_kv: int, tokens: int, d: int, page_table: Optional[torch.Tensor] = None,
@@ -389,7 +394,11 @@ class Cache16:
         self.desc = ss_cache16(as_ss_tensor(K), as_ss_tensor(V), K.shape[0], K.shape[2],
                                1 if page_table is None else page_table.shape[1], _ptr(page_table))
         self.ref = C.byref(self.desc)
-        self.known = marshal().cache(C.addressof(self.desc), 16, self.H_kv, self.d, self.requests, self.device)
+
+    @functools.cached_property
+    def known(self):
+        """What the extension module's calls take for this cache."""
+        return marshal().cache(C.addressof(self.desc), 16, self.H_kv, self.d, self.requests, self.device)
 
     @classmethod
     def empty(cls, outer: int, H_kv: int, tokens: int, d: int, page_table: Optional[torch.Tensor] = None,
@@ -435,8 +444,15 @@ class Context:
         self.H_q, self.H_kv, self.d = H_q, H_kv, d
         self._dev = device
         self._B = self._T = 0   # requests and queries of the open round
-        self._m = marshal()
-        self._me = self._m.context(self.handle.value, device, H_q, H_kv, d)   # None once closed
+
+    # The extension module and what its calls take for this context (None once closed); loaded by the first such call.
+    @functools.cached_property
+    def _m(self):
+        return marshal()
+
+    @functools.cached_property
+    def _me(self):
+        return self._m.context(self.handle.value, self._dev, self.H_q, self.H_kv, self.d)
 
     def _sp(self, stream) -> int:
         """cudaStream_t of `stream`, else torch's current stream on this context's device."""
