@@ -422,6 +422,9 @@ ss_status ss_kv8_append(ss_ctx* ctx, const ss_cache8* cache, ss_tensor K, ss_ten
  * 8 tokens, the CUDA cores other pages.  The split over the GPU follows the lengths on the device, so a captured
  * call follows lengths that change between replays.  Tokens that no query of the request sees may hold anything, NaN
  * included; a value that is not finite in a token that only some of them see may make the others' rows NaN.
+ * Softmax weights enter the product with V rounded: to 2^-16 of themselves over a bf16 cache, to 2^-8 where a kv-head has
+ * more than 16 rows (T_q * H_q / H_kv) at head dim 128, to 2^-8.8 over 8 bits; row sums and LSE are those of the unrounded
+ * ones, in fp32.  With SS_FLAG_FORCE_SIMT, and on the CUDA cores, weights stay fp32, at several times the time.
  *
  * ss_decode_window, ss_decode8_window: the T_q queries of a request are the newest tokens of its cache, query t
  * at position valid_len[b] - T_q + t - a decoding step (T_q = 1), or a piece of a prompt, after ss_kv_append or

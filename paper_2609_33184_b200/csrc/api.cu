@@ -1408,7 +1408,11 @@ static void window_mode(ss::Attn8Params* p, int bits, int64_t tiles) {
 // Measured, head dim 128, groups of 4, with 32 / 16 / 8 rows in us: 8 heads, 24 positions over a window of 128, bf16 8.5 /
 // 7.3 / 7.4; of 1000 10.6 / 9.3 / 12.8, 8 bits 10.9 / 9.4 / 9.9; of 4000 14.7 / 16.9 / 26.3 and 14.4 / 13.9 / 20.7; 1 head,
 // 8 positions over 128, bf16 8.0 / 6.7 / 5.8, 8 bits 8.1 / 6.7 / 5.2; 64 heads over 128 9.4 / 8.6 / 10.0 and 9.7 / 8.2 /
-// 8.8, over 1000 15.0 / 15.6 / 20.4 and 14.0 / 12.2 / 14.5.
+// 8.8, over 1000 15.0 / 15.6 / 20.4 and 14.0 / 12.2 / 14.5.  Head dim 64, groups of 4: 8 heads, 24 positions over 128 7.2 / 6.3 /
+// 6.9 and 7.3 / 7.0 / 6.7, over 4000 12.1 / 12.9 / 19.8 and 13.1 / 14.2 / 14.9; 1 head over 1000 8.3 / 7.1 / 6.2 and 8.6 / 7.6 / 6.1.
+// Head dim 128, groups of 8: 8 heads, 24 positions over 128 8.8 / 8.3 / 9.3 and 9.0 / 8.2 / 8.7, over 1000 11.5 / 13.9 / 19.4
+// and 12.2 / 12.1 / 14.5; groups of 1 over 128 7.9 / 6.9 / 6.0 and 7.9 / 6.8 / 5.7.  In 72 such cases (head dims 64 and 128,
+// groups of 1, 4 and 8, windows of 128 to 4000) what is taken here is at most 9 % over the best of the three.
 static int window_rows(int bits, int64_t heads, int R, int64_t walked) {
   for (int most = ss::kMinRows8; most < ss::kRows8; most *= 2) {
     const int64_t units = heads * ((R + most - 1) / most);

@@ -1,7 +1,7 @@
 // Argument marshalling of the calls that a program makes once or twice per layer and step: checks a call's tensors
-// and passes their addresses and strides to the C entry point.  (With ctypes, checks in Python and structures
-// built one by one, a call of four tensors took 7.5 us of the host, more than its kernel takes of the GPU; here
-// 0.5 us and the launch.)  Functions return the entry point's status; tensors that do not fit raise AssertionError.
+// and passes their addresses and strides to the C entry point.  (Without the launch a call of four tensors takes 0.5 us of
+// the host; with ctypes, checks in Python and structures built one by one it was 7.5 us, more than its kernel takes of
+// the GPU.  Called one by one, 64 new tokens were appended in 9.5 us, now in 3.5.)  Functions return the entry point's status; tensors that do not fit raise AssertionError.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include <torch/csrc/autograd/python_variable.h>
