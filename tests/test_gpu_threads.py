@@ -62,7 +62,7 @@ def test_other_threads_run_while_a_call_waits_for_the_queue(what):
     assert ctx.ss_poll_status() == (0, 0)
     ctx.close()
     assert took > 0.5, "the queue took all calls: nothing was waited for"
-    assert gaps[0] < 0.25, gaps[0]
+    assert gaps[0] < took / 2, (gaps[0], took)                # (as long as the wait, where it stands still)
 
 
 def test_threads_with_a_context_each():
